@@ -326,6 +326,152 @@ onela_status_t onela_select_beams_noalloc(int32_t num_requests, int32_t prev_wid
                                           int32_t* tokens_out, float* scores_out,
                                           void* stream);
 
+/* ---- The gated delta rule over whole sequences ---------------------------
+ * Eq. 1 over N packed sequences of any lengths, for every token and value head
+ *   S_t = alpha_t S_{t-1} + beta_t (v_t - alpha_t S_{t-1} k_t) k_t^T,
+ *   o_t = scale S_t q_t,        alpha_t = exp(log_alpha_t),
+ * with the outputs of every token, a state to start from and the last state
+ * (what a layer's prompt pass needs around the decode entry points, whose s0
+ * the last state is), its gradients (training), and the same token by token on
+ * a pool of states (serving without beams).  The decay is given as its logarithm:
+ * that is what a model's gate yields, and the gradient by it stays finite
+ * where alpha vanishes.
+ *   q, k         device [total_tokens][H_K][d_k] io dtype
+ *   v            device [total_tokens][H_V][d_v] io dtype
+ *   log_alpha    device fp32 [total_tokens][H_V]; below -1e5 (-inf among it)
+ *                alpha is 0: the token forgets all before it, and the gradient
+ *                by its log_alpha is 0
+ *   beta         device fp32 [total_tokens][H_V]
+ *   seq_offsets  device int32 [num_seqs + 1], rising from 0 to total_tokens:
+ *                sequence n has the tokens seq_offsets[n] .. seq_offsets[n+1] - 1
+ *                (none is a length too); NULL: total_tokens / num_seqs tokens
+ *                each.  It is read on the device; offsets out of range or order
+ *                are cut to the tensors, so that they give wrong sequences
+ *                but no access outside.
+ * q, k and v may stand inside wider rows (a projection's output): q_stride,
+ * k_stride and v_stride are the elements between two tokens (0: dense); a
+ * token's heads are dense.  All other tensors are dense.  Rows start on 16 bytes.
+ * Supported (d_k, d_v) and dtypes: those of onela_config_t.  States are fp32
+ * [num_seqs][H_V][d_v][d_k]. */
+typedef struct {
+  int32_t num_seqs;      /* N */
+  int32_t num_qk_heads;  /* H_K */
+  int32_t num_v_heads;   /* H_V, a multiple of H_K */
+  int32_t d_k;
+  int32_t d_v;
+  int32_t io_dtype;      /* onela_dtype_t of q, k, v, the outputs and gradients of such */
+  int64_t total_tokens;  /* tokens of all sequences together, < 2^31 */
+  int64_t q_stride, k_stride, v_stride;
+  float scale;           /* of the outputs; Eq. 1 itself has none (1) */
+} onela_delta_config_t;
+
+/* Bytes of workspace of onela_delta_rule_forward (backward = 0) or
+ * onela_delta_rule_backward (backward = 1) for sequences of any lengths with
+ * this total: per 64-token chunk and value head the state at its entry and the
+ * chunk's factors (backward: their adjoints too).  0 for an invalid cfg.  The
+ * contents need no preparation and mean nothing afterwards. */
+size_t onela_delta_rule_workspace_bytes(const onela_delta_config_t* cfg, int32_t backward);
+
+/* Outputs and last states, in chunks of 64 tokens on the matrix cores.
+ *   initial_state  the state before each sequence, or NULL (0)
+ *   o              device [total_tokens][H_V][d_v] io dtype
+ *   final_state    the state after each sequence, or NULL; may be initial_state
+ *   workspace      device, 256-byte aligned, used only by the enqueued work
+ * Errors: ONELA_EINVAL, ONELA_ECAPACITY (workspace too small), ONELA_EHIP. */
+onela_status_t onela_delta_rule_forward(const onela_delta_config_t* cfg,
+                                        const int32_t* seq_offsets, const void* q,
+                                        const void* k, const void* v, const float* log_alpha,
+                                        const float* beta, const float* initial_state, void* o,
+                                        float* final_state, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+
+/* Gradients of a scalar of o and final_state by every input.  Nothing is kept from
+ * the forward call: the states are formed again from the inputs.
+ *   d_o              device [total_tokens][H_V][d_v] io dtype, dense
+ *   d_final_state    or NULL (0)
+ *   dq, dk, dv       dense, io dtype; dq and dk are the sums over the value heads
+ *                    of their group
+ *   dlog_alpha,dbeta fp32 [total_tokens][H_V]
+ *   d_initial_state  or NULL (not wanted); may be d_final_state
+ * Results do not depend on timing.  Errors as for the forward call. */
+onela_status_t onela_delta_rule_backward(
+    const onela_delta_config_t* cfg, const int32_t* seq_offsets, const void* q, const void* k,
+    const void* v, const float* log_alpha, const float* beta, const float* initial_state,
+    const void* d_o, const float* d_final_state, void* dq, void* dk, void* dv,
+    float* dlog_alpha, float* dbeta, float* d_initial_state, void* workspace,
+    size_t workspace_bytes, void* stream);
+
+/* The same recurrence token by token, one launch and no workspace: for one token (or
+ * a few) per sequence.
+ *   state       device fp32 [num_slots][H_V][d_v][d_k], updated in place
+ *   slots       device int32 [num_seqs]: the state of each sequence; NULL: sequence
+ *               n has state n (num_slots >= num_seqs).  A slot outside
+ *               [0, num_slots) (a padded batch's -1) leaves every state as it is, and
+ *               the sequence's outputs are 0.  Two sequences must not share a slot.
+ *   o           device [total_tokens][H_V][d_v] io dtype
+ * Errors: ONELA_EINVAL, ONELA_ECAPACITY (num_slots < num_seqs without slots),
+ * ONELA_EHIP. */
+onela_status_t onela_delta_rule_step(const onela_delta_config_t* cfg,
+                                     const int32_t* seq_offsets, const void* q, const void* k,
+                                     const void* v, const float* log_alpha, const float* beta,
+                                     float* state, int32_t num_slots, const int32_t* slots,
+                                     void* o, void* stream);
+
+/* ---- Norm and rotation of queries and keys -------------------------------
+ * What q and k pass before they enter a layer, both in one launch: each row x (one
+ * token's head, head_dim columns) becomes w x r with r = (sum x^2 + eps)^-1/2
+ * (ONELA_NORM_L2: the delta rule's queries and keys) or (mean x^2 + eps)^-1/2
+ * (ONELA_NORM_RMS), then the first rotary_dim columns are turned by the token's
+ * position: the pairs (i, i + rotary_dim / 2) (ONELA_ROTATE_HALVES) or (2 i, 2 i + 1)
+ * (ONELA_ROTATE_PAIRS), i < rotary_dim / 2, become (a c - b s, b c + a s).
+ *   q, k       device [num_tokens][heads][head_dim] io dtype, q_stride and k_stride
+ *              elements between tokens (0: dense), rows on 16 bytes; k and k_out
+ *              NULL with num_k_heads = 0
+ *   q_weight, k_weight  device fp32 [head_dim], or NULL (1)
+ *   positions  device int32 [num_tokens], or NULL (token t is at position t).  The
+ *              outputs of a token whose position is outside the table are NaN.
+ *   cos_sin    device fp32 [table_rows][rotary_dim]: the rotary_dim / 2 cosines of a
+ *              position, then its sines; NULL with rotary_dim = 0
+ *   q_out, k_out  device, dense, io dtype
+ * head_dim: a multiple of 8 up to 512; rotary_dim: 0 or a multiple of 16 up to
+ * head_dim.  fp32 inside, one rounding at the store. */
+typedef enum { ONELA_NORM_L2 = 0, ONELA_NORM_RMS = 1 } onela_norm_t;
+typedef enum { ONELA_ROTATE_HALVES = 0, ONELA_ROTATE_PAIRS = 1 } onela_rotation_t;
+typedef struct {
+  int64_t num_tokens;  /* < 2^31 */
+  int32_t num_q_heads;
+  int32_t num_k_heads; /* 0: queries alone */
+  int32_t head_dim;
+  int32_t rotary_dim;
+  int32_t table_rows;  /* positions in cos_sin */
+  int32_t io_dtype;    /* onela_dtype_t */
+  int32_t norm;        /* onela_norm_t */
+  int32_t rotation;    /* onela_rotation_t */
+  int64_t q_stride, k_stride;
+  float eps;
+} onela_norm_config_t;
+
+/* Errors: ONELA_EINVAL, ONELA_EHIP. */
+onela_status_t onela_qk_norm_rope(const onela_norm_config_t* cfg, const void* q, const void* k,
+                                  const float* q_weight, const float* k_weight,
+                                  const int32_t* positions, const float* cos_sin, void* q_out,
+                                  void* k_out, void* stream);
+
+/* Gradients by q and k (dense, io dtype) and by the weights (fp32 [head_dim], sums over
+ * all tokens and heads in a fixed order; NULL: not wanted) from those of the outputs
+ * (d_q_out, d_k_out: dense, io dtype).  q and k are the forward call's inputs.
+ * workspace: onela_qk_norm_rope_workspace_bytes(cfg) bytes (0 for an invalid cfg),
+ * 256-byte aligned; NULL when no weight gradient is wanted.
+ * Errors: ONELA_EINVAL, ONELA_ECAPACITY, ONELA_EHIP. */
+size_t onela_qk_norm_rope_workspace_bytes(const onela_norm_config_t* cfg);
+onela_status_t onela_qk_norm_rope_backward(const onela_norm_config_t* cfg, const void* q,
+                                           const void* k, const float* q_weight,
+                                           const float* k_weight, const int32_t* positions,
+                                           const float* cos_sin, const void* d_q_out,
+                                           const void* d_k_out, void* dq, void* dk,
+                                           float* dq_weight, float* dk_weight, void* workspace,
+                                           size_t workspace_bytes, void* stream);
+
 /* ---- Capacity model (host only) -----------------------------------------
  * Persistent recurrent-state bytes after `steps` decode steps for one GDN
  * layer (Sec. 4.4): one S_ctx per request and value head (state_bytes per

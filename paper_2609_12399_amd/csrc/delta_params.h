@@ -1,0 +1,41 @@
+// Arguments of the delta-rule kernels (kernels_delta.hip, kernel_delta_step.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "host_plan.h"
+
+namespace onela {
+
+struct DeltaParams {
+  const void *q, *k, *v;    // [total][heads][d], token strides qs, ks, vs
+  const void* d_o;          // [total][HV][DV] io dtype (backward)
+  const float *la, *beta;   // [total][HV]
+  const float *s_in;        // [N][HV][DV][DK] or null
+  const float *ds_in;       // gradient of the final state, or null (backward)
+  float *s_out, *ds_out;    // final state / gradient of the initial state, or null
+  void *o;                  // [total][HV][DV] io dtype
+  void *dq, *dk, *dv;       // dense, io dtype
+  float *dla, *db;          // [total][HV]
+  const int* offsets;       // [N + 1] or null: N sequences of L tokens
+  long total, qs, ks, vs;
+  float scale;
+  int N, HK, HV, DV, L, nch_l;  // nch_l: chunks of a sequence of L tokens (no offsets)
+  long slots;               // chunk slots
+  // workspace, per (chunk slot, value head)
+  uint4* tf;     // [kDeltaFactor]  T fragments, three bf16 parts
+  uint4* tr;     // the same of the transposed, reversed T (backward)
+  float* gates;  // [kDeltaGates][64]
+  float* sws;    // [DV][DK]  state before the chunk
+  float* ews;    // [DV][64]  e
+  float* dsws;   // [DV][DK]  adjoint of the state after the chunk (backward)
+  float* hws;    // [DV][64]  beta times the chunk's own part of dD, then dV (backward)
+  // recurrent step
+  float* pool;       // [num_slots][HV][DV][DK]
+  const int* slot;   // [N] or null
+  int num_slots;
+};
+
+}  // namespace onela

@@ -3,6 +3,7 @@
 #include "host_plan.h"
 
 #include <algorithm>
+#include <cstdint>
 
 namespace onela {
 
@@ -201,6 +202,90 @@ onela_status_t check_select(int R, int prev_width, int vocab, int width, SelectP
   if (n > kSelectMaxCandidates || !select_plan(R, unsigned(n), unsigned(width), plan))
     return ONELA_EINVAL;
   return ONELA_OK;
+}
+
+// ---- delta rule over sequences ---------------------------------------------------
+
+onela_status_t delta_shape_of(const onela_delta_config_t* c, bool ragged, DeltaShape* out) {
+  if (!c) return ONELA_EINVAL;
+  if (c->num_seqs < 1 || c->num_qk_heads < 1 || c->num_v_heads < 1 ||
+      c->num_v_heads % c->num_qk_heads || c->total_tokens < 0 || c->total_tokens > INT32_MAX)
+    return ONELA_EINVAL;
+  if (c->io_dtype != ONELA_F32 && c->io_dtype != ONELA_BF16) return ONELA_EINVAL;
+  if (!ragged && c->total_tokens % c->num_seqs) return ONELA_EINVAL;
+  Shape head{};
+  head.dk = c->d_k;
+  head.dv = c->d_v;
+  head.bf16 = c->io_dtype == ONELA_BF16;
+  if (!decode_supported(head)) return ONELA_EINVAL;
+  DeltaShape s{};
+  s.N = c->num_seqs;
+  s.HK = c->num_qk_heads;
+  s.HV = c->num_v_heads;
+  s.dk = c->d_k;
+  s.dv = c->d_v;
+  s.bf16 = head.bf16;
+  s.total = long(c->total_tokens);
+  s.scale = c->scale;
+  // rows start on 16 bytes; 64 tokens' rows are reached with 31-bit byte offsets
+  const int64_t qk = int64_t(s.HK) * s.dk, v = int64_t(s.HV) * s.dv, per16 = s.bf16 ? 8 : 4;
+  const int64_t most = (int64_t(1) << 31) / (kDeltaChunk * 4) - 1;
+  auto stride = [&](int64_t given, int64_t dense, long* to) {
+    const int64_t x = given ? given : dense;
+    if (x < dense || x % per16 || x > most) return false;
+    *to = long(x);
+    return true;
+  };
+  if (!stride(c->q_stride, qk, &s.qs) || !stride(c->k_stride, qk, &s.ks) ||
+      !stride(c->v_stride, v, &s.vs) || v > most)
+    return ONELA_EINVAL;
+  if (ragged) {
+    s.slots = s.total / kDeltaChunk + s.N;
+  } else {
+    s.L = int(s.total / s.N);
+    s.slots = long(s.N) * ((s.L + kDeltaChunk - 1) / kDeltaChunk);
+  }
+  // one workgroup per slot, value head and 16 state rows at most
+  const double groups = double(std::max(s.slots, long(s.N))) * s.HV * (s.dv / 16);
+  if (groups >= 2147483648.0) return ONELA_EINVAL;
+  *out = s;
+  return ONELA_OK;
+}
+
+size_t delta_workspace_bytes(const DeltaShape& s, bool backward) {
+  // T, the state at the chunk's entry and e; backward also T reversed, the
+  // adjoint of the state after the chunk and dV (all multiples of 256 bytes)
+  const size_t part = kDeltaFactorBytes + sizeof(float) * size_t(s.dv) * (s.dk + kDeltaChunk);
+  const size_t gates = sizeof(float) * kDeltaGates * kDeltaChunk;
+  return size_t(s.slots) * s.HV * (gates + part * (backward ? 2 : 1));
+}
+
+// ---- norm and rotation of queries and keys ----------------------------------------
+
+onela_status_t check_norm(const onela_norm_config_t* c) {
+  if (!c) return ONELA_EINVAL;
+  if (c->num_tokens < 0 || c->num_tokens > INT32_MAX || c->num_q_heads < 1 || c->num_k_heads < 0)
+    return ONELA_EINVAL;
+  if (c->head_dim < 8 || c->head_dim > 512 || c->head_dim % 8) return ONELA_EINVAL;
+  if (c->rotary_dim < 0 || c->rotary_dim > c->head_dim || c->rotary_dim % 16) return ONELA_EINVAL;
+  if (c->rotary_dim && c->table_rows < 1) return ONELA_EINVAL;
+  if (c->io_dtype != ONELA_F32 && c->io_dtype != ONELA_BF16) return ONELA_EINVAL;
+  if (c->norm != ONELA_NORM_L2 && c->norm != ONELA_NORM_RMS) return ONELA_EINVAL;
+  if (c->rotation != ONELA_ROTATE_HALVES && c->rotation != ONELA_ROTATE_PAIRS) return ONELA_EINVAL;
+  if (!(c->eps >= 0.f)) return ONELA_EINVAL;
+  const int64_t per16 = c->io_dtype == ONELA_BF16 ? 8 : 4;
+  const int64_t q = int64_t(c->num_q_heads) * c->head_dim, k = int64_t(c->num_k_heads) * c->head_dim;
+  if (c->q_stride && (c->q_stride < q || c->q_stride % per16)) return ONELA_EINVAL;
+  if (c->k_stride && (c->k_stride < k || c->k_stride % per16)) return ONELA_EINVAL;
+  // (a workgroup takes four rows or more)
+  if (double(c->num_tokens) * (double(c->num_q_heads) + c->num_k_heads) >= 8589934592.0 ||
+      double(c->num_q_heads) + c->num_k_heads >= 1073741824.0)
+    return ONELA_EINVAL;
+  return ONELA_OK;
+}
+
+size_t norm_workspace_bytes(const onela_norm_config_t* c) {
+  return sizeof(float) * 2 * size_t(kNormBlocks) * size_t(c->head_dim);
 }
 
 // ---- per-step protocol --------------------------------------------------------

@@ -94,6 +94,29 @@ bool select_plan(int R, unsigned N, unsigned W, SelectPlan* plan);
 // entry point.
 constexpr size_t kSelectScratchBytes = size_t(32) << 20;
 
+// ---- delta rule over sequences ---------------------------------------------------
+constexpr int kDeltaChunk = 64;                          // tokens per chunk
+constexpr size_t kDeltaFactorBytes = 6 * 3 * 1024;       // split T of a chunk and head
+constexpr int kDeltaGates = 5;                           // fp32 values per token and head
+
+struct DeltaShape {
+  int N, HK, HV, dk, dv;
+  bool bf16;
+  long total;       // tokens
+  long qs, ks, vs;  // elements between tokens
+  float scale;
+  int L;            // tokens per sequence when there are no offsets (total / N)
+  long slots;       // chunk slots: enough for sequences of any lengths
+};
+// The shape of a configuration, or ONELA_EINVAL.  ragged: the lengths come as offsets.
+onela_status_t delta_shape_of(const onela_delta_config_t* cfg, bool ragged, DeltaShape* out);
+size_t delta_workspace_bytes(const DeltaShape& s, bool backward);
+
+// ---- norm and rotation of queries and keys ----------------------------------------
+constexpr int kNormBlocks = 1024;  // most workgroups of the backward pass
+onela_status_t check_norm(const onela_norm_config_t* cfg);
+size_t norm_workspace_bytes(const onela_norm_config_t* cfg);
+
 // ---- validation and the per-step protocol -----------------------------------
 
 // The Shape of a configuration, or ONELA_EINVAL.

@@ -66,6 +66,29 @@ hipError_t launch_prefill_chunked(const Shape& s, int prompt_len, const void* k,
                                   const float* alpha, const float* beta, float* s0_out,
                                   void* workspace, hipStream_t st);
 
+// ---- delta rule over sequences ------------------------------------------------
+struct DeltaParams;
+hipError_t launch_delta_rule(const DeltaShape& s, DeltaParams p, bool backward, void* workspace,
+                             hipStream_t st);
+hipError_t launch_delta_step(const DeltaShape& s, const DeltaParams& p, hipStream_t st);
+
+// ---- norm and rotation of queries and keys --------------------------------------
+struct NormParams {
+  const void *q, *k;    // [T][H][D], token strides qs, ks
+  const void *dqo, *dko;  // gradients of the outputs, dense (backward)
+  const float *wq, *wk;  // [D] or null
+  const int* positions;  // [T] or null: token t is at position t
+  const float* cos_sin;  // [table][rot]: cosines, then sines
+  void *qo, *ko, *dq, *dk;  // dense
+  float *dwq, *dwk;      // [D] or null
+  float* partial;        // [workgroups][2][D], or null: no weight gradients
+  long rows, qs, ks;
+  float eps, inv_n;      // 1 / D (RMS) or 1 (L2)
+  int HQ, HK, D, rot, table;
+  bool pairs;
+};
+hipError_t launch_norm_rope(const NormParams& p, bool bf16, bool backward, hipStream_t st);
+
 // ---- global top-W beam selection ------------------------------------------
 // Device address of the allocation-free entry point's scratch array on the
 // current device.

@@ -8,6 +8,7 @@
 #include <new>
 
 #include "../../include/onela.h"
+#include "delta_params.h"
 #include "internal.h"
 
 using onela::aligned16;
@@ -385,6 +386,217 @@ onela_status_t onela_select_beams_noalloc(int32_t num_requests, int32_t prev_wid
                                             beam_scores, parents_out, tokens_out, scores_out,
                                             ws, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ONELA_OK : ONELA_EHIP;
+}
+
+// ---- delta rule over sequences ----------------------------------------------------
+
+namespace {
+// What the three entry points share: ONELA_EINVAL unless the tensors of the
+// sequences are there and aligned.
+onela_status_t delta_inputs(const onela_delta_config_t* cfg, const int32_t* offsets,
+                            const void* q, const void* k, const void* v, const float* la,
+                            const float* beta, onela::DeltaShape* s, onela::DeltaParams* p) {
+  const onela_status_t rc = onela::delta_shape_of(cfg, offsets != nullptr, s);
+  if (rc != ONELA_OK) return rc;
+  if (offsets && !aligned4(offsets)) return ONELA_EINVAL;
+  if (s->total > 0 && (!q || !k || !v || !la || !beta)) return ONELA_EINVAL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned4(la) || !aligned4(beta))
+    return ONELA_EINVAL;
+  *p = onela::DeltaParams{};
+  p->q = q;
+  p->k = k;
+  p->v = v;
+  p->la = la;
+  p->beta = beta;
+  p->offsets = offsets;
+  p->total = s->total;
+  p->qs = s->qs;
+  p->ks = s->ks;
+  p->vs = s->vs;
+  p->scale = s->scale;
+  p->N = s->N;
+  p->HK = s->HK;
+  p->HV = s->HV;
+  p->DV = s->dv;
+  p->L = s->L;
+  p->nch_l = (s->L + onela::kDeltaChunk - 1) / onela::kDeltaChunk;
+  p->slots = s->slots;
+  return ONELA_OK;
+}
+
+onela_status_t delta_workspace(const onela::DeltaShape& s, bool backward, const void* workspace,
+                               size_t bytes) {
+  const size_t need = onela::delta_workspace_bytes(s, backward);
+  if (need > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0))
+    return ONELA_EINVAL;
+  return bytes < need ? ONELA_ECAPACITY : ONELA_OK;
+}
+}  // namespace
+
+size_t onela_delta_rule_workspace_bytes(const onela_delta_config_t* cfg, int32_t backward) {
+  // (any lengths: as many chunk slots as ragged sequences can need, or more)
+  onela::DeltaShape s;
+  if (onela::delta_shape_of(cfg, true, &s) != ONELA_OK) return 0;
+  return onela::delta_workspace_bytes(s, backward != 0);
+}
+
+onela_status_t onela_delta_rule_forward(const onela_delta_config_t* cfg,
+                                        const int32_t* seq_offsets, const void* q,
+                                        const void* k, const void* v, const float* log_alpha,
+                                        const float* beta, const float* initial_state, void* o,
+                                        float* final_state, void* workspace,
+                                        size_t workspace_bytes, void* stream) {
+  onela::DeltaShape s;
+  onela::DeltaParams p;
+  onela_status_t rc = delta_inputs(cfg, seq_offsets, q, k, v, log_alpha, beta, &s, &p);
+  if (rc != ONELA_OK) return rc;
+  if ((s.total > 0 && !o) || !aligned16(o) || !aligned16(initial_state) || !aligned16(final_state))
+    return ONELA_EINVAL;
+  rc = delta_workspace(s, false, workspace, workspace_bytes);
+  if (rc != ONELA_OK) return rc;
+  p.s_in = initial_state;
+  p.s_out = final_state;
+  p.o = o;
+  const hipError_t e =
+      onela::launch_delta_rule(s, p, false, workspace, static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+onela_status_t onela_delta_rule_backward(
+    const onela_delta_config_t* cfg, const int32_t* seq_offsets, const void* q, const void* k,
+    const void* v, const float* log_alpha, const float* beta, const float* initial_state,
+    const void* d_o, const float* d_final_state, void* dq, void* dk, void* dv,
+    float* dlog_alpha, float* dbeta, float* d_initial_state, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  onela::DeltaShape s;
+  onela::DeltaParams p;
+  onela_status_t rc = delta_inputs(cfg, seq_offsets, q, k, v, log_alpha, beta, &s, &p);
+  if (rc != ONELA_OK) return rc;
+  if (s.total > 0 && (!d_o || !dq || !dk || !dv || !dlog_alpha || !dbeta)) return ONELA_EINVAL;
+  if (!aligned16(d_o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) ||
+      !aligned4(dlog_alpha) || !aligned4(dbeta) || !aligned16(initial_state) ||
+      !aligned16(d_final_state) || !aligned16(d_initial_state))
+    return ONELA_EINVAL;
+  rc = delta_workspace(s, true, workspace, workspace_bytes);
+  if (rc != ONELA_OK) return rc;
+  p.s_in = initial_state;
+  p.ds_in = d_final_state;
+  p.ds_out = d_initial_state;
+  p.d_o = d_o;
+  p.dq = dq;
+  p.dk = dk;
+  p.dv = dv;
+  p.dla = dlog_alpha;
+  p.db = dbeta;
+  const hipError_t e =
+      onela::launch_delta_rule(s, p, true, workspace, static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+onela_status_t onela_delta_rule_step(const onela_delta_config_t* cfg,
+                                     const int32_t* seq_offsets, const void* q, const void* k,
+                                     const void* v, const float* log_alpha, const float* beta,
+                                     float* state, int32_t num_slots, const int32_t* slots,
+                                     void* o, void* stream) {
+  onela::DeltaShape s;
+  onela::DeltaParams p;
+  const onela_status_t rc = delta_inputs(cfg, seq_offsets, q, k, v, log_alpha, beta, &s, &p);
+  if (rc != ONELA_OK) return rc;
+  if (num_slots < 1 || !state || !aligned16(state) || !aligned4(slots)) return ONELA_EINVAL;
+  if ((s.total > 0 && !o) || !aligned16(o)) return ONELA_EINVAL;
+  if (!slots && num_slots < s.N) return ONELA_ECAPACITY;
+  if (s.total == 0) return ONELA_OK;
+  p.pool = state;
+  p.num_slots = num_slots;
+  p.slot = slots;
+  p.o = o;
+  const hipError_t e = onela::launch_delta_step(s, p, static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+// ---- norm and rotation of queries and keys --------------------------------------
+
+namespace {
+onela_status_t norm_inputs(const onela_norm_config_t* c, const void* q, const void* k,
+                           const float* wq, const float* wk, const int32_t* positions,
+                           const float* cos_sin, onela::NormParams* p) {
+  const onela_status_t rc = onela::check_norm(c);
+  if (rc != ONELA_OK) return rc;
+  if (c->num_tokens > 0 && (!q || (c->num_k_heads > 0 && !k) || (c->rotary_dim > 0 && !cos_sin)))
+    return ONELA_EINVAL;
+  if (!aligned16(q) || !aligned16(k) || !aligned4(wq) || !aligned4(wk) || !aligned4(positions) ||
+      !aligned4(cos_sin))
+    return ONELA_EINVAL;
+  *p = onela::NormParams{};
+  p->q = q;
+  p->k = k;
+  p->wq = wq;
+  p->wk = wk;
+  p->positions = positions;
+  p->cos_sin = cos_sin;
+  p->HQ = c->num_q_heads;
+  p->HK = c->num_k_heads;
+  p->D = c->head_dim;
+  p->rot = c->rotary_dim;
+  p->table = c->table_rows;
+  p->pairs = c->rotation == ONELA_ROTATE_PAIRS;
+  p->rows = long(c->num_tokens) * (p->HQ + p->HK);
+  p->qs = c->q_stride ? long(c->q_stride) : long(p->HQ) * p->D;
+  p->ks = c->k_stride ? long(c->k_stride) : long(p->HK) * p->D;
+  p->eps = c->eps;
+  p->inv_n = c->norm == ONELA_NORM_RMS ? 1.f / float(p->D) : 1.f;
+  return ONELA_OK;
+}
+}  // namespace
+
+onela_status_t onela_qk_norm_rope(const onela_norm_config_t* cfg, const void* q, const void* k,
+                                  const float* q_weight, const float* k_weight,
+                                  const int32_t* positions, const float* cos_sin, void* q_out,
+                                  void* k_out, void* stream) {
+  onela::NormParams p;
+  const onela_status_t rc = norm_inputs(cfg, q, k, q_weight, k_weight, positions, cos_sin, &p);
+  if (rc != ONELA_OK) return rc;
+  if ((p.rows > 0 && (!q_out || (p.HK > 0 && !k_out))) || !aligned16(q_out) || !aligned16(k_out))
+    return ONELA_EINVAL;
+  p.qo = q_out;
+  p.ko = k_out;
+  const hipError_t e = onela::launch_norm_rope(p, cfg->io_dtype == ONELA_BF16, false,
+                                               static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+size_t onela_qk_norm_rope_workspace_bytes(const onela_norm_config_t* cfg) {
+  return onela::check_norm(cfg) == ONELA_OK ? onela::norm_workspace_bytes(cfg) : 0;
+}
+
+onela_status_t onela_qk_norm_rope_backward(const onela_norm_config_t* cfg, const void* q,
+                                           const void* k, const float* q_weight,
+                                           const float* k_weight, const int32_t* positions,
+                                           const float* cos_sin, const void* d_q_out,
+                                           const void* d_k_out, void* dq, void* dk,
+                                           float* dq_weight, float* dk_weight, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
+  onela::NormParams p;
+  const onela_status_t rc = norm_inputs(cfg, q, k, q_weight, k_weight, positions, cos_sin, &p);
+  if (rc != ONELA_OK) return rc;
+  if (p.rows > 0 && (!d_q_out || !dq || (p.HK > 0 && (!d_k_out || !dk)))) return ONELA_EINVAL;
+  if (!aligned16(d_q_out) || !aligned16(d_k_out) || !aligned16(dq) || !aligned16(dk) ||
+      !aligned4(dq_weight) || !aligned4(dk_weight))
+    return ONELA_EINVAL;
+  if (dq_weight || dk_weight) {
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return ONELA_EINVAL;
+    if (workspace_bytes < onela::norm_workspace_bytes(cfg)) return ONELA_ECAPACITY;
+    p.partial = static_cast<float*>(workspace);
+  }
+  p.dqo = d_q_out;
+  p.dko = d_k_out;
+  p.dq = dq;
+  p.dk = dk;
+  p.dwq = dq_weight;
+  p.dwk = dk_weight;
+  const hipError_t e = onela::launch_norm_rope(p, cfg->io_dtype == ONELA_BF16, true,
+                                               static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
 }
 
 }  // extern "C"

@@ -22,6 +22,8 @@ ONELA_ECAPACITY, ONELA_EHIP, ONELA_ENOMEM = 4, 5, 6
 ONELA_F32, ONELA_BF16 = 0, 1
 ONELA_RECORD_INPUTS, ONELA_RECORD_DELTA = 0, 1
 ONELA_RECORDS_COPY, ONELA_RECORDS_BORROW = 0, 1
+ONELA_NORM_L2, ONELA_NORM_RMS = 0, 1
+ONELA_ROTATE_HALVES, ONELA_ROTATE_PAIRS = 0, 1
 
 STATUS_NAMES = {0: "ONELA_OK", 1: "ONELA_EINVAL", 2: "ONELA_ESTEP", 3: "ONELA_EPARENT",
                 4: "ONELA_ECAPACITY", 5: "ONELA_EHIP", 6: "ONELA_ENOMEM"}
@@ -33,7 +35,11 @@ EXPORTED = ["onela_status_str", "onela_check_config", "onela_workspace_bytes", "
             "onela_prefill_state", "onela_fullstate_workspace_bytes", "onela_fullstate_step",
             "onela_capacity_bytes", "onela_fullstate_capacity_bytes",
             "onela_select_workspace_bytes", "onela_select_beams", "onela_select_beams_noalloc",
-            "onela_prefill_workspace_bytes", "onela_prefill_state_chunked"]
+            "onela_prefill_workspace_bytes", "onela_prefill_state_chunked",
+            "onela_delta_rule_workspace_bytes", "onela_delta_rule_forward",
+            "onela_delta_rule_backward", "onela_delta_rule_step",
+            "onela_qk_norm_rope_workspace_bytes", "onela_qk_norm_rope",
+            "onela_qk_norm_rope_backward"]
 
 
 class OnelaError(RuntimeError):
@@ -63,6 +69,45 @@ def make_config(num_requests, num_qk_heads, num_v_heads, d_k, d_v, max_beams, ma
                           max_steps, io_dtype, record_kind, record_storage)
 
 
+class onela_delta_config_t(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_qk_heads", ctypes.c_int32),
+                ("num_v_heads", ctypes.c_int32), ("d_k", ctypes.c_int32),
+                ("d_v", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("total_tokens", ctypes.c_int64), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("scale", ctypes.c_float)]
+
+
+def make_delta_config(num_seqs, total_tokens, num_qk_heads, num_v_heads, d_k, d_v, io_dtype,
+                      scale=1.0, q_stride=0, k_stride=0, v_stride=0) -> onela_delta_config_t:
+    if isinstance(io_dtype, str):
+        io_dtype = {"bf16": ONELA_BF16, "f32": ONELA_F32}[io_dtype]
+    return onela_delta_config_t(num_seqs, num_qk_heads, num_v_heads, d_k, d_v, io_dtype,
+                                total_tokens, q_stride, k_stride, v_stride, scale)
+
+
+class onela_norm_config_t(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int64), ("num_q_heads", ctypes.c_int32),
+                ("num_k_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("table_rows", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("rotation", ctypes.c_int32), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("eps", ctypes.c_float)]
+
+
+def make_norm_config(num_tokens, num_q_heads, num_k_heads, head_dim, io_dtype, norm="l2",
+                     rotary_dim=0, table_rows=0, rotation="halves", eps=1e-6, q_stride=0,
+                     k_stride=0) -> onela_norm_config_t:
+    if isinstance(io_dtype, str):
+        io_dtype = {"bf16": ONELA_BF16, "f32": ONELA_F32}[io_dtype]
+    if isinstance(norm, str):
+        norm = {"l2": ONELA_NORM_L2, "rms": ONELA_NORM_RMS}[norm]
+    if isinstance(rotation, str):
+        rotation = {"halves": ONELA_ROTATE_HALVES, "pairs": ONELA_ROTATE_PAIRS}[rotation]
+    return onela_norm_config_t(num_tokens, num_q_heads, num_k_heads, head_dim, rotary_dim,
+                               table_rows, io_dtype, norm, rotation, q_stride, k_stride, eps)
+
+
 _lib = None
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -82,6 +127,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     import torch  # noqa: F401
     lib = ctypes.CDLL(path)
     cfgp = ctypes.POINTER(onela_config_t)
+    deltap = ctypes.POINTER(onela_delta_config_t)
+    normp = ctypes.POINTER(onela_norm_config_t)
     sig = {
         "onela_status_str": ([_I32], ctypes.c_char_p),
         "onela_check_config": ([cfgp], _I32),
@@ -105,6 +152,13 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "onela_select_beams_noalloc": ([_I32] * 4 + [_P] * 6, _I32),
         "onela_prefill_workspace_bytes": ([cfgp, _I32], ctypes.c_size_t),
         "onela_prefill_state_chunked": ([cfgp, _I32] + [_P] * 6 + [ctypes.c_size_t, _P], _I32),
+        "onela_delta_rule_workspace_bytes": ([deltap, _I32], ctypes.c_size_t),
+        "onela_delta_rule_forward": ([deltap] + [_P] * 10 + [ctypes.c_size_t, _P], _I32),
+        "onela_delta_rule_backward": ([deltap] + [_P] * 16 + [ctypes.c_size_t, _P], _I32),
+        "onela_delta_rule_step": ([deltap] + [_P] * 7 + [_I32] + [_P] * 3, _I32),
+        "onela_qk_norm_rope_workspace_bytes": ([normp], ctypes.c_size_t),
+        "onela_qk_norm_rope": ([normp] + [_P] * 9, _I32),
+        "onela_qk_norm_rope_backward": ([normp] + [_P] * 13 + [ctypes.c_size_t, _P], _I32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -129,6 +183,22 @@ def _dev(x, name: str, optional: bool = False):
             raise ValueError(f"{name} must be contiguous")
         return x.data_ptr()
     raise TypeError(f"{name}: unsupported pointer type {type(x)}")
+
+
+def _rows(x, name: str, stride: int, optional: bool = False):
+    """Device address of a [tokens][heads][width] tensor whose tokens lie ``stride``
+    elements apart (0: dense) and whose heads are dense; else as :func:`_dev`."""
+    if not stride or not hasattr(x, "data_ptr"):
+        return _dev(x, name, optional)
+    if not getattr(x, "is_cuda", False):
+        raise ValueError(f"{name} must be a GPU tensor")
+    if x.dim() != 3 or (x.numel() and (
+            (x.shape[2] > 1 and x.stride(2) != 1) or
+            (x.shape[1] > 1 and x.stride(1) != x.shape[2]) or
+            (x.shape[0] > 1 and x.stride(0) != stride))):
+        raise ValueError(f"{name} must be [tokens][heads][width] with {stride} elements "
+                         "between tokens and dense heads")
+    return x.data_ptr()
 
 
 def _stream(stream):
@@ -286,3 +356,80 @@ def onela_prefill_state_chunked(cfg: onela_config_t, prompt_len: int, k, v, alph
         _dev(alpha, "alpha", opt), _dev(beta, "beta", opt), _dev(s0_out, "s0_out"),
         _dev(workspace, "workspace", optional=True), int(workspace_bytes), _stream(stream)),
         "onela_prefill_state_chunked")
+
+
+def onela_delta_rule_workspace_bytes(cfg: onela_delta_config_t, backward: bool = False) -> int:
+    return load_library().onela_delta_rule_workspace_bytes(ctypes.byref(cfg), int(backward))
+
+
+def onela_delta_rule_forward(cfg: onela_delta_config_t, seq_offsets, q, k, v, log_alpha, beta,
+                             initial_state, o, final_state, workspace=None,
+                             workspace_bytes: int = 0, stream=None):
+    none = cfg.total_tokens == 0
+    _check(load_library().onela_delta_rule_forward(
+        ctypes.byref(cfg), _dev(seq_offsets, "seq_offsets", True),
+        _rows(q, "q", cfg.q_stride, none), _rows(k, "k", cfg.k_stride, none),
+        _rows(v, "v", cfg.v_stride, none), _dev(log_alpha, "log_alpha", none),
+        _dev(beta, "beta", none), _dev(initial_state, "initial_state", True), _dev(o, "o", none),
+        _dev(final_state, "final_state", True), _dev(workspace, "workspace", True),
+        int(workspace_bytes), _stream(stream)), "onela_delta_rule_forward")
+
+
+def onela_delta_rule_backward(cfg: onela_delta_config_t, seq_offsets, q, k, v, log_alpha, beta,
+                              initial_state, d_o, d_final_state, dq, dk, dv, dlog_alpha, dbeta,
+                              d_initial_state, workspace=None, workspace_bytes: int = 0,
+                              stream=None):
+    none = cfg.total_tokens == 0
+    _check(load_library().onela_delta_rule_backward(
+        ctypes.byref(cfg), _dev(seq_offsets, "seq_offsets", True),
+        _rows(q, "q", cfg.q_stride, none), _rows(k, "k", cfg.k_stride, none),
+        _rows(v, "v", cfg.v_stride, none), _dev(log_alpha, "log_alpha", none),
+        _dev(beta, "beta", none), _dev(initial_state, "initial_state", True),
+        _dev(d_o, "d_o", none), _dev(d_final_state, "d_final_state", True), _dev(dq, "dq", none),
+        _dev(dk, "dk", none), _dev(dv, "dv", none), _dev(dlog_alpha, "dlog_alpha", none),
+        _dev(dbeta, "dbeta", none), _dev(d_initial_state, "d_initial_state", True),
+        _dev(workspace, "workspace", True), int(workspace_bytes), _stream(stream)),
+        "onela_delta_rule_backward")
+
+
+def onela_delta_rule_step(cfg: onela_delta_config_t, seq_offsets, q, k, v, log_alpha, beta,
+                          state, num_slots: int, slots, o, stream=None):
+    none = cfg.total_tokens == 0
+    _check(load_library().onela_delta_rule_step(
+        ctypes.byref(cfg), _dev(seq_offsets, "seq_offsets", True),
+        _rows(q, "q", cfg.q_stride, none), _rows(k, "k", cfg.k_stride, none),
+        _rows(v, "v", cfg.v_stride, none), _dev(log_alpha, "log_alpha", none),
+        _dev(beta, "beta", none), _dev(state, "state"), num_slots, _dev(slots, "slots", True),
+        _dev(o, "o", none), _stream(stream)), "onela_delta_rule_step")
+
+
+def onela_qk_norm_rope_workspace_bytes(cfg: onela_norm_config_t) -> int:
+    return load_library().onela_qk_norm_rope_workspace_bytes(ctypes.byref(cfg))
+
+
+def onela_qk_norm_rope(cfg: onela_norm_config_t, q, k, q_weight, k_weight, positions, cos_sin,
+                       q_out, k_out, stream=None):
+    none = cfg.num_tokens == 0
+    _check(load_library().onela_qk_norm_rope(
+        ctypes.byref(cfg), _rows(q, "q", cfg.q_stride, none),
+        _rows(k, "k", cfg.k_stride, none or cfg.num_k_heads == 0),
+        _dev(q_weight, "q_weight", True), _dev(k_weight, "k_weight", True),
+        _dev(positions, "positions", True), _dev(cos_sin, "cos_sin", True),
+        _dev(q_out, "q_out", none), _dev(k_out, "k_out", none or cfg.num_k_heads == 0),
+        _stream(stream)), "onela_qk_norm_rope")
+
+
+def onela_qk_norm_rope_backward(cfg: onela_norm_config_t, q, k, q_weight, k_weight, positions,
+                                cos_sin, d_q_out, d_k_out, dq, dk, dq_weight=None,
+                                dk_weight=None, workspace=None, workspace_bytes: int = 0,
+                                stream=None):
+    none = cfg.num_tokens == 0
+    nokey = none or cfg.num_k_heads == 0
+    _check(load_library().onela_qk_norm_rope_backward(
+        ctypes.byref(cfg), _rows(q, "q", cfg.q_stride, none), _rows(k, "k", cfg.k_stride, nokey),
+        _dev(q_weight, "q_weight", True), _dev(k_weight, "k_weight", True),
+        _dev(positions, "positions", True), _dev(cos_sin, "cos_sin", True),
+        _dev(d_q_out, "d_q_out", none), _dev(d_k_out, "d_k_out", nokey), _dev(dq, "dq", none),
+        _dev(dk, "dk", nokey), _dev(dq_weight, "dq_weight", True),
+        _dev(dk_weight, "dk_weight", True), _dev(workspace, "workspace", True),
+        int(workspace_bytes), _stream(stream)), "onela_qk_norm_rope_backward")

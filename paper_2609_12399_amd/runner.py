@@ -200,3 +200,157 @@ class BeamSelector:
                               beam_scores, self.parents, self.tokens, self.scores,
                               self.workspace, self.ws_bytes, self.stream)
         return self.parents, self.tokens, self.scores
+
+
+def _io_tensor_dtype(io: str):
+    torch = _torch()
+    return {"bf16": torch.bfloat16, "f32": torch.float32}[io]
+
+
+def _token_stride(x) -> int:
+    """Elements between the tokens of a [tokens][heads][width] view (0: dense)."""
+    return 0 if x.is_contiguous() else x.stride(0)
+
+
+class DeltaRule:
+    """The gated delta rule over whole sequences (onela_delta_rule_forward and, with
+    ``backward``, onela_delta_rule_backward) for fixed sizes: owns the workspace and
+    the output tensors, which every call writes again.
+
+    Sequences are packed: ``seq_offsets`` [N + 1] gives their bounds in the
+    ``total_tokens`` tokens, None N equal lengths.  q, k and v may be views into
+    wider rows (a projection's output)."""
+
+    def __init__(self, num_seqs: int, total_tokens: int, num_qk_heads: int, num_v_heads: int,
+                 d_k: int, d_v: int, io: str = "bf16", scale: float = 1.0,
+                 backward: bool = False, device="cuda:0", stream=None):
+        torch = _torch()
+        self.cfg = ab.make_delta_config(num_seqs, total_tokens, num_qk_heads, num_v_heads, d_k,
+                                        d_v, io, scale)
+        self.ws_bytes = ab.onela_delta_rule_workspace_bytes(self.cfg, backward)
+        if self.ws_bytes == 0:
+            raise ab.OnelaError(ab.ONELA_EINVAL, "onela_delta_rule_workspace_bytes")
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+        self.stream = stream
+        self.is_backward = backward
+
+        def tensor(heads, width, dtype):
+            shape = (total_tokens, heads) + ((width,) if width else ())
+            return torch.empty(shape, dtype=dtype, device=device)
+
+        dt, f32 = _io_tensor_dtype(io), torch.float32
+        state = (num_seqs, num_v_heads, d_v, d_k)
+        if backward:
+            self.dq, self.dk = tensor(num_qk_heads, d_k, dt), tensor(num_qk_heads, d_k, dt)
+            self.dv = tensor(num_v_heads, d_v, dt)
+            self.dlog_alpha, self.dbeta = tensor(num_v_heads, 0, f32), tensor(num_v_heads, 0, f32)
+            self.d_initial_state = torch.empty(state, dtype=f32, device=device)
+        else:
+            self.o = tensor(num_v_heads, d_v, dt)
+            self.final_state = torch.empty(state, dtype=f32, device=device)
+
+    def _set_strides(self, q, k, v):
+        self.cfg.q_stride, self.cfg.k_stride = _token_stride(q), _token_stride(k)
+        self.cfg.v_stride = _token_stride(v)
+
+    def forward(self, q, k, v, log_alpha, beta, seq_offsets=None, initial_state=None):
+        """(o, final_state)"""
+        if self.is_backward:
+            raise ValueError("this object holds the backward call's tensors")
+        self._set_strides(q, k, v)
+        ab.onela_delta_rule_forward(self.cfg, seq_offsets, q, k, v, log_alpha, beta,
+                                    initial_state, self.o, self.final_state, self.workspace,
+                                    self.ws_bytes, self.stream)
+        return self.o, self.final_state
+
+    def backward(self, q, k, v, log_alpha, beta, d_o, seq_offsets=None, initial_state=None,
+                 d_final_state=None):
+        """(dq, dk, dv, dlog_alpha, dbeta, d_initial_state or None without one)"""
+        if not self.is_backward:
+            raise ValueError("this object holds the forward call's tensors")
+        self._set_strides(q, k, v)
+        ds = None if initial_state is None else self.d_initial_state
+        ab.onela_delta_rule_backward(self.cfg, seq_offsets, q, k, v, log_alpha, beta,
+                                     initial_state, d_o, d_final_state, self.dq, self.dk,
+                                     self.dv, self.dlog_alpha, self.dbeta, ds, self.workspace,
+                                     self.ws_bytes, self.stream)
+        return self.dq, self.dk, self.dv, self.dlog_alpha, self.dbeta, ds
+
+
+class DeltaRuleStep:
+    """The recurrent form on a pool of ``num_slots`` states (onela_delta_rule_step) for
+    fixed sizes: owns the output tensor."""
+
+    def __init__(self, num_seqs: int, total_tokens: int, num_qk_heads: int, num_v_heads: int,
+                 d_k: int, d_v: int, io: str, num_slots: int, scale: float = 1.0,
+                 device="cuda:0", stream=None):
+        torch = _torch()
+        self.cfg = ab.make_delta_config(num_seqs, total_tokens, num_qk_heads, num_v_heads, d_k,
+                                        d_v, io, scale)
+        self.num_slots, self.stream = num_slots, stream
+        self.o = torch.empty((total_tokens, num_v_heads, d_v), dtype=_io_tensor_dtype(io),
+                             device=device)
+
+    def step(self, pool, slots, q, k, v, log_alpha, beta, seq_offsets=None):
+        """o; the pool's states move on in place."""
+        self.cfg.q_stride, self.cfg.k_stride = _token_stride(q), _token_stride(k)
+        self.cfg.v_stride = _token_stride(v)
+        ab.onela_delta_rule_step(self.cfg, seq_offsets, q, k, v, log_alpha, beta, pool,
+                                 self.num_slots, slots, self.o, self.stream)
+        return self.o
+
+
+class QkNormRope:
+    """Norm and rotation of queries and keys (onela_qk_norm_rope and, with ``backward``,
+    onela_qk_norm_rope_backward) for fixed sizes: owns the output tensors and the
+    workspace.  q and k may be views into wider rows."""
+
+    def __init__(self, num_tokens: int, num_q_heads: int, num_k_heads: int, head_dim: int,
+                 io: str = "bf16", norm: str = "l2", rotary_dim: int = 0,
+                 rotation: str = "halves", eps: float = 1e-6, backward: bool = False,
+                 device="cuda:0", stream=None):
+        torch = _torch()
+        self.cfg = ab.make_norm_config(num_tokens, num_q_heads, num_k_heads, head_dim, io, norm,
+                                       rotary_dim, max(1, rotary_dim), rotation, eps)
+        self.ws_bytes = ab.onela_qk_norm_rope_workspace_bytes(self.cfg)
+        if self.ws_bytes == 0:
+            raise ab.OnelaError(ab.ONELA_EINVAL, "onela_qk_norm_rope_workspace_bytes")
+        self.stream = stream
+        self.is_backward = backward
+
+        def like(heads):
+            return torch.empty((num_tokens, heads, head_dim), dtype=_io_tensor_dtype(io),
+                               device=device)
+
+        self.q, self.k = like(num_q_heads), like(num_k_heads)
+        if backward:
+            self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+            self.dw = torch.empty((2, head_dim), dtype=torch.float32, device=device)
+
+    def _set(self, q, k, cos_sin):
+        self.cfg.q_stride = _token_stride(q)
+        self.cfg.k_stride = 0 if k is None else _token_stride(k)
+        if cos_sin is not None:
+            self.cfg.table_rows = cos_sin.shape[0]
+
+    def forward(self, q, k, q_weight=None, k_weight=None, positions=None, cos_sin=None):
+        """(q, k) normed and turned"""
+        if self.is_backward:
+            raise ValueError("this object holds the backward call's tensors")
+        self._set(q, k, cos_sin)
+        ab.onela_qk_norm_rope(self.cfg, q, k, q_weight, k_weight, positions, cos_sin, self.q,
+                              self.k, self.stream)
+        return self.q, self.k
+
+    def backward(self, q, k, d_q_out, d_k_out, q_weight=None, k_weight=None, positions=None,
+                 cos_sin=None):
+        """(dq, dk, dq_weight, dk_weight; None for a weight that is not given)"""
+        if not self.is_backward:
+            raise ValueError("this object holds the forward call's tensors")
+        self._set(q, k, cos_sin)
+        dwq = None if q_weight is None else self.dw[0]
+        dwk = None if k_weight is None else self.dw[1]
+        ab.onela_qk_norm_rope_backward(self.cfg, q, k, q_weight, k_weight, positions, cos_sin,
+                                       d_q_out, d_k_out, self.q, self.k, dwq, dwk,
+                                       self.workspace, self.ws_bytes, self.stream)
+        return self.q, self.k, dwq, dwk
