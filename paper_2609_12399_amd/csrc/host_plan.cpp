@@ -285,7 +285,7 @@ onela_status_t check_norm(const onela_norm_config_t* c) {
 }
 
 size_t norm_workspace_bytes(const onela_norm_config_t* c) {
-  return sizeof(float) * 2 * size_t(kNormBlocks) * size_t(c->head_dim);
+  return sizeof(float) * size_t(kNormBlocks) * size_t(c->head_dim);
 }
 
 // ---- per-step protocol --------------------------------------------------------

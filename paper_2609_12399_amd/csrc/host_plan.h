@@ -113,7 +113,7 @@ onela_status_t delta_shape_of(const onela_delta_config_t* cfg, bool ragged, Delt
 size_t delta_workspace_bytes(const DeltaShape& s, bool backward);
 
 // ---- norm and rotation of queries and keys ----------------------------------------
-constexpr int kNormBlocks = 1024;  // most workgroups of the backward pass
+constexpr int kNormBlocks = 2048;  // most workgroups of the backward pass
 onela_status_t check_norm(const onela_norm_config_t* cfg);
 size_t norm_workspace_bytes(const onela_norm_config_t* cfg);
 

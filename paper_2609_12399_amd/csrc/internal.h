@@ -81,7 +81,7 @@ struct NormParams {
   const float* cos_sin;  // [table][rot]: cosines, then sines
   void *qo, *ko, *dq, *dk;  // dense
   float *dwq, *dwk;      // [D] or null
-  float* partial;        // [workgroups][2][D], or null: no weight gradients
+  float* partial;        // [workgroups][D], or null: no weight gradients
   long rows, qs, ks;
   float eps, inv_n;      // 1 / D (RMS) or 1 (L2)
   int HQ, HK, D, rot, table;
