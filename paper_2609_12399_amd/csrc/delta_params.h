@@ -9,6 +9,12 @@
 
 namespace onela {
 
+// Rows of a chunk's gates in the workspace, 64 values each.  Factors of K S^T in X
+// (-gamma), of T X in the state's update (beta sigma), of Q S^T and of P e in the outputs, each
+// with the scales of its operands undone; then single values: gamma_{C-1}, the
+// largest beta sigma, the keys' inverse scale.
+enum { kGateY, kGateZ, kGateO, kGateP, kGateOne };
+
 struct DeltaParams {
   const void *q, *k, *v;    // [total][heads][d], token strides qs, ks, vs
   const void* d_o;          // [total][HV][DV] io dtype (backward)
@@ -32,6 +38,10 @@ struct DeltaParams {
   float* ews;    // [DV][64]  e
   float* dsws;   // [DV][DK]  adjoint of the state after the chunk (backward)
   float* hws;    // [DV][64]  beta times the chunk's own part of dD, then dV (backward)
+  uint4 *kimg, *qimg;  // per (slot, query/key head): the LDS image Swz<DK>[NP] of the fp16
+                       // parts of keys and queries
+  uint4* tp;     // T fragments, two fp16 parts [6][2][64]
+  uint4* pf;     // P fragments, two fp16 parts [6][2][64]
   // recurrent step
   float* pool;       // [num_slots][HV][DV][DK]
   const int* slot;   // [N] or null

@@ -253,10 +253,12 @@ onela_status_t delta_shape_of(const onela_delta_config_t* c, bool ragged, DeltaS
 }
 
 size_t delta_workspace_bytes(const DeltaShape& s, bool backward) {
-  // T, the state at the chunk's entry and e; backward also T reversed, the
-  // adjoint of the state after the chunk and dV (all multiples of 256 bytes)
-  const size_t part = kDeltaFactorBytes + sizeof(float) * size_t(s.dv) * (s.dk + kDeltaChunk);
   const size_t gates = sizeof(float) * kDeltaGates * kDeltaChunk;
+  if (!backward) {
+    const size_t np = s.bf16 ? 1 : 2, image = np * delta_image_bytes(s.dk);
+    return size_t(s.slots) * (s.HV * (gates + 6 * 1024 * 4) + s.HK * 2 * image);
+  }
+  const size_t part = kDeltaFactorBytes + sizeof(float) * size_t(s.dv) * (s.dk + kDeltaChunk);
   return size_t(s.slots) * s.HV * (gates + part * (backward ? 2 : 1));
 }
 

@@ -1397,18 +1397,26 @@ hipError_t launch_delta_rule(const DeltaShape& s, DeltaParams p, bool backward, 
     at += bytes;
     return x;
   };
+  if (!backward) {
+    const size_t np = s.bf16 ? 1 : 2, image = size_t(s.slots) * s.HK * np * delta_image_bytes(s.dk);
+    p.kimg = reinterpret_cast<uint4*>(take(image));
+    p.qimg = reinterpret_cast<uint4*>(take(image));
+    p.tp = reinterpret_cast<uint4*>(take(cus * 6 * 2 * 1024));
+    p.pf = reinterpret_cast<uint4*>(take(cus * 6 * 2 * 1024));
+    p.gates = reinterpret_cast<float*>(take(cus * kDeltaGates * kC * 4));
+    const hipError_t e = launch_delta_prep(s, p, st);
+    return e == hipSuccess ? launch_delta_forward(s, p, st) : e;
+  }
   p.tf = reinterpret_cast<uint4*>(take(cus * kDeltaFactorBytes));
   p.gates = reinterpret_cast<float*>(take(cus * kDeltaGates * kC * 4));
   p.sws = reinterpret_cast<float*>(take(cus * s.dv * s.dk * 4));
   p.ews = reinterpret_cast<float*>(take(cus * s.dv * kC * 4));
-  if (backward) {
-    p.tr = reinterpret_cast<uint4*>(take(cus * kDeltaFactorBytes));
-    p.dsws = reinterpret_cast<float*>(take(cus * s.dv * s.dk * 4));
-    p.hws = reinterpret_cast<float*>(take(cus * s.dv * kC * 4));
-  }
+  p.tr = reinterpret_cast<uint4*>(take(cus * kDeltaFactorBytes));
+  p.dsws = reinterpret_cast<float*>(take(cus * s.dv * s.dk * 4));
+  p.hws = reinterpret_cast<float*>(take(cus * s.dv * kC * 4));
 #define ONELA_DELTA_SHAPE(DK, DV, NP)                      \
   if (s.dk == DK && s.dv == DV && s.bf16 == (NP == 1))     \
-    return backward ? run<DK, DV, NP, true>(p, st) : run<DK, DV, NP, false>(p, st);
+    return run<DK, DV, NP, true>(p, st);
   ONELA_DELTA_SHAPE(32, 32, 1)
   ONELA_DELTA_SHAPE(64, 64, 1)
   ONELA_DELTA_SHAPE(128, 128, 1)

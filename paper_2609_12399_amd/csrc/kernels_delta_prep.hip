@@ -1,0 +1,359 @@
+// The delta rule's chunks, first launch (see kernels_delta.hip): what the chain over the
+// chunks needs of each and that no chunk needs of another.
+#include "delta_tiles.h"
+
+namespace onela {
+namespace {
+
+constexpr int kThreads = 256;
+
+// 8-element pieces of rows [64][DK] of one head on their way: the tensor's own bits.
+template <int DK, int NP>
+struct Pieces {
+  static constexpr int NV = (kC * DK / 8) / kThreads;
+  u32x4 r[NV][NP];
+  __device__ void load(const void* base, long at, long stride, int n, int tid) {
+    constexpr int kIo = NP == 1 ? 2 : 4;
+    const unsigned st = unsigned(stride) * kIo;
+    const auto rs = rows_buffer(base, at * kIo, DK * kIo, st, n);
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const int e = tid + q * kThreads;
+      const unsigned o = unsigned(e / (DK / 8)) * st + (e % (DK / 8)) * (8 * kIo);
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        r[q][i] = __builtin_amdgcn_raw_buffer_load_b128(rs, o + 16 * i, 0, 0);
+    }
+  }
+  // largest magnitude of this thread's elements
+  __device__ float largest() const {
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    if constexpr (NP == 1) {
+      us2 m = {0, 0};
+#pragma unroll
+      for (int q = 0; q < NV; ++q)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          m = __builtin_elementwise_max(m, __builtin_bit_cast(us2, r[q][0][j] & 0x7fff7fffu));
+      return __uint_as_float(unsigned(max(m.x, m.y)) << 16);
+    } else {
+      unsigned m = 0;
+#pragma unroll
+      for (int q = 0; q < NV; ++q)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, r[q][j >> 2][j & 3] & 0x7fffffffu);
+      return __uint_as_float(m);
+    }
+  }
+  // the elements times s as fp16 parts into LDS tiles
+  template <typename Tile>
+  __device__ void store(Tile* tile, float s, int tid) const {
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      const int e = tid + q * kThreads;
+      f32x4 x, y;
+      if constexpr (NP == 1) {
+        const u32x4 v = r[q][0];
+        x = f32x4{bf16_lo_to_float(v.x), bf16_hi_to_float(v.x), bf16_lo_to_float(v.y),
+                  bf16_hi_to_float(v.y)};
+        y = f32x4{bf16_lo_to_float(v.z), bf16_hi_to_float(v.z), bf16_lo_to_float(v.w),
+                  bf16_hi_to_float(v.w)};
+      } else {
+        x = __builtin_bit_cast(f32x4, r[q][0]);
+        y = __builtin_bit_cast(f32x4, r[q][1]);
+      }
+      uint4 p[NP];
+      parts8<NP>(x, y, s, p);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        tile[i].put(e / (DK / 8), e % (DK / 8), __builtin_bit_cast(u32x4, p[i]));
+      }
+    }
+  }
+};
+
+template <int DK, int NP>
+struct PrepLds {
+  union {
+    struct {
+      Swz<DK> K[NP], Q[NP];  // fp16 parts
+    } kq;
+    float T[kC][kC + 4];  // then T
+  };
+  float M[kC][kC + 4];  // B diag(beta); its diagonal blocks then hold those of T
+  double g[kC];         // sums of log2(alpha)
+  alignas(16) float be[kC], bs[kC], it[kC];  // beta, beta sigma, inverse scales of T's rows
+  float most[4][2];     // per wave: the largest key and query
+};
+
+// One chunk of one value head: the fp16 images of its keys and queries, T = (I + B
+// diag(beta))^-1 and P in the fragment order of the chain, and the gates.  Four waves.
+//   The inverse goes by 16-token blocks: the four diagonal blocks by forward
+// substitution, one per wave with a column per lane, then each wave the blocks below
+// the diagonal block of its block column, T_ij = -T_ii sum_k M_ik T_kj, in fp32 matrix
+// instructions with T_kj in the accumulator layout as the next operand.
+//   Bound: latency of that chain; several workgroups share a compute unit.
+template <int DK, int NP>
+__global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaParams p) {
+  __shared__ __align__(16) PrepLds<DK, NP> sh;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, lq = lane >> 4;
+  const long slot = blockIdx.x / p.HV;
+  const int hv = int(blockIdx.x - slot * p.HV), G = p.HV / p.HK, hk = hv / G;
+  const Chunk ch = chunk_of(p, slot);
+  if (ch.n <= 0) return;
+  const long cu = long(blockIdx.x);
+  float* const gt = p.gates + cu * (kDeltaGates * kC);
+  Pieces<DK, NP> rk, rq;
+  rk.load(p.k, ch.t0 * p.ks + hk * DK, p.ks, ch.n, tid);
+  rq.load(p.q, ch.t0 * p.qs + hk * DK, p.qs, ch.n, tid);
+  double g = 0.0, last = 0.0;
+  float be = 0.f;
+  if (w == 0) {  // lane t holds token t
+    const long ti = (ch.t0 + min(lane, ch.n - 1)) * p.HV + hv;
+    float la = p.la[ti];
+    be = p.beta[ti];
+    la = la < -1e5f ? -1e5f : la;
+    g = lane < ch.n ? double(la) * 1.4426950408889634 : 0.0;
+    be = lane < ch.n ? be : 0.f;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const double u = __shfl_up(g, d);
+      if (lane >= d) g += u;
+    }
+    last = __shfl(g, 63);
+    sh.g[lane] = g;
+    sh.be[lane] = be;
+  }
+  {
+    float mk = rk.largest(), mq = rq.largest();
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      mk = fmaxf(mk, __shfl_xor(mk, d));
+      mq = fmaxf(mq, __shfl_xor(mq, d));
+    }
+    if (lane == 0) {
+      sh.most[w][0] = mk;
+      sh.most[w][1] = mq;
+    }
+  }
+  __syncthreads();
+  const float sk = scale_for_rows(fmaxf(fmaxf(sh.most[0][0], sh.most[1][0]),
+                                   fmaxf(sh.most[2][0], sh.most[3][0])));
+  const float sq = scale_for_rows(fmaxf(fmaxf(sh.most[0][1], sh.most[1][1]),
+                                   fmaxf(sh.most[2][1], sh.most[3][1])));
+  const float ik = inverse_pow2(sk), iq = inverse_pow2(sq);
+  rk.store(sh.kq.K, sk, tid);
+  rq.store(sh.kq.Q, sq, tid);
+  if (w == 0) {
+    const float gam = exp2_fast(float(g)), bs = be * exp2_fast(float(last - g));
+    gt[kGateY * kC + lane] = -gam * ik;
+    sh.bs[lane] = bs;
+    gt[kGateO * kC + lane] = p.scale * gam * iq;
+    if (lane == 0) {
+      gt[kGateOne * kC] = exp2_fast(float(last));
+      gt[kGateOne * kC + 2] = ik;
+    }
+  }
+  __syncthreads();
+  if (hv == hk * G) {  // one of the group's heads keeps the images, as they stand in LDS
+    constexpr int NI = sizeof(sh.kq.K) / 16;
+    uint4* const ki = p.kimg + (slot * p.HK + hk) * NI;
+    uint4* const qi = p.qimg + (slot * p.HK + hk) * NI;
+    for (int e = tid; e < NI; e += kThreads) {
+      ki[e] = reinterpret_cast<const uint4*>(sh.kq.K)[e];
+      qi[e] = reinterpret_cast<const uint4*>(sh.kq.Q)[e];
+    }
+  }
+  const int kb = Swz<DK>::off(lr, lq);
+  constexpr int KR = 32 * Swz<DK>::LD;
+  const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+  // rows x of a against rows y of b, 16 each: lane (lr, lq) holds (16 a + 4 lq + i, 16 b + lr)
+  auto dots = [&](const Swz<DK>* x, int a, const Swz<DK>* y, int b) {
+    f32x4 acc[2] = {z, z};
+#pragma unroll
+    for (int h = 0; h < DK / 32; ++h) {
+      uint4 u[NP], v[NP];
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        u[i] = row_frag(x[i], kb, 2 * h, 2 * h + 1, KR * a);
+        v[i] = row_frag(y[i], kb, 2 * h, 2 * h + 1, KR * b);
+      }
+      for_products<NP, NP>([&](int i, int j) { acc[h & 1] = mfma_f16(u[i], v[j], acc[h & 1]); });
+    }
+    return acc[0] + acc[1];
+  };
+  // M(i, j) = Gamma(i, j) (k_i . k_j) beta_j of a tile, 0 on and above the diagonal
+  auto tile = [&](int a, int b) {
+    const f32x4 acc = dots(sh.kq.K, a, sh.kq.K, b);
+    const int j = 16 * b + lr;
+    const double gj = sh.g[j];
+    const float bk = sh.be[j] * ik * ik;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int i = 16 * a + 4 * lq + q;
+      sh.M[i][j] = j < i ? exp2_fast(float(sh.g[i] - gj)) * bk * acc[q] : 0.f;
+    }
+  };
+  // (1, 0), (2, 0), (2, 1), (3, 0); (3, 1), (3, 2); the diagonal block w
+  tile(w == 0 ? 1 : w < 3 ? 2 : 3, w == 2 ? 1 : 0);
+  if (w < 2) tile(3, w + 1);
+  tile(w, w);
+  // row tile of P per wave: the longer rows to the waves with fewer tiles above
+  const int pa = w == 0 ? 2 : w == 1 ? 1 : w == 2 ? 3 : 0;
+  f32x4 pt[4];
+  {
+    // P(t, j) = scale Gamma(t, j) (q_t . k_j) beta_j, j <= t, of 16 tokens t per wave: a lane
+    // holds four neighbouring j of one token, half a fragment
+    const int t = 16 * pa + lr;
+    const double gq = sh.g[t];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      pt[b] = z;
+      if (b > pa) continue;
+      const f32x4 acc = dots(sh.kq.K, b, sh.kq.Q, pa);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int j = 16 * b + 4 * lq + q;
+        pt[b][q] = j <= t ? p.scale * (ik * iq) * exp2_fast(float(gq - sh.g[j])) * sh.be[j] * acc[q]
+                          : 0.f;
+      }
+    }
+  }
+  f32x4 tc[4];  // blocks (w + d, w) of T, rows 4 lq + component, column lr
+  {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    float x[16];
+    f32x4 m[16][4];
+#pragma unroll
+    for (int i = 1; i < 16; ++i)
+#pragma unroll
+      for (int q = 0; q < (i + 3) / 4; ++q)
+        m[i][q] = *reinterpret_cast<const f32x4*>(&sh.M[16 * w + i][16 * w + 4 * q]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = i == lr ? 1.f : 0.f;
+#pragma unroll
+    for (int j = 0; j < 15; ++j)
+#pragma unroll
+      for (int i = j + 1; i < 16; ++i) x[i] = fmaf(-m[i][j >> 2][j & 3], x[j], x[i]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      tc[0][q] = lq == 0 ? x[q] : lq == 1 ? x[4 + q] : lq == 2 ? x[8 + q] : x[12 + q];
+      sh.M[16 * w + 4 * lq + q][16 * w + lr] = tc[0][q];
+    }
+  }
+  __syncthreads();  // (keys and queries are not read any more: T takes their place)
+#pragma unroll
+  for (int d = 1; d < 4; ++d) {
+    if (w + d >= 4) break;
+    const int i = w + d;
+    f32x4 a0 = z, a1 = z;
+#pragma unroll
+    for (int e = 0; e < d; ++e) {
+      const f32x4 mm = *reinterpret_cast<const f32x4*>(&sh.M[16 * i + lr][16 * (w + e) + 4 * lq]);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        f32x4& acc = (s & 1) ? a1 : a0;
+        acc = mfma4(mm[s], tc[e][s], acc);
+      }
+    }
+    const f32x4 pr = a0 + a1;
+    const f32x4 tt = *reinterpret_cast<const f32x4*>(&sh.M[16 * i + lr][16 * i + 4 * lq]);
+    f32x4 b0 = z, b1 = z;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      f32x4& acc = (s & 1) ? b1 : b0;
+      acc = mfma4(tt[s], pr[s], acc);
+    }
+    tc[d] = -(b0 + b1);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sh.T[16 * i + 4 * lq + q][16 * w + lr] = tc[d][q];
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    sh.T[16 * w + 4 * lq + q][16 * w + lr] = tc[0][q];
+    // the blocks above the diagonal that a 32-token step covers
+    if (w & 1) sh.T[16 * (w - 1) + 4 * lq + q][16 * w + lr] = 0.f;
+  }
+  __syncthreads();
+  {
+    // T fragments of row tile w: a lane holds row 16 w + lr and the columns 32 h + 4 lq +
+    // 0..3 and 32 h + 16 + 4 lq + 0..3, the order in which the chain's accumulators hold
+    // the tokens; each row scaled by its largest element
+    const int t = 16 * w + lr, c0 = 4 * lq;
+    f32x4 x[4];
+    float most = 0.f;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      if (b >= 2 && w < 2) break;
+      x[b] = *reinterpret_cast<const f32x4*>(&sh.T[t][16 * b + c0]);
+      most = max4abs(most, x[b]);
+    }
+    const float s = scale_for(max_over_rows(most));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (h > 0 && w < 2) break;
+      const int f = w < 2 ? w : 2 * w - 2 + h;
+      uint4 part[2];
+      parts8<2>(x[2 * h], x[2 * h + 1], s, part);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) p.tp[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
+    }
+    if (lq == 0) {  // the rows' scales go into the gates that their e passes
+      sh.it[t] = inverse_pow2(s);
+      gt[kGateZ * kC + t] = sh.bs[t] * inverse_pow2(s);
+    }
+  }
+  __syncthreads();
+  if (w == 3) {  // (the wave with the shortest rows of P)
+    float most = fabsf(sh.bs[lane] * sh.it[lane]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
+    if (lane == 0) gt[kGateOne * kC + 1] = most;
+  }
+  {
+    const int t = 16 * pa + lr;
+    float most = 0.f;
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      pt[b] *= *reinterpret_cast<const f32x4*>(&sh.it[16 * b + 4 * lq]);
+      most = max4abs(most, pt[b]);
+    }
+    const float s = scale_for(max_over_rows(most));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (h > 0 && pa < 2) break;
+      const int f = pa < 2 ? pa : 2 * pa - 2 + h;
+      uint4 part[2];
+      parts8<2>(pt[2 * h], pt[2 * h + 1], s, part);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) p.pf[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
+    }
+    if (lq == 0) gt[kGateP * kC + t] = inverse_pow2(s);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_delta_prep(const DeltaShape& s, const DeltaParams& p, hipStream_t st) {
+  const unsigned cus = unsigned(p.slots) * unsigned(p.HV);
+  if (!cus) return hipSuccess;
+#define ONELA_DELTA_PREP(DK, NP)                          \
+  if (s.dk == DK && s.bf16 == (NP == 1)) {                \
+    delta_prep_kernel<DK, NP><<<cus, kThreads, 0, st>>>(p); \
+    return hipGetLastError();                             \
+  }
+  ONELA_DELTA_PREP(32, 1)
+  ONELA_DELTA_PREP(64, 1)
+  ONELA_DELTA_PREP(128, 1)
+  ONELA_DELTA_PREP(256, 1)
+  ONELA_DELTA_PREP(32, 2)
+  ONELA_DELTA_PREP(64, 2)
+  ONELA_DELTA_PREP(128, 2)
+#undef ONELA_DELTA_PREP
+  return hipErrorInvalidValue;
+}
+
+}  // namespace onela

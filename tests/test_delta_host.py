@@ -97,13 +97,15 @@ def test_step_arguments_refused(lib):
 
 
 def test_delta_workspace_bytes(lib):
-    """Per chunk slot and value head: T (18 KiB), five gate rows, the state and e; backward
-    T, the state's adjoint and dV again.  Slots for sequences of any lengths."""
-    slots, HV, d = 128 // 64 + 2, 4, 128
-    part = 18 * 1024 + 4 * d * d + 4 * d * 64
-    assert ab.onela_delta_rule_workspace_bytes(delta()) == slots * HV * (part + 5 * 64 * 4)
-    assert ab.onela_delta_rule_workspace_bytes(delta(), True) == slots * HV * (2 * part +
-                                                                               5 * 64 * 4)
+    """Grows with the chunk slots that sequences of any lengths can need (one more than
+    their whole chunks for each), not with their number alone; backward needs more."""
+    one = ab.onela_delta_rule_workspace_bytes(delta(num_seqs=1, total_tokens=0))
+    assert one > 0 and one % 256 == 0
+    for seqs, tokens in ((2, 128), (5, 63), (1, 64 * 100 + 1)):
+        cfg = delta(num_seqs=seqs, total_tokens=tokens)
+        assert ab.onela_delta_rule_workspace_bytes(cfg) == one * (tokens // 64 + seqs)
+        assert ab.onela_delta_rule_workspace_bytes(cfg, True) > \
+            ab.onela_delta_rule_workspace_bytes(cfg)
 
 
 BAD_NORM = [dict(num_tokens=-1), dict(num_tokens=1 << 31), dict(num_q_heads=0),
