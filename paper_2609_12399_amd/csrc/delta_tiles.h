@@ -219,6 +219,16 @@ __device__ inline float max4abs(float m, const f32x4& x) {
   return fmaxf(m, fmaxf(fabsf(x.z), fabsf(x.w)));
 }
 
+// Maximum over the wave, in every lane.
+__device__ inline float max_over_rows(float m);
+__device__ inline float wave_max(float m) {
+  m = fmaxf(m, dpp<0xB1>(m));   // quad_perm [1,0,3,2]
+  m = fmaxf(m, dpp<0x4E>(m));   // quad_perm [2,3,0,1]
+  m = fmaxf(m, dpp<0x141>(m));  // row_half_mirror
+  m = fmaxf(m, dpp<0x140>(m));  // row_mirror
+  return max_over_rows(m);
+}
+
 // Maximum (sum) over the four lanes lr, lr + 16, lr + 32, lr + 48.
 __device__ inline float max_over_rows(float m) {
   const unsigned v = __float_as_uint(m);

@@ -74,16 +74,20 @@ struct Pieces {
 
 template <int DK, int NP>
 struct PrepLds {
-  union {
-    struct {
-      Swz<DK> K[NP], Q[NP];  // fp16 parts
-    } kq;
-    float T[kC][kC + 4];  // then T
+  struct KQ {
+    Swz<DK> K[NP], Q[NP];  // fp16 parts
   };
-  float M[kC][kC + 4];  // B diag(beta); its diagonal blocks then hold those of T
-  double g[kC];         // sums of log2(alpha)
-  alignas(16) float be[kC], bs[kC], it[kC];  // beta, beta sigma, inverse scales of T's rows
-  float most[4][2];     // per wave: the largest key and query
+  struct MT {
+    float T[kC][kC + 4];
+    float M[kC][kC + 4];  // B diag(beta); its diagonal blocks then hold those of T
+  };
+  union {
+    KQ kq;
+    MT mt;  // after the products of keys and queries
+  };
+  double g[kC];                          // sums of log2(alpha)
+  alignas(16) float be[kC], bs[kC], ip[kC];  // beta, beta sigma, inverse scales of P's rows
+  float most[4][3];                      // per wave: the largest key, query, element of T
 };
 
 // One chunk of one value head: the fp16 images of its keys and queries, T = (I + B
@@ -92,9 +96,10 @@ struct PrepLds {
 // substitution, one per wave with a column per lane, then each wave the blocks below
 // the diagonal block of its block column, T_ij = -T_ii sum_k M_ik T_kj, in fp32 matrix
 // instructions with T_kj in the accumulator layout as the next operand.
-//   Bound: latency of that chain; several workgroups share a compute unit.
+//   Bound: latency of that chain, and the writes; the workgroup's LDS (36 KB up to d_k =
+// 128) and registers are held to four workgroups per compute unit.
 template <int DK, int NP>
-__global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaParams p) {
+__global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_kernel(DeltaParams p) {
   __shared__ __align__(16) PrepLds<DK, NP> sh;
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -105,57 +110,42 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaParams p) {
   if (ch.n <= 0) return;
   const long cu = long(blockIdx.x);
   float* const gt = p.gates + cu * (kDeltaGates * kC);
-  Pieces<DK, NP> rk, rq;
-  rk.load(p.k, ch.t0 * p.ks + hk * DK, p.ks, ch.n, tid);
-  rq.load(p.q, ch.t0 * p.qs + hk * DK, p.qs, ch.n, tid);
-  double g = 0.0, last = 0.0;
-  float be = 0.f;
-  if (w == 0) {  // lane t holds token t
-    const long ti = (ch.t0 + min(lane, ch.n - 1)) * p.HV + hv;
-    float la = p.la[ti];
-    be = p.beta[ti];
-    la = la < -1e5f ? -1e5f : la;
-    g = lane < ch.n ? double(la) * 1.4426950408889634 : 0.0;
-    be = lane < ch.n ? be : 0.f;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const double u = __shfl_up(g, d);
-      if (lane >= d) g += u;
-    }
-    last = __shfl(g, 63);
-    sh.g[lane] = g;
-    sh.be[lane] = be;
-  }
+  const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+  float sk, sq;
   {
-    float mk = rk.largest(), mq = rq.largest();
+    Pieces<DK, NP> rk, rq;
+    rk.load(p.k, ch.t0 * p.ks + hk * DK, p.ks, ch.n, tid);
+    rq.load(p.q, ch.t0 * p.qs + hk * DK, p.qs, ch.n, tid);
+    if (w == 0) {  // lane t holds token t
+      const long ti = (ch.t0 + min(lane, ch.n - 1)) * p.HV + hv;
+      float la = p.la[ti];
+      float be = p.beta[ti];
+      la = la < -1e5f ? -1e5f : la;
+      double g = lane < ch.n ? double(la) * 1.4426950408889634 : 0.0;
+      be = lane < ch.n ? be : 0.f;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      mk = fmaxf(mk, __shfl_xor(mk, d));
-      mq = fmaxf(mq, __shfl_xor(mq, d));
+      for (int d = 1; d < 64; d *= 2) {
+        const double u = __shfl_up(g, d);
+        if (lane >= d) g += u;
+      }
+      sh.g[lane] = g;
+      sh.be[lane] = be;
+      sh.bs[lane] = be * exp2_fast(float(__shfl(g, 63) - g));
     }
+    const float mk = wave_max(rk.largest()), mq = wave_max(rq.largest());
     if (lane == 0) {
       sh.most[w][0] = mk;
       sh.most[w][1] = mq;
     }
+    __syncthreads();
+    sk = scale_for_rows(fmaxf(fmaxf(sh.most[0][0], sh.most[1][0]),
+                              fmaxf(sh.most[2][0], sh.most[3][0])));
+    sq = scale_for_rows(fmaxf(fmaxf(sh.most[0][1], sh.most[1][1]),
+                              fmaxf(sh.most[2][1], sh.most[3][1])));
+    rk.store(sh.kq.K, sk, tid);
+    rq.store(sh.kq.Q, sq, tid);
   }
-  __syncthreads();
-  const float sk = scale_for_rows(fmaxf(fmaxf(sh.most[0][0], sh.most[1][0]),
-                                   fmaxf(sh.most[2][0], sh.most[3][0])));
-  const float sq = scale_for_rows(fmaxf(fmaxf(sh.most[0][1], sh.most[1][1]),
-                                   fmaxf(sh.most[2][1], sh.most[3][1])));
   const float ik = inverse_pow2(sk), iq = inverse_pow2(sq);
-  rk.store(sh.kq.K, sk, tid);
-  rq.store(sh.kq.Q, sq, tid);
-  if (w == 0) {
-    const float gam = exp2_fast(float(g)), bs = be * exp2_fast(float(last - g));
-    gt[kGateY * kC + lane] = -gam * ik;
-    sh.bs[lane] = bs;
-    gt[kGateO * kC + lane] = p.scale * gam * iq;
-    if (lane == 0) {
-      gt[kGateOne * kC] = exp2_fast(float(last));
-      gt[kGateOne * kC + 2] = ik;
-    }
-  }
   __syncthreads();
   if (hv == hk * G) {  // one of the group's heads keeps the images, as they stand in LDS
     constexpr int NI = sizeof(sh.kq.K) / 16;
@@ -168,7 +158,6 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaParams p) {
   }
   const int kb = Swz<DK>::off(lr, lq);
   constexpr int KR = 32 * Swz<DK>::LD;
-  const f32x4 z = {0.f, 0.f, 0.f, 0.f};
   // rows x of a against rows y of b, 16 each: lane (lr, lq) holds (16 a + 4 lq + i, 16 b + lr)
   auto dots = [&](const Swz<DK>* x, int a, const Swz<DK>* y, int b) {
     f32x4 acc[2] = {z, z};
@@ -184,142 +173,28 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaParams p) {
     }
     return acc[0] + acc[1];
   };
-  // M(i, j) = Gamma(i, j) (k_i . k_j) beta_j of a tile, 0 on and above the diagonal
-  auto tile = [&](int a, int b) {
-    const f32x4 acc = dots(sh.kq.K, a, sh.kq.K, b);
-    const int j = 16 * b + lr;
-    const double gj = sh.g[j];
-    const float bk = sh.be[j] * ik * ik;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int i = 16 * a + 4 * lq + q;
-      sh.M[i][j] = j < i ? exp2_fast(float(sh.g[i] - gj)) * bk * acc[q] : 0.f;
-    }
-  };
-  // (1, 0), (2, 0), (2, 1), (3, 0); (3, 1), (3, 2); the diagonal block w
-  tile(w == 0 ? 1 : w < 3 ? 2 : 3, w == 2 ? 1 : 0);
-  if (w < 2) tile(3, w + 1);
-  tile(w, w);
-  // row tile of P per wave: the longer rows to the waves with fewer tiles above
-  const int pa = w == 0 ? 2 : w == 1 ? 1 : w == 2 ? 3 : 0;
-  f32x4 pt[4];
   {
-    // P(t, j) = scale Gamma(t, j) (q_t . k_j) beta_j, j <= t, of 16 tokens t per wave: a lane
-    // holds four neighbouring j of one token, half a fragment
+    // P(t, j) = scale Gamma(t, j) (q_t . k_j) beta_j, j <= t, of 16 tokens t per wave (the
+    // longer rows to the waves with fewer tiles of M): a lane holds four neighbouring j
+    // of one token, half a fragment
+    const int pa = w == 0 ? 2 : w == 1 ? 1 : w == 2 ? 3 : 0;
     const int t = 16 * pa + lr;
     const double gq = sh.g[t];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      pt[b] = z;
-      if (b > pa) continue;
-      const f32x4 acc = dots(sh.kq.K, b, sh.kq.Q, pa);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int j = 16 * b + 4 * lq + q;
-        pt[b][q] = j <= t ? p.scale * (ik * iq) * exp2_fast(float(gq - sh.g[j])) * sh.be[j] * acc[q]
-                          : 0.f;
-      }
-    }
-  }
-  f32x4 tc[4];  // blocks (w + d, w) of T, rows 4 lq + component, column lr
-  {
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    float x[16];
-    f32x4 m[16][4];
-#pragma unroll
-    for (int i = 1; i < 16; ++i)
-#pragma unroll
-      for (int q = 0; q < (i + 3) / 4; ++q)
-        m[i][q] = *reinterpret_cast<const f32x4*>(&sh.M[16 * w + i][16 * w + 4 * q]);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = i == lr ? 1.f : 0.f;
-#pragma unroll
-    for (int j = 0; j < 15; ++j)
-#pragma unroll
-      for (int i = j + 1; i < 16; ++i) x[i] = fmaf(-m[i][j >> 2][j & 3], x[j], x[i]);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      tc[0][q] = lq == 0 ? x[q] : lq == 1 ? x[4 + q] : lq == 2 ? x[8 + q] : x[12 + q];
-      sh.M[16 * w + 4 * lq + q][16 * w + lr] = tc[0][q];
-    }
-  }
-  __syncthreads();  // (keys and queries are not read any more: T takes their place)
-#pragma unroll
-  for (int d = 1; d < 4; ++d) {
-    if (w + d >= 4) break;
-    const int i = w + d;
-    f32x4 a0 = z, a1 = z;
-#pragma unroll
-    for (int e = 0; e < d; ++e) {
-      const f32x4 mm = *reinterpret_cast<const f32x4*>(&sh.M[16 * i + lr][16 * (w + e) + 4 * lq]);
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        f32x4& acc = (s & 1) ? a1 : a0;
-        acc = mfma4(mm[s], tc[e][s], acc);
-      }
-    }
-    const f32x4 pr = a0 + a1;
-    const f32x4 tt = *reinterpret_cast<const f32x4*>(&sh.M[16 * i + lr][16 * i + 4 * lq]);
-    f32x4 b0 = z, b1 = z;
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      f32x4& acc = (s & 1) ? b1 : b0;
-      acc = mfma4(tt[s], pr[s], acc);
-    }
-    tc[d] = -(b0 + b1);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) sh.T[16 * i + 4 * lq + q][16 * w + lr] = tc[d][q];
-  }
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    sh.T[16 * w + 4 * lq + q][16 * w + lr] = tc[0][q];
-    // the blocks above the diagonal that a 32-token step covers
-    if (w & 1) sh.T[16 * (w - 1) + 4 * lq + q][16 * w + lr] = 0.f;
-  }
-  __syncthreads();
-  {
-    // T fragments of row tile w: a lane holds row 16 w + lr and the columns 32 h + 4 lq +
-    // 0..3 and 32 h + 16 + 4 lq + 0..3, the order in which the chain's accumulators hold
-    // the tokens; each row scaled by its largest element
-    const int t = 16 * w + lr, c0 = 4 * lq;
+    const float c = p.scale * (ik * iq);
     f32x4 x[4];
     float most = 0.f;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      if (b >= 2 && w < 2) break;
-      x[b] = *reinterpret_cast<const f32x4*>(&sh.T[t][16 * b + c0]);
+      x[b] = z;
+      if (b > pa) continue;
+      const f32x4 acc = dots(sh.kq.K, b, sh.kq.Q, pa);
+      const f32x4 be = *reinterpret_cast<const f32x4*>(&sh.be[16 * b + 4 * lq]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int j = 16 * b + 4 * lq + q;
+        x[b][q] = j <= t ? c * exp2_fast(float(gq - sh.g[j])) * be[q] * acc[q] : 0.f;
+      }
       most = max4abs(most, x[b]);
-    }
-    const float s = scale_for(max_over_rows(most));
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (h > 0 && w < 2) break;
-      const int f = w < 2 ? w : 2 * w - 2 + h;
-      uint4 part[2];
-      parts8<2>(x[2 * h], x[2 * h + 1], s, part);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) p.tp[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
-    }
-    if (lq == 0) {  // the rows' scales go into the gates that their e passes
-      sh.it[t] = inverse_pow2(s);
-      gt[kGateZ * kC + t] = sh.bs[t] * inverse_pow2(s);
-    }
-  }
-  __syncthreads();
-  if (w == 3) {  // (the wave with the shortest rows of P)
-    float most = fabsf(sh.bs[lane] * sh.it[lane]);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-    if (lane == 0) gt[kGateOne * kC + 1] = most;
-  }
-  {
-    const int t = 16 * pa + lr;
-    float most = 0.f;
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      pt[b] *= *reinterpret_cast<const f32x4*>(&sh.it[16 * b + 4 * lq]);
-      most = max4abs(most, pt[b]);
     }
     const float s = scale_for(max_over_rows(most));
 #pragma unroll
@@ -327,11 +202,138 @@ __global__ __launch_bounds__(kThreads) void delta_prep_kernel(DeltaParams p) {
       if (h > 0 && pa < 2) break;
       const int f = pa < 2 ? pa : 2 * pa - 2 + h;
       uint4 part[2];
-      parts8<2>(pt[2 * h], pt[2 * h + 1], s, part);
+      parts8<2>(x[2 * h], x[2 * h + 1], s, part);
 #pragma unroll
       for (int i = 0; i < 2; ++i) p.pf[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
     }
-    if (lq == 0) gt[kGateP * kC + t] = inverse_pow2(s);
+    if (lq == 0) sh.ip[t] = inverse_pow2(s);
+  }
+  {
+    // M(i, j) = Gamma(i, j) (k_i . k_j) beta_j, 0 on and above the diagonal: the tiles (1, 0),
+    // (2, 0), (2, 1), (3, 0); (3, 1), (3, 2); the diagonal block w
+    f32x4 m[3];
+    auto tile = [&](int a, int b) {
+      f32x4 acc = dots(sh.kq.K, a, sh.kq.K, b);
+      const int j = 16 * b + lr;
+      const double gj = sh.g[j];
+      const float bk = sh.be[j] * ik * ik;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int i = 16 * a + 4 * lq + q;
+        acc[q] = j < i ? exp2_fast(float(sh.g[i] - gj)) * bk * acc[q] : 0.f;
+      }
+      return acc;
+    };
+    const int a0 = w == 0 ? 1 : w < 3 ? 2 : 3, b0 = w == 2 ? 1 : 0;
+    m[0] = tile(a0, b0);
+    m[1] = tile(w, w);
+    if (w < 2) m[2] = tile(3, w + 1);
+    __syncthreads();  // keys and queries are not read any more: M and T take their place
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      sh.mt.M[16 * a0 + 4 * lq + q][16 * b0 + lr] = m[0][q];
+      sh.mt.M[16 * w + 4 * lq + q][16 * w + lr] = m[1][q];
+      if (w < 2) sh.mt.M[48 + 4 * lq + q][16 * (w + 1) + lr] = m[2][q];
+    }
+  }
+  auto& M = sh.mt.M;
+  auto& T = sh.mt.T;
+  f32x4 tc[4];  // blocks (w + d, w) of T, rows 4 lq + component, column lr
+  {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = i == lr ? 1.f : 0.f;
+    // row i of the inverse from the rows before it
+#pragma unroll
+    for (int i = 1; i < 16; ++i) {
+      f32x4 m[4];
+#pragma unroll
+      for (int q = 0; q < (i + 3) / 4; ++q)
+        m[q] = *reinterpret_cast<const f32x4*>(&M[16 * w + i][16 * w + 4 * q]);
+      float s0 = x[i], s1 = 0.f;
+#pragma unroll
+      for (int j = 0; j < i; ++j) {
+        float& s = (j & 1) ? s1 : s0;
+        s = fmaf(-m[j >> 2][j & 3], x[j], s);
+      }
+      x[i] = s0 + s1;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      tc[0][q] = lq == 0 ? x[q] : lq == 1 ? x[4 + q] : lq == 2 ? x[8 + q] : x[12 + q];
+      M[16 * w + 4 * lq + q][16 * w + lr] = tc[0][q];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int d = 1; d < 4; ++d) {
+    if (w + d >= 4) break;
+    const int i = w + d;
+    f32x4 a0 = z, a1 = z;
+#pragma unroll
+    for (int e = 0; e < d; ++e) {
+      const f32x4 mm = *reinterpret_cast<const f32x4*>(&M[16 * i + lr][16 * (w + e) + 4 * lq]);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        f32x4& acc = (s & 1) ? a1 : a0;
+        acc = mfma4(mm[s], tc[e][s], acc);
+      }
+    }
+    const f32x4 pr = a0 + a1;
+    const f32x4 tt = *reinterpret_cast<const f32x4*>(&M[16 * i + lr][16 * i + 4 * lq]);
+    f32x4 b0 = z, b1 = z;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      f32x4& acc = (s & 1) ? b1 : b0;
+      acc = mfma4(tt[s], pr[s], acc);
+    }
+    tc[d] = -(b0 + b1);
+  }
+  {
+    float most = 0.f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      if (w + d >= 4) break;
+      most = max4abs(most, tc[d]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) T[16 * (w + d) + 4 * lq + q][16 * w + lr] = tc[d][q];
+    }
+    most = wave_max(most);
+    if (lane == 0) sh.most[w][2] = most;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)  // the blocks above the diagonal that a 32-token step covers
+      if (w & 1) T[16 * (w - 1) + 4 * lq + q][16 * w + lr] = 0.f;
+  }
+  __syncthreads();
+  const float s = scale_for(fmaxf(fmaxf(sh.most[0][2], sh.most[1][2]),
+                                  fmaxf(sh.most[2][2], sh.most[3][2])));
+  // T fragments of row tile w: a lane holds row 16 w + lr and the columns 32 h + 4 lq +
+  // 0..3 and 32 h + 16 + 4 lq + 0..3, the order in which the chain's accumulators hold
+  // the tokens
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (h > 0 && w < 2) break;
+    const int f = w < 2 ? w : 2 * w - 2 + h, t = 16 * w + lr, c0 = 32 * h + 4 * lq;
+    uint4 part[2];
+    parts8<2>(*reinterpret_cast<const f32x4*>(&T[t][c0]),
+              *reinterpret_cast<const f32x4*>(&T[t][c0 + 16]), s, part);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p.tp[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
+  }
+  if (w == 0) {
+    const float it = inverse_pow2(s), gam = exp2_fast(float(sh.g[lane])), bs = sh.bs[lane] * it;
+    gt[kGateY * kC + lane] = -gam * ik;
+    gt[kGateO * kC + lane] = p.scale * gam * iq;
+    gt[kGateZ * kC + lane] = bs;
+    gt[kGateP * kC + lane] = sh.ip[lane] * it;
+    const float most = wave_max(fabsf(bs));
+    if (lane == 0) {
+      gt[kGateOne * kC] = exp2_fast(float(sh.g[63]));
+      gt[kGateOne * kC + 1] = most;
+      gt[kGateOne * kC + 2] = ik;
+    }
   }
 }
 
