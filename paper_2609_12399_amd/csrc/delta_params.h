@@ -42,6 +42,11 @@ struct DeltaParams {
                        // parts of keys and queries
   uint4* tp;     // T fragments, two fp16 parts [6][2][64]
   uint4* pf;     // P fragments, two fp16 parts [6][2][64]
+  // segments of the chain
+  int cps, nseg_l;     // chunks per segment; segments of a sequence of L tokens
+  long seg_slots;
+  float* segs;         // [slot][HV][DV][DK]  the state after each segment but a sequence's last
+  float* sega;         // [slot][HV][DK][DK]  transition matrices of the segments between
   // recurrent step
   float* pool;       // [num_slots][HV][DV][DK]
   const int* slot;   // [N] or null

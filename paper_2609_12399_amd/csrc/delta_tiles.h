@@ -65,6 +65,32 @@ __device__ inline Chunk chunk_of(const DeltaParams& p, long slot) {
   return {s.t0 + c * kC, int(min(long(kC), s.len - c * kC))};
 }
 
+// Segments: stretches of p.cps chunks that run at once, slots as for chunks (without
+// segments p.cps is larger than any sequence and slot n is sequence n).
+struct Segment {
+  int n, j, nseg;  // sequence, number within it (no segment outside [0, nseg)), how many it has
+  Seq sq;
+  int cb, ce;      // chunks
+};
+__device__ inline int segments_of(const DeltaParams& p, const Seq& sq) {
+  return max(((sq.len + kC - 1) / kC + p.cps - 1) / p.cps, 1);
+}
+__device__ inline long first_segment(const DeltaParams& p, const Seq& sq, int n) {
+  return p.offsets ? sq.slot / p.cps + n : long(n) * p.nseg_l;
+}
+__device__ inline Segment segment_of(const DeltaParams& p, long slot) {
+  Segment s;
+  s.n = p.offsets ? find_seq(p, slot, [&](long o, int n) { return (o / kC + n) / p.cps + n; })
+                  : int(slot / p.nseg_l);
+  s.sq = seq_of(p, s.n);
+  s.nseg = segments_of(p, s.sq);
+  const long j = slot - first_segment(p, s.sq, s.n);
+  s.j = j >= 0 && j < s.nseg ? int(j) : -1;
+  s.cb = s.j * p.cps;
+  s.ce = int(min(long(s.cb) + p.cps, long(s.sq.len + kC - 1) / kC));
+  return s;
+}
+
 // ---- memory ------------------------------------------------------------------------
 
 __device__ inline __amdgpu_buffer_rsrc_t buffer(const void* base, unsigned bytes) {
@@ -214,9 +240,13 @@ __device__ inline void for_products(F&& f) {
   f(0, 0);
 }
 
+// max(m, |x|) of values m >= 0 (as medians and integers: fmaxf would first make each operand
+// canonical).
 __device__ inline float max4abs(float m, const f32x4& x) {
-  m = fmaxf(m, fmaxf(fabsf(x.x), fabsf(x.y)));
-  return fmaxf(m, fmaxf(fabsf(x.z), fabsf(x.w)));
+  const float inf = __builtin_inff();
+  const unsigned a = __float_as_uint(__builtin_amdgcn_fmed3f(fabsf(x.x), fabsf(x.y), inf));
+  const unsigned b = __float_as_uint(__builtin_amdgcn_fmed3f(fabsf(x.z), fabsf(x.w), inf));
+  return __uint_as_float(max(__float_as_uint(m), max(a, b)));
 }
 
 // Maximum over the wave, in every lane.

@@ -252,11 +252,59 @@ onela_status_t delta_shape_of(const onela_delta_config_t* c, bool ragged, DeltaS
   return ONELA_OK;
 }
 
+namespace {
+// Segment slots that sequences of any lengths can need, and their bytes: a state and
+// a transition matrix each.
+long segment_slots(const DeltaShape& s, long cps) { return s.slots / cps + s.N; }
+size_t segment_bytes(const DeltaShape& s) {
+  return sizeof(float) * size_t(s.HV) * s.dk * (s.dv + s.dk);
+}
+// Most segment slots that are used, whatever the device: segments of two chunks, and at most
+// some 1024 workgroups with outputs at once (more do not run faster).
+long most_segment_slots(const DeltaShape& s) {
+  const long groups = std::max(1, s.dv / 128);
+  return std::min(s.slots / 2 + s.N, 1024 / (s.HV * groups) + 2 * long(s.N));
+}
+}  // namespace
+
+DeltaSegments delta_segments(const DeltaShape& s, bool ragged) {
+  DeltaSegments none{1 << 30, 1, long(s.N), false};
+  const long nch = ragged ? s.total / kDeltaChunk / s.N + 1
+                          : (s.L + kDeltaChunk - 1) / kDeltaChunk;
+  if (nch < 4 || s.cus <= 0) return none;
+  const long waves = std::min(s.dv / 32, 4);
+  const long gb = s.dv / (32 * waves), ga = s.dk / (32 * waves);
+  const long units = long(s.N) * s.HV, cus = s.cus;
+  // Times per chunk in ns of a workgroup alone on a compute unit: with outputs, without
+  const long full = 4700, bare = 2800, chain = 1400;
+  auto rounds = [&](long wgs) { return (wgs + cus - 1) / cus; };
+  auto cost = [&](long cps) {
+    const long n = (nch + cps - 1) / cps;
+    long t = rounds(units * gb * n) * std::min(cps, nch) * full;
+    if (n > 1)
+      t += rounds(units * (gb + (n - 2) * (gb + ga))) * cps * bare + 4000 + chain * (n - 1);
+    return t;
+  };
+  long best = nch, t = cost(nch);
+  for (long n = 2; n <= nch / 2 && n <= 32; ++n) {
+    const long cps = (nch + n - 1) / n;
+    if (cps >= 2 && cost(cps) < t) {
+      t = cost(cps);
+      best = cps;
+    }
+  }
+  if (best == nch) return none;
+  DeltaSegments d{int(best), int((nch + best - 1) / best), 0, true};
+  d.slots = ragged ? segment_slots(s, best) : long(s.N) * d.nseg_l;
+  return d.slots <= most_segment_slots(s) ? d : none;
+}
+
 size_t delta_workspace_bytes(const DeltaShape& s, bool backward) {
   const size_t gates = sizeof(float) * kDeltaGates * kDeltaChunk;
   if (!backward) {
     const size_t np = s.bf16 ? 1 : 2, image = np * delta_image_bytes(s.dk);
-    return size_t(s.slots) * (s.HV * (gates + 6 * 1024 * 4) + s.HK * 2 * image);
+    return size_t(s.slots) * (s.HV * (gates + 6 * 1024 * 4) + s.HK * 2 * image) +
+           size_t(most_segment_slots(s)) * segment_bytes(s);
   }
   const size_t part = kDeltaFactorBytes + sizeof(float) * size_t(s.dv) * (s.dk + kDeltaChunk);
   return size_t(s.slots) * s.HV * (gates + part * (backward ? 2 : 1));

@@ -110,10 +110,19 @@ struct DeltaShape {
   float scale;
   int L;            // tokens per sequence when there are no offsets (total / N)
   long slots;       // chunk slots: enough for sequences of any lengths
+  int cus = 0;      // compute units of the device (0: not known)
 };
 // The shape of a configuration, or ONELA_EINVAL.  ragged: the lengths come as offsets.
 onela_status_t delta_shape_of(const onela_delta_config_t* cfg, bool ragged, DeltaShape* out);
 size_t delta_workspace_bytes(const DeltaShape& s, bool backward);
+// Chunks per segment of the chain and, with more than one segment, the slots (see
+// kernels_delta_scan.hip); 1 << 30 chunks and one slot per sequence without segments.
+struct DeltaSegments {
+  int cps, nseg_l;  // nseg_l: segments of a sequence of L tokens (no offsets)
+  long slots;
+  bool many;
+};
+DeltaSegments delta_segments(const DeltaShape& s, bool ragged);
 
 // ---- norm and rotation of queries and keys ----------------------------------------
 constexpr int kNormBlocks = 2048;  // most workgroups of the backward pass

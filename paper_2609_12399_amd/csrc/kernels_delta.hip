@@ -1404,6 +1404,14 @@ hipError_t launch_delta_rule(const DeltaShape& s, DeltaParams p, bool backward, 
     p.tp = reinterpret_cast<uint4*>(take(cus * 6 * 2 * 1024));
     p.pf = reinterpret_cast<uint4*>(take(cus * 6 * 2 * 1024));
     p.gates = reinterpret_cast<float*>(take(cus * kDeltaGates * kC * 4));
+    const DeltaSegments sg = delta_segments(s, p.offsets != nullptr);
+    p.cps = sg.cps;
+    p.nseg_l = sg.nseg_l;
+    p.seg_slots = sg.slots;
+    if (sg.many) {
+      p.segs = reinterpret_cast<float*>(take(size_t(sg.slots) * s.HV * s.dv * s.dk * 4));
+      p.sega = reinterpret_cast<float*>(take(size_t(sg.slots) * s.HV * s.dk * s.dk * 4));
+    }
     const hipError_t e = launch_delta_prep(s, p, st);
     return e == hipSuccess ? launch_delta_forward(s, p, st) : e;
   }

@@ -22,10 +22,18 @@ constexpr int kScanWaves = DV / 32 < 4 ? DV / 32 : 4;
 // their largest value; the bound grows with every update by what 64 tokens can add at
 // most, and where it leaves [2^8, 2^15] the rows are scaled anew.  The true values are some
 // 2^7 below the bound, far inside what two fp16 parts hold to 22 bits of the largest.
-template <int DK, int DV, int NP>
+//
+// Segments.  One chain per 128 rows leaves most of the chip idle for few heads, so a
+// sequence can be cut into segments of p.cps chunks that run at once: S_out = S_in A + B.
+// With SEG the kernel forms, without outputs, for every segment but the sequence's last
+// the state that it leaves: of the first the true one, of the others B (from S_in =
+// 0) and, by the same code on the rows of the identity and V = 0, A.
+// delta_combine_kernel chains them, and then every segment starts from its true state.
+template <int DK, int DV, int NP, bool SEG>
 __global__ __launch_bounds__(64 * kScanWaves<DV>, DK >= 256 || NP == 2 ? 1 : 2)
 void delta_forward_kernel(DeltaParams p) {
   constexpr int NW = kScanWaves<DV>, GB = DV / (32 * NW);
+  constexpr int GA = SEG ? DK / (32 * NW) : 0;
   constexpr int NB = DK / 16;
   constexpr int PS = NB / 2 < 4 ? NB / 2 : 4;
   auto t0 = [](int h) constexpr { return h / PS * (2 * PS) + h % PS; };
@@ -33,24 +41,31 @@ void delta_forward_kernel(DeltaParams p) {
   constexpr int kImage = sizeof(Swz<DK>) * NP, kFrags = 6 * 2 * 1024;
   constexpr int kGateBytes = kDeltaGates * kC * 4;
   __shared__ __align__(16) Swz<DK> sK[2][NP];
-  __shared__ __align__(16) Swz<DK> sQ[NP];
+  __shared__ __align__(16) Swz<DK> sQ[SEG ? 1 : NP];
   __shared__ __align__(16) uint4 sT[kFrags / 16];
-  __shared__ __align__(16) uint4 sP[kFrags / 16];
+  __shared__ __align__(16) uint4 sP[SEG ? 1 : kFrags / 16];
   __shared__ __align__(16) float sG[kDeltaGates][kC];
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lq = lane >> 4;
-  const int grp = blockIdx.x % GB, unit = blockIdx.x / GB;
-  const int n = unit / p.HV, hv = unit - n * p.HV, hk = hv / (p.HV / p.HK);
+  const int item = int(blockIdx.x % (GB + GA));
+  const bool ident = SEG && item >= GB;  // rows of A
+  const int grp = ident ? item - GB : item;
+  const long su = blockIdx.x / (GB + GA);  // segment slot and value head
+  const int hv = int(su % p.HV), hk = hv / (p.HV / p.HK);
+  const Segment sg = segment_of(p, su / p.HV);
+  if (sg.j < 0 || (SEG && (sg.j + 1 == sg.nseg || (ident && sg.j == 0)))) return;
+  const Seq& sq = sg.sq;
   const int row0 = 32 * (NW * grp + w) + 2 * lr;  // this lane's rows: row0, row0 + 1
-  const Seq sq = seq_of(p, n);
-  const int nch = (sq.len + kC - 1) / kC;
+  const int nch = sg.ce;
   const f32x4 z = {0.f, 0.f, 0.f, 0.f};
 
   // st[u][b][i] = sc S(row0 + u, 16 b + 4 lq + i)
   f32x4 st[2][NB];
   float sc = 1.f, bound = 0.f;
-  const long sat = (long(unit) * DV + row0) * DK + 4 * lq;
+  const long rows = long(row0) * DK + 4 * lq;
+  const float* from = sg.j == 0 ? p.s_in : SEG ? nullptr : p.segs + (su - p.HV) * (DV * DK);
+  if (sg.j == 0 && from) from += (long(sg.n) * p.HV + hv) * (DV * DK);
   auto rescale = [&](float f) __attribute__((always_inline)) {
     const float to = fminf(fmaxf(sc * f, 0x1p-100f), 0x1p100f);
     f = to * inverse_pow2(sc);
@@ -65,28 +80,31 @@ void delta_forward_kernel(DeltaParams p) {
   for (int u = 0; u < 2; ++u)
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      st[u][b] = p.s_in ? *reinterpret_cast<const f32x4*>(p.s_in + sat + u * DK + 16 * b) : z;
+      st[u][b] = from ? *reinterpret_cast<const f32x4*>(from + rows + u * DK + 16 * b) : z;
+      if (ident)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) st[u][b][i] = 16 * b + 4 * lq + i == row0 + u ? 1.f : 0.f;
       bound = max4abs(bound, st[u][b]);
     }
   bound = max_over_rows(bound);
-  if (p.s_in) rescale(bound > 0.f ? scale_for(bound) : 1.f);
+  if (from || ident) rescale(bound > 0.f ? scale_for(bound) : 1.f);
 
   auto load_kq = [&](int c) __attribute__((always_inline)) {
     const long at = ((sq.slot + c) * p.HK + hk) * (kImage / 16);
     dma<kImage, NW>(p.kimg + at, sK[c & 1], w, lane);
-    dma<kImage, NW>(p.qimg + at, sQ, w, lane);
+    if constexpr (!SEG) dma<kImage, NW>(p.qimg + at, sQ, w, lane);
   };
   auto load_tp = [&](int c) __attribute__((always_inline)) {
     const long cu = (sq.slot + c) * p.HV + hv;
     dma<kFrags, NW>(p.tp + cu * (kFrags / 16), sT, w, lane);
-    dma<kFrags, NW>(p.pf + cu * (kFrags / 16), sP, w, lane);
+    if constexpr (!SEG) dma<kFrags, NW>(p.pf + cu * (kFrags / 16), sP, w, lane);
     dma<kGateBytes, NW>(p.gates + cu * (kDeltaGates * kC), sG, w, lane);
   };
   // values V(t = 16 a + 4 lq + i, row0 + u), raw
   const unsigned vs = unsigned(p.vs) * kIo;
   unsigned vr[16][NP];
   auto load_v = [&](int c) __attribute__((always_inline)) {
-    const int m = min(kC, sq.len - c * kC);
+    const int m = ident ? 0 : min(kC, sq.len - c * kC);  // (A: no values)
     const auto rs = rows_buffer(p.v, ((sq.t0 + long(c) * kC) * p.vs + hv * DV) * kIo, DV * kIo, vs, m);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -129,12 +147,12 @@ void delta_forward_kernel(DeltaParams p) {
     }
   };
 
-  if (nch > 0) {
-    load_kq(0);
-    load_tp(0);
-    load_v(0);
+  if (sg.cb < nch) {
+    load_kq(sg.cb);
+    load_tp(sg.cb);
+    load_v(sg.cb);
   }
-  for (int c = 0; c < nch; ++c) {
+  for (int c = sg.cb; c < nch; ++c) {
     const Swz<DK>* const K = sK[c & 1];
     dma_wait();
     __syncthreads();  // this chunk's operands are in LDS
@@ -153,7 +171,7 @@ void delta_forward_kernel(DeltaParams p) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
           kf[a][i] = row_frag(K[i], kb, t0(h), t0(h) + PS, KR * a);
-          qf[a][i] = row_frag(sQ[i], kb, t0(h), t0(h) + PS, KR * a);
+          if constexpr (!SEG) qf[a][i] = row_frag(sQ[i], kb, t0(h), t0(h) + PS, KR * a);
         }
 #pragma unroll
       for (int u = 0; u < 2; ++u) parts8(st[u][t0(h)], st[u][t0(h) + PS], sp[u]);
@@ -162,10 +180,11 @@ void delta_forward_kernel(DeltaParams p) {
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int a = 0; a < 4; ++a) y[u][a] = mfma_f16(kf[a][i], sp[u][j], y[u][a]);
+        if constexpr (!SEG)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int a = 0; a < 4; ++a) o[u][a] = mfma_f16(qf[a][i], sp[u][j], o[u][a]);
+            for (int a = 0; a < 4; ++a) o[u][a] = mfma_f16(qf[a][i], sp[u][j], o[u][a]);
       });
     }
     // X = V - gamma Y, scaled for the lane's two rows
@@ -239,7 +258,7 @@ void delta_forward_kernel(DeltaParams p) {
       }
     }
     // P e, and the outputs
-    {
+    if constexpr (!SEG) {
       f32x4 q[2][4];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -299,21 +318,97 @@ void delta_forward_kernel(DeltaParams p) {
       }
     }
   }
-  if (p.s_out) {
+  float* to = nullptr;
+  if constexpr (SEG)
+    to = ident ? p.sega + su * (DK * DK) : p.segs + su * (DV * DK);
+  else if (p.s_out && sg.j + 1 == sg.nseg)
+    to = p.s_out + (long(sg.n) * p.HV + hv) * (DV * DK);
+  if (to) {
     const float inv = inverse_pow2(sc);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        *reinterpret_cast<f32x4*>(p.s_out + sat + u * DK + 16 * b) = inv * st[u][b];
+        *reinterpret_cast<f32x4*>(to + rows + u * DK + 16 * b) = inv * st[u][b];
+  }
+}
+
+// The true states after the segments of one (sequence, value head, 16 state rows): S_0 as
+// it is, then S_j = S_{j-1} A_j + B_j, in B_j's place.  Wave w holds the columns 16 w ..
+// 16 w + 15 as an accumulator tile of S^T; the tiles, cut into three bf16 parts, are exchanged
+// through LDS as operands (one barrier per segment), A_j's rows come from memory, requested one
+// segment ahead.  Bound: latency of the chain over the segments.
+template <int DK, int DV>
+__global__ __launch_bounds__(4 * DK) void delta_combine_kernel(DeltaParams p) {
+  constexpr int NH = DK / 32, NRB = DV / 16;
+  __shared__ uint4 xs[2][NH][3][64];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 15, lq = lane >> 4;
+  const int unit = blockIdx.x / NRB, rb = blockIdx.x % NRB;
+  const int n = unit / p.HV, hv = unit - n * p.HV;
+  const Seq sq = seq_of(p, n);
+  const long slot0 = first_segment(p, sq, n);
+  const int last = segments_of(p, sq) - 2;  // the last segment that leaves a state
+  if (last < 1) return;
+  const long at = long(16 * rb + lr) * DK + 16 * w + 4 * lq;
+  auto state = [&](int j) { return p.segs + ((slot0 + j) * p.HV + hv) * (DV * DK) + at; };
+  f32x4 st = *reinterpret_cast<const f32x4*>(state(0));
+  // A^T(16 w + lr, k): slots k = 32 h + 4 lq + i and 32 h + 16 + 4 lq + i
+  f32x4 a[NH][2];
+  auto load = [&](int j, int h) {
+    const float* q = p.sega + ((slot0 + min(j, last)) * p.HV + hv) * (DK * DK) +
+                     (32 * h + 4 * lq) * DK + 16 * w + lr;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[h][u][i] = q[(16 * u + i) * DK];
+  };
+  f32x4 bn = *reinterpret_cast<const f32x4*>(state(1));
+#pragma unroll
+  for (int h = 0; h < NH; ++h) load(1, h);
+  for (int j = 1; j <= last; ++j) {
+    const int x = j & 1;
+    uint4 d[3];
+    cut3(st, st, d[0], d[1], d[2]);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      reinterpret_cast<uint2*>(&xs[x][w >> 1][i][lane])[w & 1] = make_uint2(d[i].x, d[i].y);
+    __syncthreads();
+    f32x4 hi[2] = {}, lo[4] = {};
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      const uint4 dh = xs[x][h][0][lane], dm = xs[x][h][1][lane], dl = xs[x][h][2][lane];
+      uint4 t[3];
+      cut3(a[h][0], a[h][1], t[0], t[1], t[2]);
+      load(j + 1, h);  // (into the registers just read)
+      const int e = h & 1;
+      hi[e] = mfma_bf16(t[0], dh, hi[e]);
+      lo[e] = mfma_bf16(t[2], dh, lo[e]);
+      lo[2 + e] = mfma_bf16(t[1], dm, lo[2 + e]);
+      lo[e] = mfma_bf16(t[0], dl, lo[e]);
+      lo[2 + e] = mfma_bf16(t[1], dh, lo[2 + e]);
+      lo[e] = mfma_bf16(t[0], dm, lo[e]);
+    }
+    st = bn + ((hi[0] + hi[1]) + ((lo[0] + lo[1]) + (lo[2] + lo[3])));
+    bn = *reinterpret_cast<const f32x4*>(state(min(j + 1, last)));
+    *reinterpret_cast<f32x4*>(state(j)) = st;
   }
 }
 
 template <int DK, int DV, int NP>
 hipError_t run(const DeltaParams& p, hipStream_t st) {
-  constexpr int NW = kScanWaves<DV>;
-  const unsigned wgs = unsigned(p.N) * unsigned(p.HV) * (DV / (32 * NW));
-  delta_forward_kernel<DK, DV, NP><<<wgs, 64 * NW, 0, st>>>(p);
+  constexpr int NW = kScanWaves<DV>, GB = DV / (32 * NW), GA = DK / (32 * NW);
+  const unsigned units = unsigned(p.seg_slots) * unsigned(p.HV);
+  if (p.sega) {
+    delta_forward_kernel<DK, DV, NP, true><<<units * (GB + GA), 64 * NW, 0, st>>>(p);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    delta_combine_kernel<DK, DV>
+        <<<unsigned(p.N) * unsigned(p.HV) * (DV / 16), 4 * DK, 0, st>>>(p);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  delta_forward_kernel<DK, DV, NP, false><<<units * GB, 64 * NW, 0, st>>>(p);
   return hipGetLastError();
 }
 

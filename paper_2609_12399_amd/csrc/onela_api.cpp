@@ -454,6 +454,7 @@ onela_status_t onela_delta_rule_forward(const onela_delta_config_t* cfg,
     return ONELA_EINVAL;
   rc = delta_workspace(s, false, workspace, workspace_bytes);
   if (rc != ONELA_OK) return rc;
+  s.cus = device_compute_units();
   p.s_in = initial_state;
   p.s_out = final_state;
   p.o = o;
