@@ -20,7 +20,7 @@ BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["host_plan.cpp", "onela_api.cpp", "kernels_records.hip", "kernel_decode.hip", "kernel_replay.hip",
            "kernels_fullstate.hip", "kernels_select.hip", "kernels_prefill.hip",
            "kernels_delta.hip", "kernels_delta_prep.hip", "kernels_delta_scan.hip",
-           "kernel_delta_step.hip", "kernel_norm_rope.hip"]
+           "kernels_delta_reverse.hip", "kernels_delta_grad.hip", "kernel_delta_step.hip", "kernel_norm_rope.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

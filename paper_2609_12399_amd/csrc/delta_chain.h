@@ -1,0 +1,222 @@
+// The state's rows of one wave in the delta rule's chains (kernels_delta_scan.hip,
+// kernels_delta_reverse.hip) and the products they take part in.
+#pragma once
+
+#include "delta_tiles.h"
+
+namespace onela {
+
+// Waves of a chain's workgroup: 32 state rows each, at most 128 per workgroup.
+template <int DV>
+constexpr int kChainWaves = DV / 32 < 4 ? DV / 32 : 4;
+
+// Bytes of a triangular matrix's fragments, and of a chunk's gates.
+constexpr int kFragBytes = 6 * 2 * 1024;
+
+// 32 rows of the state per wave as two column tiles of S^T (tile u, lane lr: row row0 + u,
+// row0 = 32 w + 2 lr), in registers: st[u][b][i] = sc S(row0 + u, 16 b + 4 lq + i).
+//
+// Scales (powers of two).  sc keeps the lane's two rows inside what two fp16 parts hold, by a
+// bound on their largest value; the bound grows with every update by what 64 tokens
+// can add at most, and where it leaves [2^12, 2^15] the rows are scaled anew.  The true
+// values, and those that the updates add, are some 2^7 below their bounds; parts lose bits only
+// below 2^-3.
+template <int DK>
+struct ChainState {
+  static constexpr int NB = DK / 16;
+  // The 32-deep step h of a contraction over the columns covers the tiles t0(h) and t0(h) + PS:
+  // PS = 4 puts a row operand's two pieces 128 bytes apart (one two-address read).
+  static constexpr int PS = NB / 2 < 4 ? NB / 2 : 4;
+  static constexpr int t0(int h) { return h / PS * (2 * PS) + h % PS; }
+  static constexpr int KR = 32 * Swz<DK>::LD;  // bytes of 16 rows of an operand tile
+
+  f32x4 st[2][NB];
+  float sc, bound;
+
+  __device__ void rescale(float f) {
+    const float to = fminf(fmaxf(sc * f, 0x1p-100f), 0x1p100f);
+    f = to * inverse_pow2(sc);
+    sc = to;
+    bound *= f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) st[u][b] *= f;
+  }
+  // from: the lane's first row (null: zeros), or the rows of the identity
+  __device__ void init(const float* from, bool ident, int row0, int lq) {
+    sc = 1.f;
+    bound = 0.f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        st[u][b] = from ? *reinterpret_cast<const f32x4*>(from + u * DK + 16 * b)
+                        : f32x4{0.f, 0.f, 0.f, 0.f};
+        if (ident)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) st[u][b][i] = 16 * b + 4 * lq + i == row0 + u ? 1.f : 0.f;
+        bound = max4abs(bound, st[u][b]);
+      }
+    bound = max_over_rows(bound);
+    if (from || ident) rescale(bound > 0.f ? scale_for(bound) : 1.f);
+  }
+  __device__ void store(float* to) const {
+    const float inv = inverse_pow2(sc);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        *reinterpret_cast<f32x4*>(to + u * DK + 16 * b) = inv * st[u][b];
+  }
+  // Makes room for an update S <- g S + (64 tokens' keys times values of at most `most`;
+  // keys are scaled below 2^3): the bound after it.
+  __device__ void make_room(float g, float most) {
+    float next = fmaf(g, bound, 0x1p9f * most * sc);
+    const bool off = !(next <= 32768.f && next >= 4096.f) && next > 0.f;
+    if (__any(off)) {
+      const float was = sc;
+      rescale(off ? scale_for(next) : 1.f);
+      next *= sc * inverse_pow2(was);
+    }
+    bound = next;
+  }
+};
+
+// y[u][a] += rows of A (16 a ..) times S^T, and with TWO the same of B into o: the operand
+// tiles have NP parts, the state two.
+template <int DK, int NP, bool TWO>
+__device__ __attribute__((always_inline)) inline void rows_times_state(
+    const Swz<DK>* A, const Swz<DK>* B, const ChainState<DK>& s, int kb, f32x4 (&y)[2][4],
+    f32x4 (&o)[2][4]) {
+  using C = ChainState<DK>;
+#pragma unroll
+  for (int h = 0; h < DK / 32; ++h) {
+    uint4 sp[2][2], af[4][NP], bf[4][NP];
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        af[a][i] = row_frag(A[i], kb, C::t0(h), C::t0(h) + C::PS, C::KR * a);
+        if constexpr (TWO) bf[a][i] = row_frag(B[i], kb, C::t0(h), C::t0(h) + C::PS, C::KR * a);
+      }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) parts8(s.st[u][C::t0(h)], s.st[u][C::t0(h) + C::PS], sp[u]);
+    for_products<NP, 2>([&](int i, int j) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) y[u][a] = mfma_f16(af[a][i], sp[u][j], y[u][a]);
+      if constexpr (TWO)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int a = 0; a < 4; ++a) o[u][a] = mfma_f16(bf[a][i], sp[u][j], o[u][a]);
+    });
+  }
+}
+
+// acc[u][a] += F x[u], F a lower triangular 64 x 64 matrix in two parts whose fragments are in
+// LDS, x in NX parts (tokens 32 h .. of column tile u: x[u][h]).
+template <int NX>
+__device__ __attribute__((always_inline)) inline void triangle(const uint4* F,
+                                                               const uint4 (&x)[2][2][NX],
+                                                               f32x4 (&acc)[2][4], int lane) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint4 f[4][2];
+#pragma unroll
+    for (int a = 2 * h; a < 4; ++a)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) f[a][i] = F[((a < 2 ? a : 2 * a - 2 + h) * 2 + i) * 64 + lane];
+    for_products<2, NX>([&](int i, int j) {
+#pragma unroll
+      for (int a = 2 * h; a < 4; ++a)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) acc[u][a] = mfma_f16(f[a][i], x[u][h][j], acc[u][a]);
+    });
+  }
+}
+
+// S^T <- g S^T + A^T x (and + B^T y with TWO): A, B operand tiles in NP parts, x, y in two.
+template <int DK, int NP, bool TWO>
+__device__ __attribute__((always_inline)) inline void update_state(
+    ChainState<DK>& s, float g, const Swz<DK>* A, const uint4 (&x)[2][2][2], const Swz<DK>* B,
+    const uint4 (&y)[2][2][2], int tb) {
+  using C = ChainState<DK>;
+  constexpr int NG = C::NB < 4 ? C::NB : 4;
+#pragma unroll
+  for (int b0 = 0; b0 < C::NB; b0 += NG) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int b = 0; b < NG; ++b) s.st[u][b0 + b] *= g;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint4 kt[NG][NP];
+      auto add = [&](const Swz<DK>* T, const uint4 (&z)[2][2][2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < NG; ++b)
+#pragma unroll
+          for (int i = 0; i < NP; ++i) kt[b][i] = col_frag(T[i], tb, b0 + b, 2 * C::KR * h);
+        for_products<NP, 2>([&](int i, int j) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int b = 0; b < NG; ++b)
+              s.st[u][b0 + b] = mfma_f16(kt[b][i], z[u][h][j], s.st[u][b0 + b]);
+        });
+      };
+      add(A, x);
+      if constexpr (TWO) add(B, y);
+    }
+  }
+}
+
+// Two neighbouring columns of the 16 tokens t(i) = 16 (i / 4) + 4 lq + i % 4 of a lane, raw.
+// REV: of token 63 - t.
+template <int NP, bool REV = false>
+struct Columns {
+  unsigned r[16][NP];
+  __device__ void load(__amdgpu_buffer_rsrc_t rs, unsigned stride, int lq, unsigned at) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const unsigned t = 16 * (i >> 2) + (i & 3);
+      const unsigned o = unsigned(REV ? 12 - 4 * lq : 4 * lq) * stride + at,
+                     so = (REV ? 51 - t : t) * stride;
+      if constexpr (NP == 1) {
+        r[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rs, o, so, 0);
+      } else {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b64(rs, o, so, 0);
+        r[i][0] = x[0];
+        r[i][1] = x[1];
+      }
+    }
+  }
+  __device__ float get(int i, int u) const {
+    if constexpr (NP == 1)
+      return u ? bf16_hi_to_float(r[i][0]) : bf16_lo_to_float(r[i][0]);
+    else
+      return __uint_as_float(r[i][u]);
+  }
+  __device__ f32x4 tile(int a, int u) const {
+    return f32x4{get(4 * a, u), get(4 * a + 1, u), get(4 * a + 2, u), get(4 * a + 3, u)};
+  }
+};
+// The same stored, rounded to the tensor's type.
+template <int NP, bool REV = false>
+__device__ inline void store_columns(__amdgpu_buffer_rsrc_t rs, unsigned stride, int lq, unsigned at,
+                                     int i, float x0, float x1) {
+  const unsigned t = 16 * (i >> 2) + (i & 3);
+  const unsigned o = unsigned(REV ? 12 - 4 * lq : 4 * lq) * stride + at,
+                 so = (REV ? 51 - t : t) * stride;
+  if constexpr (NP == 1) {
+    __builtin_amdgcn_raw_buffer_store_b32(pack_bf16x2(x0, x1), rs, o, so, 0);
+  } else {
+    typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(x0), __float_as_uint(x1)}, rs, o,
+                                          so, 0);
+  }
+}
+
+}  // namespace onela

@@ -9,11 +9,21 @@
 
 namespace onela {
 
-// Rows of a chunk's gates in the workspace, 64 values each.  Factors of K S^T in X
-// (-gamma), of T X in the state's update (beta sigma), of Q S^T and of P e in the outputs, each
-// with the scales of its operands undone; then single values: gamma_{C-1}, the
-// largest beta sigma, the keys' inverse scale.
-enum { kGateY, kGateZ, kGateO, kGateP, kGateOne };
+// Rows of a chunk's gates in the workspace, 64 values each (operands' scales undone in
+// each).  Forward: factors of K S^T in X (-gamma), of T X in the state's update (beta sigma), of
+// Q S^T and of P e in the outputs; single values.  Backward: factors of K dS^T (beta sigma)
+// and of P^T dO in X; -gamma; beta sigma; beta; sums of log2(alpha) as float pairs; single values.
+enum {
+  kGateY, kGateZ, kGateO, kGateP, kGateOne, kGateStage = 8,
+  kRevY = 8, kRevP, kRevZ, kRevBS, kRevBeta, kRevHi, kRevLo, kRevOne
+};
+// Single values.  Forward: gamma_{C-1}; the largest factor kGateZ; the keys' inverse scale; the
+// largest row sum of scaled |T|; the scale of T X; T's inverse scale.
+enum { kOneG, kOneZ, kOneK, kOneT, kOneE, kOneIT };
+// Backward: gamma_{C-1}; the keys' and queries' inverse scales; the largest column sum of scaled
+// |T|; T's inverse scale; the largest gamma; then, as they come, bounds on the state, e, the
+// adjoint, dV and dO.
+enum { kRevG, kRevK, kRevQ, kRevT, kRevIT, kRevGam, kMaxS = 8, kMaxE, kMaxD, kMaxV, kMaxO };
 
 struct DeltaParams {
   const void *q, *k, *v;    // [total][heads][d], token strides qs, ks, vs
@@ -31,13 +41,14 @@ struct DeltaParams {
   int N, HK, HV, DV, L, nch_l;  // nch_l: chunks of a sequence of L tokens (no offsets)
   long slots;               // chunk slots
   // workspace, per (chunk slot, value head)
-  uint4* tf;     // [kDeltaFactor]  T fragments, three bf16 parts
-  uint4* tr;     // the same of the transposed, reversed T (backward)
-  float* gates;  // [kDeltaGates][64]
-  float* sws;    // [DV][DK]  state before the chunk
-  float* ews;    // [DV][64]  e
+  float* gates;  // [gate_rows][64]
+  int gate_rows; // kDeltaGates, backward twice that
+  uint4* tr;     // as tp and pf, of T and P transposed with their tokens in reverse order
+  uint4* pr;     // (backward)
+  float* sws;    // [DV][DK]  state before the chunk (backward)
+  float* ews;    // [DV][64]  e (backward)
   float* dsws;   // [DV][DK]  adjoint of the state after the chunk (backward)
-  float* hws;    // [DV][64]  beta times the chunk's own part of dD, then dV (backward)
+  float* hws;    // [DV][64]  dV (backward)
   uint4 *kimg, *qimg;  // per (slot, query/key head): the LDS image Swz<DK>[NP] of the fp16
                        // parts of keys and queries
   uint4* tp;     // T fragments, two fp16 parts [6][2][64]

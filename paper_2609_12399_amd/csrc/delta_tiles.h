@@ -168,9 +168,10 @@ __device__ inline float inverse_pow2(float s) {
   return __uint_as_float(0x7f000000u - __float_as_uint(s));
 }
 
-// The same to [2^6, 2^7), for keys and queries: bf16 values stay exact down to 2^-20 of the
-// largest, and products with a state leave room below fp16's largest value.
-__device__ inline float scale_for_rows(float m) { return scale_for(m) * 0x1p-7f; }
+// The same to [2^2, 2^3), for keys and queries: bf16 values stay exact down to 2^-16 of the
+// largest, with an error of 2^-28 of it below, and the values that products with them add
+// to a state stay large where the state's bound (delta_chain.h) limits their sum.
+__device__ inline float scale_for_rows(float m) { return scale_for(m) * 0x1p-11f; }
 
 __device__ inline unsigned pack_f16x2(float a, float b) {
   return __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{a, b}, half2v));
@@ -275,6 +276,13 @@ __device__ inline float sum_over_rows(float m) {
   const unsigned u = __float_as_uint(m);
   const auto q = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+
+// Raises *to (>= 0, in memory) to the wave's largest m >= 0.  Bits of floats >= 0 rise with
+// them, and a maximum does not depend on the order.
+__device__ inline void note_max(float* to, float m, int lane) {
+  m = wave_max(m);
+  if (lane == 0) atomicMax(reinterpret_cast<unsigned*>(to), __float_as_uint(m));
 }
 
 }  // namespace onela

@@ -300,14 +300,15 @@ DeltaSegments delta_segments(const DeltaShape& s, bool ragged) {
 }
 
 size_t delta_workspace_bytes(const DeltaShape& s, bool backward) {
-  const size_t gates = sizeof(float) * kDeltaGates * kDeltaChunk;
-  if (!backward) {
-    const size_t np = s.bf16 ? 1 : 2, image = np * delta_image_bytes(s.dk);
-    return size_t(s.slots) * (s.HV * (gates + 6 * 1024 * 4) + s.HK * 2 * image) +
-           size_t(most_segment_slots(s)) * segment_bytes(s);
-  }
-  const size_t part = kDeltaFactorBytes + sizeof(float) * size_t(s.dv) * (s.dk + kDeltaChunk);
-  return size_t(s.slots) * s.HV * (gates + part * (backward ? 2 : 1));
+  // per slot and value head T, P and the gates; backward T and P reversed, more gates,
+  // the state and its adjoint, e and dV; per slot and query/key head the keys' and
+  // queries' images; the segments
+  const size_t np = s.bf16 ? 1 : 2;
+  const size_t gates = sizeof(float) * kDeltaGates * kDeltaChunk * (backward ? 2 : 1);
+  const size_t head = gates + kDeltaFragBytes * (backward ? 3 : 2) +
+                      (backward ? 2 * sizeof(float) * size_t(s.dv) * (s.dk + kDeltaChunk) : 0);
+  return size_t(s.slots) * (s.HV * head + s.HK * 2 * np * delta_image_bytes(s.dk)) +
+         size_t(most_segment_slots(s)) * segment_bytes(s);
 }
 
 // ---- norm and rotation of queries and keys ----------------------------------------

@@ -95,9 +95,9 @@ bool select_plan(int R, unsigned N, unsigned W, SelectPlan* plan);
 constexpr size_t kSelectScratchBytes = size_t(32) << 20;
 
 // ---- delta rule over sequences ---------------------------------------------------
-constexpr int kDeltaChunk = 64;                          // tokens per chunk
-constexpr size_t kDeltaFactorBytes = 6 * 3 * 1024;       // split T of a chunk and head
-constexpr int kDeltaGates = 8;                           // fp32 values per token and head
+constexpr int kDeltaChunk = 64;                   // tokens per chunk
+constexpr size_t kDeltaFragBytes = 6 * 2 * 1024;  // a triangular matrix of a chunk in two parts
+constexpr int kDeltaGates = 8;                    // fp32 values per token and head (backward: 16)
 
 // Bytes of one fp16 plane of a chunk's keys as it stands in LDS.
 constexpr size_t delta_image_bytes(int dk) { return size_t(kDeltaChunk) * (dk < 64 ? dk + 16 : dk) * 2; }

@@ -70,8 +70,13 @@ hipError_t launch_prefill_chunked(const Shape& s, int prompt_len, const void* k,
 struct DeltaParams;
 hipError_t launch_delta_rule(const DeltaShape& s, DeltaParams p, bool backward, void* workspace,
                              hipStream_t st);
-hipError_t launch_delta_prep(const DeltaShape& s, const DeltaParams& p, hipStream_t st);
-hipError_t launch_delta_forward(const DeltaShape& s, const DeltaParams& p, hipStream_t st);
+hipError_t launch_delta_prep(const DeltaShape& s, const DeltaParams& p, bool backward,
+                             hipStream_t st);
+hipError_t launch_delta_forward(const DeltaShape& s, const DeltaParams& p, bool save,
+                                hipStream_t st);
+hipError_t launch_delta_combine(const DeltaShape& s, const DeltaParams& p, hipStream_t st);
+hipError_t launch_delta_reverse(const DeltaShape& s, const DeltaParams& p, hipStream_t st);
+hipError_t launch_delta_grad(const DeltaShape& s, const DeltaParams& p, hipStream_t st);
 hipError_t launch_delta_step(const DeltaShape& s, const DeltaParams& p, hipStream_t st);
 
 // ---- norm and rotation of queries and keys --------------------------------------

@@ -87,18 +87,19 @@ struct PrepLds {
   };
   double g[kC];                          // sums of log2(alpha)
   alignas(16) float be[kC], bs[kC], ip[kC];  // beta, beta sigma, inverse scales of P's rows
-  float most[4][3];                      // per wave: the largest key, query, element of T
+  float most[4][5];  // per wave: the largest key, query, element of T, row and column sum of it
 };
 
 // One chunk of one value head: the fp16 images of its keys and queries, T = (I + B
-// diag(beta))^-1 and P in the fragment order of the chain, and the gates.  Four waves.
+// diag(beta))^-1 and P in the fragment order of the chain, and the gates; for the backward
+// pass, in P's place, T and P transposed with their tokens in reverse order.  Four waves.
 //   The inverse goes by 16-token blocks: the four diagonal blocks by forward
 // substitution, one per wave with a column per lane, then each wave the blocks below
 // the diagonal block of its block column, T_ij = -T_ii sum_k M_ik T_kj, in fp32 matrix
 // instructions with T_kj in the accumulator layout as the next operand.
 //   Bound: latency of that chain, and the writes; the workgroup's LDS (36 KB up to d_k =
 // 128) and registers are held to four workgroups per compute unit.
-template <int DK, int NP>
+template <int DK, int NP, bool BWD>
 __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_kernel(DeltaParams p) {
   __shared__ __align__(16) PrepLds<DK, NP> sh;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -109,7 +110,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
   const Chunk ch = chunk_of(p, slot);
   if (ch.n <= 0) return;
   const long cu = long(blockIdx.x);
-  float* const gt = p.gates + cu * (kDeltaGates * kC);
+  float* const gt = p.gates + cu * (p.gate_rows * kC);
   const f32x4 z = {0.f, 0.f, 0.f, 0.f};
   float sk, sq;
   {
@@ -159,15 +160,16 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
   const int kb = Swz<DK>::off(lr, lq);
   constexpr int KR = 32 * Swz<DK>::LD;
   // rows x of a against rows y of b, 16 each: lane (lr, lq) holds (16 a + 4 lq + i, 16 b + lr)
-  auto dots = [&](const Swz<DK>* x, int a, const Swz<DK>* y, int b) {
+  // (base: the lane's first piece of row lr, or of row 15 - lr for rows in reverse order)
+  auto dots = [&](const Swz<DK>* x, int a, const Swz<DK>* y, int b, int base) {
     f32x4 acc[2] = {z, z};
 #pragma unroll
     for (int h = 0; h < DK / 32; ++h) {
       uint4 u[NP], v[NP];
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        u[i] = row_frag(x[i], kb, 2 * h, 2 * h + 1, KR * a);
-        v[i] = row_frag(y[i], kb, 2 * h, 2 * h + 1, KR * b);
+        u[i] = row_frag(x[i], base, 2 * h, 2 * h + 1, KR * a);
+        v[i] = row_frag(y[i], base, 2 * h, 2 * h + 1, KR * b);
       }
       for_products<NP, NP>([&](int i, int j) { acc[h & 1] = mfma_f16(u[i], v[j], acc[h & 1]); });
     }
@@ -176,23 +178,32 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
   {
     // P(t, j) = scale Gamma(t, j) (q_t . k_j) beta_j, j <= t, of 16 tokens t per wave (the
     // longer rows to the waves with fewer tiles of M): a lane holds four neighbouring j
-    // of one token, half a fragment
+    // of one token, half a fragment; backward of 16 tokens j and four neighbouring t
     const int pa = w == 0 ? 2 : w == 1 ? 1 : w == 2 ? 3 : 0;
-    const int t = 16 * pa + lr;
+    const int t = BWD ? kC - 1 - 16 * pa - lr : 16 * pa + lr;  // backward: the token j
     const double gq = sh.g[t];
-    const float c = p.scale * (ik * iq);
+    const float c = p.scale * (ik * iq) * (BWD ? sh.be[t] : 1.f);
     f32x4 x[4];
     float most = 0.f;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       x[b] = z;
       if (b > pa) continue;
-      const f32x4 acc = dots(sh.kq.K, b, sh.kq.Q, pa);
-      const f32x4 be = *reinterpret_cast<const f32x4*>(&sh.be[16 * b + 4 * lq]);
+      if constexpr (!BWD) {
+        const f32x4 acc = dots(sh.kq.K, b, sh.kq.Q, pa, kb);
+        const f32x4 be = *reinterpret_cast<const f32x4*>(&sh.be[16 * b + 4 * lq]);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int j = 16 * b + 4 * lq + q;
-        x[b][q] = j <= t ? c * exp2_fast(float(gq - sh.g[j])) * be[q] * acc[q] : 0.f;
+        for (int q = 0; q < 4; ++q) {
+          const int j = 16 * b + 4 * lq + q;
+          x[b][q] = j <= t ? c * exp2_fast(float(gq - sh.g[j])) * be[q] * acc[q] : 0.f;
+        }
+      } else {
+        const f32x4 acc = dots(sh.kq.Q, 3 - b, sh.kq.K, 3 - pa, Swz<DK>::off(15 - lr, lq));
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int i = kC - 1 - 16 * b - 4 * lq - q;
+          x[b][q] = t <= i ? c * exp2_fast(float(sh.g[i] - gq)) * acc[q] : 0.f;
+        }
       }
       most = max4abs(most, x[b]);
     }
@@ -204,7 +215,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
       uint4 part[2];
       parts8<2>(x[2 * h], x[2 * h + 1], s, part);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) p.pf[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
+      for (int i = 0; i < 2; ++i) (BWD ? p.pr : p.pf)[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
     }
     if (lq == 0) sh.ip[t] = inverse_pow2(s);
   }
@@ -213,7 +224,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
     // (2, 0), (2, 1), (3, 0); (3, 1), (3, 2); the diagonal block w
     f32x4 m[3];
     auto tile = [&](int a, int b) {
-      f32x4 acc = dots(sh.kq.K, a, sh.kq.K, b);
+      f32x4 acc = dots(sh.kq.K, a, sh.kq.K, b, kb);
       const int j = 16 * b + lr;
       const double gj = sh.g[j];
       const float bk = sh.be[j] * ik * ik;
@@ -311,41 +322,84 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
                                   fmaxf(sh.most[2][2], sh.most[3][2])));
   // T fragments of row tile w: a lane holds row 16 w + lr and the columns 32 h + 4 lq +
   // 0..3 and 32 h + 16 + 4 lq + 0..3, the order in which the chain's accumulators hold
-  // the tokens
+  // the tokens; transposed and reversed, rows and columns count from the chunk's end and
+  // change places
+  {
+    float sums[2] = {0.f, 0.f};
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (h > 0 && w < 2) break;
-    const int f = w < 2 ? w : 2 * w - 2 + h, t = 16 * w + lr, c0 = 32 * h + 4 * lq;
-    uint4 part[2];
-    parts8<2>(*reinterpret_cast<const f32x4*>(&T[t][c0]),
-              *reinterpret_cast<const f32x4*>(&T[t][c0 + 16]), s, part);
+    for (int h = 0; h < 2; ++h) {
+      if (h > 0 && w < 2) break;
+      const int f = w < 2 ? w : 2 * w - 2 + h, t = 16 * w + lr, c0 = 32 * h + 4 * lq;
+      f32x4 x[2][2];
+      x[0][0] = *reinterpret_cast<const f32x4*>(&T[t][c0]);
+      x[0][1] = *reinterpret_cast<const f32x4*>(&T[t][c0 + 16]);
+      if constexpr (BWD)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) p.tp[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
+        for (int j = 0; j < 4; ++j) {
+          x[1][0][j] = T[kC - 1 - (c0 + j)][kC - 1 - t];
+          x[1][1][j] = T[kC - 1 - (c0 + 16 + j)][kC - 1 - t];
+        }
+#pragma unroll
+      for (int r = 0; r < (BWD ? 2 : 1); ++r) {
+        uint4 part[2];
+        parts8<2>(x[r][0], x[r][1], s, part);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          (r ? p.tr : p.tp)[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[r] += fabsf(x[r][0][i]) + fabsf(x[r][1][i]);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < (BWD ? 2 : 1); ++r) {
+      const float most = wave_max(sum_over_rows(sums[r]));
+      if (lane == 0) sh.most[w][3 + r] = most;
+    }
   }
+  __syncthreads();
   if (w == 0) {
-    const float it = inverse_pow2(s), gam = exp2_fast(float(sh.g[lane])), bs = sh.bs[lane] * it;
+    auto most = [&](int i) {
+      return fmaxf(fmaxf(sh.most[0][i], sh.most[1][i]), fmaxf(sh.most[2][i], sh.most[3][i])) * s;
+    };
+    const float it = inverse_pow2(s), gam = exp2_fast(float(sh.g[lane])), bs = sh.bs[lane];
+    const float all = exp2_fast(float(sh.g[63]));
+    const float se = scale_for(most(3) * 0x1p14f);
+    const float mz = wave_max(fabsf(bs * it));
     gt[kGateY * kC + lane] = -gam * ik;
     gt[kGateO * kC + lane] = p.scale * gam * iq;
-    gt[kGateZ * kC + lane] = bs;
-    gt[kGateP * kC + lane] = sh.ip[lane] * it;
-    const float most = wave_max(fabsf(bs));
-    if (lane == 0) {
-      gt[kGateOne * kC] = exp2_fast(float(sh.g[63]));
-      gt[kGateOne * kC + 1] = most;
-      gt[kGateOne * kC + 2] = ik;
+    gt[kGateZ * kC + lane] = bs * it;
+    gt[kGateP * kC + lane] = BWD ? 0.f : sh.ip[lane] * it * inverse_pow2(se);
+    gt[kGateOne * kC + lane] = lane == kOneG ? all : lane == kOneZ ? mz : lane == kOneK ? ik
+                             : lane == kOneT ? most(3) : lane == kOneE ? se : it;
+    if constexpr (BWD) {
+      const float hi = float(sh.g[lane]), mg = wave_max(gam);
+      gt[kRevY * kC + lane] = bs * ik;
+      gt[kRevP * kC + lane] = sh.ip[lane];
+      gt[kRevZ * kC + lane] = -gam;
+      gt[kRevBS * kC + lane] = bs;
+      gt[kRevBeta * kC + lane] = sh.be[lane];
+      gt[kRevHi * kC + lane] = hi;
+      gt[kRevLo * kC + lane] = float(sh.g[lane] - double(hi));
+      gt[kRevOne * kC + lane] = lane == kRevG ? all : lane == kRevK ? ik : lane == kRevQ ? iq
+                              : lane == kRevT ? most(4) : lane == kRevIT ? it
+                              : lane == kRevGam ? mg : 0.f;
     }
   }
 }
 
 }  // namespace
 
-hipError_t launch_delta_prep(const DeltaShape& s, const DeltaParams& p, hipStream_t st) {
+hipError_t launch_delta_prep(const DeltaShape& s, const DeltaParams& p, bool backward,
+                             hipStream_t st) {
   const unsigned cus = unsigned(p.slots) * unsigned(p.HV);
   if (!cus) return hipSuccess;
-#define ONELA_DELTA_PREP(DK, NP)                          \
-  if (s.dk == DK && s.bf16 == (NP == 1)) {                \
-    delta_prep_kernel<DK, NP><<<cus, kThreads, 0, st>>>(p); \
-    return hipGetLastError();                             \
+#define ONELA_DELTA_PREP(DK, NP)                                   \
+  if (s.dk == DK && s.bf16 == (NP == 1)) {                         \
+    if (backward)                                                  \
+      delta_prep_kernel<DK, NP, true><<<cus, kThreads, 0, st>>>(p);  \
+    else                                                           \
+      delta_prep_kernel<DK, NP, false><<<cus, kThreads, 0, st>>>(p); \
+    return hipGetLastError();                                      \
   }
   ONELA_DELTA_PREP(32, 1)
   ONELA_DELTA_PREP(64, 1)

@@ -1,16 +1,16 @@
-// The delta rule's chain over the chunks (see kernels_delta.hip).
-#include "delta_tiles.h"
+// The delta rule's chain over the chunks, forward (see kernels_delta.hip), and the chain over
+// the segments of either direction.
+#include "delta_chain.h"
 
 namespace onela {
 namespace {
 
-// Waves of a scan workgroup: 32 state rows each, at most 128 per workgroup.
-template <int DV>
-constexpr int kScanWaves = DV / 32 < 4 ? DV / 32 : 4;
+// What a walk over the chunks leaves: the outputs and the last state; the state after a
+// segment; or for the backward pass the state before and e of every chunk.
+enum { kOutputs, kSegment, kSave };
 
-// The chain over the chunks of one (sequence, value head) with its outputs: up to 128 rows of
-// the state per workgroup, 32 per wave as two column tiles of S^T (tile u, lane lr: row 2 lr
-// + u), which stay in registers.  Per chunk
+// The chain over the chunks of one (sequence, value head): up to 128 rows of the state per
+// workgroup, 32 per wave, in registers (ChainState).  Per chunk
 //   Y = K S^T, X = V - gamma Y, e = T X, O = scale gamma Q S^T + P e, S^T <- g S^T + K^T (beta sigma e)
 // with all products chained in registers: the order of tokens and columns within a
 // 32-deep step is that of the accumulators.
@@ -18,33 +18,28 @@ constexpr int kScanWaves = DV / 32 < 4 ? DV / 32 : 4;
 // Operands come to LDS straight from memory in the layout that is read there: the next
 // chunk's keys and queries during T X and P e, its T, P and gates during the update.
 //
-// Scales (powers of two).  Each lane's two rows are kept as st = sc S with a bound on
-// their largest value; the bound grows with every update by what 64 tokens can add at
-// most, and where it leaves [2^8, 2^15] the rows are scaled anew.  The true values are some
-// 2^7 below the bound, far inside what two fp16 parts hold to 22 bits of the largest.
-//
 // Segments.  One chain per 128 rows leaves most of the chip idle for few heads, so a
 // sequence can be cut into segments of p.cps chunks that run at once: S_out = S_in A + B.
-// With SEG the kernel forms, without outputs, for every segment but the sequence's last
-// the state that it leaves: of the first the true one, of the others B (from S_in =
-// 0) and, by the same code on the rows of the identity and V = 0, A.
+// kSegment forms, without outputs, for every segment but the sequence's last the
+// state that it leaves: of the first the true one, of the others B (from S_in = 0)
+// and, by the same code on the rows of the identity and V = 0, A.
 // delta_combine_kernel chains them, and then every segment starts from its true state.
-template <int DK, int DV, int NP, bool SEG>
-__global__ __launch_bounds__(64 * kScanWaves<DV>, DK >= 256 || NP == 2 ? 1 : 2)
+//
+// Bound: vector and matrix instructions (about 4 and 16 cycles each) take turns; at 512
+// workgroups of 16 chunks the matrix cores are busy 31% of the time, the vector units 34%.
+template <int DK, int DV, int NP, int KIND>
+__global__ __launch_bounds__(64 * kChainWaves<DV>, DK >= 256 || NP == 2 ? 1 : 2)
 void delta_forward_kernel(DeltaParams p) {
-  constexpr int NW = kScanWaves<DV>, GB = DV / (32 * NW);
+  constexpr bool SEG = KIND == kSegment, OUT = KIND == kOutputs;
+  constexpr int NW = kChainWaves<DV>, GB = DV / (32 * NW);
   constexpr int GA = SEG ? DK / (32 * NW) : 0;
-  constexpr int NB = DK / 16;
-  constexpr int PS = NB / 2 < 4 ? NB / 2 : 4;
-  auto t0 = [](int h) constexpr { return h / PS * (2 * PS) + h % PS; };
   constexpr int kIo = NP == 1 ? 2 : 4;
-  constexpr int kImage = sizeof(Swz<DK>) * NP, kFrags = 6 * 2 * 1024;
-  constexpr int kGateBytes = kDeltaGates * kC * 4;
+  constexpr int kImage = sizeof(Swz<DK>) * NP;
   __shared__ __align__(16) Swz<DK> sK[2][NP];
-  __shared__ __align__(16) Swz<DK> sQ[SEG ? 1 : NP];
-  __shared__ __align__(16) uint4 sT[kFrags / 16];
-  __shared__ __align__(16) uint4 sP[SEG ? 1 : kFrags / 16];
-  __shared__ __align__(16) float sG[kDeltaGates][kC];
+  __shared__ __align__(16) Swz<DK> sQ[OUT ? NP : 1];
+  __shared__ __align__(16) uint4 sT[kFragBytes / 16];
+  __shared__ __align__(16) uint4 sP[OUT ? kFragBytes / 16 : 1];
+  __shared__ __align__(16) float sG[kGateStage][kC];
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, lq = lane >> 4;
@@ -60,92 +55,33 @@ void delta_forward_kernel(DeltaParams p) {
   const int nch = sg.ce;
   const f32x4 z = {0.f, 0.f, 0.f, 0.f};
 
-  // st[u][b][i] = sc S(row0 + u, 16 b + 4 lq + i)
-  f32x4 st[2][NB];
-  float sc = 1.f, bound = 0.f;
+  ChainState<DK> s;
   const long rows = long(row0) * DK + 4 * lq;
-  const float* from = sg.j == 0 ? p.s_in : SEG ? nullptr : p.segs + (su - p.HV) * (DV * DK);
-  if (sg.j == 0 && from) from += (long(sg.n) * p.HV + hv) * (DV * DK);
-  auto rescale = [&](float f) __attribute__((always_inline)) {
-    const float to = fminf(fmaxf(sc * f, 0x1p-100f), 0x1p100f);
-    f = to * inverse_pow2(sc);
-    sc = to;
-    bound *= f;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) st[u][b] *= f;
-  };
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      st[u][b] = from ? *reinterpret_cast<const f32x4*>(from + rows + u * DK + 16 * b) : z;
-      if (ident)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) st[u][b][i] = 16 * b + 4 * lq + i == row0 + u ? 1.f : 0.f;
-      bound = max4abs(bound, st[u][b]);
-    }
-  bound = max_over_rows(bound);
-  if (from || ident) rescale(bound > 0.f ? scale_for(bound) : 1.f);
-
+  {
+    const float* from = sg.j == 0 ? p.s_in : SEG ? nullptr : p.segs + (su - p.HV) * (DV * DK);
+    if (sg.j == 0 && from) from += (long(sg.n) * p.HV + hv) * (DV * DK);
+    s.init(from ? from + rows : nullptr, ident, row0, lq);
+  }
   auto load_kq = [&](int c) __attribute__((always_inline)) {
     const long at = ((sq.slot + c) * p.HK + hk) * (kImage / 16);
     dma<kImage, NW>(p.kimg + at, sK[c & 1], w, lane);
-    if constexpr (!SEG) dma<kImage, NW>(p.qimg + at, sQ, w, lane);
+    if constexpr (OUT) dma<kImage, NW>(p.qimg + at, sQ, w, lane);
   };
   auto load_tp = [&](int c) __attribute__((always_inline)) {
     const long cu = (sq.slot + c) * p.HV + hv;
-    dma<kFrags, NW>(p.tp + cu * (kFrags / 16), sT, w, lane);
-    if constexpr (!SEG) dma<kFrags, NW>(p.pf + cu * (kFrags / 16), sP, w, lane);
-    dma<kGateBytes, NW>(p.gates + cu * (kDeltaGates * kC), sG, w, lane);
+    dma<kFragBytes, NW>(p.tp + cu * (kFragBytes / 16), sT, w, lane);
+    if constexpr (OUT) dma<kFragBytes, NW>(p.pf + cu * (kFragBytes / 16), sP, w, lane);
+    dma<kGateStage * kC * 4, NW>(p.gates + cu * (p.gate_rows * kC), sG, w, lane);
   };
-  // values V(t = 16 a + 4 lq + i, row0 + u), raw
   const unsigned vs = unsigned(p.vs) * kIo;
-  unsigned vr[16][NP];
+  Columns<NP> v;
   auto load_v = [&](int c) __attribute__((always_inline)) {
     const int m = ident ? 0 : min(kC, sq.len - c * kC);  // (A: no values)
-    const auto rs = rows_buffer(p.v, ((sq.t0 + long(c) * kC) * p.vs + hv * DV) * kIo, DV * kIo, vs, m);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const unsigned o = unsigned(4 * lq) * vs + row0 * kIo, so = (16 * (i >> 2) + (i & 3)) * vs;
-      if constexpr (NP == 1) {
-        vr[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rs, o, so, 0);
-      } else {
-        const auto x = __builtin_amdgcn_raw_buffer_load_b64(rs, o, so, 0);
-        vr[i][0] = x[0];
-        vr[i][1] = x[1];
-      }
-    }
-  };
-  auto value = [&](int i, int u) {
-    if constexpr (NP == 1)
-      return u ? bf16_hi_to_float(vr[i][0]) : bf16_lo_to_float(vr[i][0]);
-    else
-      return __uint_as_float(vr[i][u]);
+    v.load(rows_buffer(p.v, ((sq.t0 + long(c) * kC) * p.vs + hv * DV) * kIo, DV * kIo, vs, m), vs,
+           lq, row0 * kIo);
   };
   auto gate = [&](int row, int a) { return *reinterpret_cast<const f32x4*>(&sG[row][16 * a + 4 * lq]); };
   const int kb = Swz<DK>::off(lr, lq), tb = Swz<DK>::off(4 * lq + (lr >> 2), lr & 3);
-  constexpr int KR = 32 * Swz<DK>::LD;  // bytes of 16 rows
-  // acc[u][a] += F x[u] over a lower triangular 64 x 64 matrix in two parts, F's fragments in LDS
-  auto triangle = [&](const uint4* F, const uint4 (&x)[2][2][2], f32x4 (&acc)[2][4])
-      __attribute__((always_inline)) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint4 f[4][2];
-#pragma unroll
-      for (int a = 2 * h; a < 4; ++a)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          f[a][i] = F[((a < 2 ? a : 2 * a - 2 + h) * 2 + i) * 64 + lane];
-      for_products<2, 2>([&](int i, int j) {
-#pragma unroll
-        for (int a = 2 * h; a < 4; ++a)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) acc[u][a] = mfma_f16(f[a][i], x[u][h][j], acc[u][a]);
-      });
-    }
-  };
 
   if (sg.cb < nch) {
     load_kq(sg.cb);
@@ -156,37 +92,16 @@ void delta_forward_kernel(DeltaParams p) {
     const Swz<DK>* const K = sK[c & 1];
     dma_wait();
     __syncthreads();  // this chunk's operands are in LDS
-    const float inv = inverse_pow2(sc);
+    const long cu = (sq.slot + c) * p.HV + hv;
+    const float inv = inverse_pow2(s.sc), before = s.bound * inv;
+    if constexpr (KIND == kSave) s.store(p.sws + cu * (DV * DK) + rows);
     // Y = K S^T and Q S^T
     f32x4 y[2][4], o[2][4];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int a = 0; a < 4; ++a) y[u][a] = o[u][a] = z;
-#pragma unroll
-    for (int h = 0; h < DK / 32; ++h) {
-      uint4 sp[2][2], kf[4][NP], qf[4][NP];
-#pragma unroll
-      for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          kf[a][i] = row_frag(K[i], kb, t0(h), t0(h) + PS, KR * a);
-          if constexpr (!SEG) qf[a][i] = row_frag(sQ[i], kb, t0(h), t0(h) + PS, KR * a);
-        }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) parts8(st[u][t0(h)], st[u][t0(h) + PS], sp[u]);
-      for_products<NP, 2>([&](int i, int j) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int a = 0; a < 4; ++a) y[u][a] = mfma_f16(kf[a][i], sp[u][j], y[u][a]);
-        if constexpr (!SEG)
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int a = 0; a < 4; ++a) o[u][a] = mfma_f16(qf[a][i], sp[u][j], o[u][a]);
-      });
-    }
+    rows_times_state<DK, NP, OUT>(K, sQ, s, kb, y, o);
     // X = V - gamma Y, scaled for the lane's two rows
     uint4 xp[2][2][2];
     float ix;
@@ -199,55 +114,34 @@ void delta_forward_kernel(DeltaParams p) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[u][a][i] = fmaf(g[i], y[u][a][i], value(4 * a + i, u));
+          for (int i = 0; i < 4; ++i) x[u][a][i] = fmaf(g[i], y[u][a][i], v.get(4 * a + i, u));
           m = max4abs(m, x[u][a]);
         }
       }
-      const float s = scale_for(max_over_rows(m));
-      ix = inverse_pow2(s);
+      const float f = scale_for(max_over_rows(m));
+      ix = inverse_pow2(f);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        parts8<2>(x[u][0], x[u][1], s, xp[u][0]);
-        parts8<2>(x[u][2], x[u][3], s, xp[u][1]);
+        parts8<2>(x[u][0], x[u][1], f, xp[u][0]);
+        parts8<2>(x[u][2], x[u][3], f, xp[u][1]);
       }
     }
     __syncthreads();  // all have read the queries, and the last chunk's keys
     if (c + 1 < nch) load_kq(c + 1);
-    // e = T X (each token's row times its scale of T: the gates undo it)
+    // e = T X, times T's scale: the gates undo it
     f32x4 e[2][4];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int a = 0; a < 4; ++a) e[u][a] = z;
-    triangle(sT, xp, e);
+    triangle(sT, xp, e, lane);
     uint4 ep[2][2][2], zp[2][2][2];
-    float ie;
-    const float g = sG[kGateOne][0];
+    const float g = sG[kGateOne][kOneG], ik = sG[kGateOne][kOneK];
     {
-      float m = 0.f;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) m = max4abs(m, e[u][a]);
-      m = max_over_rows(m);
-      const float s = scale_for(m);
-      ie = inverse_pow2(s) * ix;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        parts8<2>(e[u][0], e[u][1], s, ep[u][0]);
-        parts8<2>(e[u][2], e[u][3], s, ep[u][1]);
-      }
-      // what the update adds, in units of sc, and the rows' bound after it
-      const float most = m * ix * (sG[kGateOne][1] * sG[kGateOne][2]);
-      float next = fmaf(g, bound, 0x1p13f * most * sc);
-      const bool off = !(next <= 32768.f && next >= 256.f) && next > 0.f;
-      if (__any(off)) {
-        const float was = sc;
-        rescale(off ? scale_for(next) : 1.f);
-        next *= sc * inverse_pow2(was);
-      }
-      bound = next;
-      const float cz = ix * sc * sG[kGateOne][2];
+      // |T X| in these units, by the largest row sum of |T|
+      const float m = sG[kGateOne][kOneT] * 0x1p14f;
+      s.make_room(g, m * ix * (sG[kGateOne][kOneZ] * ik));
+      const float cz = ix * s.sc * ik;
       f32x4 gz[4];
 #pragma unroll
       for (int a = 0; a < 4; ++a) gz[a] = gate(kGateZ, a) * cz;
@@ -257,14 +151,20 @@ void delta_forward_kernel(DeltaParams p) {
         parts8(e[u][2], e[u][3], gz[2], gz[3], zp[u][1]);
       }
     }
-    // P e, and the outputs
-    if constexpr (!SEG) {
+    if constexpr (OUT) {
+      // P e, and the outputs
+      const float f = sG[kGateOne][kOneE];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        parts8<2>(e[u][0], e[u][1], f, ep[u][0]);
+        parts8<2>(e[u][2], e[u][3], f, ep[u][1]);
+      }
       f32x4 q[2][4];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int a = 0; a < 4; ++a) q[u][a] = z;
-      triangle(sP, ep, q);
+      triangle(sP, ep, q, lane);
       const int m = min(kC, sq.len - c * kC);
       const unsigned os = unsigned(p.HV) * (DV * kIo);
       // a buffer that ends with the sequence's last token: stores past it are dropped
@@ -272,65 +172,37 @@ void delta_forward_kernel(DeltaParams p) {
                                   os, m);
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
-        const f32x4 go = gate(kGateO, a) * inv, gp = gate(kGateP, a) * ie;
+        const f32x4 go = gate(kGateO, a) * inv, gp = gate(kGateP, a) * ix;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x0 = fmaf(go[i], o[0][a][i], gp[i] * q[0][a][i]);
-          const float x1 = fmaf(go[i], o[1][a][i], gp[i] * q[1][a][i]);
-          const unsigned at = unsigned(4 * lq) * os + row0 * kIo, so = (16 * a + i) * os;
-          if constexpr (NP == 1) {
-            __builtin_amdgcn_raw_buffer_store_b32(pack_bf16x2(x0, x1), rs, at, so, 0);
-          } else {
-            typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-            __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(x0), __float_as_uint(x1)},
-                                                  rs, at, so, 0);
-          }
-        }
+        for (int i = 0; i < 4; ++i)
+          store_columns<NP>(rs, os, lq, row0 * kIo, 4 * a + i,
+                            fmaf(go[i], o[0][a][i], gp[i] * q[0][a][i]),
+                            fmaf(go[i], o[1][a][i], gp[i] * q[1][a][i]));
       }
+    }
+    if constexpr (KIND == kSave) {
+      const float f = sG[kGateOne][kOneIT] * ix;
+      float* const one = p.gates + (cu * p.gate_rows + kRevOne) * kC;
+      note_max(one + kMaxS, before, lane);
+      note_max(one + kMaxE, sG[kGateOne][kOneT] * 0x1p14f * f, lane);
+      float* const d = p.ews + (cu * DV + row0) * kC + 4 * lq;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+          *reinterpret_cast<f32x4*>(d + u * kC + 16 * a) = f * e[u][a];
     }
     __syncthreads();  // all have read T, P and the gates
     if (c + 1 < nch) {
       load_tp(c + 1);
       load_v(c + 1);
     }
-    // S^T <- g S^T + K^T (beta sigma e)
-    constexpr int NG = NB < 4 ? NB : 4;
-#pragma unroll
-    for (int b0 = 0; b0 < NB; b0 += NG) {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int b = 0; b < NG; ++b) st[u][b0 + b] *= g;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint4 kt[NG][NP];
-#pragma unroll
-        for (int b = 0; b < NG; ++b)
-#pragma unroll
-          for (int i = 0; i < NP; ++i) kt[b][i] = col_frag(K[i], tb, b0 + b, 2 * KR * h);
-        for_products<NP, 2>([&](int i, int j) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int b = 0; b < NG; ++b)
-              st[u][b0 + b] = mfma_f16(kt[b][i], zp[u][h][j], st[u][b0 + b]);
-        });
-      }
-    }
+    update_state<DK, NP, false>(s, g, K, zp, K, zp, tb);
   }
-  float* to = nullptr;
   if constexpr (SEG)
-    to = ident ? p.sega + su * (DK * DK) : p.segs + su * (DV * DK);
+    s.store((ident ? p.sega + su * (DK * DK) : p.segs + su * (DV * DK)) + rows);
   else if (p.s_out && sg.j + 1 == sg.nseg)
-    to = p.s_out + (long(sg.n) * p.HV + hv) * (DV * DK);
-  if (to) {
-    const float inv = inverse_pow2(sc);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-        *reinterpret_cast<f32x4*>(to + rows + u * DK + 16 * b) = inv * st[u][b];
-  }
+    s.store(p.s_out + (long(sg.n) * p.HV + hv) * (DV * DK) + rows);
 }
 
 // The true states after the segments of one (sequence, value head, 16 state rows): S_0 as
@@ -396,11 +268,11 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(DeltaParams p) {
 }
 
 template <int DK, int DV, int NP>
-hipError_t run(const DeltaParams& p, hipStream_t st) {
-  constexpr int NW = kScanWaves<DV>, GB = DV / (32 * NW), GA = DK / (32 * NW);
+hipError_t run(const DeltaParams& p, bool save, hipStream_t st) {
+  constexpr int NW = kChainWaves<DV>, GB = DV / (32 * NW), GA = DK / (32 * NW);
   const unsigned units = unsigned(p.seg_slots) * unsigned(p.HV);
   if (p.sega) {
-    delta_forward_kernel<DK, DV, NP, true><<<units * (GB + GA), 64 * NW, 0, st>>>(p);
+    delta_forward_kernel<DK, DV, NP, kSegment><<<units * (GB + GA), 64 * NW, 0, st>>>(p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     delta_combine_kernel<DK, DV>
@@ -408,15 +280,19 @@ hipError_t run(const DeltaParams& p, hipStream_t st) {
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  delta_forward_kernel<DK, DV, NP, false><<<units * GB, 64 * NW, 0, st>>>(p);
+  if (save)
+    delta_forward_kernel<DK, DV, NP, kSave><<<units * GB, 64 * NW, 0, st>>>(p);
+  else
+    delta_forward_kernel<DK, DV, NP, kOutputs><<<units * GB, 64 * NW, 0, st>>>(p);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_delta_forward(const DeltaShape& s, const DeltaParams& p, hipStream_t st) {
+hipError_t launch_delta_forward(const DeltaShape& s, const DeltaParams& p, bool save,
+                                hipStream_t st) {
 #define ONELA_DELTA_SCAN(DK, DV, NP) \
-  if (s.dk == DK && s.dv == DV && s.bf16 == (NP == 1)) return run<DK, DV, NP>(p, st);
+  if (s.dk == DK && s.dv == DV && s.bf16 == (NP == 1)) return run<DK, DV, NP>(p, save, st);
   ONELA_DELTA_SCAN(32, 32, 1)
   ONELA_DELTA_SCAN(64, 64, 1)
   ONELA_DELTA_SCAN(128, 128, 1)
@@ -428,6 +304,24 @@ hipError_t launch_delta_forward(const DeltaShape& s, const DeltaParams& p, hipSt
   ONELA_DELTA_SCAN(64, 64, 2)
   ONELA_DELTA_SCAN(128, 128, 2)
 #undef ONELA_DELTA_SCAN
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_delta_combine(const DeltaShape& s, const DeltaParams& p, hipStream_t st) {
+  const unsigned wgs = unsigned(p.N) * unsigned(p.HV) * unsigned(s.dv / 16);
+#define ONELA_DELTA_COMBINE(DK, DV)                         \
+  if (s.dk == DK && s.dv == DV) {                           \
+    delta_combine_kernel<DK, DV><<<wgs, 4 * DK, 0, st>>>(p); \
+    return hipGetLastError();                               \
+  }
+  ONELA_DELTA_COMBINE(32, 32)
+  ONELA_DELTA_COMBINE(64, 64)
+  ONELA_DELTA_COMBINE(128, 128)
+  ONELA_DELTA_COMBINE(128, 256)
+  ONELA_DELTA_COMBINE(128, 512)
+  ONELA_DELTA_COMBINE(256, 256)
+  ONELA_DELTA_COMBINE(256, 512)
+#undef ONELA_DELTA_COMBINE
   return hipErrorInvalidValue;
 }
 

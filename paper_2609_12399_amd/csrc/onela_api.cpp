@@ -480,6 +480,7 @@ onela_status_t onela_delta_rule_backward(
     return ONELA_EINVAL;
   rc = delta_workspace(s, true, workspace, workspace_bytes);
   if (rc != ONELA_OK) return rc;
+  s.cus = device_compute_units();
   p.s_in = initial_state;
   p.ds_in = d_final_state;
   p.ds_out = d_initial_state;
