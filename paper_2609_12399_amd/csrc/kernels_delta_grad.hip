@@ -47,7 +47,7 @@ struct GradLds {
 // requested a block ahead), the states' rows straight into operands.
 //   Bound: HBM (the states and their adjoints, e and dV, each read once).
 template <int DK, int NP, int NW>
-__global__ __launch_bounds__(64 * NW) void delta_grad_kernel(DeltaParams p) {
+__global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
   constexpr int TH = 64 * NW, CT = DK / (16 * NW), MT = (10 + NW - 1) / NW;
   constexpr int kIo = NP == 1 ? 2 : 4;
   constexpr int kImage = sizeof(Swz<DK>) * NP;
@@ -64,7 +64,6 @@ __global__ __launch_bounds__(64 * NW) void delta_grad_kernel(DeltaParams p) {
   const unsigned os = unsigned(p.HV) * p.DV * kIo;
   dma<kImage, NW>(p.kimg + (slot * p.HK + hk) * (kImage / 16), sh.K, w, lane);
   dma<kImage, NW>(p.qimg + (slot * p.HK + hk) * (kImage / 16), sh.Q, w, lane);
-  const int kb = Swz<DK>::off(lr, lq), tb = Swz<DK>::off(4 * lq + (lr >> 2), lr & 3);
   const int eb = Swz<kC, kNB>::off(4 * lq + (lr >> 2), lr & 3);
   constexpr int KR = 32 * Swz<DK>::LD;
   const f32x4 z = {0.f, 0.f, 0.f, 0.f};
@@ -242,6 +241,12 @@ __global__ __launch_bounds__(64 * NW) void delta_grad_kernel(DeltaParams p) {
         }
       }
     }
+    // (the lane's place as the compiler has not seen it: else it holds the addresses of all
+    // that follows in registers throughout the loops above)
+    int lane2 = lane;
+    asm("" : "+v"(lane2));
+    const int lr = lane2 & 15, lq = lane2 >> 4;
+    const int kb = Swz<DK>::off(lr, lq), tb = Swz<DK>::off(4 * lq + (lr >> 2), lr & 3);
     // rows' dot products with q and k, and the parts of dQ and dK from the states
     ss = group_sum<64>(ss);
     if (lane == 0) sh.ss[w] = ss;
@@ -257,27 +262,24 @@ __global__ __launch_bounds__(64 * NW) void delta_grad_kernel(DeltaParams p) {
         f32x4 dots[3] = {z, z, z};
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-          const int col = 16 * (CT * w + c) + lr;
           qS[a][c] *= iO * iS;
           kS[a][c] *= iV * iS;
           eD[a][c] *= iE * iD;
+          // q and k of this lane's tokens and column: a transposed read gives all four
+          f32x4 qv = z, kv = z;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int o = Swz<DK>::off(t0 + i, col >> 2) + 2 * (col & 3);
-            float qv = 0.f, kv = 0.f;
-#pragma unroll
-            for (int u = NP - 1; u >= 0; --u) {
-              auto el = [&](const Swz<DK>& t) {
-                return float(*reinterpret_cast<const _Float16*>(
-                    reinterpret_cast<const char*>(t.x) + o));
-              };
-              qv += el(sh.Q[u]);
-              kv += el(sh.K[u]);
-            }
-            dots[0][i] = fmaf(qv, qS[a][c][i], dots[0][i]);
-            dots[1][i] = fmaf(kv, kS[a][c][i], dots[1][i]);
-            dots[2][i] = fmaf(kv, eD[a][c][i], dots[2][i]);
+          for (int u = NP - 1; u >= 0; --u) {
+            auto four = [&](const Swz<DK>& t) {
+              const uint2 x = lds_tr4(t.template at<uint16_t>(tb, CT * w + c, KR * a));
+              const half2v lo = __builtin_bit_cast(half2v, x.x), hi = __builtin_bit_cast(half2v, x.y);
+              return f32x4{float(lo.x), float(lo.y), float(hi.x), float(hi.y)};
+            };
+            qv += four(sh.Q[u]);
+            kv += four(sh.K[u]);
           }
+          dots[0] += qv * qS[a][c];
+          dots[1] += kv * kS[a][c];
+          dots[2] += kv * eD[a][c];
           aq[a][c] += (-p.scale * ga) * qS[a][c];
           ak[a][c] += gb * eD[a][c] + ga * kS[a][c];
         }
@@ -492,7 +494,7 @@ __global__ __launch_bounds__(64 * NW) void delta_grad_kernel(DeltaParams p) {
 
 template <int DK, int NP>
 hipError_t run(const DeltaParams& p, hipStream_t st) {
-  constexpr int NW = DK / 16 < 8 ? DK / 16 : 8;
+  constexpr int NW = DK / 16 < 4 ? DK / 16 : DK >= 256 ? 8 : 4;
   auto grad = delta_grad_kernel<DK, NP, NW>;
   constexpr size_t lds = sizeof(GradLds<DK, NP>);
   static_assert(lds <= 160 * 1024, "one workgroup's LDS");
