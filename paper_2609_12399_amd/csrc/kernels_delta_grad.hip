@@ -40,6 +40,16 @@ struct GradLds {
   float ss[8], most[8];
 };
 
+// A lane's place that the compiler has not seen before: what is addressed by it is formed where
+// it is used, and not held in registers throughout the loops before.
+struct Lane {
+  int lr, lq;
+};
+__device__ inline Lane unseen(int lane) {
+  asm("" : "+v"(lane));
+  return {lane & 15, lane >> 4};
+}
+
 // Gradients of one chunk and one query/key head (the value heads of its group in
 // turn, their dQ and dK summed in registers).  Wave w holds the key columns 16 CT w ..
 // of dQ and dK; the tiles of the token by token products are dealt out to the waves.
@@ -241,17 +251,13 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
         }
       }
     }
-    // (the lane's place as the compiler has not seen it: else it holds the addresses of all
-    // that follows in registers throughout the loops above)
-    int lane2 = lane;
-    asm("" : "+v"(lane2));
-    const int lr = lane2 & 15, lq = lane2 >> 4;
-    const int kb = Swz<DK>::off(lr, lq), tb = Swz<DK>::off(4 * lq + (lr >> 2), lr & 3);
     // rows' dot products with q and k, and the parts of dQ and dK from the states
     ss = group_sum<64>(ss);
     if (lane == 0) sh.ss[w] = ss;
     const float ik = gate(kRevOne)[kRevK], iq = gate(kRevOne)[kRevQ];
     {
+      const Lane l = unseen(lane);
+      const int lr = l.lr, lq = l.lq, tb = Swz<DK>::off(4 * lq + (lr >> 2), lr & 3);
       const float iS = inverse_pow2(sS), iV = inverse_pow2(sV), iE = inverse_pow2(sE),
                   iO = inverse_pow2(sO), iD = inverse_pow2(sD);
 #pragma unroll
@@ -283,13 +289,16 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
           aq[a][c] += (-p.scale * ga) * qS[a][c];
           ak[a][c] += gb * eD[a][c] + ga * kS[a][c];
         }
+        // lane lr keeps the sum lr = 4 u + i of the 16 lanes
+        float mine = 0.f;
 #pragma unroll
         for (int u = 0; u < 3; ++u)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float s = group_sum<16>(dots[u][i]) * (u == 0 ? iq : ik);
-            if (lr == 0) sh.dots[w][u][t0 + i] = s;
+            const float s = group_sum<16>(dots[u][i]);
+            mine = lr == 4 * u + i ? s : mine;
           }
+        if (lr < 12) sh.dots[w][lr >> 2][t0 + (lr & 3)] = mine * (lr < 4 ? iq : ik);
       }
     }
     // the tiles of L and M and their sums
@@ -300,6 +309,8 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
     for (int m = 0; m < MT; ++m) {
       const int x = w + m * NW;
       if (x >= 10) break;
+      const Lane l = unseen(lane);
+      const int lr = l.lr, lq = l.lq, kb = Swz<DK>::off(lr, lq);
       int a, b;
       tile_of(x, a, b);
       f32x4 qk = z, kk = z;
@@ -321,7 +332,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
       kk *= ik * ik;
       const int j = 16 * b + lr;
       const float hj = gate(kRevHi)[j], lj = gate(kRevLo)[j], bj = gate(kRevBeta)[j];
-      float cz = 0.f, cb = 0.f;
+      float cz = 0.f, cb = 0.f, mine = 0.f;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int i = 16 * a + 4 * lq + q;
@@ -334,8 +345,9 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
         cb += px * qk[q] - nx * kk[q];
         cz += zz;
         const float rz = group_sum<16>(zz);
-        if (lr == 0) sh.zrow[b][i] = rz;
+        mine = lr == q ? rz : mine;
       }
+      if (lr < 4) sh.zrow[b][16 * a + 4 * lq + lr] = mine;
       most = max4abs(max4abs(most, lt[m]), mt[m]);
       cz = sum_over_rows(cz);
       cb = sum_over_rows(cb);
@@ -354,6 +366,8 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
     for (int m = 0; m < MT; ++m) {
       const int x = w + m * NW;
       if (x >= 10) break;
+      const Lane ln = unseen(lane);
+      const int lr = ln.lr, lq = ln.lq;
       int a, b;
       tile_of(x, a, b);
       unsigned l0[2], l1[2], m0[2], m1[2];
@@ -393,6 +407,8 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
     // dQ += L K, dK += L^T Q + (M + M^T) K
     {
       const float il = inverse_pow2(sl);
+      const Lane l = unseen(lane);
+      const int lr = l.lr, lq = l.lq, tb = Swz<DK>::off(4 * lq + (lr >> 2), lr & 3);
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
         f32x4 x0[CT], x1[CT], x2[CT];
@@ -471,25 +487,29 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
       }
     }
   }
+  // (buffers that end with the last token: stores past it are dropped)
+  const unsigned ds = unsigned(p.HK) * (DK * kIo);
+  const long first = (ch.t0 * p.HK + hk) * (DK * kIo);
+  const auto qr = rows_buffer(p.dq, first, DK * kIo, ds, ch.n),
+             kr = rows_buffer(p.dk, first, DK * kIo, ds, ch.n);
+  const Lane l = unseen(lane);
+  const unsigned at = unsigned(4 * l.lq) * ds + (16 * CT * w + l.lr) * kIo;
 #pragma unroll
   for (int a = 0; a < 4; ++a)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = 16 * a + 4 * lq + i;
-      if (t >= ch.n) continue;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
-        const long at = ((ch.t0 + t) * p.HK + hk) * DK + 16 * (CT * w + c) + lr;
+        const unsigned so = unsigned(16 * a + i) * ds + 16 * c * kIo;
         if constexpr (NP == 1) {
           const unsigned u = pack_bf16x2(aq[a][c][i], ak[a][c][i]);
-          static_cast<uint16_t*>(p.dq)[at] = uint16_t(u);
-          static_cast<uint16_t*>(p.dk)[at] = uint16_t(u >> 16);
+          __builtin_amdgcn_raw_buffer_store_b16(uint16_t(u), qr, at, so, 0);
+          __builtin_amdgcn_raw_buffer_store_b16(uint16_t(u >> 16), kr, at, so, 0);
         } else {
-          static_cast<float*>(p.dq)[at] = aq[a][c][i];
-          static_cast<float*>(p.dk)[at] = ak[a][c][i];
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(aq[a][c][i]), qr, at, so, 0);
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(ak[a][c][i]), kr, at, so, 0);
         }
       }
-    }
 }
 
 template <int DK, int NP>
