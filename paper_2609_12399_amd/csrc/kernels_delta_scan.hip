@@ -208,8 +208,8 @@ void delta_forward_kernel(DeltaParams p) {
 // The true states after the segments of one (sequence, value head, 16 state rows): S_0 as
 // it is, then S_j = S_{j-1} A_j + B_j, in B_j's place.  Wave w holds the columns 16 w ..
 // 16 w + 15 as an accumulator tile of S^T; the tiles, cut into three bf16 parts, are exchanged
-// through LDS as operands (one barrier per segment), A_j's rows come from memory, requested one
-// segment ahead.  Bound: latency of the chain over the segments.
+// through LDS as operands (one barrier per segment), A_j's rows come from memory, requested two
+// segments ahead.  Bound: latency of the chain over the segments.
 template <int DK, int DV>
 __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(DeltaParams p) {
   constexpr int NH = DK / 32, NRB = DV / 16;
@@ -225,20 +225,21 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(DeltaParams p) {
   const long at = long(16 * rb + lr) * DK + 16 * w + 4 * lq;
   auto state = [&](int j) { return p.segs + ((slot0 + j) * p.HV + hv) * (DV * DK) + at; };
   f32x4 st = *reinterpret_cast<const f32x4*>(state(0));
-  // A^T(16 w + lr, k): slots k = 32 h + 4 lq + i and 32 h + 16 + 4 lq + i
-  f32x4 a[NH][2];
-  auto load = [&](int j, int h) {
-    const float* q = p.sega + ((slot0 + min(j, last)) * p.HV + hv) * (DK * DK) +
-                     (32 * h + 4 * lq) * DK + 16 * w + lr;
+  // A^T(16 w + lr, k): slots k = 32 h + 4 lq + i and 32 h + 16 + 4 lq + i; AHEAD segments' in
+  // flight (1024 threads leave no registers for two)
+  constexpr int AHEAD = DK < 256 ? 2 : 1;
+  f32x4 a[AHEAD][NH][2], bn[AHEAD];
+  auto load = [&](int j, f32x4 (&to)[2], int h) __attribute__((always_inline)) {
+    const auto rs = buffer(p.sega + ((slot0 + min(j, last)) * p.HV + hv) * (DK * DK), DK * DK * 4);
+    const unsigned at0 = unsigned(4 * lq * DK + 16 * w + lr) * 4;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) a[h][u][i] = q[(16 * u + i) * DK];
+      for (int i = 0; i < 4; ++i)
+        to[u][i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+            rs, at0, unsigned(32 * h + 16 * u + i) * (DK * 4), 0));
   };
-  f32x4 bn = *reinterpret_cast<const f32x4*>(state(1));
-#pragma unroll
-  for (int h = 0; h < NH; ++h) load(1, h);
-  for (int j = 1; j <= last; ++j) {
+  auto step = [&](int j, f32x4 (&aj)[NH][2], f32x4& bj) __attribute__((always_inline)) {
     const int x = j & 1;
     uint4 d[3];
     cut3(st, st, d[0], d[1], d[2]);
@@ -251,8 +252,8 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(DeltaParams p) {
     for (int h = 0; h < NH; ++h) {
       const uint4 dh = xs[x][h][0][lane], dm = xs[x][h][1][lane], dl = xs[x][h][2][lane];
       uint4 t[3];
-      cut3(a[h][0], a[h][1], t[0], t[1], t[2]);
-      load(j + 1, h);  // (into the registers just read)
+      cut3(aj[h][0], aj[h][1], t[0], t[1], t[2]);
+      load(j + AHEAD, aj[h], h);  // (into the registers just read)
       const int e = h & 1;
       hi[e] = mfma_bf16(t[0], dh, hi[e]);
       lo[e] = mfma_bf16(t[2], dh, lo[e]);
@@ -261,9 +262,22 @@ __global__ __launch_bounds__(4 * DK) void delta_combine_kernel(DeltaParams p) {
       lo[2 + e] = mfma_bf16(t[1], dh, lo[2 + e]);
       lo[e] = mfma_bf16(t[0], dm, lo[e]);
     }
-    st = bn + ((hi[0] + hi[1]) + ((lo[0] + lo[1]) + (lo[2] + lo[3])));
-    bn = *reinterpret_cast<const f32x4*>(state(min(j + 1, last)));
+    st = bj + ((hi[0] + hi[1]) + ((lo[0] + lo[1]) + (lo[2] + lo[3])));
+    bj = *reinterpret_cast<const f32x4*>(state(min(j + AHEAD, last)));
     *reinterpret_cast<f32x4*>(state(j)) = st;
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    bn[i] = *reinterpret_cast<const f32x4*>(state(min(1 + i, last)));
+#pragma unroll
+    for (int h = 0; h < NH; ++h) load(1 + i, a[i][h], h);
+  }
+  for (int j = 1; j <= last; j += AHEAD) {
+    step(j, a[0], bn[0]);
+    if constexpr (AHEAD == 2) {
+      if (j + 1 > last) break;
+      step(j + 1, a[1], bn[1]);
+    }
   }
 }
 

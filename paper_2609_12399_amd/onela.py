@@ -201,10 +201,25 @@ def _rows(x, name: str, stride: int, optional: bool = False):
     return x.data_ptr()
 
 
+_torch_stream = None
+
+
+def _current_stream() -> int:
+    """hipStream_t of torch's current stream."""
+    global _torch_stream
+    if _torch_stream is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:  # the public way builds a Stream object for every call
+            _torch_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+        else:
+            _torch_stream = lambda: raw(torch.cuda.current_device())  # noqa: E731
+    return _torch_stream()
+
+
 def _stream(stream):
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
