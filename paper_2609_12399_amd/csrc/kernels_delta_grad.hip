@@ -6,10 +6,10 @@ namespace {
 
 constexpr int kNB = 32;  // columns of the values taken at a time
 
-// 64 rows of 64 fp16 elements that are written in pieces of 4 and read by rows (padded by 16
-// bytes).
+// 64 rows of 64 fp16 elements that are written in pieces of 4 and read by rows (padded by 8
+// bytes: 16 rows' pieces in 16 different places of the 128-byte bank row).
 struct Square {
-  uint16_t x[kC][kC + 8];
+  uint16_t x[kC][kC + 4];
 };
 
 // The lower triangle's tile x (of 10): row block a, column block b <= a.
@@ -21,7 +21,7 @@ __device__ inline void tile_of(int x, int& a, int& b) {
 template <int NP>
 struct GradStage {
   Swz<kC, kNB> e[2], dv[2];        // [columns][tokens], two parts
-  uint16_t dO[NP][kC][kNB + 16];   // [tokens][columns]
+  uint16_t dO[NP][kC][kNB + 4];   // [tokens][columns]
 };
 
 template <int DK, int NP>
@@ -130,7 +130,9 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
     const int hv = hk * G + hg;
     const long cu = slot * p.HV + hv;
     if (hg > 0) __syncthreads();  // (the last head's readers are done)
-    for (int i = tid; i < kGateStage * kC; i += TH)
+    int at0 = tid;
+    asm("" : "+v"(at0));
+    for (int i = at0; i < kGateStage * kC; i += TH)
       (&sh.gates[0][0])[i] = p.gates[(cu * p.gate_rows + kGateStage) * kC + i];
     auto gate = [&](int row) { return sh.gates[row - kGateStage]; };
     // scales, from the bounds that the chains left (the same for every lane)
@@ -188,7 +190,11 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
         parts8<NP>(y0, y1, sO, part);
 #pragma unroll
         for (int i = 0; i < NP; ++i)
-          *reinterpret_cast<uint4*>(&x.dO[i][e / (kNB / 8)][8 * (e % (kNB / 8))]) = part[i];
+        {
+          uint2* const to = reinterpret_cast<uint2*>(&x.dO[i][e / (kNB / 8)][8 * (e % (kNB / 8))]);
+          to[0] = make_uint2(part[i].x, part[i].y);
+          to[1] = make_uint2(part[i].z, part[i].w);
+        }
       }
       uint4 sp[CT][2], dp[CT][2];
 #pragma unroll
@@ -453,7 +459,8 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
     }
     // dbeta and dlog_alpha (the dot products and sums passed the barriers above)
     if (w == 0) {
-      const int t = lane;
+      int t = lane;
+      asm("" : "+v"(t));
       float dt[3] = {0.f, 0.f, 0.f};
       for (int i = 0; i < NW; ++i)
 #pragma unroll
@@ -514,7 +521,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
 
 template <int DK, int NP>
 hipError_t run(const DeltaParams& p, hipStream_t st) {
-  constexpr int NW = DK / 16 < 4 ? DK / 16 : DK >= 256 ? 8 : 4;
+  constexpr int NW = DK / 16 < 8 ? DK / 16 : 8;
   auto grad = delta_grad_kernel<DK, NP, NW>;
   constexpr size_t lds = sizeof(GradLds<DK, NP>);
   static_assert(lds <= 160 * 1024, "one workgroup's LDS");
