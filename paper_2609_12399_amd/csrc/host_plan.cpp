@@ -275,14 +275,23 @@ DeltaSegments delta_segments(const DeltaShape& s, bool ragged) {
   const long waves = std::min(s.dv / 32, 4);
   const long gb = s.dv / (32 * waves), ga = s.dk / (32 * waves);
   const long units = long(s.N) * s.HV, cus = s.cus;
-  // Times per chunk in ns of a workgroup alone on a compute unit: with outputs, without
-  const long full = 4700, bare = 2800, chain = 1400;
-  auto rounds = [&](long wgs) { return (wgs + cus - 1) / cus; };
+  // Times in ns: of a chunk with outputs and without, of a chained segment, and of the two more
+  // launches.  A chunk takes up to 1.4 times as long where every compute unit has a
+  // workgroup (their operands share the memory).  Measured, us per forward / backward call:
+  // 1 x 4096 tokens x 16 heads of 128 315 / 917 in one segment, 116 / 373 in 8, 114 / 364 in
+  // 16 (taken), 130 / 402 in 22; 8 x 1024 x 16 heads 122 / 512 in one (taken), 138 / 541 in
+  // two; 1 x 4096 x 8 heads of 256 514 / 1550 in one, 213 / 693 in 8 (taken), 262 / 790 in
+  // 16; 1 x 2048 x 4 heads of 64 124 / 274 in one, 44 / 103 in 16 (taken).
+  const long full = s.dk >= 256 ? 7300 : s.dk == 128 ? 4700 : 3300;
+  const long bare = s.dk >= 256 ? 4500 : s.dk == 128 ? 2800 : 2000;
+  const long chain = s.dk >= 256 ? 4600 : s.dk == 128 ? 2300 : 800, more = 12000;
+  auto spread = [&](long wgs, long per) {
+    return (wgs + cus - 1) / cus * per * (10 * cus + 4 * std::min(wgs, cus)) / (10 * cus);
+  };
   auto cost = [&](long cps) {
     const long n = (nch + cps - 1) / cps;
-    long t = rounds(units * gb * n) * std::min(cps, nch) * full;
-    if (n > 1)
-      t += rounds(units * (gb + (n - 2) * (gb + ga))) * cps * bare + 4000 + chain * (n - 1);
+    long t = spread(units * gb * n, std::min(cps, nch) * full);
+    if (n > 1) t += spread(units * (gb + (n - 2) * (gb + ga)), cps * bare) + more + chain * (n - 1);
     return t;
   };
   long best = nch, t = cost(nch);

@@ -176,13 +176,16 @@ def _dev(x, name: str, optional: bool = False):
         raise ValueError(f"{name} must not be None")
     if isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        if not getattr(x, "is_cuda", False):
-            raise ValueError(f"{name} must be a GPU tensor")
-        if not x.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-        return x.data_ptr()
-    raise TypeError(f"{name}: unsupported pointer type {type(x)}")
+    try:
+        if x.is_cuda and x.is_contiguous():
+            return x.data_ptr()
+    except AttributeError:
+        pass
+    if not hasattr(x, "data_ptr"):
+        raise TypeError(f"{name}: unsupported pointer type {type(x)}")
+    if not getattr(x, "is_cuda", False):
+        raise ValueError(f"{name} must be a GPU tensor")
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _rows(x, name: str, stride: int, optional: bool = False):
