@@ -370,3 +370,51 @@ def test_offsets_beyond_32_bits():
         (k, [15]), (k, [15]), (v, [60, 63]), (la, [60, 63]), (beta, [60, 63]))], 1.0)
     check("o", o[tail][200:, [60, 63]], want[200:], 1, "bf16")
     check("state", last[N - 1:, [60, 63]], state, 1)
+
+
+# ---- the chain in segments --------------------------------------------------------------
+# Long sequences of few heads are cut into segments that run at once (the number is the
+# library's choice by the device's compute units); a chained segment adds one product with its
+# transition matrix (2^-24 of its largest terms), within the bars above.
+
+@pytest.mark.parametrize("lengths,HK,HV,dk,dv,io,equal", [
+    ([64 * 21 + 5], 1, 2, 64, 64, "bf16", False), ([64 * 16], 1, 1, 128, 128, "bf16", True),
+    ([64 * 9 + 1, 3, 64 * 14], 1, 2, 128, 128, "bf16", False),
+    ([64 * 12] * 3, 1, 1, 32, 32, "f32", True), ([64 * 13 - 1, 0, 64 * 5], 1, 3, 64, 64, "f32", False),
+    ([64 * 10 + 30], 1, 1, 256, 256, "bf16", False), ([64 * 9], 1, 1, 128, 256, "bf16", True),
+    ([64 * 11 + 17], 1, 1, 128, 128, "f32", False)])
+def test_segments(lengths, HK, HV, dk, dv, io, equal):
+    run_both(lengths, HK, HV, dk, dv, io, seed=7, equal=equal, alpha_mu=-5.0)
+
+
+@pytest.mark.parametrize("size", [1e-6, 1e6])
+def test_magnitudes(size):
+    """Values and states scaled by a power of ten: results scale with them (parts of fp32
+    operands carry scales of their own; nothing overflows or vanishes)."""
+    def tweak(x):
+        x[2].mul_(size)
+    x, g = draw([140], 1, 2, 64, 64, "f32", 5)
+    tweak(x)
+    s0 = size * torch.randn((1, 2, 64, 64), generator=g).to(DEV)
+    do = torch.randn((140, 2, 64), generator=g).to(DEV) / size
+    ds = torch.randn((1, 2, 64, 64), generator=g).to(DEV) / size
+    host = [f64(t) for t in x]
+    o, last, _ = ref.forward([140], *host, 1.0, f64(s0))
+    fo, fs = op_of([140], 1, 2, 64, 64, "f32", 1.0).forward(*x, None, s0)
+    check("o", fo, o, 1)
+    check("final state", fs, last, 1)
+    want = ref.backward([140], *host, 1.0, f64(s0), f64(do), f64(ds))
+    got = op_of([140], 1, 2, 64, 64, "f32", 1.0, True).backward(*x, do, None, s0, ds)
+    for name, a, w, bar in zip(("dq", "dk", "dv", "dla", "db", "ds"), got, want,
+                               (F32, F32, F32, SUMS, F32, F32)):
+        check(name, a, w, 1, bar=bar)
+
+
+def test_keys_and_queries_of_any_size():
+    """Unnormalised keys (small ones beside large ones, whole tokens of zeros) and queries."""
+    def tweak(x):
+        x[1].mul_(0.02 + torch.arange(x[1].shape[0], device=DEV)[:, None, None] % 7 * 0.2)
+        x[1][5] = 0
+        x[0].mul_(300.0)
+    run_both([130], 1, 2, 64, 64, "f32", tweak=tweak)
+    run_both([130], 1, 2, 64, 64, "bf16", tweak=tweak)
