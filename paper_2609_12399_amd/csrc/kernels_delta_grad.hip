@@ -18,9 +18,12 @@ __device__ inline void tile_of(int x, int& a, int& b) {
   b = x - a * (a + 1) / 2;
 }
 
+// [columns][tokens], only read transposed.
+using Columns32 = Swz<kC, kNB, 15>;
+
 template <int NP>
 struct GradStage {
-  Swz<kC, kNB> e[2], dv[2];        // [columns][tokens], two parts
+  Columns32 e[2], dv[2];           // two parts
   uint16_t dO[NP][kC][kNB + 4];   // [tokens][columns]
 };
 
@@ -74,7 +77,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
   const unsigned os = unsigned(p.HV) * p.DV * kIo;
   dma<kImage, NW>(p.kimg + (slot * p.HK + hk) * (kImage / 16), sh.K, w, lane);
   dma<kImage, NW>(p.qimg + (slot * p.HK + hk) * (kImage / 16), sh.Q, w, lane);
-  const int eb = Swz<kC, kNB>::off(4 * lq + (lr >> 2), lr & 3);
+  const int eb = Columns32::off(4 * lq + (lr >> 2), lr & 3);
   constexpr int KR = 32 * Swz<DK>::LD;
   const f32x4 z = {0.f, 0.f, 0.f, 0.f};
   f32x4 aq[4][CT], ak[4][CT];  // dQ, dK(t = 16 a + 4 lq + i, 16 (CT w + c) + lr)
@@ -159,9 +162,9 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
       // (this buffer's last readers passed the barrier of the block before)
 #pragma unroll
       for (int q = 0; q < NE; ++q) {
-        const int e = tid + q * TH, o = Swz<kC, kNB>::off(e / 16, e % 16);
+        const int e = tid + q * TH, o = Columns32::off(e / 16, e % 16);
         unsigned u[2], v[2];
-        auto put = [&](const f32x4& y, float s, Swz<kC, kNB>* to) {
+        auto put = [&](const f32x4& y, float s, Columns32* to) {
           parts2<2>(y.x, y.y, s, u);
           parts2<2>(y.z, y.w, s, v);
 #pragma unroll

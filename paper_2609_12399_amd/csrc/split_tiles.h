@@ -93,13 +93,14 @@ __device__ inline uint2 lds_tr4(const uint16_t* a) {
 // tokens against padded rows; with 16 pieces per row only f's low 3 bits are used, so
 // that the two pieces of a key operand stay a constant apart).  Narrower rows
 // are padded instead.
-template <int COLS, int ROWS = 64>
+// Tiles that are only read transposed take all four bits from 16 pieces on (MASK).
+template <int COLS, int ROWS = 64, int MASK = COLS >= 128 ? 15 : 7>
 struct Swz {
   static constexpr bool kXor = COLS >= 64;
   static constexpr int LD = kXor ? COLS : COLS + 16;
   uint16_t x[ROWS * LD];
   __device__ static int f(int row) {
-    return (((row & 3) << 2) | ((row >> 2) & 3)) & (COLS >= 128 ? 15 : 7);
+    return (((row & 3) << 2) | ((row >> 2) & 3)) & MASK;
   }
   // Byte offset of (row, piece): f(row) has the four low bits, so the pieces
   // 4 j + m of one lane are the XOR of its piece m with 4 j, j < 4, and the rest
