@@ -121,6 +121,9 @@ __device__ inline void dma(const void* from, void* to, int w, int lane) {
           (__attribute__((address_space(3))) void*)(static_cast<char*>(to) + b * 1024), 16, 0, 0);
   }
 }
+// Barrier for what the waves exchange through LDS by ordinary reads and writes: loads and
+// stores of memory stay in flight across it (__syncthreads waits for all stores).
+__device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ inline void dma_wait() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
 
 // Row operand of a tile of 16 rows (lane row lr, first piece lq): the two pieces

@@ -367,7 +367,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
     }
     most = wave_max(most);
     if (lane == 0) sh.most[w] = most;
-    __syncthreads();  // (all have read the last columns)
+    lds_barrier();  // (all have read the last columns)
 #pragma unroll
     for (int i = 0; i < NW; ++i) most = fmaxf(most, sh.most[i]);
     const float sl = scale_for(most);
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
       const int r = 16 * (tr ? a + 1 : a) + (l & 15), c = 16 * (tr ? a : a + 1) + 4 * (l >> 4);
       *reinterpret_cast<uint2*>(&(tr ? sh.p.lt : sh.p.l)[i].x[r][c]) = make_uint2(0u, 0u);
     }
-    __syncthreads();
+    lds_barrier();
     // dQ += L K, dK += L^T Q + (M + M^T) K
     {
       const float il = inverse_pow2(sl);

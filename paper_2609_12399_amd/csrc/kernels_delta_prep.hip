@@ -85,7 +85,7 @@ struct PrepLds {
     KQ kq;
     MT mt;  // after the products of keys and queries
   };
-  double g[kC];                          // sums of log2(alpha)
+  alignas(16) float gh[kC], gl[kC];          // sums of log2(alpha) as hi + lo
   alignas(16) float be[kC], bs[kC], ip[kC];  // beta, beta sigma, inverse scales of P's rows
   float most[4][5];  // per wave: the largest key, query, element of T, row and column sum of it
 };
@@ -129,7 +129,8 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
         const double u = __shfl_up(g, d);
         if (lane >= d) g += u;
       }
-      sh.g[lane] = g;
+      sh.gh[lane] = float(g);
+      sh.gl[lane] = float(g - double(float(g)));
       sh.be[lane] = be;
       sh.bs[lane] = be * exp2_fast(float(__shfl(g, 63) - g));
     }
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
       sh.most[w][0] = mk;
       sh.most[w][1] = mq;
     }
-    __syncthreads();
+    lds_barrier();
     sk = scale_for_rows(fmaxf(fmaxf(sh.most[0][0], sh.most[1][0]),
                               fmaxf(sh.most[2][0], sh.most[3][0])));
     sq = scale_for_rows(fmaxf(fmaxf(sh.most[0][1], sh.most[1][1]),
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
     rq.store(sh.kq.Q, sq, tid);
   }
   const float ik = inverse_pow2(sk), iq = inverse_pow2(sq);
-  __syncthreads();
+  lds_barrier();
   if (hv == hk * G) {  // one of the group's heads keeps the images, as they stand in LDS
     constexpr int NI = sizeof(sh.kq.K) / 16;
     uint4* const ki = p.kimg + (slot * p.HK + hk) * NI;
@@ -159,6 +160,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
   }
   const int kb = Swz<DK>::off(lr, lq);
   constexpr int KR = 32 * Swz<DK>::LD;
+  auto four = [&](const float* x) { return *reinterpret_cast<const f32x4*>(x); };
   // rows x of a against rows y of b, 16 each: lane (lr, lq) holds (16 a + 4 lq + i, 16 b + lr)
   // (base: the lane's first piece of row lr, or of row 15 - lr for rows in reverse order)
   auto dots = [&](const Swz<DK>* x, int a, const Swz<DK>* y, int b, int base) {
@@ -181,7 +183,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
     // of one token, half a fragment; backward of 16 tokens j and four neighbouring t
     const int pa = w == 0 ? 2 : w == 1 ? 1 : w == 2 ? 3 : 0;
     const int t = BWD ? kC - 1 - 16 * pa - lr : 16 * pa + lr;  // backward: the token j
-    const double gq = sh.g[t];
+    const float hq = sh.gh[t], lo = sh.gl[t];
     const float c = p.scale * (ik * iq) * (BWD ? sh.be[t] : 1.f);
     f32x4 x[4];
     float most = 0.f;
@@ -191,18 +193,21 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
       if (b > pa) continue;
       if constexpr (!BWD) {
         const f32x4 acc = dots(sh.kq.K, b, sh.kq.Q, pa, kb);
-        const f32x4 be = *reinterpret_cast<const f32x4*>(&sh.be[16 * b + 4 * lq]);
+        const int j0 = 16 * b + 4 * lq;
+        const f32x4 be = four(&sh.be[j0]), h = four(&sh.gh[j0]), l = four(&sh.gl[j0]);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int j = 16 * b + 4 * lq + q;
-          x[b][q] = j <= t ? c * exp2_fast(float(gq - sh.g[j])) * be[q] * acc[q] : 0.f;
+          const float y = c * exp2_fast((hq - h[q]) + (lo - l[q])) * be[q] * acc[q];
+          x[b][q] = j0 + q <= t ? y : 0.f;
         }
       } else {
         const f32x4 acc = dots(sh.kq.Q, 3 - b, sh.kq.K, 3 - pa, Swz<DK>::off(15 - lr, lq));
+        const int i0 = kC - 4 - 16 * b - 4 * lq;
+        const f32x4 h = four(&sh.gh[i0]), l = four(&sh.gl[i0]);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int i = kC - 1 - 16 * b - 4 * lq - q;
-          x[b][q] = t <= i ? c * exp2_fast(float(sh.g[i] - gq)) * acc[q] : 0.f;
+          const float y = c * exp2_fast((h[3 - q] - hq) + (l[3 - q] - lo)) * acc[q];
+          x[b][q] = t <= i0 + 3 - q ? y : 0.f;
         }
       }
       most = max4abs(most, x[b]);
@@ -225,13 +230,14 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
     f32x4 m[3];
     auto tile = [&](int a, int b) {
       f32x4 acc = dots(sh.kq.K, a, sh.kq.K, b, kb);
-      const int j = 16 * b + lr;
-      const double gj = sh.g[j];
+      const int j = 16 * b + lr, i0 = 16 * a + 4 * lq;
+      const float hj = sh.gh[j], lj = sh.gl[j];
+      const f32x4 h = four(&sh.gh[i0]), l = four(&sh.gl[i0]);
       const float bk = sh.be[j] * ik * ik;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int i = 16 * a + 4 * lq + q;
-        acc[q] = j < i ? exp2_fast(float(sh.g[i] - gj)) * bk * acc[q] : 0.f;
+        const float y = exp2_fast((h[q] - hj) + (l[q] - lj)) * bk * acc[q];
+        acc[q] = j < i0 + q ? y : 0.f;
       }
       return acc;
     };
@@ -239,7 +245,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
     m[0] = tile(a0, b0);
     m[1] = tile(w, w);
     if (w < 2) m[2] = tile(3, w + 1);
-    __syncthreads();  // keys and queries are not read any more: M and T take their place
+    lds_barrier();  // keys and queries are not read any more: M and T take their place
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       sh.mt.M[16 * a0 + 4 * lq + q][16 * b0 + lr] = m[0][q];
@@ -277,7 +283,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
       M[16 * w + 4 * lq + q][16 * w + lr] = tc[0][q];
     }
   }
-  __syncthreads();
+  lds_barrier();
 #pragma unroll
   for (int d = 1; d < 4; ++d) {
     if (w + d >= 4) break;
@@ -317,7 +323,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
     for (int q = 0; q < 4; ++q)  // the blocks above the diagonal that a 32-token step covers
       if (w & 1) T[16 * (w - 1) + 4 * lq + q][16 * w + lr] = 0.f;
   }
-  __syncthreads();
+  lds_barrier();
   const float s = scale_for(fmaxf(fmaxf(sh.most[0][2], sh.most[1][2]),
                                   fmaxf(sh.most[2][2], sh.most[3][2])));
   // T fragments of row tile w: a lane holds row 16 w + lr and the columns 32 h + 4 lq +
@@ -356,13 +362,13 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
       if (lane == 0) sh.most[w][3 + r] = most;
     }
   }
-  __syncthreads();
+  lds_barrier();
   if (w == 0) {
     auto most = [&](int i) {
       return fmaxf(fmaxf(sh.most[0][i], sh.most[1][i]), fmaxf(sh.most[2][i], sh.most[3][i])) * s;
     };
-    const float it = inverse_pow2(s), gam = exp2_fast(float(sh.g[lane])), bs = sh.bs[lane];
-    const float all = exp2_fast(float(sh.g[63]));
+    const float it = inverse_pow2(s), gam = exp2_fast(sh.gh[lane]), bs = sh.bs[lane];
+    const float all = exp2_fast(sh.gh[63]);
     const float se = scale_for(most(3) * 0x1p14f);
     const float mz = wave_max(fabsf(bs * it));
     gt[kGateY * kC + lane] = -gam * ik;
@@ -372,14 +378,14 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
     gt[kGateOne * kC + lane] = lane == kOneG ? all : lane == kOneZ ? mz : lane == kOneK ? ik
                              : lane == kOneT ? most(3) : lane == kOneE ? se : it;
     if constexpr (BWD) {
-      const float hi = float(sh.g[lane]), mg = wave_max(gam);
+      const float mg = wave_max(gam);
       gt[kRevY * kC + lane] = bs * ik;
       gt[kRevP * kC + lane] = sh.ip[lane];
       gt[kRevZ * kC + lane] = -gam;
       gt[kRevBS * kC + lane] = bs;
       gt[kRevBeta * kC + lane] = sh.be[lane];
-      gt[kRevHi * kC + lane] = hi;
-      gt[kRevLo * kC + lane] = float(sh.g[lane] - double(hi));
+      gt[kRevHi * kC + lane] = sh.gh[lane];
+      gt[kRevLo * kC + lane] = sh.gl[lane];
       gt[kRevOne * kC + lane] = lane == kRevG ? all : lane == kRevK ? ik : lane == kRevQ ? iq
                               : lane == kRevT ? most(4) : lane == kRevIT ? it
                               : lane == kRevGam ? mg : 0.f;
