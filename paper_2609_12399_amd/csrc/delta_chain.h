@@ -83,6 +83,43 @@ struct ChainState {
   }
 };
 
+// The transition matrix A of a segment in memory, as operands of A^T S^T: two fp16 parts of
+// A^T(16 b + lr, k), of the lanes' slots k = 32 h + 4 lq + i and 32 h + 16 + 4 lq + i; and the
+// scale that the rows k of every h carry.
+template <int DK>
+struct SegmentMatrix {
+  uint4 x[DK / 16][DK / 32][2][64];
+  float scale[64];
+};
+
+// Stores the rows of A that the wave holds as its state (rows 32 h .. 32 h + 31 of A).
+template <int DK>
+__device__ inline void store_matrix(const ChainState<DK>& s, SegmentMatrix<DK>* to, int h,
+                                    int lane) {
+  static_assert(sizeof(SegmentMatrix<DK>) == delta_matrix_bytes(DK), "");
+  const int lr = lane & 15, lq = lane >> 4;
+  const float inv = inverse_pow2(s.sc);
+  float m = 0.f;
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int b = 0; b < ChainState<DK>::NB; ++b) m = max4abs(m, s.st[u][b]);
+  const float f = scale_for(wave_max(m * inv)), g = f * inv;
+  if (lane == 0) to->scale[h] = f;
+#pragma unroll
+  for (int b = 0; b < ChainState<DK>::NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // rows 32 h + 2 lr + u, u < 2: two neighbouring slots
+      unsigned p[2];
+      parts2<2>(s.st[0][b][i], s.st[1][b][i], g, p);
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        reinterpret_cast<unsigned*>(&to->x[b][h][q][16 * ((lr & 7) >> 1) + 4 * lq + i])
+            [(lr & 1) + 2 * (lr >> 3)] = p[q];
+    }
+}
+
 // y[u][a] += rows of A (16 a ..) times S^T, and with TWO the same of B into o: the operand
 // tiles have NP parts, the state two.
 template <int DK, int NP, bool TWO>

@@ -57,7 +57,7 @@ struct DeltaParams {
   int cps, nseg_l;     // chunks per segment; segments of a sequence of L tokens
   long seg_slots;
   float* segs;         // [slot][HV][DV][DK]  the state after each segment but a sequence's last
-  float* sega;         // [slot][HV][DK][DK]  transition matrices of the segments between
+  char* sega;          // [slot][HV]  transition matrices of the segments between (SegmentMatrix)
   // recurrent step
   float* pool;       // [num_slots][HV][DV][DK]
   const int* slot;   // [N] or null

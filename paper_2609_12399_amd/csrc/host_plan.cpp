@@ -257,7 +257,7 @@ namespace {
 // a transition matrix each.
 long segment_slots(const DeltaShape& s, long cps) { return s.slots / cps + s.N; }
 size_t segment_bytes(const DeltaShape& s) {
-  return sizeof(float) * size_t(s.HV) * s.dk * (s.dv + s.dk);
+  return size_t(s.HV) * (sizeof(float) * size_t(s.dk) * s.dv + delta_matrix_bytes(s.dk));
 }
 // Most segment slots that are used, whatever the device: segments of two chunks, and at most
 // some 1024 workgroups with outputs at once (more do not run faster).

@@ -102,6 +102,10 @@ constexpr int kDeltaGates = 8;                    // fp32 values per token and h
 // Bytes of one fp16 plane of a chunk's keys as it stands in LDS.
 constexpr size_t delta_image_bytes(int dk) { return size_t(kDeltaChunk) * (dk < 64 ? dk + 16 : dk) * 2; }
 
+// Bytes of a segment's transition matrix: two fp16 parts, and a scale for every 32 rows (256
+// bytes).
+constexpr size_t delta_matrix_bytes(int dk) { return size_t(dk) * dk * 4 + 256; }
+
 struct DeltaShape {
   int N, HK, HV, dk, dv;
   bool bf16;

@@ -73,7 +73,7 @@ hipError_t launch_delta_rule(const DeltaShape& s, DeltaParams p, bool backward, 
   p.seg_slots = sg.slots;
   if (sg.many) {
     take(p.segs, size_t(sg.slots) * s.HV * s.dv * s.dk * 4);
-    take(p.sega, size_t(sg.slots) * s.HV * s.dk * s.dk * 4);
+    take(p.sega, size_t(sg.slots) * s.HV * delta_matrix_bytes(s.dk));
   }
   if (!backward) {
     take(p.pf, cus * kDeltaFragBytes);

@@ -252,8 +252,10 @@ void delta_reverse_kernel(DeltaParams p) {
       }
     }
   }
-  if constexpr (SEG)
-    s.store((ident ? p.sega + su * (DK * DK) : p.segs + su * (DV * DK)) + rows);
+  if (SEG && ident)
+    store_matrix<DK>(s, reinterpret_cast<SegmentMatrix<DK>*>(p.sega) + su, NW * grp + w, lane);
+  else if (SEG)
+    s.store(p.segs + su * (DV * DK) + rows);
   else if (p.ds_out && sg.j + 1 == sg.nseg)
     s.store(p.ds_out + (long(sg.n) * p.HV + hv) * (DV * DK) + rows);
 }

@@ -199,84 +199,106 @@ void delta_forward_kernel(DeltaParams p) {
     }
     update_state<DK, NP, false>(s, g, K, zp, K, zp, tb);
   }
-  if constexpr (SEG)
-    s.store((ident ? p.sega + su * (DK * DK) : p.segs + su * (DV * DK)) + rows);
+  if (SEG && ident)
+    store_matrix<DK>(s, reinterpret_cast<SegmentMatrix<DK>*>(p.sega) + su, NW * grp + w, lane);
+  else if (SEG)
+    s.store(p.segs + su * (DV * DK) + rows);
   else if (p.s_out && sg.j + 1 == sg.nseg)
     s.store(p.s_out + (long(sg.n) * p.HV + hv) * (DV * DK) + rows);
 }
 
 // The true states after the segments of one (sequence, value head, 16 state rows): S_0 as
-// it is, then S_j = S_{j-1} A_j + B_j, in B_j's place.  Wave w holds the columns 16 w ..
-// 16 w + 15 as an accumulator tile of S^T; the tiles, cut into three bf16 parts, are exchanged
-// through LDS as operands (one barrier per segment), A_j's rows come from memory, requested two
-// segments ahead.  Bound: latency of the chain over the segments.
+// it is, then S_j = S_{j-1} A_j + B_j, in B_j's place.  Wave w holds the columns 32 w ..
+// 32 w + 31 as two accumulator tiles of S^T; as two fp16 parts under a scale per row they are
+// exchanged through LDS (one barrier per segment), A_j's operands come straight from
+// memory, requested ahead.  A head's workgroups are a multiple of 8 apart where the heads
+// are, so that they share an L2.  Bound: latency of the chain over the segments.
 template <int DK, int DV>
-__global__ __launch_bounds__(4 * DK) void delta_combine_kernel(DeltaParams p) {
-  constexpr int NH = DK / 32, NRB = DV / 16;
-  __shared__ uint4 xs[2][NH][3][64];
+__global__ __launch_bounds__(2 * DK) void delta_combine_kernel(DeltaParams p) {
+  constexpr int NH = DK / 32;
+  using A = SegmentMatrix<DK>;
+  __shared__ uint4 xs[2][NH][2][64];
+  __shared__ float xi[2][NH][16];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 15, lq = lane >> 4;
-  const int unit = blockIdx.x / NRB, rb = blockIdx.x % NRB;
+  const int units = p.N * p.HV, rb = blockIdx.x / units, unit = blockIdx.x - rb * units;
   const int n = unit / p.HV, hv = unit - n * p.HV;
   const Seq sq = seq_of(p, n);
   const long slot0 = first_segment(p, sq, n);
   const int last = segments_of(p, sq) - 2;  // the last segment that leaves a state
   if (last < 1) return;
-  const long at = long(16 * rb + lr) * DK + 16 * w + 4 * lq;
+  const long at = long(16 * rb + lr) * DK + 32 * w + 4 * lq;
   auto state = [&](int j) { return p.segs + ((slot0 + j) * p.HV + hv) * (DV * DK) + at; };
-  f32x4 st = *reinterpret_cast<const f32x4*>(state(0));
-  // A^T(16 w + lr, k): slots k = 32 h + 4 lq + i and 32 h + 16 + 4 lq + i; AHEAD segments' in
-  // flight (1024 threads leave no registers for two)
+  const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+  f32x4 st[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) st[t] = *reinterpret_cast<const f32x4*>(state(0) + 16 * t);
+  // segments ahead: two but for d_k = 256, whose eight waves' registers hold one
   constexpr int AHEAD = DK < 256 ? 2 : 1;
-  f32x4 a[AHEAD][NH][2], bn[AHEAD];
-  auto load = [&](int j, f32x4 (&to)[2], int h) __attribute__((always_inline)) {
-    const auto rs = buffer(p.sega + ((slot0 + min(j, last)) * p.HV + hv) * (DK * DK), DK * DK * 4);
-    const unsigned at0 = unsigned(4 * lq * DK + 16 * w + lr) * 4;
+  u32x4 a[AHEAD][NH][2][2];
+  f32x4 bn[AHEAD][2];
+  float as[AHEAD][NH];
+  auto load = [&](int j, int e, int h) __attribute__((always_inline)) {
+    const A* const m =
+        reinterpret_cast<const A*>(p.sega) + (slot0 + min(j, last)) * p.HV + hv;
+    as[e][h] = m->scale[h];
+    const auto rs = buffer(m, sizeof(A));
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        to[u][i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
-            rs, at0, unsigned(32 * h + 16 * u + i) * (DK * 4), 0));
+      for (int i = 0; i < 2; ++i)
+        a[e][h][t][i] = __builtin_amdgcn_raw_buffer_load_b128(
+            rs, 16 * lane, unsigned(((2 * w + t) * NH + h) * 2 + i) * 1024, 0);
   };
-  auto step = [&](int j, f32x4 (&aj)[NH][2], f32x4& bj) __attribute__((always_inline)) {
-    const int x = j & 1;
-    uint4 d[3];
-    cut3(st, st, d[0], d[1], d[2]);
+  auto load_next = [&](int j, int e) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
-      reinterpret_cast<uint2*>(&xs[x][w >> 1][i][lane])[w & 1] = make_uint2(d[i].x, d[i].y);
-    __syncthreads();
-    f32x4 hi[2] = {}, lo[4] = {};
+    for (int t = 0; t < 2; ++t)
+      bn[e][t] = *reinterpret_cast<const f32x4*>(state(min(j, last)) + 16 * t);
+  };
+  auto step = [&](int j, int e) __attribute__((always_inline)) {
+    const int x = j & 1;
+    {
+      uint4 d[2];
+      const float s = scale_for(max_over_rows(max4abs(max4abs(0.f, st[0]), st[1])));
+      parts8<2>(st[0], st[1], s, d);
+      xs[x][w][0][lane] = d[0];
+      xs[x][w][1][lane] = d[1];
+      if (lq == 0) xi[x][w][lr] = inverse_pow2(s);
+    }
+    lds_barrier();
+    f32x4 y[2] = {bn[e][0], bn[e][1]};
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
-      const uint4 dh = xs[x][h][0][lane], dm = xs[x][h][1][lane], dl = xs[x][h][2][lane];
-      uint4 t[3];
-      cut3(aj[h][0], aj[h][1], t[0], t[1], t[2]);
-      load(j + AHEAD, aj[h], h);  // (into the registers just read)
-      const int e = h & 1;
-      hi[e] = mfma_bf16(t[0], dh, hi[e]);
-      lo[e] = mfma_bf16(t[2], dh, lo[e]);
-      lo[2 + e] = mfma_bf16(t[1], dm, lo[2 + e]);
-      lo[e] = mfma_bf16(t[0], dl, lo[e]);
-      lo[2 + e] = mfma_bf16(t[1], dh, lo[2 + e]);
-      lo[e] = mfma_bf16(t[0], dm, lo[e]);
+      const uint4 d[2] = {xs[x][h][0][lane], xs[x][h][1][lane]};
+      const float inv = xi[x][h][lr] * inverse_pow2(as[e][h]);
+      f32x4 acc[2] = {z, z};
+      for_products<2, 2>([&](int i, int q) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          acc[t] = mfma_f16(__builtin_bit_cast(uint4, a[e][h][t][i]), d[q], acc[t]);
+      });
+      load(j + AHEAD, e, h);  // (into the registers just read)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) y[t] += inv * acc[t];
     }
-    st = bj + ((hi[0] + hi[1]) + ((lo[0] + lo[1]) + (lo[2] + lo[3])));
-    bj = *reinterpret_cast<const f32x4*>(state(min(j + AHEAD, last)));
-    *reinterpret_cast<f32x4*>(state(j)) = st;
+    load_next(j + AHEAD, e);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      st[t] = y[t];
+      *reinterpret_cast<f32x4*>(state(j) + 16 * t) = y[t];
+    }
   };
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) {
-    bn[i] = *reinterpret_cast<const f32x4*>(state(min(1 + i, last)));
 #pragma unroll
-    for (int h = 0; h < NH; ++h) load(1 + i, a[i][h], h);
+    for (int h = 0; h < NH; ++h) load(1 + i, i, h);
+    load_next(1 + i, i);
   }
   for (int j = 1; j <= last; j += AHEAD) {
-    step(j, a[0], bn[0]);
+    step(j, 0);
     if constexpr (AHEAD == 2) {
       if (j + 1 > last) break;
-      step(j + 1, a[1], bn[1]);
+      step(j + 1, 1);
     }
   }
 }
@@ -290,7 +312,7 @@ hipError_t run(const DeltaParams& p, bool save, hipStream_t st) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     delta_combine_kernel<DK, DV>
-        <<<unsigned(p.N) * unsigned(p.HV) * (DV / 16), 4 * DK, 0, st>>>(p);
+        <<<unsigned(p.N) * unsigned(p.HV) * (DV / 16), 2 * DK, 0, st>>>(p);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -325,7 +347,7 @@ hipError_t launch_delta_combine(const DeltaShape& s, const DeltaParams& p, hipSt
   const unsigned wgs = unsigned(p.N) * unsigned(p.HV) * unsigned(s.dv / 16);
 #define ONELA_DELTA_COMBINE(DK, DV)                         \
   if (s.dk == DK && s.dv == DV) {                           \
-    delta_combine_kernel<DK, DV><<<wgs, 4 * DK, 0, st>>>(p); \
+    delta_combine_kernel<DK, DV><<<wgs, 2 * DK, 0, st>>>(p); \
     return hipGetLastError();                               \
   }
   ONELA_DELTA_COMBINE(32, 32)
