@@ -278,13 +278,13 @@ DeltaSegments delta_segments(const DeltaShape& s, bool ragged) {
   // Times in ns: of a chunk with outputs and without, of a chained segment, and of the two more
   // launches.  A chunk takes up to 1.4 times as long where every compute unit has a
   // workgroup (their operands share the memory).  Measured, us per forward / backward call:
-  // 1 x 4096 tokens x 16 heads of 128 315 / 917 in one segment, 116 / 373 in 8, 114 / 364 in
-  // 16 (taken), 130 / 402 in 22; 8 x 1024 x 16 heads 122 / 512 in one (taken), 138 / 541 in
-  // two; 1 x 4096 x 8 heads of 256 514 / 1550 in one, 213 / 693 in 8 (taken), 262 / 790 in
-  // 16; 1 x 2048 x 4 heads of 64 124 / 274 in one, 44 / 103 in 16 (taken).
+  // 1 x 4096 tokens x 16 heads of 128 316 / 914 in one segment, 110 / 355 in 8, 106 / 341 in
+  // 16 (taken), 120 / 377 in 22; 8 x 1024 x 16 heads 122 / 494 in one (taken), 138 / 528 in
+  // two; 1 x 4096 x 8 heads of 256 514 / 1540 in one, 183 / 632 in 8 (taken), 200 / 663 in
+  // 16; 1 x 2048 x 4 heads of 64 123 / 273 in one, 41 / 97 in 16 (taken).
   const long full = s.dk >= 256 ? 7300 : s.dk == 128 ? 4700 : 3300;
   const long bare = s.dk >= 256 ? 4500 : s.dk == 128 ? 2800 : 2000;
-  const long chain = s.dk >= 256 ? 4600 : s.dk == 128 ? 2300 : 800, more = 12000;
+  const long chain = s.dk >= 256 ? 3600 : s.dk == 128 ? 1700 : 900, more = 12000;
   auto spread = [&](long wgs, long per) {
     return (wgs + cus - 1) / cus * per * (10 * cus + 4 * std::min(wgs, cus)) / (10 * cus);
   };
