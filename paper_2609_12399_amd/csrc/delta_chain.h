@@ -69,6 +69,17 @@ struct ChainState {
       for (int b = 0; b < NB; ++b)
         *reinterpret_cast<f32x4*>(to + u * DK + 16 * b) = inv * st[u][b];
   }
+  // The same for the gradients (DeltaParams::sws), whole lines at a time: `to` is the state's
+  // column block 0, place 32 times the wave's rows.
+  template <int DV>
+  __device__ void store_tiles(float* to, int lane) const {
+    const float inv = inverse_pow2(sc);
+    f32x4* const at = reinterpret_cast<f32x4*>(to) + 4 * (lane & 15) + (lane >> 4);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) at[4 * DV * b + 64 * u] = inv * st[u][b];
+  }
   // Makes room for an update S <- g S + (64 tokens' keys times values of at most `most`;
   // keys are scaled below 2^3): the bound after it.
   __device__ void make_room(float g, float most) {

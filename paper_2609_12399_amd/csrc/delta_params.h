@@ -45,10 +45,12 @@ struct DeltaParams {
   int gate_rows; // kDeltaGates, backward twice that
   uint4* tr;     // as tp and pf, of T and P transposed with their tokens in reverse order
   uint4* pr;     // (backward)
-  float* sws;    // [DV][DK]  state before the chunk (backward)
-  float* ews;    // [DV][64]  e (backward)
-  float* dsws;   // [DV][DK]  adjoint of the state after the chunk (backward)
-  float* hws;    // [DV][64]  dV (backward)
+  // Backward: what the chains leave, place 32 g + 16 u + m of the values' columns being column
+  // 32 g + 2 m + u (a wave's store then covers whole lines)
+  float* sws;    // [DK/16][DV places][16]  state before the chunk
+  float* ews;    // [DV/32][4][32 places][16 tokens]  e
+  float* dsws;   // as sws: adjoint of the state after the chunk
+  float* hws;    // as ews: dV
   uint4 *kimg, *qimg;  // per (slot, query/key head): the LDS image Swz<DK>[NP] of the fp16
                        // parts of keys and queries
   uint4* tp;     // T fragments, two fp16 parts [6][2][64]

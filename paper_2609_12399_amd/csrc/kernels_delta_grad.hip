@@ -87,9 +87,9 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
     for (int c = 0; c < CT; ++c) aq[a][c] = ak[a][c] = z;
   const int blocks = p.DV / kNB;
 
-  // the next 32 columns of the values: e and dV [columns][tokens], dO, and this lane's
-  // operands of the states, S(n, k = 16 (CT w + c) + lr) at n = n0 + 4 lq + i and
-  // n0 + 16 + 4 lq + i
+  // the next 32 columns of the values: e and dV, dO, and this lane's operands of the
+  // states, S(n, k = 16 (CT w + c) + lr) at the places n0 + 4 lq + i and n0 + 16 + 4 lq + i
+  // (place 16 u + m of 32 columns is column 2 m + u, the order in which the chains leave them)
   constexpr int NE = kNB * kC / 4 / TH, NO = (kC * kNB / 8 + TH - 1) / TH;
   f32x4 re[NE], rd[NE], s0[CT][2], d0[CT][2];
   u32x4 ro[NO][NP];
@@ -115,14 +115,14 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
     }
     const auto sr = buffer(p.sws + cu * (p.DV * DK), p.DV * (DK * 4)),
                dr = buffer(p.dsws + cu * (p.DV * DK), p.DV * (DK * 4));
-    const unsigned at = unsigned(4 * lq * DK + 16 * CT * w + lr) * 4;
+    const unsigned at = unsigned(16 * CT * w * p.DV + 64 * lq + lr) * 4;
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const unsigned so = unsigned(n0 + 16 * u + i) * (DK * 4) + 64 * c;
+          const unsigned so = unsigned(c * p.DV + n0 + 16 * u + i) * 64;
           s0[c][u][i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sr, at, so, 0));
           d0[c][u][i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(dr, at, so, 0));
         }
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
       // (this buffer's last readers passed the barrier of the block before)
 #pragma unroll
       for (int q = 0; q < NE; ++q) {
-        const int e = tid + q * TH, o = Columns32::off(e / 16, e % 16);
+        const int e = tid + q * TH, o = Columns32::off(e / 4 % 32, e / 128 * 4 + e % 4);
         unsigned u[2], v[2];
         auto put = [&](const f32x4& y, float s, Columns32* to) {
           parts2<2>(y.x, y.y, s, u);
@@ -189,14 +189,13 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
           y0 = __builtin_bit_cast(f32x4, ro[q][0]);
           y1 = __builtin_bit_cast(f32x4, ro[q][1]);
         }
-        uint4 part[NP];
-        parts8<NP>(y0, y1, sO, part);
+        uint4 part[NP];  // even columns and odd ones
+        parts8<NP>(f32x4{y0.x, y0.z, y1.x, y1.z}, f32x4{y0.y, y0.w, y1.y, y1.w}, sO, part);
 #pragma unroll
-        for (int i = 0; i < NP; ++i)
-        {
-          uint2* const to = reinterpret_cast<uint2*>(&x.dO[i][e / (kNB / 8)][8 * (e % (kNB / 8))]);
-          to[0] = make_uint2(part[i].x, part[i].y);
-          to[1] = make_uint2(part[i].z, part[i].w);
+        for (int i = 0; i < NP; ++i) {
+          uint16_t* const to = &x.dO[i][e / (kNB / 8)][4 * (e % (kNB / 8))];
+          *reinterpret_cast<uint2*>(to) = make_uint2(part[i].x, part[i].y);
+          *reinterpret_cast<uint2*>(to + 16) = make_uint2(part[i].z, part[i].w);
         }
       }
       uint4 sp[CT][2], dp[CT][2];

@@ -87,7 +87,8 @@ void delta_reverse_kernel(DeltaParams p) {
     dma<kImage, NW>(p.qimg + image_at(c), sQ, w, lane);
     const long cu = (sq.slot + c) * p.HV + hv;
     const float inv = inverse_pow2(s.sc), before = s.bound * inv;
-    if constexpr (!SEG) s.store(p.dsws + cu * (DV * DK) + rows);
+    if constexpr (!SEG)
+      s.template store_tiles<DV>(p.dsws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
     // Y = K S^T
     f32x4 y[2][4];
 #pragma unroll
@@ -195,13 +196,14 @@ void delta_reverse_kernel(DeltaParams p) {
         note_max(top + kMaxD, before, lane);
         note_max(top + kMaxV, mv, lane);
         note_max(top + kMaxO, mo, lane);
-        float* const d = p.hws + (cu * DV + row0) * kC + 60 - 4 * lq;
+        f32x4* const d = reinterpret_cast<f32x4*>(p.hws + cu * (DV * kC)) +
+                         512 * (NW * grp + w) + 4 * lr + (3 - lq);
         const auto rs = rows_of(p.dv, c, min(kC, sq.len - c * kC));
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const f32x4 x0 = f * e[0][a], x1 = f * e[1][a];
-          *reinterpret_cast<f32x4*>(d - 16 * a) = back(x0);
-          *reinterpret_cast<f32x4*>(d + kC - 16 * a) = back(x1);
+          d[128 * (3 - a)] = back(x0);
+          d[128 * (3 - a) + 64] = back(x1);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             store_columns<NP, true>(rs, os, lq, row0 * kIo, 4 * a + i, x0[i], x1[i]);

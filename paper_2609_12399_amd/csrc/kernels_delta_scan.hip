@@ -94,7 +94,8 @@ void delta_forward_kernel(DeltaParams p) {
     __syncthreads();  // this chunk's operands are in LDS
     const long cu = (sq.slot + c) * p.HV + hv;
     const float inv = inverse_pow2(s.sc), before = s.bound * inv;
-    if constexpr (KIND == kSave) s.store(p.sws + cu * (DV * DK) + rows);
+    if constexpr (KIND == kSave)
+      s.template store_tiles<DV>(p.sws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
     // Y = K S^T and Q S^T
     f32x4 y[2][4], o[2][4];
 #pragma unroll
@@ -185,12 +186,12 @@ void delta_forward_kernel(DeltaParams p) {
       float* const one = p.gates + (cu * p.gate_rows + kRevOne) * kC;
       note_max(one + kMaxS, before, lane);
       note_max(one + kMaxE, sG[kGateOne][kOneT] * 0x1p14f * f, lane);
-      float* const d = p.ews + (cu * DV + row0) * kC + 4 * lq;
+      f32x4* const d =
+          reinterpret_cast<f32x4*>(p.ews + cu * (DV * kC)) + 512 * (NW * grp + w) + 4 * lr + lq;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int a = 0; a < 4; ++a)
-          *reinterpret_cast<f32x4*>(d + u * kC + 16 * a) = f * e[u][a];
+        for (int a = 0; a < 4; ++a) d[128 * a + 64 * u] = f * e[u][a];
     }
     __syncthreads();  // all have read T, P and the gates
     if (c + 1 < nch) {
