@@ -73,7 +73,7 @@ struct Segment {
   int cb, ce;      // chunks
 };
 __device__ inline int segments_of(const DeltaParams& p, const Seq& sq) {
-  return max(((sq.len + kC - 1) / kC + p.cps - 1) / p.cps, 1);
+  return max((delta_chunks(sq.len) + p.cps - 1) / p.cps, 1);
 }
 __device__ inline long first_segment(const DeltaParams& p, const Seq& sq, int n) {
   return p.offsets ? sq.slot / p.cps + n : long(n) * p.nseg_l;
@@ -87,7 +87,7 @@ __device__ inline Segment segment_of(const DeltaParams& p, long slot) {
   const long j = slot - first_segment(p, s.sq, s.n);
   s.j = j >= 0 && j < s.nseg ? int(j) : -1;
   s.cb = s.j * p.cps;
-  s.ce = int(min(long(s.cb) + p.cps, long(s.sq.len + kC - 1) / kC));
+  s.ce = int(min(long(s.cb) + p.cps, long(delta_chunks(s.sq.len))));
   return s;
 }
 

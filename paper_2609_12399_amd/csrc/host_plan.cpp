@@ -243,7 +243,7 @@ onela_status_t delta_shape_of(const onela_delta_config_t* c, bool ragged, DeltaS
     s.slots = s.total / kDeltaChunk + s.N;
   } else {
     s.L = int(s.total / s.N);
-    s.slots = long(s.N) * ((s.L + kDeltaChunk - 1) / kDeltaChunk);
+    s.slots = long(s.N) * delta_chunks(s.L);
   }
   // one workgroup per slot, value head and 16 state rows at most
   const double groups = double(std::max(s.slots, long(s.N))) * s.HV * (s.dv / 16);
@@ -270,7 +270,7 @@ long most_segment_slots(const DeltaShape& s) {
 DeltaSegments delta_segments(const DeltaShape& s, bool ragged) {
   DeltaSegments none{1 << 30, 1, long(s.N), false};
   const long nch = ragged ? s.total / kDeltaChunk / s.N + 1
-                          : (s.L + kDeltaChunk - 1) / kDeltaChunk;
+                          : delta_chunks(s.L);
   if (nch < 4 || s.cus <= 0) return none;
   const long waves = std::min(s.dv / 32, 4);
   const long gb = s.dv / (32 * waves), ga = s.dk / (32 * waves);

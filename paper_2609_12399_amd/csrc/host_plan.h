@@ -96,6 +96,10 @@ constexpr size_t kSelectScratchBytes = size_t(32) << 20;
 
 // ---- delta rule over sequences ---------------------------------------------------
 constexpr int kDeltaChunk = 64;                   // tokens per chunk
+// Chunks of a sequence (for any int: not by adding first).
+constexpr int delta_chunks(int tokens) {
+  return tokens / kDeltaChunk + (tokens % kDeltaChunk ? 1 : 0);
+}
 constexpr size_t kDeltaFragBytes = 6 * 2 * 1024;  // a triangular matrix of a chunk in two parts
 constexpr int kDeltaGates = 8;                    // fp32 values per token and head (backward: 16)
 

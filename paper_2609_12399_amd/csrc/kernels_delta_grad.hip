@@ -58,7 +58,13 @@ __device__ inline Lane unseen(int lane) {
 // of dQ and dK; the tiles of the token by token products are dealt out to the waves.
 // The values' columns come 32 at a time, e, dV and dO through LDS (the next ones
 // requested a block ahead), the states' rows straight into operands.
-//   Bound: HBM (the states and their adjoints, e and dV, each read once).
+//   Bound: latency of its phases, one workgroup per compute unit (256 registers, 86 KB of LDS
+// at d_k = 128).  16 x 1024 tokens x 32 heads of 128 take 0.80 ms (2.5 TB/s; matrix
+// cores 11% busy, vector units 31%); per chunk and head the four column blocks are 13 us, near
+// the rate at which their states can arrive, and the products of tokens with tokens, the
+// rows' sums and the last products with Q and K another 13, no part above 2.  Writing L and
+// M + M^T both ways or reading them transposed, and the next head's gates ahead of its
+// first block, measured the same; non-temporal loads of the states 2% slower.
 template <int DK, int NP, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
   constexpr int TH = 64 * NW, CT = DK / (16 * NW), MT = (10 + NW - 1) / NW;

@@ -25,8 +25,12 @@ enum { kOutputs, kSegment, kSave };
 // and, by the same code on the rows of the identity and V = 0, A.
 // delta_combine_kernel chains them, and then every segment starts from its true state.
 //
-// Bound: vector and matrix instructions (about 4 and 16 cycles each) take turns; at 512
-// workgroups of 16 chunks the matrix cores are busy 31% of the time, the vector units 34%.
+// Bound: vector and matrix instructions (about 4 and 16 cycles each) take turns.  16 x 1024
+// tokens x 32 heads of 128 (512 workgroups of 16 chunks) with outputs 170 us, 836 TFLOP/s of
+// fp16 products: matrix cores 31% busy, vector units 33%, waves waiting 24%; kSave 244 us
+// (3.3 TB/s written), kSegment 36 us for 16 segments of 4096 tokens x 16 heads.  Barriers that
+// leave the stores in flight, operand reads a step ahead and one wave per SIMD with 512
+// registers were all slower.
 template <int DK, int DV, int NP, int KIND>
 __global__ __launch_bounds__(64 * kChainWaves<DV>, DK >= 256 || NP == 2 ? 1 : 2)
 void delta_forward_kernel(DeltaParams p) {
@@ -213,7 +217,9 @@ void delta_forward_kernel(DeltaParams p) {
 // 32 w + 31 as two accumulator tiles of S^T; as two fp16 parts under a scale per row they are
 // exchanged through LDS (one barrier per segment), A_j's operands come straight from
 // memory, requested ahead.  A head's workgroups are a multiple of 8 apart where the heads
-// are, so that they share an L2.  Bound: latency of the chain over the segments.
+// are, so that they share an L2.  Bound: latency of the chain over the segments (1.5 us each
+// for 16 heads of 128, 2.6 for 8 of 256: A_j's operands, 64 and 256 KB per workgroup).  With A in
+// fp32 rows, cut into bf16 parts by every workgroup, 2.6 and 5.5; through LDS tiles 3.2 and 2.7.
 template <int DK, int DV>
 __global__ __launch_bounds__(2 * DK) void delta_combine_kernel(DeltaParams p) {
   constexpr int NH = DK / 32;

@@ -419,7 +419,7 @@ onela_status_t delta_inputs(const onela_delta_config_t* cfg, const int32_t* offs
   p->HV = s->HV;
   p->DV = s->dv;
   p->L = s->L;
-  p->nch_l = (s->L + onela::kDeltaChunk - 1) / onela::kDeltaChunk;
+  p->nch_l = onela::delta_chunks(s->L);
   p->slots = s->slots;
   return ONELA_OK;
 }
