@@ -12,7 +12,7 @@
 // D idle); the partner columns of a half-turn pair are another lane's 8 and
 // come by a lane exchange.  Queries and keys are one list of rows, so that one launch
 // takes both.  Bound: HBM; 16384 tokens x 32 heads of 128 in bf16 take 40 us, 6.7 TB/s (part of
-// it from the memory-side cache), ten rows 4.2 us of latency.
+// it from the memory-side cache), 80 rows 4.2 us of latency.
 #include "device_common.h"
 #include "internal.h"
 
