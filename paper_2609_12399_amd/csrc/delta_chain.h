@@ -24,10 +24,8 @@ constexpr int kFragBytes = 6 * 2 * 1024;
 template <int DK>
 struct ChainState {
   static constexpr int NB = DK / 16;
-  // The 32-deep step h of a contraction over the columns covers the tiles t0(h) and t0(h) + PS:
-  // PS = 4 puts a row operand's two pieces 128 bytes apart (one two-address read).
-  static constexpr int PS = NB / 2 < 4 ? NB / 2 : 4;
-  static constexpr int t0(int h) { return h / PS * (2 * PS) + h % PS; }
+  static constexpr int PS = Steps<DK>::PS;
+  static constexpr int t0(int h) { return Steps<DK>::t0(h); }
   static constexpr int KR = 32 * Swz<DK>::LD;  // bytes of 16 rows of an operand tile
 
   f32x4 st[2][NB];

@@ -126,6 +126,14 @@ __device__ inline void dma(const void* from, void* to, int w, int lane) {
 __device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ inline void dma_wait() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
 
+// The 32-deep step h of a contraction over DK columns covers the tiles t0(h) and t0(h) + PS
+// of 16: PS = 4 puts a row operand's two pieces 128 bytes apart (one two-address read).
+template <int DK>
+struct Steps {
+  static constexpr int PS = DK / 32 < 4 ? DK / 32 : 4;
+  static constexpr int t0(int h) { return h / PS * (2 * PS) + h % PS; }
+};
+
 // Row operand of a tile of 16 rows (lane row lr, first piece lq): the two pieces
 // at column blocks b0 and b1 of 16, i.e. slots 0..3 are the columns 16 b0 + 4 lq
 // + i and slots 4..7 the columns 16 b1 + 4 lq + i.

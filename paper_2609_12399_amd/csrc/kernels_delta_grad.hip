@@ -333,9 +333,9 @@ __global__ __launch_bounds__(64 * NW, 1) void delta_grad_kernel(DeltaParams p) {
         uint4 qf[NP], ka[NP], kf[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-          qf[i] = row_frag(sh.Q[i], kb, 2 * h, 2 * h + 1, KR * a);
-          ka[i] = row_frag(sh.K[i], kb, 2 * h, 2 * h + 1, KR * a);
-          kf[i] = row_frag(sh.K[i], kb, 2 * h, 2 * h + 1, KR * b);
+          qf[i] = row_frag(sh.Q[i], kb, Steps<DK>::t0(h), Steps<DK>::t0(h) + Steps<DK>::PS, KR * a);
+          ka[i] = row_frag(sh.K[i], kb, Steps<DK>::t0(h), Steps<DK>::t0(h) + Steps<DK>::PS, KR * a);
+          kf[i] = row_frag(sh.K[i], kb, Steps<DK>::t0(h), Steps<DK>::t0(h) + Steps<DK>::PS, KR * b);
         }
         for_products<NP, NP>([&](int i, int j) {
           qk = mfma_f16(qf[i], kf[j], qk);

@@ -166,18 +166,18 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
   // rows x of a against rows y of b, 16 each: lane (lr, lq) holds (16 a + 4 lq + i, 16 b + lr)
   // (base: the lane's first piece of row lr, or of row 15 - lr for rows in reverse order)
   auto dots = [&](const Swz<DK>* x, int a, const Swz<DK>* y, int b, int base) {
-    f32x4 acc[2] = {z, z};
+    f32x4 acc = z;
 #pragma unroll
     for (int h = 0; h < DK / 32; ++h) {
       uint4 u[NP], v[NP];
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        u[i] = row_frag(x[i], base, 2 * h, 2 * h + 1, KR * a);
-        v[i] = row_frag(y[i], base, 2 * h, 2 * h + 1, KR * b);
+        u[i] = row_frag(x[i], base, Steps<DK>::t0(h), Steps<DK>::t0(h) + Steps<DK>::PS, KR * a);
+        v[i] = row_frag(y[i], base, Steps<DK>::t0(h), Steps<DK>::t0(h) + Steps<DK>::PS, KR * b);
       }
-      for_products<NP, NP>([&](int i, int j) { acc[h & 1] = mfma_f16(u[i], v[j], acc[h & 1]); });
+      for_products<NP, NP>([&](int i, int j) { acc = mfma_f16(u[i], v[j], acc); });
     }
-    return acc[0] + acc[1];
+    return acc;
   };
   {
     // P(t, j) = scale Gamma(t, j) (q_t . k_j) beta_j, j <= t, of 16 tokens t per wave (the
