@@ -97,10 +97,11 @@ struct PrepLds {
 // substitution, one per wave with a column per lane, then each wave the blocks below
 // the diagonal block of its block column, T_ij = -T_ii sum_k M_ik T_kj, in fp32 matrix
 // instructions with T_kj in the accumulator layout as the next operand.
-//   Bound: latency of that chain and the vector instructions around it (65% of the time
-// busy at four workgroups per compute unit, to which the LDS, 36 KB up to d_k = 128, and
-// the registers are held).  8192 chunks and heads of 128 take 113 us, 4.4 TB/s read and
-// written; with decays from 64-bit differences behind branches 7% more.
+//   Bound: HBM for many chunks, mostly what it leaves for the chain: 8192 chunks and value heads
+// of 128 (two to a key head) take 108 us, 4.6 TB/s; for few the latency of the inverse.  Vector
+// units 62% busy at four workgroups per compute unit, to which the LDS (36 KB up to d_k
+// = 128) and the registers are held.  With decays from 64-bit differences behind branches 7%
+// more, with operands whose pieces no one read fetches 3%.
 template <int DK, int NP, bool BWD>
 __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_kernel(DeltaParams p) {
   __shared__ __align__(16) PrepLds<DK, NP> sh;
