@@ -27,11 +27,10 @@ enum { kOutputs, kSegment, kSave };
 //
 // Bound: vector and matrix instructions (about 4 and 16 cycles each) take turns.  16 x 1024
 // tokens x 32 heads of 128 (512 workgroups of 16 chunks) with outputs 170 us, 836 TFLOP/s of
-// fp16 products: matrix cores 27 to 31% busy, vector units 28 to 33%, waves
-// waiting 24%; kSave 244 us
-// (3.3 TB/s written), kSegment 36 us for 16 segments of 4096 tokens x 16 heads.  Barriers that
-// leave the stores in flight, operand reads a step ahead and one wave per SIMD with 512
-// registers were all slower.
+// fp16 products: matrix cores 27 to 31% busy, vector units 28 to 33%, waves waiting 24%;
+// kSave 244 us (3.3 TB/s written), kSegment 36 us for 16 segments of 4096 tokens x 16 heads.
+// Barriers that leave the stores in flight, operand reads a step ahead and one wave per SIMD
+// with 512 registers were all slower.
 template <int DK, int DV, int NP, int KIND>
 __global__ __launch_bounds__(64 * kChainWaves<DV>, DK >= 256 || NP == 2 ? 1 : 2)
 void delta_forward_kernel(DeltaParams p) {
