@@ -92,6 +92,34 @@ struct ChainState {
   }
 };
 
+// Where a chain's first segment of several keeps the state that it starts from (kernels_delta_scan.hip):
+// the last segment's place, su being the first's (segment slot and value head).
+template <int DK, int DV>
+__device__ inline float* kept_start(const DeltaParams& p, const Segment& sg, long su) {
+  return p.segs + (su + long(sg.nseg - 1) * p.HV) * (DV * DK);
+}
+// The state of a value head that a segment starts from (null: zeros): of a sequence's first the
+// caller's (given: [N][HV][DV][DK] or null), of the others none while the segments' own states are
+// formed (SEG), and then what the segment before leaves.
+template <int DK, int DV, bool SEG>
+__device__ inline const float* start_of(const DeltaParams& p, const Segment& sg, long su, int hv,
+                                        const float* given) {
+  if (sg.j > 0) return SEG ? nullptr : p.segs + (su - p.HV) * (DV * DK);
+  if (!given) return nullptr;
+  if (!SEG && sg.nseg > 1) return kept_start<DK, DV>(p, sg, su);
+  return given + (long(sg.n) * p.HV + hv) * (DV * DK);
+}
+// The lane's two rows of a state, as ChainState reads them.
+template <int DK>
+__device__ inline void copy_rows(const float* from, float* to) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u)
+#pragma unroll
+    for (int b = 0; b < DK / 16; ++b)
+      *reinterpret_cast<f32x4*>(to + u * DK + 16 * b) =
+          *reinterpret_cast<const f32x4*>(from + u * DK + 16 * b);
+}
+
 // The transition matrix A of a segment in memory, as operands of A^T S^T: two fp16 parts of
 // A^T(16 b + lr, k), of the lanes' slots k = 32 h + 4 lq + i and 32 h + 16 + 4 lq + i; and the
 // scale that the rows k of every h carry.

@@ -58,7 +58,8 @@ struct DeltaParams {
   // segments of the chain
   int cps, nseg_l;     // chunks per segment; segments of a sequence of L tokens
   long seg_slots;
-  float* segs;         // [slot][HV][DV][DK]  the state after each segment but a sequence's last
+  float* segs;         // [slot][HV][DV][DK]  the state after each segment but a sequence's last; in
+                       // the last one's place the state that the sequence starts from
   char* sega;          // [slot][HV]  transition matrices of the segments between (SegmentMatrix)
   // recurrent step
   float* pool;       // [num_slots][HV][DV][DK]

@@ -11,7 +11,7 @@ namespace {
 //   Y = K S^T, X = P^T dO + beta sigma Y, dV = T^T X,
 //   S^T <- g S^T - K^T (gamma dV) + Q^T (scale gamma dO);
 // it leaves dV (as a tensor and in fp32 for the gradients) and the adjoint before each
-// update.  SEG: segments, counted from the sequence's end, as there.
+// update.  SEG: segments, counted from the sequence's end, as there (p.ds_out may be p.ds_in).
 //   Bound: as there, and the stores of the adjoints.  16 x 1024 tokens x 32 heads of 128 take
 // 306 us (3.1 TB/s written; 318 with a state's rows stored 64 bytes at a time in place of
 // whole lines, 355 with those as non-temporal stores).
@@ -46,9 +46,9 @@ void delta_reverse_kernel(DeltaParams p) {
   ChainState<DK> s;
   const long rows = long(row0) * DK + 4 * lq;
   {
-    const float* from = sg.j == 0 ? p.ds_in : SEG ? nullptr : p.segs + (su - p.HV) * (DV * DK);
-    if (sg.j == 0 && from) from += (long(sg.n) * p.HV + hv) * (DV * DK);
+    const float* from = start_of<DK, DV, SEG>(p, sg, su, hv, p.ds_in);
     s.init(from ? from + rows : nullptr, ident, row0, lq);
+    if (SEG && from) copy_rows<DK>(from + rows, kept_start<DK, DV>(p, sg, su) + rows);
   }
   auto image_at = [&](int c) { return ((sq.slot + c) * p.HK + hk) * (kImage / 16); };
   auto load_tp = [&](int c) __attribute__((always_inline)) {

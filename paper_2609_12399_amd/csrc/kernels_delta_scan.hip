@@ -24,6 +24,11 @@ enum { kOutputs, kSegment, kSave };
 // state that it leaves: of the first the true one, of the others B (from S_in = 0)
 // and, by the same code on the rows of the identity and V = 0, A.
 // delta_combine_kernel chains them, and then every segment starts from its true state.
+// The last state may be stored where the state to start from is (p.s_out == p.s_in), and in
+// that last launch nothing orders the workgroup of a sequence's first segment, which would
+// read it, before that of its last, which stores it.  So kSegment's first segment keeps
+// the rows that it starts from in the last segment's place of p.segs, which holds nothing
+// else, and the last launch reads them there.
 //
 // Bound: vector and matrix instructions (about 4 and 16 cycles each) take turns.  16 x 1024
 // tokens x 32 heads of 128 (512 workgroups of 16 chunks) with outputs 170 us, 836 TFLOP/s of
@@ -62,9 +67,9 @@ void delta_forward_kernel(DeltaParams p) {
   ChainState<DK> s;
   const long rows = long(row0) * DK + 4 * lq;
   {
-    const float* from = sg.j == 0 ? p.s_in : SEG ? nullptr : p.segs + (su - p.HV) * (DV * DK);
-    if (sg.j == 0 && from) from += (long(sg.n) * p.HV + hv) * (DV * DK);
+    const float* from = start_of<DK, DV, SEG>(p, sg, su, hv, p.s_in);
     s.init(from ? from + rows : nullptr, ident, row0, lq);
+    if (SEG && from) copy_rows<DK>(from + rows, kept_start<DK, DV>(p, sg, su) + rows);
   }
   auto load_kq = [&](int c) __attribute__((always_inline)) {
     const long at = ((sq.slot + c) * p.HK + hk) * (kImage / 16);

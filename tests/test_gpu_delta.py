@@ -418,3 +418,25 @@ def test_keys_and_queries_of_any_size():
         x[0].mul_(300.0)
     run_both([130], 1, 2, 64, 64, "f32", tweak=tweak)
     run_both([130], 1, 2, 64, 64, "bf16", tweak=tweak)
+
+
+@pytest.mark.parametrize("lengths,HK,HV,d,io", [
+    ([64 * 32], 4, 4, 64, "bf16"), ([64 * 20 + 3], 1, 2, 64, "f32"),
+    ([64 * 24 - 7, 0, 40, 64 * 11], 1, 2, 128, "bf16"), ([64 * 16], 1, 1, 256, "bf16")])
+def test_states_in_place_in_segments(lengths, HK, HV, d, io):
+    """final_state may be initial_state and d_initial_state d_final_state where the chain is cut
+    into segments: bit for bit the results of the calls with tensors of their own."""
+    x, g = draw(lengths, HK, HV, d, d, io, seed=11)
+    shape = (len(lengths), HV, d, d)
+    s0, ds = (torch.randn(shape, generator=g).to(DEV) for _ in range(2))
+    do, off = torch.randn(x[2].shape, generator=g).to(x[2]), offsets(lengths)
+    want = op_of(lengths, HK, HV, d, d, io, 1.0).forward(*x, off, s0)
+    op = op_of(lengths, HK, HV, d, d, io, 1.0)
+    op.final_state = s0.clone()
+    for a, b in zip(op.forward(*x, off, op.final_state), want):
+        assert torch.equal(a, b)
+    want = op_of(lengths, HK, HV, d, d, io, 1.0, True).backward(*x, do, off, s0, ds)
+    op = op_of(lengths, HK, HV, d, d, io, 1.0, True)
+    op.d_initial_state = ds.clone()
+    for a, b in zip(op.backward(*x, do, off, s0, op.d_initial_state), want):
+        assert torch.equal(a, b)
