@@ -17,10 +17,11 @@ constexpr int kFragBytes = 6 * 2 * 1024;
 // row0 = 32 w + 2 lr), in registers: st[u][b][i] = sc S(row0 + u, 16 b + 4 lq + i).
 //
 // Scales (powers of two).  sc keeps the lane's two rows inside what two fp16 parts hold, by a
-// bound on their largest value; the bound grows with every update by what 64 tokens
-// can add at most, and where it leaves [2^12, 2^15] the rows are scaled anew.  The true
-// values, and those that the updates add, are some 2^7 below their bounds; parts lose bits only
-// below 2^-3.
+// bound on their largest value; the bound grows with every update by what 64 tokens of the
+// largest size among them can add at most (the values of the update are measured, so that tokens
+// that add nothing leave it), and where it leaves [2^12, 2^15] in the rows' scale they are
+// scaled anew.  The true values, and those that the updates add, are some 2^7 below their bounds;
+// parts lose bits only below 2^-3.
 template <int DK>
 struct ChainState {
   static constexpr int NB = DK / 16;
@@ -29,17 +30,11 @@ struct ChainState {
   static constexpr int KR = 32 * Swz<DK>::LD;  // bytes of 16 rows of an operand tile
 
   f32x4 st[2][NB];
-  float sc, bound;
+  float sc, bound;  // bound: of the true values
 
-  __device__ void rescale(float f) {
-    const float to = fminf(fmaxf(sc * f, 0x1p-100f), 0x1p100f);
-    f = to * inverse_pow2(sc);
-    sc = to;
-    bound *= f;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) st[u][b] *= f;
+  // The scale for rows of at most `most` > 0, no further from 1 than products with it can be.
+  __device__ static float row_scale(float most) {
+    return fminf(fmaxf(scale_for(fminf(most, 0x1p126f)), 0x1p-112f), 0x1p100f);
   }
   // from: the lane's first row (null: zeros), or the rows of the identity
   __device__ void init(const float* from, bool ident, int row0, int lq) {
@@ -57,7 +52,11 @@ struct ChainState {
         bound = max4abs(bound, st[u][b]);
       }
     bound = max_over_rows(bound);
-    if (from || ident) rescale(bound > 0.f ? scale_for(bound) : 1.f);
+    if (bound > 0.f) sc = row_scale(bound);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) st[u][b] *= sc;
   }
   __device__ void store(float* to) const {
     const float inv = inverse_pow2(sc);
@@ -79,16 +78,16 @@ struct ChainState {
       for (int b = 0; b < NB; ++b) at[4 * DV * b + 64 * u] = inv * st[u][b];
   }
   // Makes room for an update S <- g S + (64 tokens' keys times values of at most `most`;
-  // keys are scaled below 2^3): the bound after it.
-  __device__ void make_room(float g, float most) {
-    float next = fmaf(g, bound, 0x1p9f * most * sc);
-    const bool off = !(next <= 32768.f && next >= 4096.f) && next > 0.f;
-    if (__any(off)) {
-      const float was = sc;
-      rescale(off ? scale_for(next) : 1.f);
-      next *= sc * inverse_pow2(was);
-    }
-    bound = next;
+  // keys are scaled below 2^3): the factor that the rows take in it, g and the change of their
+  // scale in one (by itself the change could overflow where g undoes it).
+  __device__ float make_room(float g, float most) {
+    bound = fmaf(g, bound, 0x1p9f * most);
+    const float at = bound * sc;
+    float to = sc;
+    if (bound > 0.f && !(at <= 32768.f && at >= 4096.f)) to = fminf(row_scale(bound), sc * 0x1p100f);
+    g *= to * inverse_pow2(sc);
+    sc = to;
+    return g;
   }
 };
 

@@ -17,13 +17,11 @@ enum {
   kGateY, kGateZ, kGateO, kGateP, kGateOne, kGateStage = 8,
   kRevY = 8, kRevP, kRevZ, kRevBS, kRevBeta, kRevHi, kRevLo, kRevOne
 };
-// Single values.  Forward: gamma_{C-1}; the largest factor kGateZ; the keys' inverse scale; the
-// largest row sum of scaled |T|; the scale of T X; T's inverse scale.
-enum { kOneG, kOneZ, kOneK, kOneT, kOneE, kOneIT };
-// Backward: gamma_{C-1}; the keys' and queries' inverse scales; the largest column sum of scaled
-// |T|; T's inverse scale; the largest gamma; then, as they come, bounds on the state, e, the
-// adjoint, dV and dO.
-enum { kRevG, kRevK, kRevQ, kRevT, kRevIT, kRevGam, kMaxS = 8, kMaxE, kMaxD, kMaxV, kMaxO };
+// Single values.  Forward: gamma_{C-1}; the keys' inverse scale; the scale of T X; T's inverse scale.
+enum { kOneG, kOneK, kOneE, kOneIT };
+// Backward: gamma_{C-1}; the keys' and queries' inverse scales; T's inverse scale; then, as they
+// come, the largest magnitudes of e, dV and dO and bounds on those of the state and the adjoint.
+enum { kRevG, kRevK, kRevQ, kRevIT, kMaxS = 8, kMaxE, kMaxD, kMaxV, kMaxO };
 
 struct DeltaParams {
   const void *q, *k, *v;    // [total][heads][d], token strides qs, ks, vs

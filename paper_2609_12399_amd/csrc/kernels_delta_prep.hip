@@ -87,7 +87,7 @@ struct PrepLds {
   };
   alignas(16) float gh[kC], gl[kC];          // sums of log2(alpha) as hi + lo
   alignas(16) float be[kC], bs[kC], ip[kC];  // beta, beta sigma, inverse scales of P's rows
-  float most[4][5];  // per wave: the largest key, query, element of T, row and column sum of it
+  float most[4][4];  // per wave: the largest key, query, element of T, row sum of it
 };
 
 // One chunk of one value head: the fp16 images of its keys and queries, T = (I + B
@@ -334,7 +334,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
   // the tokens; transposed and reversed, rows and columns count from the chunk's end and
   // change places
   {
-    float sums[2] = {0.f, 0.f};
+    float sum = 0.f;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if (h > 0 && w < 2) break;
@@ -355,33 +355,30 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           (r ? p.tr : p.tp)[(cu * 6 + f) * 128 + i * 64 + lane] = part[i];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sums[r] += fabsf(x[r][0][i]) + fabsf(x[r][1][i]);
       }
-    }
+      if constexpr (!BWD)
 #pragma unroll
-    for (int r = 0; r < (BWD ? 2 : 1); ++r) {
-      const float most = wave_max(sum_over_rows(sums[r]));
-      if (lane == 0) sh.most[w][3 + r] = most;
+        for (int i = 0; i < 4; ++i) sum += fabsf(x[0][0][i]) + fabsf(x[0][1][i]);
+    }
+    if constexpr (!BWD) {
+      sum = wave_max(sum_over_rows(sum));
+      if (lane == 0) sh.most[w][3] = sum;
     }
   }
   lds_barrier();
   if (w == 0) {
-    auto most = [&](int i) {
-      return fmaxf(fmaxf(sh.most[0][i], sh.most[1][i]), fmaxf(sh.most[2][i], sh.most[3][i])) * s;
-    };
     const float it = inverse_pow2(s), gam = exp2_fast(sh.gh[lane]), bs = sh.bs[lane];
     const float all = exp2_fast(sh.gh[63]);
-    const float se = scale_for(most(3) * 0x1p14f);
-    const float mz = wave_max(fabsf(bs * it));
+    // (X is scaled below 2^14)
+    const float se = BWD ? 1.f
+                         : scale_for(fmaxf(fmaxf(sh.most[0][3], sh.most[1][3]),
+                                           fmaxf(sh.most[2][3], sh.most[3][3])) * s * 0x1p14f);
     gt[kGateY * kC + lane] = -gam * ik;
     gt[kGateO * kC + lane] = p.scale * gam * iq;
     gt[kGateZ * kC + lane] = bs * it;
     gt[kGateP * kC + lane] = BWD ? 0.f : sh.ip[lane] * it * inverse_pow2(se);
-    gt[kGateOne * kC + lane] = lane == kOneG ? all : lane == kOneZ ? mz : lane == kOneK ? ik
-                             : lane == kOneT ? most(3) : lane == kOneE ? se : it;
+    gt[kGateOne * kC + lane] = lane == kOneG ? all : lane == kOneK ? ik : lane == kOneE ? se : it;
     if constexpr (BWD) {
-      const float mg = wave_max(gam);
       gt[kRevY * kC + lane] = bs * ik;
       gt[kRevP * kC + lane] = sh.ip[lane];
       gt[kRevZ * kC + lane] = -gam;
@@ -390,8 +387,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
       gt[kRevHi * kC + lane] = sh.gh[lane];
       gt[kRevLo * kC + lane] = sh.gl[lane];
       gt[kRevOne * kC + lane] = lane == kRevG ? all : lane == kRevK ? ik : lane == kRevQ ? iq
-                              : lane == kRevT ? most(4) : lane == kRevIT ? it
-                              : lane == kRevGam ? mg : 0.f;
+                              : lane == kRevIT ? it : 0.f;
     }
   }
 }

@@ -89,7 +89,7 @@ void delta_reverse_kernel(DeltaParams p) {
     __syncthreads();  // this chunk's keys, T, P and gates are in LDS; all have left the last update
     dma<kImage, NW>(p.qimg + image_at(c), sQ, w, lane);
     const long cu = (sq.slot + c) * p.HV + hv;
-    const float inv = inverse_pow2(s.sc), before = s.bound * inv;
+    const float inv = inverse_pow2(s.sc), before = s.bound;
     if constexpr (!SEG)
       s.template store_tiles<DV>(p.dsws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
     // Y = K S^T
@@ -172,46 +172,50 @@ void delta_reverse_kernel(DeltaParams p) {
       for (int a = 0; a < 4; ++a) e[u][a] = z;
     triangle(sT, xp, e, lane);
     uint4 zp[2][2][2], op[2][2][2];
-    const float g = one(kRevG);
+    float g;
     {
-      const float f = one(kRevIT) * ix, ik = one(kRevK), iq = one(kRevQ), gm = one(kRevGam);
-      const float mv = one(kRevT) * 0x1p14f * f;  // |T^T X|, by T's largest column sum
-      s.make_room(g, gm * (mv * ik + fabsf(p.scale) * mo * iq));
-      const float cz = f * s.sc * ik, co = -p.scale * s.sc * iq;
-      f32x4 gz[4], go[4];
-#pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const f32x4 ng = back(gate(kRevZ, a));
-        gz[a] = ng * cz;
-        go[a] = ng * co;
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          // (back to front within fours, the order of the update's column operands)
-          parts8(back(e[u][2 * h]), back(e[u][2 * h + 1]), gz[2 * h], gz[2 * h + 1], zp[u][h]);
-          parts8(back(v.tile(2 * h, u)), back(v.tile(2 * h + 1, u)), go[2 * h], go[2 * h + 1],
-                 op[u][h]);
-        }
+      const float f = one(kRevIT) * ix, cz = f * one(kRevK), co = -p.scale * one(kRevQ);
       if constexpr (!SEG) {
-        float* const top = p.gates + (cu * p.gate_rows + kRevOne) * kC;
-        note_max(top + kMaxD, before, lane);
-        note_max(top + kMaxV, mv, lane);
-        note_max(top + kMaxO, mo, lane);
         f32x4* const d = reinterpret_cast<f32x4*>(p.hws + cu * (DV * kC)) +
                          512 * (NW * grp + w) + 4 * lr + (3 - lq);
         const auto rs = rows_of(p.dv, c, min(kC, sq.len - c * kC));
+        float m = 0.f;
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
           const f32x4 x0 = f * e[0][a], x1 = f * e[1][a];
+          m = max4abs(max4abs(m, x0), x1);
           d[128 * (3 - a)] = back(x0);
           d[128 * (3 - a) + 64] = back(x1);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             store_columns<NP, true>(rs, os, lq, row0 * kIo, 4 * a + i, x0[i], x1[i]);
         }
+        float* const top = p.gates + (cu * p.gate_rows + kRevOne) * kC;
+        note_max(top + kMaxD, before, lane);
+        note_max(top + kMaxV, m, lane);
+        note_max(top + kMaxO, mo, lane);
       }
+      // gamma dV and gamma dO, negative
+      f32x4 od[2][4];
+      float mz = 0.f, md = 0.f;
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const f32x4 ng = gate(kRevZ, a);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          mz = max4abs(mz, e[u][a] *= ng);
+          md = max4abs(md, od[u][a] = v.tile(a, u) * ng);
+        }
+      }
+      g = s.make_room(one(kRevG), max_over_rows(mz) * cz + max_over_rows(md) * fabsf(co));
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          // (back to front within fours, the order of the update's column operands)
+          parts8<2>(back(e[u][2 * h]), back(e[u][2 * h + 1]), cz * s.sc, zp[u][h]);
+          parts8<2>(back(od[u][2 * h]), back(od[u][2 * h + 1]), co * s.sc, op[u][h]);
+        }
     }
     __syncthreads();  // all have read T, P and the gates
     if (more) {

@@ -102,7 +102,7 @@ void delta_forward_kernel(DeltaParams p) {
     dma_wait();
     __syncthreads();  // this chunk's operands are in LDS
     const long cu = (sq.slot + c) * p.HV + hv;
-    const float inv = inverse_pow2(s.sc), before = s.bound * inv;
+    const float inv = inverse_pow2(s.sc), before = s.bound;
     if constexpr (KIND == kSave)
       s.template store_tiles<DV>(p.sws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
     // Y = K S^T and Q S^T
@@ -146,29 +146,50 @@ void delta_forward_kernel(DeltaParams p) {
       for (int a = 0; a < 4; ++a) e[u][a] = z;
     triangle(sT, xp, e, lane);
     uint4 ep[2][2][2], zp[2][2][2];
-    const float g = sG[kGateOne][kOneG], ik = sG[kGateOne][kOneK];
-    {
-      // |T X| in these units, by the largest row sum of |T|
-      const float m = sG[kGateOne][kOneT] * 0x1p14f;
-      s.make_room(g, m * ix * (sG[kGateOne][kOneZ] * ik));
-      const float cz = ix * s.sc * ik;
-      f32x4 gz[4];
-#pragma unroll
-      for (int a = 0; a < 4; ++a) gz[a] = gate(kGateZ, a) * cz;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        parts8(e[u][0], e[u][1], gz[0], gz[1], zp[u][0]);
-        parts8(e[u][2], e[u][3], gz[2], gz[3], zp[u][1]);
-      }
-    }
     if constexpr (OUT) {
-      // P e, and the outputs
       const float f = sG[kGateOne][kOneE];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         parts8<2>(e[u][0], e[u][1], f, ep[u][0]);
         parts8<2>(e[u][2], e[u][3], f, ep[u][1]);
       }
+    }
+    if constexpr (KIND == kSave) {
+      const float f = sG[kGateOne][kOneIT] * ix;
+      f32x4* const d =
+          reinterpret_cast<f32x4*>(p.ews + cu * (DV * kC)) + 512 * (NW * grp + w) + 4 * lr + lq;
+      float m = 0.f;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          m = max4abs(m, e[u][a]);
+          d[128 * a + 64 * u] = f * e[u][a];
+        }
+      float* const one = p.gates + (cu * p.gate_rows + kRevOne) * kC;
+      note_max(one + kMaxS, before, lane);
+      note_max(one + kMaxE, m * f, lane);
+    }
+    // beta sigma e, in the place of e
+    float g;
+    {
+      float m = 0.f;
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const f32x4 gz = gate(kGateZ, a);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) m = max4abs(m, e[u][a] *= gz);
+      }
+      const float f = ix * sG[kGateOne][kOneK];
+      g = s.make_room(sG[kGateOne][kOneG], max_over_rows(m) * f);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        parts8<2>(e[u][0], e[u][1], f * s.sc, zp[u][0]);
+        parts8<2>(e[u][2], e[u][3], f * s.sc, zp[u][1]);
+      }
+    }
+    if constexpr (OUT) {
+      // P e, and the outputs
       f32x4 q[2][4];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -189,18 +210,6 @@ void delta_forward_kernel(DeltaParams p) {
                             fmaf(go[i], o[0][a][i], gp[i] * q[0][a][i]),
                             fmaf(go[i], o[1][a][i], gp[i] * q[1][a][i]));
       }
-    }
-    if constexpr (KIND == kSave) {
-      const float f = sG[kGateOne][kOneIT] * ix;
-      float* const one = p.gates + (cu * p.gate_rows + kRevOne) * kC;
-      note_max(one + kMaxS, before, lane);
-      note_max(one + kMaxE, sG[kGateOne][kOneT] * 0x1p14f * f, lane);
-      f32x4* const d =
-          reinterpret_cast<f32x4*>(p.ews + cu * (DV * kC)) + 512 * (NW * grp + w) + 4 * lr + lq;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) d[128 * a + 64 * u] = f * e[u][a];
     }
     __syncthreads();  // all have read T, P and the gates
     if (c + 1 < nch) {

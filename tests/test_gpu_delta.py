@@ -440,3 +440,42 @@ def test_states_in_place_in_segments(lengths, HK, HV, d, io):
     op.d_initial_state = ds.clone()
     for a, b in zip(op.backward(*x, do, off, s0, op.d_initial_state), want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("chunks,tail", [(3, 1), (3, 64), (20, 1), (20, 128)])
+@pytest.mark.parametrize("size", [1.0, 1e-6, 1e-8])
+def test_gradients_before_tokens_without_one(chunks, tail, size):
+    """d_o is zero over a sequence's last chunks (tokens without a label) and there is no
+    d_final_state: nothing of the empty adjoint's scale reaches the chunks before.  In one
+    segment and in several, decays near 1."""
+    n = 64 * chunks + tail
+    x, g = draw([n], 1, 2, 64, 64, "f32", 21, alpha_mu=-7.0)
+    do = size * torch.randn((n, 2, 64), generator=g)
+    do[64 * chunks - (64 if tail == 128 else 0):] = 0
+    do = do.to(DEV)
+    want = ref.backward([n], *[f64(t) for t in x], 1.0, None, f64(do), None)
+    got = op_of([n], 1, 2, 64, 64, "f32", 1.0, True).backward(*x, do, offsets([n]))
+    for name, a, w, bar in zip(("dq", "dk", "dv", "dla", "db"), got, want,
+                               (F32, F32, F32, SUMS, F32)):
+        check(name, a, w, 1, bar=bar)
+
+
+@pytest.mark.parametrize("chunks", [3, 20])
+@pytest.mark.parametrize("size", [1.0, 1e-6, 1e-8])
+def test_values_after_tokens_without_any(chunks, size):
+    """Values that are zero over the first chunks, from a zero state, and small after."""
+    n = 64 * chunks + 5
+    x, g = draw([n], 1, 2, 64, 64, "f32", 22, alpha_mu=-7.0)
+    x[2].mul_(size)
+    x[2][:64 * (chunks - 1)] = 0
+    do = torch.randn((n, 2, 64), generator=g).to(DEV)
+    host = [f64(t) for t in x]
+    o, last, _ = ref.forward([n], *host, 1.0)
+    fo, fs = op_of([n], 1, 2, 64, 64, "f32", 1.0).forward(*x, offsets([n]))
+    check("o", fo, o, 1)
+    check("final state", fs, last, 1)
+    want = ref.backward([n], *host, 1.0, None, f64(do), None)
+    got = op_of([n], 1, 2, 64, 64, "f32", 1.0, True).backward(*x, do, offsets([n]))
+    for name, a, w, bar in zip(("dq", "dk", "dv", "dla", "db"), got, want,
+                               (F32, F32, F32, SUMS, F32)):
+        check(name, a, w, 1, bar=bar)
