@@ -14,14 +14,16 @@ constexpr int kChainWaves = DV / 32 < 4 ? DV / 32 : 4;
 constexpr int kFragBytes = 6 * 2 * 1024;
 
 // 32 rows of the state per wave as two column tiles of S^T (tile u, lane lr: row row0 + u,
-// row0 = 32 w + 2 lr), in registers: st[u][b][i] = sc S(row0 + u, 16 b + 4 lq + i).
+// row0 = 32 w + 2 lr), in registers: st[u][b][i] = sc[u] S(row0 + u, 16 b + 4 lq + i).
 //
-// Scales (powers of two).  sc keeps the lane's two rows inside what two fp16 parts hold, by a
-// bound on their largest value; the bound grows with every update by what 64 tokens of the
+// Scales (powers of two).  sc[u] keeps the row inside what two fp16 parts hold, by a bound on
+// its largest value; the bound grows with every update by what 64 tokens of the
 // largest size among them can add at most (the values of the update are measured, so that tokens
-// that add nothing leave it), and where it leaves [2^12, 2^15] in the rows' scale they are
+// that add nothing leave it), and where it leaves [2^12, 2^15] in the row's scale it is
 // scaled anew.  The true values, and those that the updates add, are some 2^7 below their bounds;
-// parts lose bits only below 2^-3.
+// parts lose bits only below 2^-3.  Every row is a recurrence of its own, and nothing that is
+// scaled by a row is shared with another: small channels keep their bits beside large ones, and
+// what is not finite stays in its own.
 template <int DK>
 struct ChainState {
   static constexpr int NB = DK / 16;
@@ -30,7 +32,7 @@ struct ChainState {
   static constexpr int KR = 32 * Swz<DK>::LD;  // bytes of 16 rows of an operand tile
 
   f32x4 st[2][NB];
-  float sc, bound;  // bound: of the true values
+  float sc[2], bound[2];  // bound: of the true values
 
   // The scale for rows of at most `most` > 0, no further from 1 than products with it can be.
   __device__ static float row_scale(float most) {
@@ -38,10 +40,9 @@ struct ChainState {
   }
   // from: the lane's first row (null: zeros), or the rows of the identity
   __device__ void init(const float* from, bool ident, int row0, int lq) {
-    sc = 1.f;
-    bound = 0.f;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+      float m = 0.f;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         st[u][b] = from ? *reinterpret_cast<const f32x4*>(from + u * DK + 16 * b)
@@ -49,44 +50,46 @@ struct ChainState {
         if (ident)
 #pragma unroll
           for (int i = 0; i < 4; ++i) st[u][b][i] = 16 * b + 4 * lq + i == row0 + u ? 1.f : 0.f;
-        bound = max4abs(bound, st[u][b]);
+        m = max4abs(m, st[u][b]);
       }
-    bound = max_over_rows(bound);
-    if (bound > 0.f) sc = row_scale(bound);
+      bound[u] = max_over_rows(m);
+      sc[u] = bound[u] > 0.f ? row_scale(bound[u]) : 1.f;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int b = 0; b < NB; ++b) st[u][b] *= sc;
+      for (int b = 0; b < NB; ++b) st[u][b] *= sc[u];
+    }
   }
   __device__ void store(float* to) const {
-    const float inv = inverse_pow2(sc);
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+      const float inv = inverse_pow2(sc[u]);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
         *reinterpret_cast<f32x4*>(to + u * DK + 16 * b) = inv * st[u][b];
+    }
   }
   // The same for the gradients (DeltaParams::sws), whole lines at a time: `to` is the state's
   // column block 0, place 32 times the wave's rows.
   template <int DV>
   __device__ void store_tiles(float* to, int lane) const {
-    const float inv = inverse_pow2(sc);
     f32x4* const at = reinterpret_cast<f32x4*>(to) + 4 * (lane & 15) + (lane >> 4);
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+      const float inv = inverse_pow2(sc[u]);
 #pragma unroll
       for (int b = 0; b < NB; ++b) at[4 * DV * b + 64 * u] = inv * st[u][b];
+    }
   }
-  // Makes room for an update S <- g S + (64 tokens' keys times values of at most `most`;
-  // keys are scaled below 2^3): the factor that the rows take in it, g and the change of their
-  // scale in one (by itself the change could overflow where g undoes it).
-  __device__ float make_room(float g, float most) {
-    bound = fmaf(g, bound, 0x1p9f * most);
-    const float at = bound * sc;
-    float to = sc;
-    if (bound > 0.f && !(at <= 32768.f && at >= 4096.f)) to = fminf(row_scale(bound), sc * 0x1p100f);
-    g *= to * inverse_pow2(sc);
-    sc = to;
+  // Makes room in row u for an update S <- g S + (64 tokens' keys times values of at most
+  // `most`; keys are scaled below 2^3): the factor that the row takes in it, g and the change of
+  // its scale in one (by itself the change could overflow where g undoes it).
+  __device__ float make_room(int u, float g, float most) {
+    bound[u] = fmaf(g, bound[u], 0x1p9f * most);
+    const float at = bound[u] * sc[u];
+    float to = sc[u];
+    if (bound[u] > 0.f && !(at <= 32768.f && at >= 4096.f))
+      to = fminf(row_scale(bound[u]), to * 0x1p100f);
+    g *= to * inverse_pow2(sc[u]);
+    sc[u] = to;
     return g;
   }
 };
@@ -134,21 +137,26 @@ __device__ inline void store_matrix(const ChainState<DK>& s, SegmentMatrix<DK>* 
                                     int lane) {
   static_assert(sizeof(SegmentMatrix<DK>) == delta_matrix_bytes(DK), "");
   const int lr = lane & 15, lq = lane >> 4;
-  const float inv = inverse_pow2(s.sc);
-  float m = 0.f;
+  float g[2], most = 0.f;
 #pragma unroll
-  for (int u = 0; u < 2; ++u)
+  for (int u = 0; u < 2; ++u) {
+    float m = 0.f;
 #pragma unroll
     for (int b = 0; b < ChainState<DK>::NB; ++b) m = max4abs(m, s.st[u][b]);
-  const float f = scale_for(wave_max(m * inv)), g = f * inv;
+    g[u] = inverse_pow2(s.sc[u]);
+    most = fmaxf(most, m * g[u]);
+  }
+  const float f = scale_for(wave_max(most));
   if (lane == 0) to->scale[h] = f;
+  g[0] *= f;
+  g[1] *= f;
 #pragma unroll
   for (int b = 0; b < ChainState<DK>::NB; ++b)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       // rows 32 h + 2 lr + u, u < 2: two neighbouring slots
       unsigned p[2];
-      parts2<2>(s.st[0][b][i], s.st[1][b][i], g, p);
+      parts2(s.st[0][b][i], s.st[1][b][i], g[0], g[1], p);
 #pragma unroll
       for (int q = 0; q < 2; ++q)
         reinterpret_cast<unsigned*>(&to->x[b][h][q][16 * ((lr & 7) >> 1) + 4 * lq + i])
@@ -215,10 +223,10 @@ __device__ __attribute__((always_inline)) inline void triangle(const uint4* F,
   }
 }
 
-// S^T <- g S^T + A^T x (and + B^T y with TWO): A, B operand tiles in NP parts, x, y in two.
+// S^T <- S^T diag(g) + A^T x (and + B^T y with TWO): A, B operand tiles in NP parts, x, y in two.
 template <int DK, int NP, bool TWO>
 __device__ __attribute__((always_inline)) inline void update_state(
-    ChainState<DK>& s, float g, const Swz<DK>* A, const uint4 (&x)[2][2][2], const Swz<DK>* B,
+    ChainState<DK>& s, const float (&g)[2], const Swz<DK>* A, const uint4 (&x)[2][2][2], const Swz<DK>* B,
     const uint4 (&y)[2][2][2], int tb) {
   using C = ChainState<DK>;
   constexpr int NG = C::NB < 4 ? C::NB : 4;
@@ -227,7 +235,7 @@ __device__ __attribute__((always_inline)) inline void update_state(
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int b = 0; b < NG; ++b) s.st[u][b0 + b] *= g;
+      for (int b = 0; b < NG; ++b) s.st[u][b0 + b] *= g[u];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint4 kt[NG][NP];

@@ -198,6 +198,12 @@ __device__ inline void parts2(float a, float b, float s, unsigned (&p)[NP]) {
   }
 }
 
+// The same, each with a scale of its own.
+__device__ inline void parts2(float a, float b, float s, float t, unsigned (&p)[2]) {
+  p[0] = pack_f16x2(a * s, b * t);
+  const half2v h = __builtin_bit_cast(half2v, p[0]);
+  p[1] = pack_f16x2(fmaf(a, s, -float(h.x)), fmaf(b, t, -float(h.y)));
+}
 // The same without a scale.
 __device__ inline void parts2(float a, float b, unsigned (&p)[2]) {
   p[0] = pack_f16x2(a, b);
@@ -215,23 +221,6 @@ __device__ inline void parts8(const f32x4& x, const f32x4& y, uint4 (&p)[2]) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) p[i] = make_uint4(u[0][i], u[1][i], u[2][i], u[3][i]);
 }
-// Eight values, each with a scale of its own.
-__device__ inline void parts8(const f32x4& x, const f32x4& y, const f32x4& sx, const f32x4& sy,
-                              uint4 (&p)[2]) {
-  unsigned u[4][2];
-  auto two = [](float a, float b, float s, float t, unsigned (&q)[2]) {
-    q[0] = pack_f16x2(a * s, b * t);
-    const half2v h = __builtin_bit_cast(half2v, q[0]);
-    q[1] = pack_f16x2(fmaf(a, s, -float(h.x)), fmaf(b, t, -float(h.y)));
-  };
-  two(x.x, x.y, sx.x, sx.y, u[0]);
-  two(x.z, x.w, sx.z, sx.w, u[1]);
-  two(y.x, y.y, sy.x, sy.y, u[2]);
-  two(y.z, y.w, sy.z, sy.w, u[3]);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) p[i] = make_uint4(u[0][i], u[1][i], u[2][i], u[3][i]);
-}
-
 // Eight values (two accumulator tiles of four) as parts of an operand.
 template <int NP>
 __device__ inline void parts8(const f32x4& x, const f32x4& y, float s, uint4 (&p)[NP]) {

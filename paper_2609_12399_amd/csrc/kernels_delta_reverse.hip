@@ -89,7 +89,8 @@ void delta_reverse_kernel(DeltaParams p) {
     __syncthreads();  // this chunk's keys, T, P and gates are in LDS; all have left the last update
     dma<kImage, NW>(p.qimg + image_at(c), sQ, w, lane);
     const long cu = (sq.slot + c) * p.HV + hv;
-    const float inv = inverse_pow2(s.sc), before = s.bound;
+    const float inv[2] = {inverse_pow2(s.sc[0]), inverse_pow2(s.sc[1])};
+    const float before = fmaxf(s.bound[0], s.bound[1]);
     if constexpr (!SEG)
       s.template store_tiles<DV>(p.dsws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
     // Y = K S^T
@@ -118,45 +119,45 @@ void delta_reverse_kernel(DeltaParams p) {
     }
     // P^T dO
     f32x4 q[2][4];
-    float mo = 0.f;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        q[u][a] = z;
-        mo = max4abs(mo, v.tile(a, u));
-      }
-    mo = max_over_rows(mo);
-    const float fo = scale_for(mo);
+    float mo[2], fo[2];
     {
       uint4 op[2][2][NP];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
+        mo[u] = 0.f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) parts8<NP>(v.tile(2 * h, u), v.tile(2 * h + 1, u), fo, op[u][h]);
+        for (int a = 0; a < 4; ++a) {
+          q[u][a] = z;
+          mo[u] = max4abs(mo[u], v.tile(a, u));
+        }
+        fo[u] = scale_for(max_over_rows(mo[u]));
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          parts8<NP>(v.tile(2 * h, u), v.tile(2 * h + 1, u), fo[u], op[u][h]);
+      }
       triangle(sP, op, q, lane);
     }
-    // X = P^T dO + beta sigma Y, scaled for the lane's two rows
+    // X = P^T dO + beta sigma Y, each row with a scale of its own
     uint4 xp[2][2][2];
-    float ix;
+    float ix[2];
     {
-      const float io = inverse_pow2(fo);
       f32x4 x[2][4];
-      float m = 0.f;
+      float m[2] = {0.f, 0.f};
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
-        const f32x4 gy = gate(kRevY, a) * inv, gp = gate(kRevP, a) * io;
+        const f32x4 gy = gate(kRevY, a), gp = gate(kRevP, a);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+          const f32x4 yi = y[u][a] * inv[u], qi = q[u][a] * inverse_pow2(fo[u]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[u][a][i] = fmaf(gy[i], y[u][a][i], gp[i] * q[u][a][i]);
-          m = max4abs(m, x[u][a]);
+          for (int i = 0; i < 4; ++i) x[u][a][i] = fmaf(gy[i], yi[i], gp[i] * qi[i]);
+          m[u] = max4abs(m[u], x[u][a]);
         }
       }
-      const float f = scale_for(max_over_rows(m));
-      ix = inverse_pow2(f);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
+        const float f = scale_for(max_over_rows(m[u]));
+        ix[u] = inverse_pow2(f);
         parts8<2>(x[u][0], x[u][1], f, xp[u][0]);
         parts8<2>(x[u][2], x[u][3], f, xp[u][1]);
       }
@@ -172,9 +173,9 @@ void delta_reverse_kernel(DeltaParams p) {
       for (int a = 0; a < 4; ++a) e[u][a] = z;
     triangle(sT, xp, e, lane);
     uint4 zp[2][2][2], op[2][2][2];
-    float g;
+    float g[2];
     {
-      const float f = one(kRevIT) * ix, cz = f * one(kRevK), co = -p.scale * one(kRevQ);
+      const float f[2] = {one(kRevIT) * ix[0], one(kRevIT) * ix[1]};
       if constexpr (!SEG) {
         f32x4* const d = reinterpret_cast<f32x4*>(p.hws + cu * (DV * kC)) +
                          512 * (NW * grp + w) + 4 * lr + (3 - lq);
@@ -182,7 +183,7 @@ void delta_reverse_kernel(DeltaParams p) {
         float m = 0.f;
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-          const f32x4 x0 = f * e[0][a], x1 = f * e[1][a];
+          const f32x4 x0 = f[0] * e[0][a], x1 = f[1] * e[1][a];
           m = max4abs(max4abs(m, x0), x1);
           d[128 * (3 - a)] = back(x0);
           d[128 * (3 - a) + 64] = back(x1);
@@ -193,36 +194,39 @@ void delta_reverse_kernel(DeltaParams p) {
         float* const top = p.gates + (cu * p.gate_rows + kRevOne) * kC;
         note_max(top + kMaxD, before, lane);
         note_max(top + kMaxV, m, lane);
-        note_max(top + kMaxO, mo, lane);
+        note_max(top + kMaxO, fmaxf(mo[0], mo[1]), lane);
       }
       // gamma dV and gamma dO, negative
       f32x4 od[2][4];
-      float mz = 0.f, md = 0.f;
+      float mz[2] = {0.f, 0.f}, md[2] = {0.f, 0.f};
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
         const f32x4 ng = gate(kRevZ, a);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          mz = max4abs(mz, e[u][a] *= ng);
-          md = max4abs(md, od[u][a] = v.tile(a, u) * ng);
+          mz[u] = max4abs(mz[u], e[u][a] *= ng);
+          md[u] = max4abs(md[u], od[u][a] = v.tile(a, u) * ng);
         }
       }
-      g = s.make_room(one(kRevG), max_over_rows(mz) * cz + max_over_rows(md) * fabsf(co));
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
+        const float cz = f[u] * one(kRevK), co = -p.scale * one(kRevQ);
+        g[u] = s.make_room(u, one(kRevG),
+                           max_over_rows(mz[u]) * cz + max_over_rows(md[u]) * fabsf(co));
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           // (back to front within fours, the order of the update's column operands)
-          parts8<2>(back(e[u][2 * h]), back(e[u][2 * h + 1]), cz * s.sc, zp[u][h]);
-          parts8<2>(back(od[u][2 * h]), back(od[u][2 * h + 1]), co * s.sc, op[u][h]);
+          parts8<2>(back(e[u][2 * h]), back(e[u][2 * h + 1]), cz * s.sc[u], zp[u][h]);
+          parts8<2>(back(od[u][2 * h]), back(od[u][2 * h + 1]), co * s.sc[u], op[u][h]);
         }
+      }
     }
     __syncthreads();  // all have read T, P and the gates
     if (more) {
       load_tp(c - 1);
       load_v(c - 1);
     }
-    // S^T <- g S^T - K^T (gamma dV) + Q^T (scale gamma dO)
+    // S^T <- S^T diag(g) - K^T (gamma dV) + Q^T (scale gamma dO)
     {
       constexpr int NB = DK / 16, NG = NB < 4 ? NB : 4;
       // slots 0..3 of a column operand are the walk's rows 32 h + 4 lq + 3 - i, the tile's
@@ -238,7 +242,7 @@ void delta_reverse_kernel(DeltaParams p) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int b = 0; b < NG; ++b) s.st[u][b0 + b] *= g;
+          for (int b = 0; b < NG; ++b) s.st[u][b0 + b] *= g[u];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint4 kt[NG][NP];

@@ -102,7 +102,8 @@ void delta_forward_kernel(DeltaParams p) {
     dma_wait();
     __syncthreads();  // this chunk's operands are in LDS
     const long cu = (sq.slot + c) * p.HV + hv;
-    const float inv = inverse_pow2(s.sc), before = s.bound;
+    const float inv[2] = {inverse_pow2(s.sc[0]), inverse_pow2(s.sc[1])};
+    const float before = fmaxf(s.bound[0], s.bound[1]);
     if constexpr (KIND == kSave)
       s.template store_tiles<DV>(p.sws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
     // Y = K S^T and Q S^T
@@ -112,26 +113,27 @@ void delta_forward_kernel(DeltaParams p) {
 #pragma unroll
       for (int a = 0; a < 4; ++a) y[u][a] = o[u][a] = z;
     rows_times_state<DK, NP, OUT>(K, sQ, s, kb, y, o);
-    // X = V - gamma Y, scaled for the lane's two rows
+    // X = V - gamma Y, each row with a scale of its own
     uint4 xp[2][2][2];
-    float ix;
+    float ix[2];
     {
       f32x4 x[2][4];
-      float m = 0.f;
+      float m[2] = {0.f, 0.f};
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
-        const f32x4 g = gate(kGateY, a) * inv;
+        const f32x4 g = gate(kGateY, a);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+          const f32x4 gi = g * inv[u];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[u][a][i] = fmaf(g[i], y[u][a][i], v.get(4 * a + i, u));
-          m = max4abs(m, x[u][a]);
+          for (int i = 0; i < 4; ++i) x[u][a][i] = fmaf(gi[i], y[u][a][i], v.get(4 * a + i, u));
+          m[u] = max4abs(m[u], x[u][a]);
         }
       }
-      const float f = scale_for(max_over_rows(m));
-      ix = inverse_pow2(f);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
+        const float f = scale_for(max_over_rows(m[u]));
+        ix[u] = inverse_pow2(f);
         parts8<2>(x[u][0], x[u][1], f, xp[u][0]);
         parts8<2>(x[u][2], x[u][3], f, xp[u][1]);
       }
@@ -155,7 +157,7 @@ void delta_forward_kernel(DeltaParams p) {
       }
     }
     if constexpr (KIND == kSave) {
-      const float f = sG[kGateOne][kOneIT] * ix;
+      const float f[2] = {sG[kGateOne][kOneIT] * ix[0], sG[kGateOne][kOneIT] * ix[1]};
       f32x4* const d =
           reinterpret_cast<f32x4*>(p.ews + cu * (DV * kC)) + 512 * (NW * grp + w) + 4 * lr + lq;
       float m = 0.f;
@@ -163,29 +165,30 @@ void delta_forward_kernel(DeltaParams p) {
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-          m = max4abs(m, e[u][a]);
-          d[128 * a + 64 * u] = f * e[u][a];
+          const f32x4 x = f[u] * e[u][a];
+          m = max4abs(m, x);
+          d[128 * a + 64 * u] = x;
         }
       float* const one = p.gates + (cu * p.gate_rows + kRevOne) * kC;
       note_max(one + kMaxS, before, lane);
-      note_max(one + kMaxE, m * f, lane);
+      note_max(one + kMaxE, m, lane);
     }
     // beta sigma e, in the place of e
-    float g;
+    float g[2];
     {
-      float m = 0.f;
+      float m[2] = {0.f, 0.f};
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
         const f32x4 gz = gate(kGateZ, a);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) m = max4abs(m, e[u][a] *= gz);
+        for (int u = 0; u < 2; ++u) m[u] = max4abs(m[u], e[u][a] *= gz);
       }
-      const float f = ix * sG[kGateOne][kOneK];
-      g = s.make_room(sG[kGateOne][kOneG], max_over_rows(m) * f);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        parts8<2>(e[u][0], e[u][1], f * s.sc, zp[u][0]);
-        parts8<2>(e[u][2], e[u][3], f * s.sc, zp[u][1]);
+        const float f = ix[u] * sG[kGateOne][kOneK];
+        g[u] = s.make_room(u, sG[kGateOne][kOneG], max_over_rows(m[u]) * f);
+        parts8<2>(e[u][0], e[u][1], f * s.sc[u], zp[u][0]);
+        parts8<2>(e[u][2], e[u][3], f * s.sc[u], zp[u][1]);
       }
     }
     if constexpr (OUT) {
@@ -203,7 +206,12 @@ void delta_forward_kernel(DeltaParams p) {
                                   os, m);
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
-        const f32x4 go = gate(kGateO, a) * inv, gp = gate(kGateP, a) * ix;
+        const f32x4 go = gate(kGateO, a), gp = gate(kGateP, a);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          o[u][a] *= inv[u];
+          q[u][a] *= ix[u];
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           store_columns<NP>(rs, os, lq, row0 * kIo, 4 * a + i,

@@ -479,3 +479,68 @@ def test_values_after_tokens_without_any(chunks, size):
     for name, a, w, bar in zip(("dq", "dk", "dv", "dla", "db"), got, want,
                                (F32, F32, F32, SUMS, F32)):
         check(name, a, w, 1, bar=bar)
+
+
+def different_sizes(lengths, HK, HV, d, io):
+    """Value channels from 1 to 1e-5 beside one another, output gradients the other way round:
+    (o, final state), the gradients, and the 64-bit references of both."""
+    x, g = draw(lengths, HK, HV, d, d, io, 23, alpha_mu=-5.0)
+    size = (10.0 ** -(torch.arange(d) % 6).double()).float().to(DEV)
+    n, N = sum(lengths), len(lengths)
+    s0, ds = (torch.randn((N, HV, d, d), generator=g).to(DEV) for _ in range(2))
+    do = torch.randn((n, HV, d), generator=g).to(DEV)
+    x[2], s0 = (x[2].float() * size).to(x[2].dtype), s0 * size[:, None]
+    do, ds = (do / size).to(x[2].dtype), ds / size[:, None]
+    host = [f64(t) for t in x]
+    off = offsets(lengths)
+    got = (op_of(lengths, HK, HV, d, d, io, 1.0).forward(*x, off, s0),
+           op_of(lengths, HK, HV, d, d, io, 1.0, True).backward(*x, do, off, s0, ds))
+    return got, (ref.forward(lengths, *host, 1.0, f64(s0))[:2],
+                 ref.backward(lengths, *host, 1.0, f64(s0), f64(do), f64(ds)))
+
+
+SIZES = [([200], 1, 2, 64, "f32"), ([64 * 18], 1, 2, 64, "f32"), ([150, 70], 1, 2, 128, "bf16")]
+
+
+@pytest.mark.parametrize("lengths,HK,HV,d,io", SIZES)
+def test_channels_of_different_sizes(lengths, HK, HV, d, io):
+    """Every row of the state is a recurrence of its own, so the bars hold for each size of channel
+    by itself."""
+    (got, grads), (want, wgrads) = different_sizes(lengths, HK, HV, d, io)
+    for c in range(6):
+        check(f"o {c}", got[0][..., c::6], want[0][..., c::6], 1, io)
+        check(f"state {c}", got[1][:, :, c::6], want[1][:, :, c::6], 1)
+        check(f"dv {c}", grads[2][..., c::6], wgrads[2][..., c::6], 1, io)
+        check(f"d initial state {c}", grads[5][:, :, c::6], wgrads[5][:, :, c::6], 1)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("d,io", [(64, "f32"), (128, "bf16")])
+def test_channels_that_are_not_finite(bad, d, io):
+    """A channel of the values, a row of the state to start from, of d_o or of d_final_state that
+    is not finite: the other channels keep their bits."""
+    lengths = [150]
+    x, g = draw(lengths, 1, 2, d, d, io, 24)
+    x[2].mul_(50.0)
+    s0, ds = (10 * torch.randn((1, 2, d, d), generator=g).to(DEV) for _ in range(2))
+    do = torch.randn(x[2].shape, generator=g).to(x[2])
+    off = offsets(lengths)
+
+    def run(v, s0, do, ds):
+        o, last = op_of(lengths, 1, 2, d, d, io, 1.0).forward(*x[:2], v, *x[3:], off, s0)
+        b = op_of(lengths, 1, 2, d, d, io, 1.0, True).backward(*x[:2], v, *x[3:], do, off, s0, ds)
+        return o, last, b[2], b[5]
+
+    clean = run(x[2], s0, do, ds)
+    one, other = 6, d - 1  # and their neighbours 7 and d - 2
+    keep = [c for c in range(d) if c not in (one, other)]
+    v, s, w, e = (t.clone() for t in (x[2], s0, do, ds))
+    v[:, :, one], s[:, :, other], w[:, :, one], e[:, :, other] = bad, bad, bad, bad
+    v[70:, :, other], w[:70, :, other] = bad, bad
+    o, last, dv, d0 = run(v, s, w, e)
+    for a, b in ((o, clean[0]), (dv, clean[2])):
+        assert torch.equal(a[..., keep], b[..., keep])
+        assert not torch.isfinite(a[..., [one, other]]).any()
+    for a, b in ((last, clean[1]), (d0, clean[3])):
+        assert torch.equal(a[:, :, keep], b[:, :, keep])
+        assert not torch.isfinite(a[:, :, [one, other]]).any()
