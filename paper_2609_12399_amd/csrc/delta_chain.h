@@ -84,10 +84,9 @@ struct ChainState {
   // its scale in one (by itself the change could overflow where g undoes it).
   __device__ float make_room(int u, float g, float most) {
     bound[u] = fmaf(g, bound[u], 0x1p9f * most);
-    const float at = bound[u] * sc[u];
-    float to = sc[u];
-    if (bound[u] > 0.f && !(at <= 32768.f && at >= 4096.f))
-      to = fminf(row_scale(bound[u]), to * 0x1p100f);
+    const float at = bound[u] * sc[u], fit = fminf(row_scale(bound[u]), sc[u] * 0x1p100f);
+    const bool off = bound[u] > 0.f & !(at <= 32768.f & at >= 4096.f);
+    const float to = off ? fit : sc[u];
     g *= to * inverse_pow2(sc[u]);
     sc[u] = to;
     return g;

@@ -241,33 +241,38 @@ __device__ inline void for_products(F&& f) {
   f(0, 0);
 }
 
-// max(m, |x|) of values m >= 0 (as medians and integers: fmaxf would first make each operand
-// canonical).
+// max(m, |x|) of values m >= 0: three instructions, as medians and integers (fmaxf would first make
+// each operand canonical, and a median with an infinity that the compiler sees is fmaxf to it:
+// eight).  NaN counts as nothing beside a number.
 __device__ inline float max4abs(float m, const f32x4& x) {
-  const float inf = __builtin_inff();
+  float inf = __builtin_inff();
+  asm("" : "+s"(inf));
   const unsigned a = __float_as_uint(__builtin_amdgcn_fmed3f(fabsf(x.x), fabsf(x.y), inf));
   const unsigned b = __float_as_uint(__builtin_amdgcn_fmed3f(fabsf(x.z), fabsf(x.w), inf));
   return __uint_as_float(max(__float_as_uint(m), max(a, b)));
 }
 
-// Maximum over the wave, in every lane.
+// max(a, b) of values >= 0, whose bits rise with them (NaN is the largest).
+__device__ inline float max_bits(float a, float b) {
+  return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+}
+// Maximum of values m >= 0 over the wave, in every lane.
 __device__ inline float max_over_rows(float m);
 __device__ inline float wave_max(float m) {
-  m = fmaxf(m, dpp<0xB1>(m));   // quad_perm [1,0,3,2]
-  m = fmaxf(m, dpp<0x4E>(m));   // quad_perm [2,3,0,1]
-  m = fmaxf(m, dpp<0x141>(m));  // row_half_mirror
-  m = fmaxf(m, dpp<0x140>(m));  // row_mirror
+  m = max_bits(m, dpp<0xB1>(m));   // quad_perm [1,0,3,2]
+  m = max_bits(m, dpp<0x4E>(m));   // quad_perm [2,3,0,1]
+  m = max_bits(m, dpp<0x141>(m));  // row_half_mirror
+  m = max_bits(m, dpp<0x140>(m));  // row_mirror
   return max_over_rows(m);
 }
 
-// Maximum (sum) over the four lanes lr, lr + 16, lr + 32, lr + 48.
+// Maximum (of values m >= 0) and sum over the four lanes lr, lr + 16, lr + 32, lr + 48.
 __device__ inline float max_over_rows(float m) {
   const unsigned v = __float_as_uint(m);
   const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  m = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
-  const unsigned u = __float_as_uint(m);
+  const unsigned u = max(p[0], p[1]);
   const auto q = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+  return __uint_as_float(max(q[0], q[1]));
 }
 __device__ inline float sum_over_rows(float m) {
   const unsigned v = __float_as_uint(m);
@@ -278,11 +283,17 @@ __device__ inline float sum_over_rows(float m) {
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
 
-// Raises *to (>= 0, in memory) to the wave's largest m >= 0.  Bits of floats >= 0 rise with
+// Raises to[i] (>= 0, in memory) to the wave's largest m[i] >= 0.  Bits of floats >= 0 rise with
 // them, and a maximum does not depend on the order.
-__device__ inline void note_max(float* to, float m, int lane) {
-  m = wave_max(m);
-  if (lane == 0) atomicMax(reinterpret_cast<unsigned*>(to), __float_as_uint(m));
+template <int N>
+__device__ inline void note_max(float* to, const float (&m)[N], int lane) {
+  float mine = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float x = wave_max(m[i]);
+    mine = lane == i ? x : mine;
+  }
+  if (lane < N) atomicMax(reinterpret_cast<unsigned*>(to) + lane, __float_as_uint(mine));
 }
 
 }  // namespace onela

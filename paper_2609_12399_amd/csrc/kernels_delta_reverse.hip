@@ -90,7 +90,7 @@ void delta_reverse_kernel(DeltaParams p) {
     dma<kImage, NW>(p.qimg + image_at(c), sQ, w, lane);
     const long cu = (sq.slot + c) * p.HV + hv;
     const float inv[2] = {inverse_pow2(s.sc[0]), inverse_pow2(s.sc[1])};
-    const float before = fmaxf(s.bound[0], s.bound[1]);
+    const float before = max_bits(s.bound[0], s.bound[1]);
     if constexpr (!SEG)
       s.template store_tiles<DV>(p.dsws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
     // Y = K S^T
@@ -191,10 +191,9 @@ void delta_reverse_kernel(DeltaParams p) {
           for (int i = 0; i < 4; ++i)
             store_columns<NP, true>(rs, os, lq, row0 * kIo, 4 * a + i, x0[i], x1[i]);
         }
-        float* const top = p.gates + (cu * p.gate_rows + kRevOne) * kC;
-        note_max(top + kMaxD, before, lane);
-        note_max(top + kMaxV, m, lane);
-        note_max(top + kMaxO, fmaxf(mo[0], mo[1]), lane);
+        static_assert(kMaxV == kMaxD + 1 && kMaxO == kMaxD + 2, "");
+        note_max<3>(p.gates + (cu * p.gate_rows + kRevOne) * kC + kMaxD,
+                    {before, m, max_bits(mo[0], mo[1])}, lane);
       }
       // gamma dV and gamma dO, negative
       f32x4 od[2][4];

@@ -103,7 +103,7 @@ void delta_forward_kernel(DeltaParams p) {
     __syncthreads();  // this chunk's operands are in LDS
     const long cu = (sq.slot + c) * p.HV + hv;
     const float inv[2] = {inverse_pow2(s.sc[0]), inverse_pow2(s.sc[1])};
-    const float before = fmaxf(s.bound[0], s.bound[1]);
+    const float before = max_bits(s.bound[0], s.bound[1]);
     if constexpr (KIND == kSave)
       s.template store_tiles<DV>(p.sws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
     // Y = K S^T and Q S^T
@@ -169,27 +169,8 @@ void delta_forward_kernel(DeltaParams p) {
           m = max4abs(m, x);
           d[128 * a + 64 * u] = x;
         }
-      float* const one = p.gates + (cu * p.gate_rows + kRevOne) * kC;
-      note_max(one + kMaxS, before, lane);
-      note_max(one + kMaxE, m, lane);
-    }
-    // beta sigma e, in the place of e
-    float g[2];
-    {
-      float m[2] = {0.f, 0.f};
-#pragma unroll
-      for (int a = 0; a < 4; ++a) {
-        const f32x4 gz = gate(kGateZ, a);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) m[u] = max4abs(m[u], e[u][a] *= gz);
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const float f = ix[u] * sG[kGateOne][kOneK];
-        g[u] = s.make_room(u, sG[kGateOne][kOneG], max_over_rows(m[u]) * f);
-        parts8<2>(e[u][0], e[u][1], f * s.sc[u], zp[u][0]);
-        parts8<2>(e[u][2], e[u][3], f * s.sc[u], zp[u][1]);
-      }
+      static_assert(kMaxE == kMaxS + 1, "");
+      note_max<2>(p.gates + (cu * p.gate_rows + kRevOne) * kC + kMaxS, {before, m}, lane);
     }
     if constexpr (OUT) {
       // P e, and the outputs
@@ -217,6 +198,24 @@ void delta_forward_kernel(DeltaParams p) {
           store_columns<NP>(rs, os, lq, row0 * kIo, 4 * a + i,
                             fmaf(go[i], o[0][a][i], gp[i] * q[0][a][i]),
                             fmaf(go[i], o[1][a][i], gp[i] * q[1][a][i]));
+      }
+    }
+    // beta sigma e, in the place of e
+    float g[2];
+    {
+      float m[2] = {0.f, 0.f};
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const f32x4 gz = gate(kGateZ, a);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) m[u] = max4abs(m[u], e[u][a] *= gz);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float f = ix[u] * sG[kGateOne][kOneK];
+        g[u] = s.make_room(u, sG[kGateOne][kOneG], max_over_rows(m[u]) * f);
+        parts8<2>(e[u][0], e[u][1], f * s.sc[u], zp[u][0]);
+        parts8<2>(e[u][2], e[u][3], f * s.sc[u], zp[u][1]);
       }
     }
     __syncthreads();  // all have read T, P and the gates
