@@ -10,6 +10,10 @@ namespace onela {
 template <int DV>
 constexpr int kChainWaves = DV / 32 < 4 ? DV / 32 : 4;
 
+// Chunks after which a state's bound is taken from its rows (which costs some 50 vector
+// instructions at d_k = 128, of 900 per chunk).
+constexpr int kTighten = 8;
+
 // Bytes of a triangular matrix's fragments, and of a chunk's gates.
 constexpr int kFragBytes = 6 * 2 * 1024;
 
@@ -20,8 +24,11 @@ constexpr int kFragBytes = 6 * 2 * 1024;
 // its largest value; the bound grows with every update by what 64 tokens of the
 // largest size among them can add at most (the values of the update are measured, so that tokens
 // that add nothing leave it), and where it leaves [2^12, 2^15] in the row's scale it is
-// scaled anew.  The true values, and those that the updates add, are some 2^7 below their bounds;
-// parts lose bits only below 2^-3.  Every row is a recurrence of its own, and nothing that is
+// scaled anew.  What the tokens of a chunk add is some 2^7 below that; over many chunks without
+// decay the bound alone would rise and rise while the delta rule keeps the state where it is, so
+// it is taken from the row itself every kTighten chunks (2^10 below at worst; before every chunk
+// where the largest value is kept for the gradients anyway).  Parts lose bits only below 2^-3,
+// 2^15 below the bound.  Every row is a recurrence of its own, and nothing that is
 // scaled by a row is shared with another: small channels keep their bits beside large ones, and
 // what is not finite stays in its own.
 template <int DK>
@@ -77,6 +84,16 @@ struct ChainState {
       const float inv = inverse_pow2(sc[u]);
 #pragma unroll
       for (int b = 0; b < NB; ++b) at[4 * DV * b + 64 * u] = inv * st[u][b];
+    }
+  }
+  // Bounds from the rows themselves.
+  __device__ void tighten() {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float m = 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) m = max4abs(m, st[u][b]);
+      bound[u] = fminf(bound[u], max_over_rows(m) * inverse_pow2(sc[u]));
     }
   }
   // Makes room in row u for an update S <- g S + (64 tokens' keys times values of at most

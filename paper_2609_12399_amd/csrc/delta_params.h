@@ -20,7 +20,7 @@ enum {
 // Single values.  Forward: gamma_{C-1}; the keys' inverse scale; the scale of T X; T's inverse scale.
 enum { kOneG, kOneK, kOneE, kOneIT };
 // Backward: gamma_{C-1}; the keys' and queries' inverse scales; T's inverse scale; then, as they
-// come, the largest magnitudes of e, dV and dO and bounds on those of the state and the adjoint.
+// come, the largest magnitudes of the state, e, the adjoint, dV and dO.
 enum { kRevG, kRevK, kRevQ, kRevIT, kMaxS = 8, kMaxE, kMaxD, kMaxV, kMaxO };
 
 struct DeltaParams {

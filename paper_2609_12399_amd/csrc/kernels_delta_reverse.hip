@@ -85,6 +85,7 @@ void delta_reverse_kernel(DeltaParams p) {
     const int c = all - 1 - step;
     const Swz<DK>* const K = sK[step & 1];
     const bool more = step + 1 < sg.ce;
+    if (!SEG || (step - sg.cb) % kTighten == kTighten - 1) s.tighten();
     dma_wait();
     __syncthreads();  // this chunk's keys, T, P and gates are in LDS; all have left the last update
     dma<kImage, NW>(p.qimg + image_at(c), sQ, w, lane);

@@ -99,6 +99,7 @@ void delta_forward_kernel(DeltaParams p) {
   }
   for (int c = sg.cb; c < nch; ++c) {
     const Swz<DK>* const K = sK[c & 1];
+    if (KIND == kSave || (c - sg.cb) % kTighten == kTighten - 1) s.tighten();
     dma_wait();
     __syncthreads();  // this chunk's operands are in LDS
     const long cu = (sq.slot + c) * p.HV + hv;

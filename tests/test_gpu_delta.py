@@ -544,3 +544,39 @@ def test_channels_that_are_not_finite(bad, d, io):
     for a, b in ((last, clean[1]), (d0, clean[3])):
         assert torch.equal(a[:, :, keep], b[:, :, keep])
         assert not torch.isfinite(a[:, :, [one, other]]).any()
+
+
+@pytest.mark.parametrize("lengths,HK,HV,d,io", SIZES)
+def test_gradients_over_channels_of_different_sizes(lengths, HK, HV, d, io):
+    """The gradients by q, k and the gates are sums over channels, here of one size."""
+    (_, got), (_, want) = different_sizes(lengths, HK, HV, d, io)
+    check("dq", got[0], want[0], 1, io)
+    check("dk", got[1], want[1], 1, io)
+    check("dlog_alpha", got[3], want[3], 1, bar=SUMS)
+    check("dbeta", got[4], want[4], 1)
+
+
+def test_long_sequences_that_forget_nothing():
+    """alpha = 1 throughout, as many heads as compute units, so that the chain is not cut: the
+    recurrence in 32 bits stays near 3e-7 of the state at any length, and so has the chain."""
+    n, HV, d, heads = 32768, 256, 64, [0, 255]
+    g = torch.Generator(device=DEV).manual_seed(25)
+    k = torch.randn((n, 1, d), generator=g, device=DEV)
+    k.div_(k.norm(dim=-1, keepdim=True))
+    v = torch.randn((n, HV, d), generator=g, device=DEV)
+    beta = torch.rand((n, HV), generator=g, device=DEV)
+    la = torch.zeros_like(beta)
+    o, last = op_of([n], 1, HV, d, d, "f32", 1.0).forward(k, k, v, la, beta)
+    want, state, _ = ref.forward([n], f64(k), f64(k), *[f64(t[:, heads]) for t in (v, la, beta)],
+                                 1.0)
+    check("o", o[:, heads], want, 1)
+    check("state", last[:, heads], state, 1)
+    m = 8192
+    do = torch.randn((m, HV, d), generator=g, device=DEV)
+    x = [t[:m] for t in (k, k, v, la, beta)]
+    got = op_of([m], 1, HV, d, d, "f32", 1.0, True).backward(*x, do)
+    want = ref.backward([m], f64(x[0]), f64(x[1]), *[f64(t[:, heads]) for t in x[2:]], 1.0, None,
+                        f64(do[:, heads]), None)
+    check("dv", got[2][:, heads], want[2], 1)
+    check("dlog_alpha", got[3][:, heads], want[3], 1, bar=SUMS)
+    check("dbeta", got[4][:, heads], want[4], 1)
