@@ -174,13 +174,13 @@ def _dev(x, name: str, optional: bool = False):
         if optional:
             return None
         raise ValueError(f"{name} must not be None")
-    if isinstance(x, int):
-        return x
     try:
         if x.is_cuda and x.is_contiguous():
             return x.data_ptr()
     except AttributeError:
         pass
+    if isinstance(x, int):
+        return x
     if not hasattr(x, "data_ptr"):
         raise TypeError(f"{name}: unsupported pointer type {type(x)}")
     if not getattr(x, "is_cuda", False):
@@ -216,13 +216,15 @@ def _current_stream() -> int:
         if raw is None:  # the public way builds a Stream object for every call
             _torch_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
         else:
-            _torch_stream = lambda: raw(torch.cuda.current_device())  # noqa: E731
+            torch.cuda.current_device()  # (starts torch's runtime if nothing has)
+            device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+            _torch_stream = lambda: raw(device())  # noqa: E731
     return _torch_stream()
 
 
 def _stream(stream):
     if stream is None:
-        return _current_stream()
+        return (_torch_stream or _current_stream)()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

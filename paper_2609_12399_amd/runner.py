@@ -207,9 +207,19 @@ def _io_tensor_dtype(io: str):
     return {"bf16": torch.bfloat16, "f32": torch.float32}[io]
 
 
-def _token_stride(x) -> int:
-    """Elements between the tokens of a [tokens][heads][width] view (0: dense)."""
-    return 0 if x.is_contiguous() else x.stride(0)
+def _expect(*tensors):
+    """ValueError unless each (tensor, name, shape, dtype) has this shape and type: the kernels read
+    by the object's sizes.  (None and plain addresses are the binding's to judge.)"""
+    for x, name, shape, dtype in tensors:
+        if x is not None and not isinstance(x, int) and (x.dtype is not dtype or x.shape != shape):
+            raise ValueError(f"{name} must be {dtype} {list(shape)}, not {x.dtype} {list(x.shape)}")
+
+
+def _set_strides(cfg, q, k, v):
+    """Elements between the tokens of [tokens][heads][width] views (0: dense)."""
+    cfg.q_stride = 0 if q.is_contiguous() else q.stride(0)
+    cfg.k_stride = 0 if k.is_contiguous() else k.stride(0)
+    cfg.v_stride = 0 if v.is_contiguous() else v.stride(0)
 
 
 class DeltaRule:
@@ -240,6 +250,9 @@ class DeltaRule:
 
         dt, f32 = _io_tensor_dtype(io), torch.float32
         state = (num_seqs, num_v_heads, d_v, d_k)
+        self.dtypes = dt, f32, torch.int32
+        self.shapes = ((total_tokens, num_qk_heads, d_k), (total_tokens, num_v_heads, d_v),
+                       (total_tokens, num_v_heads), (num_seqs + 1,), state)
         if backward:
             self.dq, self.dk = tensor(num_qk_heads, d_k, dt), tensor(num_qk_heads, d_k, dt)
             self.dv = tensor(num_v_heads, d_v, dt)
@@ -249,15 +262,20 @@ class DeltaRule:
             self.o = tensor(num_v_heads, d_v, dt)
             self.final_state = torch.empty(state, dtype=f32, device=device)
 
-    def _set_strides(self, q, k, v):
-        self.cfg.q_stride, self.cfg.k_stride = _token_stride(q), _token_stride(k)
-        self.cfg.v_stride = _token_stride(v)
+    def _set(self, q, k, v, log_alpha, beta, seq_offsets, initial_state):
+        dt, f32, i32 = self.dtypes
+        qk, values, gates, bounds, state = self.shapes
+        _expect((q, "q", qk, dt), (k, "k", qk, dt), (v, "v", values, dt),
+                (log_alpha, "log_alpha", gates, f32), (beta, "beta", gates, f32),
+                (seq_offsets, "seq_offsets", bounds, i32),
+                (initial_state, "initial_state", state, f32))
+        _set_strides(self.cfg, q, k, v)
 
     def forward(self, q, k, v, log_alpha, beta, seq_offsets=None, initial_state=None):
         """(o, final_state)"""
         if self.is_backward:
             raise ValueError("this object holds the backward call's tensors")
-        self._set_strides(q, k, v)
+        self._set(q, k, v, log_alpha, beta, seq_offsets, initial_state)
         ab.onela_delta_rule_forward(self.cfg, seq_offsets, q, k, v, log_alpha, beta,
                                     initial_state, self.o, self.final_state, self.workspace,
                                     self.ws_bytes, self.stream)
@@ -268,7 +286,9 @@ class DeltaRule:
         """(dq, dk, dv, dlog_alpha, dbeta, d_initial_state or None without one)"""
         if not self.is_backward:
             raise ValueError("this object holds the forward call's tensors")
-        self._set_strides(q, k, v)
+        self._set(q, k, v, log_alpha, beta, seq_offsets, initial_state)
+        _expect((d_o, "d_o", self.shapes[1], self.dtypes[0]),
+                (d_final_state, "d_final_state", self.shapes[4], self.dtypes[1]))
         ds = None if initial_state is None else self.d_initial_state
         ab.onela_delta_rule_backward(self.cfg, seq_offsets, q, k, v, log_alpha, beta,
                                      initial_state, d_o, d_final_state, self.dq, self.dk,
@@ -288,13 +308,34 @@ class DeltaRuleStep:
         self.cfg = ab.make_delta_config(num_seqs, total_tokens, num_qk_heads, num_v_heads, d_k,
                                         d_v, io, scale)
         self.num_slots, self.stream = num_slots, stream
-        self.o = torch.empty((total_tokens, num_v_heads, d_v), dtype=_io_tensor_dtype(io),
-                             device=device)
+        self.pool = num_slots, num_v_heads, d_v, d_k
+        dt = _io_tensor_dtype(io)
+        self.dtypes = dt, torch.float32, torch.int32
+        self.shapes = ((total_tokens, num_qk_heads, d_k), (total_tokens, num_v_heads, d_v),
+                       (total_tokens, num_v_heads), (num_seqs + 1,), (num_seqs,))
+        self.o = torch.empty((total_tokens, num_v_heads, d_v), dtype=dt, device=device)
 
     def step(self, pool, slots, q, k, v, log_alpha, beta, seq_offsets=None):
         """o; the pool's states move on in place."""
-        self.cfg.q_stride, self.cfg.k_stride = _token_stride(q), _token_stride(k)
-        self.cfg.v_stride = _token_stride(v)
+        dt, f32, i32 = self.dtypes
+        qk, values, gates, bounds, seqs = self.shapes
+        try:  # (in one expression: these checks are a seventh of a single token's call)
+            fits = (q.dtype is dt and q.shape == qk and k.dtype is dt and k.shape == qk and
+                    v.dtype is dt and v.shape == values and log_alpha.dtype is f32 and
+                    log_alpha.shape == gates and beta.dtype is f32 and beta.shape == gates and
+                    pool.dtype is f32 and pool.shape == self.pool and
+                    (slots is None or slots.dtype is i32 and slots.shape == seqs) and
+                    (seq_offsets is None or seq_offsets.dtype is i32 and
+                     seq_offsets.shape == bounds))
+        except AttributeError:
+            fits = False
+        if not fits:
+            _expect((q, "q", qk, dt), (k, "k", qk, dt), (v, "v", values, dt),
+                    (log_alpha, "log_alpha", gates, f32), (beta, "beta", gates, f32),
+                    (seq_offsets, "seq_offsets", bounds, i32), (slots, "slots", seqs, i32))
+            if not isinstance(pool, int) and pool is not None:  # (more slots do no harm)
+                _expect((pool, "pool", (max(self.num_slots, *pool.shape[:1]), *self.pool[1:]), f32))
+        _set_strides(self.cfg, q, k, v)
         ab.onela_delta_rule_step(self.cfg, seq_offsets, q, k, v, log_alpha, beta, pool,
                                  self.num_slots, slots, self.o, self.stream)
         return self.o
@@ -317,6 +358,10 @@ class QkNormRope:
             raise ab.OnelaError(ab.ONELA_EINVAL, "onela_qk_norm_rope_workspace_bytes")
         self.stream = stream
         self.is_backward = backward
+        self.dtypes = _io_tensor_dtype(io), torch.float32, torch.int32
+        self.rotary_dim = rotary_dim
+        self.shapes = ((num_tokens, num_q_heads, head_dim), (num_tokens, num_k_heads, head_dim),
+                       (head_dim,), (num_tokens,))
 
         def like(heads):
             return torch.empty((num_tokens, heads, head_dim), dtype=_io_tensor_dtype(io),
@@ -327,17 +372,34 @@ class QkNormRope:
             self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
             self.dw = torch.empty((2, head_dim), dtype=torch.float32, device=device)
 
-    def _set(self, q, k, cos_sin):
-        self.cfg.q_stride = _token_stride(q)
-        self.cfg.k_stride = 0 if k is None else _token_stride(k)
+    def _set(self, q, k, q_weight, k_weight, positions, cos_sin):
+        dt, f32, i32 = self.dtypes
+        queries, keys, width, tokens = self.shapes
+        try:  # (in one expression, as the step's)
+            fits = (q.dtype is dt and q.shape == queries and
+                    (k is None or k.dtype is dt and k.shape == keys) and
+                    (q_weight is None or q_weight.dtype is f32 and q_weight.shape == width) and
+                    (k_weight is None or k_weight.dtype is f32 and k_weight.shape == width) and
+                    (positions is None or positions.dtype is i32 and positions.shape == tokens))
+        except AttributeError:
+            fits = False
+        if not fits:
+            _expect((q, "q", queries, dt), (k, "k", keys, dt), (q_weight, "q_weight", width, f32),
+                    (k_weight, "k_weight", width, f32), (positions, "positions", tokens, i32))
+        self.cfg.q_stride = 0 if q.is_contiguous() else q.stride(0)
+        self.cfg.k_stride = 0 if k is None or k.is_contiguous() else k.stride(0)
         if cos_sin is not None:
-            self.cfg.table_rows = cos_sin.shape[0]
+            table = cos_sin.shape
+            if self.rotary_dim and (cos_sin.dtype is not f32 or table[1:] != (self.rotary_dim,)):
+                raise ValueError(f"cos_sin must be {f32} [rows, {self.rotary_dim}], not "
+                                 f"{cos_sin.dtype} {list(table)}")
+            self.cfg.table_rows = table[0]
 
     def forward(self, q, k, q_weight=None, k_weight=None, positions=None, cos_sin=None):
         """(q, k) normed and turned"""
         if self.is_backward:
             raise ValueError("this object holds the backward call's tensors")
-        self._set(q, k, cos_sin)
+        self._set(q, k, q_weight, k_weight, positions, cos_sin)
         ab.onela_qk_norm_rope(self.cfg, q, k, q_weight, k_weight, positions, cos_sin, self.q,
                               self.k, self.stream)
         return self.q, self.k
@@ -347,7 +409,9 @@ class QkNormRope:
         """(dq, dk, dq_weight, dk_weight; None for a weight that is not given)"""
         if not self.is_backward:
             raise ValueError("this object holds the forward call's tensors")
-        self._set(q, k, cos_sin)
+        self._set(q, k, q_weight, k_weight, positions, cos_sin)
+        _expect((d_q_out, "d_q_out", self.shapes[0], self.dtypes[0]),
+                (d_k_out, "d_k_out", self.shapes[1], self.dtypes[0]))
         dwq = None if q_weight is None else self.dw[0]
         dwk = None if k_weight is None else self.dw[1]
         ab.onela_qk_norm_rope_backward(self.cfg, q, k, q_weight, k_weight, positions, cos_sin,
