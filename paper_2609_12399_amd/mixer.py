@@ -25,6 +25,27 @@ def _io(x) -> str:
     return {torch.bfloat16: "bf16", torch.float32: "f32"}[x.dtype]
 
 
+class _Once(torch.autograd.Function):
+    """A gradient that cannot be differentiated itself."""
+
+    @staticmethod
+    def forward(ctx, g):
+        return g.view_as(g)
+
+    @staticmethod
+    def backward(ctx, d):
+        raise RuntimeError("the gradients of the delta rule and of the norm are differentiable once")
+
+
+def _once(grads):
+    """The results of a backward pass: where it runs to be differentiated (create_graph), ones that
+    refuse it.  (torch's own mark for this lets them pass as constants when the gradients that
+    come in are some.)"""
+    if not torch.is_grad_enabled():
+        return grads
+    return tuple(None if g is None else _Once.apply(g.detach().requires_grad_()) for g in grads)
+
+
 class QkNormRopeFunction(torch.autograd.Function):
     """q, k [tokens][heads][D], weights fp32 [D] or None -> both normed and turned."""
 
@@ -42,7 +63,7 @@ class QkNormRopeFunction(torch.autograd.Function):
                                backward=True, **ctx.args)
         grads = op.backward(q, k, d_q.contiguous(), d_k.contiguous(), q_weight, k_weight,
                             positions, cos_sin)
-        return (*grads, None, None, None, None, None)
+        return (*_once(grads), None, None, None, None, None)
 
 
 class DeltaRuleFunction(torch.autograd.Function):
@@ -60,8 +81,9 @@ class DeltaRuleFunction(torch.autograd.Function):
     def backward(ctx, d_o, d_state):
         q, k, v, log_alpha, beta, seq_offsets, initial_state = ctx.saved_tensors
         op = runner.DeltaRule(*ctx.sizes, scale=ctx.scale, backward=True, device=q.device)
-        dq, dk, dv, dla, db, ds = op.backward(q, k, v, log_alpha, beta, d_o.contiguous(),
-                                              seq_offsets, initial_state, d_state.contiguous())
+        dq, dk, dv, dla, db, ds = _once(op.backward(
+            q, k, v, log_alpha, beta, d_o.contiguous(), seq_offsets, initial_state,
+            d_state.contiguous()))
         return dq, dk, dv, dla, db, None, ds, None, None
 
 

@@ -111,3 +111,15 @@ def test_norm_refuses(entries, name, shape, dtype):
     alone.forward(norm_args()["q"], None)
     with pytest.raises(ValueError, match="k"):
         alone.forward(norm_args()["q"], norm_args()["k"])
+
+
+def test_second_derivatives_are_refused():
+    """The functions' backward passes are not differentiable themselves: a penalty on their
+    gradients raises, and does not count as a constant."""
+    q, k = (torch.randn(T, HK, DK, requires_grad=True) for _ in range(2))
+    v, la, b = (torch.randn(*s, requires_grad=True) for s in ((T, HV, DV), (T, HV), (T, HV)))
+    for y in (mixer.DeltaRuleFunction.apply(q, k, v, la, b, None, None, 2, 1.0)[0],
+              mixer.QkNormRopeFunction.apply(q, k, None, None, None, None, "l2", 0, 1e-6)[0]):
+        dq, = torch.autograd.grad(y.sum(), q, create_graph=True)
+        with pytest.raises(RuntimeError, match="once"):
+            (dq.square().sum() + q.sum()).backward()
