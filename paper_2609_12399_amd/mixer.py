@@ -125,9 +125,10 @@ class DeltaMixer:
         v = rows[:, 2 * qk:].unflatten(1, (self.HV, self.dv))
         q, k = QkNormRopeFunction.apply(q, k, None, None, positions, self.cos_sin, "l2",
                                         self.rotary_dim, 1e-6)
-        gates = x.float() @ self.w_gates
-        log_alpha = -torch.nn.functional.softplus(gates[:, :self.HV] - 3.0)
-        return q, k, v, log_alpha, torch.sigmoid(gates[:, self.HV:])
+        with torch.autocast(x.device.type, enabled=False):  # (the gates are fp32 throughout)
+            gates = x.float() @ self.w_gates
+            log_alpha = -torch.nn.functional.softplus(gates[:, :self.HV] - 3.0)
+            return q, k, v, log_alpha, torch.sigmoid(gates[:, self.HV:])
 
     def __call__(self, x, seq_offsets, positions=None, initial_state=None):
         """Outputs [tokens][width] and states of packed sequences; differentiable."""
@@ -145,7 +146,7 @@ class DeltaMixer:
         """One token for each row of x on the states slots of the pool, in place."""
         q, k, v, la, b = self._inputs(x, positions)
         op = runner.DeltaRuleStep(x.shape[0], x.shape[0], self.HK, self.HV, self.dk, self.dv,
-                                  self.io, pool.shape[0], device=self.device)
+                                  _io(q), pool.shape[0], device=self.device)
         o = op.step(pool, slots, q, k, v, la.contiguous(), b.contiguous())
         return o.flatten(1) @ self.w_out
 
@@ -155,7 +156,7 @@ class DeltaMixer:
         goes through :meth:`beam_outputs`."""
         R, W = x.shape[:2]
         q, k, v, la, b = self._inputs(x.flatten(0, 1), positions)
-        q, k, v = (t.contiguous().unflatten(0, (R, W)) for t in (q, k, v))
+        q, k, v = (t.to(self.w_qkv.dtype).contiguous().unflatten(0, (R, W)) for t in (q, k, v))
         alpha = torch.exp(la).contiguous().unflatten(0, (R, W))
         return runner.DeviceStep(q, k, v, alpha, b.contiguous().unflatten(0, (R, W)), parents, W)
 

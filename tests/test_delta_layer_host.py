@@ -123,3 +123,24 @@ def test_second_derivatives_are_refused():
         dq, = torch.autograd.grad(y.sum(), q, create_graph=True)
         with pytest.raises(RuntimeError, match="once"):
             (dq.square().sum() + q.sum()).backward()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_layer_under_autocast(entries, io):
+    """torch.autocast changes the types of the layer's products: the gates stay in 32 bits, and the
+    operators take queries, keys and values as they come."""
+    layer = mixer.DeltaMixer(16, HK, HV, DK, DV, io, rotary_dim=16, max_positions=9, device="cpu")
+    x = torch.randn(T, 16).to(layer.w_qkv.dtype)
+    off, pos = torch.tensor([0, 2, T], dtype=I32), torch.arange(T, dtype=I32)
+    with torch.autocast("cpu", dtype=BF):
+        _, _, _, la, b = layer._inputs(x, pos)
+        assert la.dtype is F32 and b.dtype is F32
+        gates = x.float().double() @ layer.w_gates.double()
+        assert (b - torch.sigmoid(gates[:, HV:])).abs().max() < 1e-5
+        y, state = layer(x, off, pos)
+        layer.step(x[:2], torch.zeros(3, *STATE[1:]), torch.zeros(2, dtype=I32), pos[:2])
+        beams = layer.beam_step_inputs(x[None], positions=pos)
+        assert {t.dtype for t in (beams.q, beams.k, beams.v)} == {layer.w_qkv.dtype}
+        assert beams.alpha.dtype is F32 and beams.beta.dtype is F32
+    assert entries == ["onela_qk_norm_rope", "onela_qk_norm_rope", "onela_delta_rule_forward",
+                       "onela_qk_norm_rope", "onela_delta_rule_step", "onela_qk_norm_rope"]
