@@ -118,6 +118,8 @@ class DeltaMixer:
 
     def _inputs(self, x, positions):
         """q, k (normed, turned), v (a view of the projection), log(alpha), beta of tokens x."""
+        if self.rotary_dim and positions is None:
+            raise ValueError("a layer that rotates needs the tokens' positions")
         n, qk = x.shape[0], self.HK * self.dk
         rows = x @ self.w_qkv
         q = rows[:, :qk].unflatten(1, (self.HK, self.dk))
@@ -131,7 +133,11 @@ class DeltaMixer:
             return q, k, v, log_alpha, torch.sigmoid(gates[:, self.HV:])
 
     def __call__(self, x, seq_offsets, positions=None, initial_state=None):
-        """Outputs [tokens][width] and states of packed sequences; differentiable."""
+        """Outputs [tokens][width] and states of packed sequences; differentiable.  Without
+        positions every sequence's tokens count from 0."""
+        if self.rotary_dim and positions is None:
+            t = torch.arange(x.shape[0], dtype=torch.int32, device=x.device)
+            positions = t - seq_offsets[torch.searchsorted(seq_offsets, t, right=True) - 1]
         q, k, v, la, b = self._inputs(x, positions)
         o, state = DeltaRuleFunction.apply(q, k, v, la.contiguous(), b.contiguous(), seq_offsets,
                                            initial_state, seq_offsets.numel() - 1, 1.0)

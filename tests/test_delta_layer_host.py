@@ -144,3 +144,29 @@ def test_layer_under_autocast(entries, io):
         assert beams.alpha.dtype is F32 and beams.beta.dtype is F32
     assert entries == ["onela_qk_norm_rope", "onela_qk_norm_rope", "onela_delta_rule_forward",
                        "onela_qk_norm_rope", "onela_delta_rule_step", "onela_qk_norm_rope"]
+
+
+def test_layer_positions(monkeypatch):
+    """Without positions a packed sequence's tokens count from its own start; single tokens and
+    beams of a layer that rotates cannot be placed and are refused."""
+    seen = []
+    monkeypatch.setattr(ab, "onela_qk_norm_rope", lambda cfg, q, k, wq, wk, positions, *a, **kw:
+                        seen.append(positions))
+    layer = mixer.DeltaMixer(16, HK, HV, DK, DV, "f32", rotary_dim=16, max_positions=9,
+                             device="cpu")
+    x = torch.randn(T, 16)
+    for off, want in (([0, 2, T], [0, 1, 0, 1, 2, 3]), ([0, 0, 2, 2, T], [0, 1, 0, 1, 2, 3]),
+                      ([0, T], [0, 1, 2, 3, 4, 5])):
+        layer.prompt(x, torch.tensor(off, dtype=I32))
+        assert seen.pop().tolist() == want and not seen
+    pos = torch.tensor([4, 5, 3, 3, 2, 1], dtype=I32)
+    layer.prompt(x, torch.tensor([0, T], dtype=I32), pos)
+    assert seen.pop() is pos
+    with pytest.raises(ValueError, match="positions"):
+        layer.step(x, torch.zeros(T, *STATE[1:]), None)
+    with pytest.raises(ValueError, match="positions"):
+        layer.beam_step_inputs(x[None])
+    plain = mixer.DeltaMixer(16, HK, HV, DK, DV, "f32", device="cpu")
+    plain.step(x, torch.zeros(T, *STATE[1:]), None)
+    plain.prompt(x, torch.tensor([0, T], dtype=I32))
+    assert seen == [None, None]
