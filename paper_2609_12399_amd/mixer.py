@@ -144,8 +144,9 @@ class DeltaMixer:
         return o.flatten(1) @ self.w_out, state
 
     @torch.no_grad()
-    def prompt(self, x, seq_offsets, positions=None):
-        return self(x, seq_offsets, positions)
+    def prompt(self, x, seq_offsets, positions=None, initial_state=None):
+        """As the call, without gradients; from initial_state (another prompt's states) or zeros."""
+        return self(x, seq_offsets, positions, initial_state)
 
     @torch.no_grad()
     def step(self, x, pool, slots, positions=None):

@@ -110,3 +110,19 @@ def test_example_runs(capsys):
     mixer.main()
     out = capsys.readouterr().out
     assert "training: loss" in out and "beams:" in out
+
+
+def test_prompt_goes_on_from_states():
+    """A prompt cut in two, the second part from the first one's states, gives the whole's outputs
+    and states (two bf16 roundings each: products over other numbers of tokens may round the
+    projections the other way)."""
+    layer, lengths, off, pos, x, _ = make("bf16")
+    y, state = layer.prompt(x, off, pos)
+    a, b = 41, 3  # of each sequence's tokens, the first part
+    first = torch.cat([torch.arange(a), 70 + torch.arange(b)]).to(DEV)
+    rest = torch.cat([torch.arange(a, 70), 70 + torch.arange(b, 5)]).to(DEV)
+    at = [torch.tensor(t, dtype=torch.int32, device=DEV) for t in ([0, a, a + b], [0, 70 - a, 75 - a - b])]
+    _, mid = layer.prompt(x[first], at[0], pos[first])
+    z, end = layer.prompt(x[rest], at[1], pos[rest], initial_state=mid)
+    assert float((z.float() - y[rest].float()).abs().max()) <= 2.0 ** -6 * float(y.float().abs().max())
+    assert float((end - state).abs().max()) <= 2.0 ** -6 * float(state.abs().max())
