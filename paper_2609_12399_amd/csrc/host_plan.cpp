@@ -337,7 +337,6 @@ onela_status_t check_norm(const onela_norm_config_t* c) {
   const int64_t q = int64_t(c->num_q_heads) * c->head_dim, k = int64_t(c->num_k_heads) * c->head_dim;
   if (c->q_stride && (c->q_stride < q || c->q_stride % per16)) return ONELA_EINVAL;
   if (c->k_stride && (c->k_stride < k || c->k_stride % per16)) return ONELA_EINVAL;
-  // (a workgroup takes four rows or more)
   if (double(c->num_tokens) * (double(c->num_q_heads) + c->num_k_heads) >= 8589934592.0 ||
       double(c->num_q_heads) + c->num_k_heads >= 1073741824.0)
     return ONELA_EINVAL;

@@ -20,6 +20,9 @@ namespace onela {
 namespace {
 
 constexpr int kNormThreads = 256;
+// A grid has fewer than 2^32 threads: past that the runtime starts what is left of the number
+// in 32 bits, without an error.
+constexpr long kNormLaunch = (1l << 32) / kNormThreads - 1;
 
 template <bool BF16>
 __device__ inline void get8(const void* base, long i, float (&x)[8]) {
@@ -108,10 +111,11 @@ __device__ inline const float* angle_of(const NormParams& p, long t) {
   return pos >= 0 && pos < p.table ? p.cos_sin + long(pos) * p.rot : nullptr;
 }
 
+// Rows from `first` on: one launch takes kNormLaunch workgroups at most.
 template <int G, bool BF16>
-__global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormParams p) {
+__global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormParams p, long first) {
   const int sub = threadIdx.x % G, c0 = 8 * sub;
-  const long r = long(blockIdx.x) * (kNormThreads / G) + threadIdx.x / G;
+  const long r = first + long(blockIdx.x) * (kNormThreads / G) + threadIdx.x / G;
   if (r >= p.rows) return;  // (whole groups)
   const bool in = c0 < p.D;
   const Row row = row_of(p, r);
@@ -243,10 +247,15 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(NormParams p, int q_b
 template <int G, bool BF16>
 hipError_t run(const NormParams& p, bool backward, hipStream_t st) {
   constexpr int RW = kNormThreads / G;
-  const long groups = (p.rows + RW - 1) / RW;
   if (!backward) {
-    norm_rope_kernel<G, BF16><<<unsigned(groups), kNormThreads, 0, st>>>(p);
-    return hipGetLastError();
+    const long groups = (p.rows + RW - 1) / RW;
+    hipError_t e = hipSuccess;
+    for (long g = 0; g < groups && e == hipSuccess; g += kNormLaunch) {
+      const long n = groups - g < kNormLaunch ? groups - g : kNormLaunch;
+      norm_rope_kernel<G, BF16><<<unsigned(n), kNormThreads, 0, st>>>(p, g * RW);
+      e = hipGetLastError();
+    }
+    return e;
   }
   // workgroups for the queries' and the keys' rows, kRows rows per group and turn
   const long T = p.rows / (p.HQ + p.HK), per = RW * kRows;

@@ -156,3 +156,19 @@ def test_many_rows_same_bits_again_and_graph():
         torch.cuda.synchronize()
         for x, y in zip(a, got):
             assert torch.equal(x, y)
+
+
+def test_more_rows_than_one_launch_takes():
+    """Rows past the 2^32 threads that one grid may hold (here 2^26 rows of 64 lanes): every row
+    is written, none twice."""
+    T, D = (1 << 26) + 100, 264
+    q = torch.ones((T, 1, D), dtype=torch.bfloat16, device=DEV)
+    q[-200:] = torch.randn((200, 1, D), device=DEV).bfloat16()
+    q[:5] = q[-5:]
+    op = runner.QkNormRope(T, 1, 0, D, "bf16", norm="rms", eps=0.0, device=DEV)
+    op.q.fill_(float("nan"))
+    out, _ = op.forward(q, None)
+    for part in (slice(0, 5), slice(T - 200, T)):
+        near(out[part], ref.norm(f64(q[part]), None, True, 0.0), "bf16")
+    middle = out[5:-200].view(torch.int16)
+    assert int(middle.min()) == int(middle.max()) == 0x3f80  # 1 in bf16
