@@ -352,7 +352,10 @@ onela_status_t onela_select_beams_noalloc(int32_t num_requests, int32_t prev_wid
  * k_stride and v_stride are the elements between two tokens (0: dense); a
  * token's heads are dense.  All other tensors are dense.  Rows start on 16 bytes.
  * Supported (d_k, d_v) and dtypes: those of onela_config_t.  States are fp32
- * [num_seqs][H_V][d_v][d_k]. */
+ * [num_seqs][H_V][d_v][d_k].  Sizes whose launches would take 2^32 threads or
+ * more are ONELA_EINVAL (256 per 64-token chunk and value head, 2 d_v per
+ * sequence and value head, backward up to 512 per chunk and query/key head, in
+ * steps up to 8 d_v per sequence and value head). */
 typedef struct {
   int32_t num_seqs;      /* N */
   int32_t num_qk_heads;  /* H_K */

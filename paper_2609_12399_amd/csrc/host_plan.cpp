@@ -252,6 +252,19 @@ onela_status_t delta_shape_of(const onela_delta_config_t* c, bool ragged, DeltaS
   return ONELA_OK;
 }
 
+bool delta_grids_fit(const DeltaShape& s, bool backward) {
+  // tables; the chain (segments are cut only where the heads are few); gradients
+  const double tables = double(s.slots) * s.HV * 256, chain = double(s.N) * s.HV * (2 * s.dv);
+  const double grad = double(s.slots) * s.HK * std::min(4 * s.dk, 512);
+  return std::max(std::max(tables, chain), backward ? grad : 0.0) < kGridThreads;
+}
+
+bool delta_step_grid_fits(const DeltaShape& s) {
+  // 64 threads for 16 rows, 8 of 256 columns and 32 of 64
+  const int rows = s.dk == 256 ? 8 : s.dk == 64 ? 32 : 16;
+  return double(s.N) * s.HV * (s.dv / rows) * 64 < kGridThreads;
+}
+
 namespace {
 // Segment slots that sequences of any lengths can need, and their bytes: a state and
 // a transition matrix each.

@@ -122,6 +122,11 @@ struct DeltaShape {
 };
 // The shape of a configuration, or ONELA_EINVAL.  ragged: the lengths come as offsets.
 onela_status_t delta_shape_of(const onela_delta_config_t* cfg, bool ragged, DeltaShape* out);
+// A grid has fewer than 2^32 threads: past that the runtime starts what is left of the number
+// in 32 bits, without an error.
+constexpr double kGridThreads = 4294967296.0;
+bool delta_grids_fit(const DeltaShape& s, bool backward);
+bool delta_step_grid_fits(const DeltaShape& s);
 size_t delta_workspace_bytes(const DeltaShape& s, bool backward);
 // Chunks per segment of the chain and, with more than one segment, the slots (see
 // kernels_delta_scan.hip); 1 << 30 chunks and one slot per sequence without segments.

@@ -426,6 +426,7 @@ onela_status_t delta_inputs(const onela_delta_config_t* cfg, const int32_t* offs
 
 onela_status_t delta_workspace(const onela::DeltaShape& s, bool backward, const void* workspace,
                                size_t bytes) {
+  if (!onela::delta_grids_fit(s, backward)) return ONELA_EINVAL;
   const size_t need = onela::delta_workspace_bytes(s, backward);
   if (need > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0))
     return ONELA_EINVAL;
@@ -437,6 +438,7 @@ size_t onela_delta_rule_workspace_bytes(const onela_delta_config_t* cfg, int32_t
   // (any lengths: as many chunk slots as ragged sequences can need, or more)
   onela::DeltaShape s;
   if (onela::delta_shape_of(cfg, true, &s) != ONELA_OK) return 0;
+  if (!onela::delta_grids_fit(s, backward != 0)) return 0;
   return onela::delta_workspace_bytes(s, backward != 0);
 }
 
@@ -504,6 +506,7 @@ onela_status_t onela_delta_rule_step(const onela_delta_config_t* cfg,
   onela::DeltaParams p;
   const onela_status_t rc = delta_inputs(cfg, seq_offsets, q, k, v, log_alpha, beta, &s, &p);
   if (rc != ONELA_OK) return rc;
+  if (!onela::delta_step_grid_fits(s)) return ONELA_EINVAL;
   if (num_slots < 1 || !state || !aligned16(state) || !aligned4(slots)) return ONELA_EINVAL;
   if ((s.total > 0 && !o) || !aligned16(o)) return ONELA_EINVAL;
   if (!slots && num_slots < s.N) return ONELA_ECAPACITY;

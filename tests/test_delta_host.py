@@ -163,3 +163,27 @@ def test_binding_refuses_tensors_that_are_not_there():
         ab.onela_qk_norm_rope(norm(q_stride=256), x, x, None, None, None, None, x, x, 0)
     with pytest.raises(ValueError):
         ab.onela_delta_rule_forward(delta(), None, None, A, A, A, A, None, A, A, A, 0, 0)
+
+
+# Grids of 2^32 threads and more, which the runtime would start with fewer and without an error:
+# many chunks of small heads (256 threads a chunk and head), many short sequences of wide ones
+# (1024 threads a sequence and head of 512), gradients (512 a chunk and query/key head of 128).
+@pytest.mark.parametrize("big", [
+    dict(num_seqs=1, total_tokens=(1 << 18) * 64, num_qk_heads=64, num_v_heads=64, d_k=32, d_v=32),
+    dict(num_seqs=1 << 16, total_tokens=1 << 16, num_qk_heads=1, num_v_heads=64, d_k=128, d_v=512),
+    dict(num_seqs=1 << 17, total_tokens=1 << 17, num_qk_heads=64, num_v_heads=64),
+], ids=str)
+def test_more_threads_than_a_grid_holds(lib, big):
+    cfg = delta(**big)
+    assert backward(lib, cfg, off=A) == ab.ONELA_EINVAL
+    assert ab.onela_delta_rule_workspace_bytes(cfg, True) == 0
+    if cfg.num_seqs == 1 << 17:
+        assert ab.onela_delta_rule_workspace_bytes(cfg, False) > 0
+    else:
+        assert forward(lib, cfg, off=A) == ab.ONELA_EINVAL
+        assert ab.onela_delta_rule_workspace_bytes(cfg, False) == 0
+
+
+def test_step_with_more_threads_than_a_grid_holds(lib):
+    cfg = delta(num_seqs=1 << 18, total_tokens=1 << 18, num_qk_heads=1, num_v_heads=32)
+    assert step(lib, cfg, num=1 << 18) == ab.ONELA_EINVAL
