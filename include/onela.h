@@ -335,7 +335,10 @@ onela_status_t onela_select_beams_noalloc(int32_t num_requests, int32_t prev_wid
  * the last state is), its gradients (training), and the same token by token on
  * a pool of states (serving without beams).  The decay is given as its logarithm:
  * that is what a model's gate yields, and the gradient by it stays finite
- * where alpha vanishes.
+ * where alpha vanishes.  Where v, d_o or a state is not finite, the chunked
+ * calls give NaN in that value channel for the whole chunk of 64 tokens and all
+ * that follows from it, in no other channel's outputs, states or dv; where q, k,
+ * log_alpha or beta is not, in the chunk's value heads that read it.
  *   q, k         device [total_tokens][H_K][d_k] io dtype
  *   v            device [total_tokens][H_V][d_v] io dtype
  *   log_alpha    device fp32 [total_tokens][H_V]; below -1e5 (-inf among it)
@@ -370,9 +373,11 @@ typedef struct {
 
 /* Bytes of workspace of onela_delta_rule_forward (backward = 0) or
  * onela_delta_rule_backward (backward = 1) for sequences of any lengths with
- * this total: per 64-token chunk and value head the state at its entry and the
- * chunk's factors (backward: their adjoints too).  0 for an invalid cfg.  The
- * contents need no preparation and mean nothing afterwards. */
+ * this total: per 64-token chunk the keys and queries as operands and per value
+ * head the chunk's factors, for long sequences the states and transitions of
+ * their segments (backward: the states, adjoints and errors of every chunk too).
+ * 0 for an invalid cfg.  The contents need no preparation and mean nothing
+ * afterwards. */
 size_t onela_delta_rule_workspace_bytes(const onela_delta_config_t* cfg, int32_t backward);
 
 /* Outputs and last states, in chunks of 64 tokens on the matrix cores.
