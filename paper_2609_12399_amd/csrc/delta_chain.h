@@ -239,11 +239,10 @@ __device__ __attribute__((always_inline)) inline void triangle(const uint4* F,
   }
 }
 
-// S^T <- S^T diag(g) + A^T x (and + B^T y with TWO): A, B operand tiles in NP parts, x, y in two.
-template <int DK, int NP, bool TWO>
+// S^T <- S^T diag(g) + A^T x: A an operand tile in NP parts, x in two.
+template <int DK, int NP>
 __device__ __attribute__((always_inline)) inline void update_state(
-    ChainState<DK>& s, const float (&g)[2], const Swz<DK>* A, const uint4 (&x)[2][2][2], const Swz<DK>* B,
-    const uint4 (&y)[2][2][2], int tb) {
+    ChainState<DK>& s, const float (&g)[2], const Swz<DK>* A, const uint4 (&x)[2][2][2], int tb) {
   using C = ChainState<DK>;
   constexpr int NG = C::NB < 4 ? C::NB : 4;
 #pragma unroll
@@ -255,21 +254,17 @@ __device__ __attribute__((always_inline)) inline void update_state(
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint4 kt[NG][NP];
-      auto add = [&](const Swz<DK>* T, const uint4 (&z)[2][2][2]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int b = 0; b < NG; ++b)
+      for (int b = 0; b < NG; ++b)
 #pragma unroll
-          for (int i = 0; i < NP; ++i) kt[b][i] = col_frag(T[i], tb, b0 + b, 2 * C::KR * h);
-        for_products<NP, 2>([&](int i, int j) {
+        for (int i = 0; i < NP; ++i) kt[b][i] = col_frag(A[i], tb, b0 + b, 2 * C::KR * h);
+      for_products<NP, 2>([&](int i, int j) {
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int b = 0; b < NG; ++b)
-              s.st[u][b0 + b] = mfma_f16(kt[b][i], z[u][h][j], s.st[u][b0 + b]);
-        });
-      };
-      add(A, x);
-      if constexpr (TWO) add(B, y);
+          for (int b = 0; b < NG; ++b)
+            s.st[u][b0 + b] = mfma_f16(kt[b][i], x[u][h][j], s.st[u][b0 + b]);
+      });
     }
   }
 }

@@ -75,6 +75,36 @@ __device__ inline unsigned pack_bf16x2(float a, float b) {
 __device__ inline float bf16_lo_to_float(unsigned u) { return __uint_as_float(u << 16); }
 __device__ inline float bf16_hi_to_float(unsigned u) { return __uint_as_float(u & 0xffff0000u); }
 
+// 8 neighbouring elements (16-byte aligned) and single ones of a bf16 or fp32 tensor.
+template <bool BF16>
+__device__ inline void load8(const void* base, long i, float (&x)[8]) {
+  if constexpr (BF16) {
+    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + i);
+    const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = bf16_lo_to_float(w[j]);
+      x[2 * j + 1] = bf16_hi_to_float(w[j]);
+    }
+  } else {
+    const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + i);
+    const f32x4 a = q[0], b = q[1];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[j] = a[j];
+      x[4 + j] = b[j];
+    }
+  }
+}
+
+template <bool BF16>
+__device__ inline float load1(const void* base, long i) {
+  if constexpr (BF16)
+    return __uint_as_float(unsigned(static_cast<const uint16_t*>(base)[i]) << 16);
+  else
+    return static_cast<const float*>(base)[i];
+}
+
 // Split 8 floats into bf16 hi and lo vectors: hi = bf16(x), lo = bf16(x - hi).
 __device__ inline void split8(const float* x, uint4& hi, uint4& lo) {
   unsigned h[4], l[4];

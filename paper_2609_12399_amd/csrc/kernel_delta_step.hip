@@ -18,35 +18,6 @@ namespace onela {
 namespace {
 
 template <bool BF16>
-__device__ inline void load8(const void* base, long i, float (&x)[8]) {
-  if constexpr (BF16) {
-    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + i);
-    const unsigned w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = bf16_lo_to_float(w[j]);
-      x[2 * j + 1] = bf16_hi_to_float(w[j]);
-    }
-  } else {
-    const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + i);
-    const f32x4 a = q[0], b = q[1];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[j] = a[j];
-      x[4 + j] = b[j];
-    }
-  }
-}
-
-template <bool BF16>
-__device__ inline float load1(const void* base, long i) {
-  if constexpr (BF16)
-    return __uint_as_float(unsigned(static_cast<const uint16_t*>(base)[i]) << 16);
-  else
-    return static_cast<const float*>(base)[i];
-}
-
-template <bool BF16>
 __device__ inline void store1(void* base, long i, float x) {
   if constexpr (BF16)
     static_cast<uint16_t*>(base)[i] = uint16_t(pack_bf16x2(x, x));

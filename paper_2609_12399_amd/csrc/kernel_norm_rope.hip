@@ -25,28 +25,7 @@ constexpr int kNormThreads = 256;
 constexpr long kNormLaunch = (1l << 32) / kNormThreads - 1;
 
 template <bool BF16>
-__device__ inline void get8(const void* base, long i, float (&x)[8]) {
-  if constexpr (BF16) {
-    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + i);
-    const unsigned w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = bf16_lo_to_float(w[j]);
-      x[2 * j + 1] = bf16_hi_to_float(w[j]);
-    }
-  } else {
-    const f32x4* q = reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + i);
-    const f32x4 a = q[0], b = q[1];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[j] = a[j];
-      x[4 + j] = b[j];
-    }
-  }
-}
-
-template <bool BF16>
-__device__ inline void put8(void* base, long i, const float (&x)[8]) {
+__device__ inline void store8(void* base, long i, const float (&x)[8]) {
   if constexpr (BF16) {
     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + i) =
         make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
@@ -120,7 +99,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormParams p, l
   const bool in = c0 < p.D;
   const Row row = row_of(p, r);
   float x[8] = {};
-  if (in) get8<BF16>(row.x, row.at + c0, x);
+  if (in) load8<BF16>(row.x, row.at + c0, x);
   float s = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) s = fmaf(x[j], x[j], s);
@@ -137,7 +116,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_kernel(NormParams p, l
       for (int j = 0; j < 8; ++j) x[j] = __builtin_nanf("");
     }
   }
-  if (in) put8<BF16>(row.key ? p.ko : p.qo, row.out + c0, x);
+  if (in) store8<BF16>(row.key ? p.ko : p.qo, row.out + c0, x);
 }
 
 // The first workgroups take the queries' rows, the others the keys', in proportion; each
@@ -174,8 +153,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_backward_kernel(NormPa
       here[i] = r < rows;  // (whole groups)
       t[i] = here[i] ? r / H : 0;
       if (here[i] && in) {
-        get8<BF16>(xs, t[i] * stride + (r - t[i] * H) * p.D + c0, x[i]);
-        get8<BF16>(ds, r * p.D + c0, d[i]);
+        load8<BF16>(xs, t[i] * stride + (r - t[i] * H) * p.D + c0, x[i]);
+        load8<BF16>(ds, r * p.D + c0, d[i]);
       }
     }
 #pragma unroll
@@ -206,7 +185,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_rope_backward_kernel(NormPa
         o[j] = rn * (w[j] * d[i][j] - x[i][j] * f);
         dw[j] = fmaf(d[i][j], x[i][j] * rn, dw[j]);
       }
-      if (in) put8<BF16>(os, (r0 + long(blocks) * RW * i) * p.D + c0, o);
+      if (in) store8<BF16>(os, (r0 + long(blocks) * RW * i) * p.D + c0, o);
     }
   }
   if (!p.partial) return;

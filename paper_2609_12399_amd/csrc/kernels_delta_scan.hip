@@ -224,7 +224,7 @@ void delta_forward_kernel(DeltaParams p) {
       load_tp(c + 1);
       load_v(c + 1);
     }
-    update_state<DK, NP, false>(s, g, K, zp, K, zp, tb);
+    update_state<DK, NP>(s, g, K, zp, tb);
   }
   if (SEG && ident)
     store_matrix<DK>(s, reinterpret_cast<SegmentMatrix<DK>*>(p.sega) + su, NW * grp + w, lane);

@@ -10,6 +10,7 @@
 // sums are reduced across the LPR lanes.
 #include <type_traits>
 
+#include "device_common.h"
 #include "internal.h"
 
 namespace onela {
@@ -25,15 +26,6 @@ __device__ inline float4 load4(const void* base, long elem) {
                        __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u));
   } else {
     return *reinterpret_cast<const float4*>(static_cast<const float*>(base) + elem);
-  }
-}
-
-template <bool BF16>
-__device__ inline float load1(const void* base, long elem) {
-  if constexpr (BF16) {
-    return __uint_as_float(unsigned(static_cast<const uint16_t*>(base)[elem]) << 16);
-  } else {
-    return static_cast<const float*>(base)[elem];
   }
 }
 
