@@ -45,8 +45,9 @@ struct ChainState {
   __device__ static float row_scale(float most) {
     return fminf(fmaxf(scale_for(fminf(most, 0x1p126f)), 0x1p-112f), 0x1p100f);
   }
-  // from: the lane's first row (null: zeros), or the rows of the identity
-  __device__ void init(const float* from, bool ident, int row0, int lq) {
+  // from: the lane's first row (null: zeros), or the rows of the identity; keep: where the rows are
+  // stored as they came (or null)
+  __device__ void init(const float* from, float* keep, bool ident, int row0, int lq) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float m = 0.f;
@@ -62,7 +63,10 @@ struct ChainState {
       bound[u] = max_over_rows(m);
       sc[u] = bound[u] > 0.f ? row_scale(bound[u]) : 1.f;
 #pragma unroll
-      for (int b = 0; b < NB; ++b) st[u][b] *= sc[u];
+      for (int b = 0; b < NB; ++b) {
+        if (keep) *reinterpret_cast<f32x4*>(keep + u * DK + 16 * b) = st[u][b];
+        st[u][b] *= sc[u];
+      }
     }
   }
   __device__ void store(float* to) const {
@@ -126,16 +130,6 @@ __device__ inline const float* start_of(const DeltaParams& p, const Segment& sg,
   if (!given) return nullptr;
   if (!SEG && sg.nseg > 1) return kept_start<DK, DV>(p, sg, su);
   return given + (long(sg.n) * p.HV + hv) * (DV * DK);
-}
-// The lane's two rows of a state, as ChainState reads them.
-template <int DK>
-__device__ inline void copy_rows(const float* from, float* to) {
-#pragma unroll
-  for (int u = 0; u < 2; ++u)
-#pragma unroll
-    for (int b = 0; b < DK / 16; ++b)
-      *reinterpret_cast<f32x4*>(to + u * DK + 16 * b) =
-          *reinterpret_cast<const f32x4*>(from + u * DK + 16 * b);
 }
 
 // The transition matrix A of a segment in memory, as operands of A^T S^T: two fp16 parts of

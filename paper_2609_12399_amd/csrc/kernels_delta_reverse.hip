@@ -47,8 +47,8 @@ void delta_reverse_kernel(DeltaParams p) {
   const long rows = long(row0) * DK + 4 * lq;
   {
     const float* from = start_of<DK, DV, SEG>(p, sg, su, hv, p.ds_in);
-    s.init(from ? from + rows : nullptr, ident, row0, lq);
-    if (SEG && from) copy_rows<DK>(from + rows, kept_start<DK, DV>(p, sg, su) + rows);
+    s.init(from ? from + rows : nullptr,
+           SEG && from ? kept_start<DK, DV>(p, sg, su) + rows : nullptr, ident, row0, lq);
   }
   auto image_at = [&](int c) { return ((sq.slot + c) * p.HK + hk) * (kImage / 16); };
   auto load_tp = [&](int c) __attribute__((always_inline)) {

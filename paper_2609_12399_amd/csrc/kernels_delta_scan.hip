@@ -68,8 +68,8 @@ void delta_forward_kernel(DeltaParams p) {
   const long rows = long(row0) * DK + 4 * lq;
   {
     const float* from = start_of<DK, DV, SEG>(p, sg, su, hv, p.s_in);
-    s.init(from ? from + rows : nullptr, ident, row0, lq);
-    if (SEG && from) copy_rows<DK>(from + rows, kept_start<DK, DV>(p, sg, su) + rows);
+    s.init(from ? from + rows : nullptr,
+           SEG && from ? kept_start<DK, DV>(p, sg, su) + rows : nullptr, ident, row0, lq);
   }
   auto load_kq = [&](int c) __attribute__((always_inline)) {
     const long at = ((sq.slot + c) * p.HK + hk) * (kImage / 16);
