@@ -195,10 +195,10 @@ def _rows(x, name: str, stride: int, optional: bool = False):
         return _dev(x, name, optional)
     if not getattr(x, "is_cuda", False):
         raise ValueError(f"{name} must be a GPU tensor")
-    if x.dim() != 3 or (x.numel() and (
-            (x.shape[2] > 1 and x.stride(2) != 1) or
-            (x.shape[1] > 1 and x.stride(1) != x.shape[2]) or
-            (x.shape[0] > 1 and x.stride(0) != stride))):
+    shape, at = x.shape, x.stride()
+    if len(shape) != 3 or (0 not in shape and (
+            (shape[2] > 1 and at[2] != 1) or (shape[1] > 1 and at[1] != shape[2]) or
+            (shape[0] > 1 and at[0] != stride))):
         raise ValueError(f"{name} must be [tokens][heads][width] with {stride} elements "
                          "between tokens and dense heads")
     return x.data_ptr()
@@ -386,7 +386,7 @@ def onela_delta_rule_forward(cfg: onela_delta_config_t, seq_offsets, q, k, v, lo
                              initial_state, o, final_state, workspace=None,
                              workspace_bytes: int = 0, stream=None):
     none = cfg.total_tokens == 0
-    _check(load_library().onela_delta_rule_forward(
+    _check((_lib or load_library()).onela_delta_rule_forward(
         ctypes.byref(cfg), _dev(seq_offsets, "seq_offsets", True),
         _rows(q, "q", cfg.q_stride, none), _rows(k, "k", cfg.k_stride, none),
         _rows(v, "v", cfg.v_stride, none), _dev(log_alpha, "log_alpha", none),
@@ -400,7 +400,7 @@ def onela_delta_rule_backward(cfg: onela_delta_config_t, seq_offsets, q, k, v, l
                               d_initial_state, workspace=None, workspace_bytes: int = 0,
                               stream=None):
     none = cfg.total_tokens == 0
-    _check(load_library().onela_delta_rule_backward(
+    _check((_lib or load_library()).onela_delta_rule_backward(
         ctypes.byref(cfg), _dev(seq_offsets, "seq_offsets", True),
         _rows(q, "q", cfg.q_stride, none), _rows(k, "k", cfg.k_stride, none),
         _rows(v, "v", cfg.v_stride, none), _dev(log_alpha, "log_alpha", none),
@@ -415,7 +415,7 @@ def onela_delta_rule_backward(cfg: onela_delta_config_t, seq_offsets, q, k, v, l
 def onela_delta_rule_step(cfg: onela_delta_config_t, seq_offsets, q, k, v, log_alpha, beta,
                           state, num_slots: int, slots, o, stream=None):
     none = cfg.total_tokens == 0
-    _check(load_library().onela_delta_rule_step(
+    _check((_lib or load_library()).onela_delta_rule_step(
         ctypes.byref(cfg), _dev(seq_offsets, "seq_offsets", True),
         _rows(q, "q", cfg.q_stride, none), _rows(k, "k", cfg.k_stride, none),
         _rows(v, "v", cfg.v_stride, none), _dev(log_alpha, "log_alpha", none),
@@ -430,7 +430,7 @@ def onela_qk_norm_rope_workspace_bytes(cfg: onela_norm_config_t) -> int:
 def onela_qk_norm_rope(cfg: onela_norm_config_t, q, k, q_weight, k_weight, positions, cos_sin,
                        q_out, k_out, stream=None):
     none = cfg.num_tokens == 0
-    _check(load_library().onela_qk_norm_rope(
+    _check((_lib or load_library()).onela_qk_norm_rope(
         ctypes.byref(cfg), _rows(q, "q", cfg.q_stride, none),
         _rows(k, "k", cfg.k_stride, none or cfg.num_k_heads == 0),
         _dev(q_weight, "q_weight", True), _dev(k_weight, "k_weight", True),
@@ -445,7 +445,7 @@ def onela_qk_norm_rope_backward(cfg: onela_norm_config_t, q, k, q_weight, k_weig
                                 stream=None):
     none = cfg.num_tokens == 0
     nokey = none or cfg.num_k_heads == 0
-    _check(load_library().onela_qk_norm_rope_backward(
+    _check((_lib or load_library()).onela_qk_norm_rope_backward(
         ctypes.byref(cfg), _rows(q, "q", cfg.q_stride, none), _rows(k, "k", cfg.k_stride, nokey),
         _dev(q_weight, "q_weight", True), _dev(k_weight, "k_weight", True),
         _dev(positions, "positions", True), _dev(cos_sin, "cos_sin", True),

@@ -217,9 +217,8 @@ def _expect(*tensors):
 
 def _set_strides(cfg, q, k, v):
     """Elements between the tokens of [tokens][heads][width] views (0: dense)."""
-    cfg.q_stride = 0 if q.is_contiguous() else q.stride(0)
-    cfg.k_stride = 0 if k.is_contiguous() else k.stride(0)
-    cfg.v_stride = 0 if v.is_contiguous() else v.stride(0)
+    strides = [0 if x.is_contiguous() else x.stride(0) for x in (q, k, v)]
+    cfg.q_stride, cfg.k_stride, cfg.v_stride = strides
 
 
 class DeltaRule:
@@ -308,6 +307,7 @@ class DeltaRuleStep:
         self.cfg = ab.make_delta_config(num_seqs, total_tokens, num_qk_heads, num_v_heads, d_k,
                                         d_v, io, scale)
         self.num_slots, self.stream = num_slots, stream
+        self.dense = True  # the configuration's strides are those of dense tensors
         self.pool = num_slots, num_v_heads, d_v, d_k
         dt = _io_tensor_dtype(io)
         self.dtypes = dt, torch.float32, torch.int32
@@ -335,7 +335,10 @@ class DeltaRuleStep:
                     (seq_offsets, "seq_offsets", bounds, i32), (slots, "slots", seqs, i32))
             if not isinstance(pool, int) and pool is not None:  # (more slots do no harm)
                 _expect((pool, "pool", (max(self.num_slots, *pool.shape[:1]), *self.pool[1:]), f32))
-        _set_strides(self.cfg, q, k, v)
+        dense = q.is_contiguous() and k.is_contiguous() and v.is_contiguous()
+        if not (dense and self.dense):
+            _set_strides(self.cfg, q, k, v)
+            self.dense = dense
         ab.onela_delta_rule_step(self.cfg, seq_offsets, q, k, v, log_alpha, beta, pool,
                                  self.num_slots, slots, self.o, self.stream)
         return self.o
