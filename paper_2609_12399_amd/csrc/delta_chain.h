@@ -106,7 +106,7 @@ struct ChainState {
   __device__ float make_room(int u, float g, float most) {
     bound[u] = fmaf(g, bound[u], 0x1p9f * most);
     const float at = bound[u] * sc[u], fit = fminf(row_scale(bound[u]), sc[u] * 0x1p100f);
-    const bool off = bound[u] > 0.f & !(at <= 32768.f & at >= 4096.f);
+    const bool off = (bound[u] > 0.f) & !((at <= 32768.f) & (at >= 4096.f));  // (no branch)
     const float to = off ? fit : sc[u];
     g *= to * inverse_pow2(sc[u]);
     sc[u] = to;

@@ -295,6 +295,10 @@ DeltaSegments delta_segments(const DeltaShape& s, bool ragged) {
   // 16 (taken), 120 / 377 in 22; 8 x 1024 x 16 heads 122 / 494 in one (taken), 138 / 528 in
   // two; 1 x 4096 x 8 heads of 256 514 / 1540 in one, 183 / 632 in 8 (taken), 200 / 663 in
   // 16; 1 x 2048 x 4 heads of 64 123 / 273 in one, 41 / 97 in 16 (taken).
+  // Ragged lengths are on the device, so the choice goes by their mean: sequences of some
+  // 1000 tokens (0 to 2000) x 32 heads 359 in one, 401 to 624 cut.  One long sequence among short
+  // ones is therefore a single chain (8192 tokens x 16 heads 660 / 1611 beside 15 of one token, 193
+  // / 612 alone, where it is cut): a caller who has such batches calls for the long one by itself.
   const long full = s.dk >= 256 ? 7300 : s.dk == 128 ? 4700 : 3300;
   const long bare = s.dk >= 256 ? 4500 : s.dk == 128 ? 2800 : 2000;
   const long chain = s.dk >= 256 ? 3600 : s.dk == 128 ? 1700 : 900, more = 12000;

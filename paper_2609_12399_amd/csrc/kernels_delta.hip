@@ -35,9 +35,14 @@
 //
 // Precision.  States, e, T, decays and sums are fp32.  Every product runs on
 // v_mfma_f32_16x16x32_f16 with its fp32 operands as the sum of two fp16 parts under a
-// power-of-two scale (22 bits of a row's or tile's largest element, products of two low
+// power-of-two scale (22 bits of the largest element that shares the scale, products of two low
 // parts left out; delta_tiles.h) and bf16 tensors as one part, in which they are exact
-// (NP = 1); fp32 tensors are two parts too (NP = 2).  With three bf16 parts, which are exact,
+// (NP = 1); fp32 tensors are two parts too (NP = 2).  What shares a scale: in the chains a row of
+// a state, or a chunk's tokens in one channel of X, e, dO and dV, so that every value channel is
+// right to some 3e-7 of its own largest value (1e-5 beside 1 too; 32768 tokens without decay
+// too); keys and queries of a chunk and head (fp32 ones: 2^-27 of their largest element), T, and
+// in the gradients a chunk's S, dS, e, dV and dO of a head (2^-38 of each one's largest).  With
+// three bf16 parts, which are exact,
 // the same chain took 1.4 times as long (16 x 1000 tokens x 32 heads of 128) for an error of
 // 1e-7 in place of 1.5e-7 of the state's norm.  Decays are exp2 of differences of
 // in-chunk sums of log2(alpha) in 64 bits (a float pair where they are stored), so that a

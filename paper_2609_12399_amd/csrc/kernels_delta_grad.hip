@@ -59,7 +59,8 @@ __device__ inline Lane unseen(int lane) {
 // The values' columns come 32 at a time, e, dV and dO through LDS (the next ones
 // requested a block ahead), the states' rows straight into operands.
 //   Bound: latency of its phases, one workgroup per compute unit (256 registers, 86 KB of LDS
-// at d_k = 128).  16 x 1024 tokens x 32 heads of 128 take 0.82 ms (2.5 TB/s; matrix
+// at d_k = 128).  The registers do not hold all of it: the compiler spills 10 at d_k = 128 (fp32 19),
+// 175 at 256.  16 x 1024 tokens x 32 heads of 128 take 0.82 ms (2.5 TB/s; matrix
 // cores 11% busy, vector units 31%); per chunk and head the four column blocks are 13 us, near
 // the rate at which their states can arrive, and the products of tokens with tokens, the
 // rows' sums and the last products with Q and K another 13, no part above 2.  Writing L and

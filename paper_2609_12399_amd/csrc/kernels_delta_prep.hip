@@ -98,8 +98,8 @@ struct PrepLds {
 // the diagonal block of its block column, T_ij = -T_ii sum_k M_ik T_kj, in fp32 matrix
 // instructions with T_kj in the accumulator layout as the next operand.
 //   Bound: HBM for many chunks, mostly what it leaves for the chain: 8192 chunks and value heads
-// of 128 (two to a key head) take 108 us, 4.6 TB/s; for few the latency of the inverse.  Vector
-// units 62% busy at four workgroups per compute unit, to which the LDS (36 KB up to d_k
+// of 128 (two to a key head) take 106 us, 4.7 TB/s; for few the latency of the inverse.  Vector
+// units 57% busy at four workgroups per compute unit, to which the LDS (36 KB up to d_k
 // = 128) and the registers are held.  With decays from 64-bit differences behind branches 7%
 // more, with operands whose pieces no one read fetches 3%.
 template <int DK, int NP, bool BWD>

@@ -13,7 +13,7 @@ namespace {
 // it leaves dV (as a tensor and in fp32 for the gradients) and the adjoint before each
 // update.  SEG: segments, counted from the sequence's end, as there (p.ds_out may be p.ds_in).
 //   Bound: as there, and the stores of the adjoints.  16 x 1024 tokens x 32 heads of 128 take
-// 306 us (3.1 TB/s written; 318 with a state's rows stored 64 bytes at a time in place of
+// 302 us (3.1 TB/s written; 318 with a state's rows stored 64 bytes at a time in place of
 // whole lines, 355 with those as non-temporal stores).
 template <int DK, int DV, int NP, bool SEG>
 __global__ __launch_bounds__(64 * kChainWaves<DV>, DK >= 256 || NP == 2 ? 1 : 2)

@@ -31,9 +31,12 @@ enum { kOutputs, kSegment, kSave };
 // else, and the last launch reads them there.
 //
 // Bound: vector and matrix instructions (about 4 and 16 cycles each) take turns.  16 x 1024
-// tokens x 32 heads of 128 (512 workgroups of 16 chunks) with outputs 170 us, 836 TFLOP/s of
-// fp16 products: matrix cores 27 to 31% busy, vector units 28 to 33%, waves waiting 24%;
-// kSave 244 us (3.3 TB/s written), kSegment 36 us for 16 segments of 4096 tokens x 16 heads.
+// tokens x 32 heads of 128 (512 workgroups of 16 chunks) with outputs 173 us, 818 TFLOP/s of
+// fp16 products: matrix cores 36% busy, vector units 43%, waves waiting 22%;
+// kSave 244 us (3.3 TB/s written), kSegment 37 us for 16 segments of 4096 tokens x 16 heads.
+// (Scales per row and measured updates, with two rows to a scale and a bound instead: 170 us, and
+// small channels beside large ones lost.)  The outputs go before the update's values, whose
+// largest is waited for while the stores leave: 16 segments 31.6 us, the other way round 33.6.
 // Barriers that leave the stores in flight, operand reads a step ahead and one wave per SIMD
 // with 512 registers were all slower.
 template <int DK, int DV, int NP, int KIND>
