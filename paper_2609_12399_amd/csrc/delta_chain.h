@@ -102,15 +102,15 @@ struct ChainState {
   }
   // Makes room in row u for an update S <- g S + (64 tokens' keys times values of at most
   // `most`; keys are scaled below 2^3): the factor that the row takes in it, g and the change of
-  // its scale in one (by itself the change could overflow where g undoes it).
+  // its scale in one (by itself the change could overflow where g undoes it: a state of 1e30
+  // forgotten for values of 1e-30).
   __device__ float make_room(int u, float g, float most) {
     bound[u] = fmaf(g, bound[u], 0x1p9f * most);
-    const float at = bound[u] * sc[u], fit = fminf(row_scale(bound[u]), sc[u] * 0x1p100f);
+    const float at = bound[u] * sc[u], fit = row_scale(bound[u]);
     const bool off = (bound[u] > 0.f) & !((at <= 32768.f) & (at >= 4096.f));  // (no branch)
-    const float to = off ? fit : sc[u];
-    g *= to * inverse_pow2(sc[u]);
+    const float to = off ? fit : sc[u], f = (g * to) * inverse_pow2(sc[u]);
     sc[u] = to;
-    return g;
+    return f;
   }
 };
 

@@ -580,3 +580,23 @@ def test_long_sequences_that_forget_nothing():
     check("dv", got[2][:, heads], want[2], 1)
     check("dlog_alpha", got[3][:, heads], want[3], 1, bar=SUMS)
     check("dbeta", got[4][:, heads], want[4], 1)
+
+
+@pytest.mark.parametrize("chunks", [2, 9])
+@pytest.mark.parametrize("big,small", [(1e25, 1e-10), (1e-25, 1e10), (1e30, 1e-30)])
+def test_states_forgotten_for_values_of_another_size(big, small, chunks):
+    """alpha = 0 at the first token after a state of a size far from the values': the rows' scale
+    changes by more than a float holds, and nothing overflows or stays scaled for the old state."""
+    n = 64 * chunks
+    x, g = draw([n], 1, 2, 64, 64, "f32", 26, alpha_mu=-5.0)
+    x[2].mul_(small)
+    x[3][64] = float("-inf")
+    x[2][:64] = 0
+    x[4][:64] = 0
+    s0 = big * torch.randn((1, 2, 64, 64), generator=g).to(DEV)
+    host = [f64(t) for t in x]
+    o, last, _ = ref.forward([n], *host, 1.0, f64(s0))
+    fo, fs = op_of([n], 1, 2, 64, 64, "f32", 1.0).forward(*x, None, s0)
+    check("o before", fo[:64], o[:64], 1)
+    check("o after", fo[64:], o[64:], 1)
+    check("final state", fs, last, 1)
