@@ -78,16 +78,19 @@ struct ChainState {
         *reinterpret_cast<f32x4*>(to + u * DK + 16 * b) = inv * st[u][b];
     }
   }
-  // The same for the gradients (DeltaParams::sws), whole lines at a time: `to` is the state's
-  // column block 0, place 32 times the wave's rows.
+  // The same for the gradients (DeltaParams::sws), whole lines at a time, the rows of the state's
+  // wave w (through a buffer: one register of addresses).
   template <int DV>
-  __device__ void store_tiles(float* to, int lane) const {
-    f32x4* const at = reinterpret_cast<f32x4*>(to) + 4 * (lane & 15) + (lane >> 4);
+  __device__ void store_tiles(float* to, int w, int lane) const {
+    const auto rs = buffer(to, DV * DK * 4);
+    const unsigned at = 64 * (lane & 15) + 16 * (lane >> 4);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const float inv = inverse_pow2(sc[u]);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) at[4 * DV * b + 64 * u] = inv * st[u][b];
+      for (int b = 0; b < NB; ++b)
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, inv * st[u][b]), rs, at,
+                                               2048u * w + 64 * DV * b + 1024 * u, 0);
     }
   }
   // Bounds from the rows themselves.
@@ -108,9 +111,10 @@ struct ChainState {
     bound[u] = fmaf(g, bound[u], 0x1p9f * most);
     const float at = bound[u] * sc[u], fit = row_scale(bound[u]);
     const bool off = (bound[u] > 0.f) & !((at <= 32768.f) & (at >= 4096.f));  // (no branch)
-    const float to = off ? fit : sc[u], f = (g * to) * inverse_pow2(sc[u]);
+    const float to = off ? fit : sc[u];
+    g = ldexpf(g, (__float_as_int(to) - __float_as_int(sc[u])) >> 23);
     sc[u] = to;
-    return f;
+    return g;
   }
 };
 

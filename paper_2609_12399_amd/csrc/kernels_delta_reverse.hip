@@ -93,7 +93,7 @@ void delta_reverse_kernel(DeltaParams p) {
     const float inv[2] = {inverse_pow2(s.sc[0]), inverse_pow2(s.sc[1])};
     const float before = max_bits(s.bound[0], s.bound[1]);
     if constexpr (!SEG)
-      s.template store_tiles<DV>(p.dsws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
+      s.template store_tiles<DV>(p.dsws + cu * (DV * DK), NW * grp + w, lane);
     // Y = K S^T
     f32x4 y[2][4];
 #pragma unroll

@@ -109,7 +109,7 @@ void delta_forward_kernel(DeltaParams p) {
     const float inv[2] = {inverse_pow2(s.sc[0]), inverse_pow2(s.sc[1])};
     const float before = max_bits(s.bound[0], s.bound[1]);
     if constexpr (KIND == kSave)
-      s.template store_tiles<DV>(p.sws + cu * (DV * DK) + 512 * (NW * grp + w), lane);
+      s.template store_tiles<DV>(p.sws + cu * (DV * DK), NW * grp + w, lane);
     // Y = K S^T and Q S^T
     f32x4 y[2][4], o[2][4];
 #pragma unroll
