@@ -79,18 +79,21 @@ struct ChainState {
     }
   }
   // The same for the gradients (DeltaParams::sws), whole lines at a time, the rows of the state's
-  // wave w (through a buffer: one register of addresses).
+  // wave w.  Through buffers, which take one register of addresses, each with a base of its own:
+  // with the base's part in the instruction's scalar offset the compiler leaves no wait
+  // between a 16-byte store and the next write to its data registers, and some of what was
+  // stored was the next write's.
   template <int DV>
   __device__ void store_tiles(float* to, int w, int lane) const {
-    const auto rs = buffer(to, DV * DK * 4);
-    const unsigned at = 64 * (lane & 15) + 16 * (lane >> 4);
+    const unsigned off = 64 * (lane & 15) + 16 * (lane >> 4);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const float inv = inverse_pow2(sc[u]);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, inv * st[u][b]), rs, at,
-                                               2048u * w + 64 * DV * b + 1024 * u, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, inv * st[u][b]),
+                                               buffer(to + 512 * w + 16 * DV * b + 256 * u, 1024),
+                                               off, 0, 0);
     }
   }
   // Bounds from the rows themselves.

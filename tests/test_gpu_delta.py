@@ -600,3 +600,40 @@ def test_states_forgotten_for_values_of_another_size(big, small, chunks):
     check("o before", fo[:64], o[:64], 1)
     check("o after", fo[64:], o[64:], 1)
     check("final state", fs, last, 1)
+
+
+@pytest.mark.parametrize("lengths,HK,HV,dk,dv,io", [
+    ([2] * 9, 8, 16, 128, 256, "bf16"), ([1620, 727, 632, 99, 1979], 16, 16, 64, 64, "f32"),
+    ([343, 2605, 662, 883], 8, 16, 128, 256, "bf16"), ([300] * 24, 8, 16, 128, 128, "bf16"),
+    ([200] * 16, 4, 8, 256, 512, "bf16")])
+def test_same_bits_of_many_workgroups(lengths, HK, HV, dk, dv, io):
+    """Enough workgroups that they share compute units and memory: every call gives the same bits,
+    and single heads the reference's values."""
+    x, g = draw(lengths, HK, HV, dk, dv, io, seed=27)
+    s0 = torch.randn((len(lengths), HV, dv, dk), generator=g).to(DEV)
+    do, off = torch.randn(x[2].shape, generator=g).to(x[2]), offsets(lengths)
+    ops = [op_of(lengths, HK, HV, dk, dv, io, 1.0, b) for b in (False, True)]
+
+    def call():
+        return [t.clone() for t in (*ops[0].forward(*x, off, s0), *ops[1].backward(*x, do, off, s0))]
+
+    first = call()
+    for _ in range(5):
+        for a, b in zip(first, call()):
+            assert torch.equal(a, b)
+    G, n = HV // HK, min(sum(lengths), 400)
+    part, rows = [], 0
+    for m in lengths:
+        if rows + m <= n or not part:
+            part.append(m)
+            rows += m
+    hv = slice(HV - G, HV)  # the last query/key head and its value heads, the first sequences
+    if rows > 700:
+        return
+    host = [f64(t[:rows])[:, s] for t, s in zip(x, (slice(HK - 1, HK),) * 2 + (hv,) * 3)]
+    want = ref.backward(part, *host, 1.0, f64(s0[:len(part), hv]), f64(do[:rows, hv]), None)
+    got = first[2:]
+    check("dq", got[0][:rows, HK - 1:], want[0], 1, io)
+    check("dk", got[1][:rows, HK - 1:], want[1], 1, io)
+    check("dlog_alpha", got[3][:rows, hv], want[3], 1, bar=SUMS)
+    check("dbeta", got[4][:rows, hv], want[4], 1)
