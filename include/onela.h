@@ -480,6 +480,192 @@ onela_status_t onela_qk_norm_rope_backward(const onela_norm_config_t* cfg, const
                                            float* dq_weight, float* dk_weight, void* workspace,
                                            size_t workspace_bytes, void* stream);
 
+/* ---- Short causal convolution --------------------------------------------
+ * What a layer's projections pass before the norm and the delta rule: every channel by
+ * itself, over packed sequences,
+ *   y_t = act(bias + sum_j weight[j] x_{t - taps + 1 + j}),   0 <= j < taps,
+ * where the taps - 1 inputs before a sequence are its state (0 without one), and the state
+ * after it is its last taps - 1 inputs, older ones from the state before among them.
+ *   x            device [total_tokens][channels] io dtype, x_stride elements between
+ *                tokens (0: dense; a projection's output may be wider), rows on 16 bytes
+ *   weight       device fp32 [channels][taps];  bias  device fp32 [channels], or NULL (0)
+ *   seq_offsets  as for the delta rule (NULL: total_tokens / num_seqs tokens each).
+ *                Tokens behind the last sequence are not read, and their rows of the
+ *                outputs are left as they were
+ *   states       device [num_seqs][taps - 1][channels] io dtype, the oldest input first
+ * channels: a multiple of 8; taps 2, 3 or 4.  Sums and gradients of the weights are fp32,
+ * in a fixed order; one rounding at each store. */
+typedef enum { ONELA_ACT_NONE = 0, ONELA_ACT_SILU = 1, ONELA_ACT_SIGMOID = 2 } onela_act_t;
+typedef struct {
+  int32_t num_seqs;
+  int32_t channels;
+  int32_t taps;
+  int32_t io_dtype;      /* onela_dtype_t */
+  int32_t activation;    /* ONELA_ACT_NONE or ONELA_ACT_SILU */
+  int64_t total_tokens;  /* < 2^31 */
+  int64_t x_stride;
+} onela_conv_config_t;
+
+/* Outputs and last states, in one launch (two where final_state is initial_state).
+ *   initial_state  or NULL (0)
+ *   y              device [total_tokens][channels] io dtype, dense
+ *   final_state    or NULL; may be initial_state
+ * y must not overlap x.  Errors: ONELA_EINVAL, ONELA_EHIP. */
+onela_status_t onela_short_conv(const onela_conv_config_t* cfg, const int32_t* seq_offsets,
+                                const void* x, const float* weight, const float* bias,
+                                const void* initial_state, void* y, void* final_state,
+                                void* stream);
+
+/* Gradients of a scalar of y and final_state; nothing is kept from the forward call.
+ *   d_y, dx          dense, io dtype
+ *   d_final_state    or NULL (0)
+ *   dweight, dbias   fp32, or NULL (not wanted)
+ *   d_initial_state  or NULL (not wanted); must not be d_final_state
+ *   workspace        onela_short_conv_workspace_bytes(cfg) bytes (0 for an invalid cfg),
+ *                    256-byte aligned; NULL when neither dweight nor dbias is wanted
+ * Errors: ONELA_EINVAL, ONELA_ECAPACITY, ONELA_EHIP. */
+size_t onela_short_conv_workspace_bytes(const onela_conv_config_t* cfg);
+onela_status_t onela_short_conv_backward(const onela_conv_config_t* cfg,
+                                         const int32_t* seq_offsets, const void* x,
+                                         const float* weight, const float* bias,
+                                         const void* initial_state, const void* d_y,
+                                         const void* d_final_state, void* dx, float* dweight,
+                                         float* dbias, void* d_initial_state, void* workspace,
+                                         size_t workspace_bytes, void* stream);
+
+/* The same for one token (or a few) per sequence on pools of states, one launch:
+ *   state      device [num_slots][taps - 1][channels] io dtype
+ *   slots      device int32 [num_seqs]: the state that each sequence goes on from; NULL:
+ *              sequence n has state n
+ *   state_out  NULL: the states are updated in place, and two sequences must not share
+ *              a slot.  Else a second pool [num_slots_out][taps - 1][channels] that does
+ *              not overlap the first: sequence n's new state is its state slots_out[n]
+ *              (NULL: n), no two the same, and any number of sequences may go on from one
+ *              slot (beams of one parent).
+ * A sequence whose slot is outside [0, num_slots) (a padded batch's -1) has outputs 0 and
+ * stores no state; neither does one whose slot in state_out is outside.
+ * Errors: ONELA_EINVAL, ONELA_ECAPACITY (fewer slots than sequences without slots),
+ * ONELA_EHIP. */
+onela_status_t onela_short_conv_step(const onela_conv_config_t* cfg, const int32_t* seq_offsets,
+                                     const void* x, const float* weight, const float* bias,
+                                     void* state, int32_t num_slots, const int32_t* slots,
+                                     void* state_out, int32_t num_slots_out,
+                                     const int32_t* slots_out, void* y, void* stream);
+
+/* ---- Norms before and after a block, with its gate and residual scale ---------
+ * From a block's output to the next block's input in one pass, each row (one token's head,
+ * width columns) by itself; n(v) = v (mean v^2 + eps)^-1/2:
+ *   u = x, or after_weight n(x) with norm_after,       u *= act(gate) with a gate,
+ *   h = residual + residual_scale channel_scale u      (h = the second term without one),
+ *   y = h, or before_weight n(h) with norm_before.
+ * norm_after and a gate alone are what the delta rule's heads pass before the output
+ * projection; norm_before and a residual alone are a pre-norm layer's step.
+ *   x, gate       device [num_tokens][num_heads][width] io dtype, x_stride and gate_stride
+ *                 elements between tokens (0: dense), rows on 16 bytes; gate is there
+ *                 exactly if the configuration has an activation for it
+ *   residual      device [num_tokens][num_heads][width] residual_dtype, dense, or NULL
+ *   weights, channel_scale  device fp32 [width], or NULL (1)
+ *   y             device, dense, io dtype, or NULL (not wanted)
+ *   residual_out  h, device, dense, residual_dtype, or NULL; may be residual
+ * width: a multiple of 8 up to 16384.  fp32 inside (y is formed from h before its rounding),
+ * one rounding at each store. */
+typedef struct {
+  int64_t num_tokens;     /* < 2^31 */
+  int32_t num_heads;      /* rows per token */
+  int32_t width;
+  int32_t io_dtype;       /* onela_dtype_t of x, gate, y and their gradients */
+  int32_t residual_dtype; /* onela_dtype_t of residual, residual_out and their gradients */
+  int32_t norm_after, norm_before;  /* 0 or 1 */
+  int32_t gate_act;       /* onela_act_t; ONELA_ACT_NONE: no gate */
+  int64_t x_stride, gate_stride;
+  float residual_scale;
+  float eps;
+} onela_block_norm_config_t;
+
+/* Errors: ONELA_EINVAL (no output among them), ONELA_EHIP. */
+onela_status_t onela_block_norm(const onela_block_norm_config_t* cfg, const void* x,
+                                const void* gate, const void* residual,
+                                const float* after_weight, const float* before_weight,
+                                const float* channel_scale, void* y, void* residual_out,
+                                void* stream);
+
+/* Gradients of a scalar of y and residual_out by every input, from the forward call's inputs.
+ *   d_y             dense, io dtype, or NULL (0);  d_residual_out  dense, residual_dtype, or
+ *                   NULL (0); one of them at least
+ *   dx, dgate       dense, io dtype (dgate NULL without a gate)
+ *   d_residual      dense, residual_dtype, or NULL (not wanted); may be d_residual_out
+ *   dafter_weight, dbefore_weight, dchannel_scale  fp32 [width], sums over all rows in a
+ *                   fixed order, or NULL (not wanted)
+ *   workspace       onela_block_norm_workspace_bytes(cfg) bytes (0 for an invalid cfg),
+ *                   256-byte aligned; NULL when none of those three is wanted
+ * Errors: ONELA_EINVAL, ONELA_ECAPACITY, ONELA_EHIP. */
+size_t onela_block_norm_workspace_bytes(const onela_block_norm_config_t* cfg);
+onela_status_t onela_block_norm_backward(
+    const onela_block_norm_config_t* cfg, const void* x, const void* gate, const void* residual,
+    const float* after_weight, const float* before_weight, const float* channel_scale,
+    const void* d_y, const void* d_residual_out, void* dx, void* dgate, void* d_residual,
+    float* dafter_weight, float* dbefore_weight, float* dchannel_scale, void* workspace,
+    size_t workspace_bytes, void* stream);
+
+/* ---- Log probabilities of tokens -----------------------------------------
+ * What a model's logits say of tokens, from one read of them: with z = scale logits, a row
+ * at a time,
+ *   lse = log sum exp z,   logp(v) = z_v - lse,   entropy = -sum p log p, p = exp(logp),
+ * the num_given log probabilities of given tokens and the num_top best tokens with theirs.
+ * beam_scores - lse are the beam scores with which onela_select_beams takes the logits
+ * themselves (fp32, scale 1) in the place of log probabilities.
+ *   logits      device [num_rows][vocab] io dtype, logits_stride elements between rows
+ *               (0: dense), aligned to its elements
+ *   given       device int32 [num_rows][num_given].  A token below 0 (padding) has log
+ *               probability 0 and no gradient; one past the vocabulary has NaN
+ *   logp_out    device fp32 [num_rows][num_given]
+ *   lse_out, entropy_out       device fp32 [num_rows], or NULL (not wanted)
+ *   top_tokens_out, top_logp_out  device int32 and fp32 [num_rows][num_top], best first:
+ *               by the logit, equal ones (-0 and 0 among them) by lower token, NaN last
+ * Masked logits are -inf (or any value that far below the rest).  A row whose mask leaves
+ * nothing has lse and all log probabilities -inf and entropy 0; one with NaN or +inf has NaN.
+ * Log probabilities are formed from differences to the row's largest logit, so their
+ * errors do not grow with the logits' size.  num_given up to 256, num_top up to 64 and
+ * vocab, vocab < 2^28, scale > 0. */
+typedef struct {
+  int64_t num_rows;  /* < 2^31 */
+  int32_t vocab;
+  int32_t num_given;
+  int32_t num_top;
+  int32_t io_dtype;  /* onela_dtype_t of logits and their gradient */
+  int64_t logits_stride;
+  float scale;       /* one over the temperature */
+} onela_logprob_config_t;
+
+/* Bytes of the workspace of onela_token_logprobs: what the parts of a row leave for each other
+ * where there are few rows.  256 at least, 0 for an invalid cfg.  The contents need no
+ * preparation and mean nothing afterwards. */
+size_t onela_token_logprobs_workspace_bytes(const onela_logprob_config_t* cfg);
+
+/* workspace: device, 256-byte aligned.  Errors: ONELA_EINVAL, ONELA_ECAPACITY, ONELA_EHIP. */
+onela_status_t onela_token_logprobs(const onela_logprob_config_t* cfg, const void* logits,
+                                    const int32_t* given, float* logp_out, float* lse_out,
+                                    float* entropy_out, int32_t* top_tokens_out,
+                                    float* top_logp_out, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+/* Gradient of a scalar of the log probabilities of the given tokens (of the alternatives too,
+ * given again), lse and entropy by the logits:
+ *   dz_v = p_v (d_lse - sum_g d_logp_g - d_entropy (logp_v + entropy)) + sum_{g: given_g = v} d_logp_g
+ *   lse, entropy  what the forward call gave (entropy only with d_entropy)
+ *   d_logp        device fp32 [num_rows][num_given] (NULL with num_given = 0)
+ *   d_lse, d_entropy  device fp32 [num_rows], or NULL (0)
+ *   d_logits      device [num_rows][vocab] io dtype, dense, aligned to its elements; may be
+ *                 logits where those are dense
+ * A row whose mask leaves nothing has gradient 0.  num_top is not looked at.
+ * Errors: ONELA_EINVAL, ONELA_EHIP. */
+onela_status_t onela_token_logprobs_backward(const onela_logprob_config_t* cfg,
+                                             const void* logits, const int32_t* given,
+                                             const float* lse, const float* entropy,
+                                             const float* d_logp, const float* d_lse,
+                                             const float* d_entropy, void* d_logits,
+                                             void* stream);
+
 /* ---- Capacity model (host only) -----------------------------------------
  * Persistent recurrent-state bytes after `steps` decode steps for one GDN
  * layer (Sec. 4.4): one S_ctx per request and value head (state_bytes per

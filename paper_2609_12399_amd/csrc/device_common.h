@@ -105,6 +105,61 @@ __device__ inline float load1(const void* base, long i) {
     return static_cast<const float*>(base)[i];
 }
 
+template <bool BF16>
+__device__ inline void store8(void* base, long i, const float (&x)[8]) {
+  if constexpr (BF16) {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + i) =
+        make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                   pack_bf16x2(x[6], x[7]));
+  } else {
+    f32x4* const q = reinterpret_cast<f32x4*>(static_cast<float*>(base) + i);
+    q[0] = f32x4{x[0], x[1], x[2], x[3]};
+    q[1] = f32x4{x[4], x[5], x[6], x[7]};
+  }
+}
+
+// 8 neighbouring elements as they come from memory (16-byte aligned), and as floats.
+template <bool BF16>
+struct Raw8 {
+  uint4 w[BF16 ? 1 : 2];
+  __device__ void load(const void* base, long i) {
+    const uint4* const q = reinterpret_cast<const uint4*>(static_cast<const char*>(base) +
+                                                          i * (BF16 ? 2 : 4));
+#pragma unroll
+    for (int j = 0; j < (BF16 ? 1 : 2); ++j) w[j] = q[j];
+  }
+  __device__ void store(void* base, long i) const {
+    uint4* const q = reinterpret_cast<uint4*>(static_cast<char*>(base) + i * (BF16 ? 2 : 4));
+#pragma unroll
+    for (int j = 0; j < (BF16 ? 1 : 2); ++j) q[j] = w[j];
+  }
+  __device__ void clear() {
+#pragma unroll
+    for (int j = 0; j < (BF16 ? 1 : 2); ++j) w[j] = make_uint4(0, 0, 0, 0);
+  }
+  __device__ void floats(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < (BF16 ? 1 : 2); ++j) {
+      const unsigned u[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (BF16) {
+          x[2 * i] = bf16_lo_to_float(u[i]);
+          x[2 * i + 1] = bf16_hi_to_float(u[i]);
+        } else {
+          x[4 * j + i] = __uint_as_float(u[i]);
+        }
+      }
+    }
+  }
+};
+
+// 1 / (1 + exp(-x)) to some 2^-22: the base-2 exponential and the reciprocal are good to one
+// step each.
+__device__ inline float sigmoid(float x) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f));
+}
+
 // Split 8 floats into bf16 hi and lo vectors: hi = bf16(x), lo = bf16(x - hi).
 __device__ inline void split8(const float* x, uint4& hi, uint4& lo) {
   unsigned h[4], l[4];

@@ -364,6 +364,135 @@ size_t norm_workspace_bytes(const onela_norm_config_t* c) {
   return sizeof(float) * size_t(kNormBlocks) * size_t(c->head_dim);
 }
 
+// ---- short causal convolution -------------------------------------------------------
+
+namespace {
+bool io_ok(int32_t dtype) { return dtype == ONELA_F32 || dtype == ONELA_BF16; }
+int io_size(int32_t dtype) { return dtype == ONELA_BF16 ? 2 : 4; }
+// Elements between tokens: 0 (dense) or whole 16-byte pieces, at least a token's own (up to 2^30:
+// offsets in bytes stay below 2^63).
+bool stride_ok(int64_t stride, int64_t own, int32_t dtype) {
+  return stride == 0 || (stride >= own && stride % (16 / io_size(dtype)) == 0 &&
+                         stride <= (int64_t(1) << 30));
+}
+}  // namespace
+
+onela_status_t check_conv(const onela_conv_config_t* c, bool ragged) {
+  if (!c) return ONELA_EINVAL;
+  if (c->num_seqs < 1 || c->total_tokens < 0 || c->total_tokens > INT32_MAX) return ONELA_EINVAL;
+  if (c->channels < 8 || c->channels % 8 || c->taps < 2 || c->taps > kConvMaxTaps)
+    return ONELA_EINVAL;
+  if (!io_ok(c->io_dtype) || !stride_ok(c->x_stride, c->channels, c->io_dtype))
+    return ONELA_EINVAL;
+  if (c->activation != ONELA_ACT_NONE && c->activation != ONELA_ACT_SILU) return ONELA_EINVAL;
+  if (!ragged && c->total_tokens % c->num_seqs) return ONELA_EINVAL;
+  // a thread for every sequence's 8 channels, and for those of runs of tokens (conv_plan: 128
+  // tokens, fewer only while that makes some 2^18 threads)
+  const double groups = double(c->channels) / 8 + 64;
+  if ((double(c->num_seqs) + double(c->total_tokens) / 64 + 512) * groups >= kGridThreads / 2)
+    return ONELA_EINVAL;
+  return ONELA_OK;
+}
+
+ConvPlan conv_plan(const onela_conv_config_t* c, bool backward) {
+  // Channel groups side by side: as many as a wave has lanes, fewer where that leaves fewer
+  // lanes without channels (16 still read whole 256-byte pieces of a bf16 row).
+  const int groups = c->channels / 8;
+  int ll = 6;
+  auto padded = [&](int l) { return ((groups + (1 << l) - 1) >> l) << l; };
+  for (int l = 5; l >= 0; --l)
+    if (padded(l) < padded(ll) && (l >= 4 || groups < (1 << ll))) ll = l;
+  ConvPlan a;
+  a.lanes_log2 = ll;
+  a.blocks_c = padded(ll) >> ll;
+  // Runs: two waves per SIMD of 256 compute units, and not so short that the rows read twice
+  // (taps - 1 before a run, backward as many behind it) count.
+  const long threads = 256l * 4 * 64 * 2, tokens = long(c->total_tokens);
+  const long most = backward ? 1024l * (kConvThreads >> ll) : tokens + 1;  // runs
+  long run = tokens * padded(ll) / threads;
+  run = run < (backward ? 8 : 4) ? (backward ? 8 : 4) : run > 128 ? 128 : run;
+  if ((tokens + run - 1) / run > most) run = (tokens + most - 1) / most;
+  a.run = int(run);
+  const long per = run * (kConvThreads >> ll);
+  a.blocks_t = (tokens + per - 1) / per;
+  return a;
+}
+
+size_t conv_workspace_bytes(const onela_conv_config_t* c) {
+  const ConvPlan a = conv_plan(c, true);
+  const size_t rows = a.blocks_t > 0 ? size_t(a.blocks_t) : 1;
+  return (rows * size_t(c->taps + 1) * size_t(c->channels) * sizeof(float) + 255) / 256 * 256;
+}
+
+// ---- norms around a block ----------------------------------------------------------
+
+onela_status_t check_block_norm(const onela_block_norm_config_t* c) {
+  if (!c) return ONELA_EINVAL;
+  if (c->num_tokens < 0 || c->num_tokens > INT32_MAX || c->num_heads < 1) return ONELA_EINVAL;
+  if (c->width < 8 || c->width > 16384 || c->width % 8) return ONELA_EINVAL;
+  if (!io_ok(c->io_dtype) || !io_ok(c->residual_dtype)) return ONELA_EINVAL;
+  if ((c->norm_after | c->norm_before) & ~1) return ONELA_EINVAL;
+  if (c->gate_act < ONELA_ACT_NONE || c->gate_act > ONELA_ACT_SIGMOID) return ONELA_EINVAL;
+  const int64_t own = int64_t(c->num_heads) * c->width;
+  if (!stride_ok(c->x_stride, own, c->io_dtype) || !stride_ok(c->gate_stride, own, c->io_dtype))
+    return ONELA_EINVAL;
+  if (!(c->eps >= 0.f) || !(c->residual_scale - c->residual_scale == 0.f)) return ONELA_EINVAL;
+  if (double(c->num_tokens) * double(own) >= 1e15) return ONELA_EINVAL;
+  return ONELA_OK;
+}
+
+size_t block_norm_workspace_bytes(const onela_block_norm_config_t* c) {
+  return sizeof(float) * 3 * size_t(kBlockNormBlocks) * size_t(c->width);
+}
+
+// ---- log probabilities of tokens -----------------------------------------------------
+
+onela_status_t check_logprob(const onela_logprob_config_t* c) {
+  if (!c) return ONELA_EINVAL;
+  if (c->num_rows < 0 || c->num_rows > INT32_MAX) return ONELA_EINVAL;
+  if (c->vocab < 1 || c->vocab >= 1 << 28) return ONELA_EINVAL;
+  if (c->num_given < 0 || c->num_given > kMaxGiven) return ONELA_EINVAL;
+  if (c->num_top < 0 || c->num_top > kMaxTop || c->num_top > c->vocab) return ONELA_EINVAL;
+  if (!io_ok(c->io_dtype)) return ONELA_EINVAL;
+  if (c->logits_stride && (c->logits_stride < c->vocab || c->logits_stride > (int64_t(1) << 30)))
+    return ONELA_EINVAL;
+  if (!(c->scale > 0.f) || !(c->scale - c->scale == 0.f)) return ONELA_EINVAL;
+  // a workgroup of 256 threads for every row (backward: for every 4096 columns)
+  if (double(c->num_rows) * (1 + (c->vocab - 1) / 4096) * 256 >= kGridThreads) return ONELA_EINVAL;
+  return ONELA_OK;
+}
+
+LogprobPlan logprob_plan(const onela_logprob_config_t* c) {
+  LogprobPlan a{256, 1, c->vocab};
+  if (c->vocab <= 2048) a.threads = 64;
+  // Few rows: cut into parts until there are workgroups for the chip.
+  const int step = 8192;
+  const long chunks = (long(c->vocab) + step - 1) / step;
+  const long rows = c->num_rows > 0 ? long(c->num_rows) : 1;
+  if (chunks > 1 && rows < 512) {
+    long parts = (1024 + rows - 1) / rows;
+    if (parts > chunks) parts = chunks;
+    if (parts > 64) parts = 64;
+    const long per = (chunks + parts - 1) / parts;
+    a.columns = int(per * step);
+    a.parts = int((chunks + per - 1) / per);
+  }
+  return a;
+}
+
+size_t logprob_workspace_bytes(const onela_logprob_config_t* c) {
+  const LogprobPlan a = logprob_plan(c);
+  if (a.parts == 1) return 256;
+  const size_t n = size_t(c->num_rows) * a.parts * (4 + 2 * size_t(c->num_top)) * sizeof(float);
+  return n < 256 ? 256 : (n + 255) / 256 * 256;
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  if (!a || !b || na == 0 || nb == 0) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y ? y - x < na : x - y < nb;
+}
+
 // ---- per-step protocol --------------------------------------------------------
 // resolve(t) -> append(t) -> decode(t) (decode may repeat), or fused(t); the
 // next step starts only after the previous one was appended.

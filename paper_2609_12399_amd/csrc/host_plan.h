@@ -142,6 +142,41 @@ constexpr int kNormBlocks = 2048;  // most workgroups of the backward pass
 onela_status_t check_norm(const onela_norm_config_t* cfg);
 size_t norm_workspace_bytes(const onela_norm_config_t* cfg);
 
+// ---- short causal convolution -------------------------------------------------------
+// Threads take 8 channels and a run of tokens each; a workgroup of kConvThreads has
+// 2^lanes_log2 channel groups side by side and as many runs as that leaves.
+constexpr int kConvThreads = 256;
+constexpr int kConvMaxTaps = 4;
+struct ConvPlan {
+  int lanes_log2;   // channel groups of a workgroup
+  int run;          // tokens of a run
+  int blocks_c;     // workgroups over the channels
+  long blocks_t;    // workgroups over the tokens
+};
+onela_status_t check_conv(const onela_conv_config_t* cfg, bool ragged);
+ConvPlan conv_plan(const onela_conv_config_t* cfg, bool backward);
+size_t conv_workspace_bytes(const onela_conv_config_t* cfg);
+
+// ---- norms around a block ----------------------------------------------------------
+constexpr int kBlockNormBlocks = 1024;  // most workgroups of the backward pass
+onela_status_t check_block_norm(const onela_block_norm_config_t* cfg);
+size_t block_norm_workspace_bytes(const onela_block_norm_config_t* cfg);
+
+// ---- log probabilities of tokens -----------------------------------------------------
+constexpr int kMaxGiven = 256, kMaxTop = 64;
+// Parts that a row is cut into (1: none), each a whole number of `step` columns.
+struct LogprobPlan {
+  int threads;  // of a workgroup, one part each
+  int parts;
+  int columns;  // of a part
+};
+onela_status_t check_logprob(const onela_logprob_config_t* cfg);
+LogprobPlan logprob_plan(const onela_logprob_config_t* cfg);
+size_t logprob_workspace_bytes(const onela_logprob_config_t* cfg);
+
+// Whether two ranges of bytes share any.
+bool overlap(const void* a, size_t na, const void* b, size_t nb);
+
 // ---- validation and the per-step protocol -----------------------------------
 
 // The Shape of a configuration, or ONELA_EINVAL.

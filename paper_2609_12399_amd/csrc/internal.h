@@ -96,6 +96,67 @@ struct NormParams {
 };
 hipError_t launch_norm_rope(const NormParams& p, bool bf16, bool backward, hipStream_t st);
 
+// ---- short causal convolution ----------------------------------------------------------
+struct ConvParams {
+  const void* x;         // [total][C], token stride xs
+  const float *w, *bias;  // [C][taps], [C] or null
+  const int* offsets;    // [N + 1] or null: L tokens each
+  const void* s_in;      // [N or slots][taps - 1][C] or null: zeros
+  void* s_out;           // [N or slots_out][taps - 1][C] or null
+  void* y;               // dense
+  const void *dy, *ds_in;  // gradients of y and of the last states (or null)
+  void *dx, *ds_out;     // ds_out: of the first states, or null
+  float *dw, *db;        // [C][taps], [C], or null
+  float* partial;        // [blocks_t][taps + 1][C], or null: neither is wanted
+  const int *slot, *slot_out;  // step: [N] or null
+  long total, xs;
+  int N, C, L, slots, slots_out;
+  bool silu;
+};
+hipError_t launch_conv(const ConvParams& p, const ConvPlan& plan, int taps, bool bf16,
+                       hipStream_t st);
+hipError_t launch_conv_backward(const ConvParams& p, const ConvPlan& plan, int taps, bool bf16,
+                                hipStream_t st);
+hipError_t launch_conv_step(const ConvParams& p, int taps, bool bf16, hipStream_t st);
+
+// ---- norms around a block -----------------------------------------------------------
+struct BlockNormParams {
+  const void *x, *gate;  // [T][H][D], token strides xs, gs; gate null: none
+  const void* res;       // dense, or null
+  const float *wa, *wb, *cs;  // [D] or null: ones
+  void *y, *h;           // dense, or null
+  const void *dy, *dh;   // dense, or null: zeros
+  void *dx, *dgate, *dres;  // dense; dgate, dres null: not wanted
+  float *dwa, *dwb, *dcs;   // [D] or null
+  float* partial;        // [workgroups][3][D], or null: none of these is wanted
+  long rows, xs, gs;
+  float scale, eps;
+  int H, D;
+  bool after, before, silu;
+};
+hipError_t launch_block_norm(const BlockNormParams& p, bool bf16, bool res_bf16, int cus,
+                             hipStream_t st);
+hipError_t launch_block_norm_backward(const BlockNormParams& p, bool bf16, bool res_bf16, int cus,
+                                      hipStream_t st);
+
+// ---- log probabilities of tokens --------------------------------------------------------
+struct LogprobParams {
+  const void* x;         // [R][V], row stride xs
+  const int* given;      // [R][G]
+  float *logp, *lse, *entropy;  // [R][G], [R], [R] or null
+  int* top;              // [R][K]
+  float* top_logp;
+  float* parts;          // [R][parts][4 + 2 K]: sums and the best of every part
+  const float *lse_in, *entropy_in, *dlogp, *dlse, *dentropy;  // backward
+  void* dx;              // dense
+  long R, xs;
+  float scale;
+  int V, G, K;
+};
+hipError_t launch_logprobs(const LogprobParams& p, const LogprobPlan& plan, bool bf16,
+                           hipStream_t st);
+hipError_t launch_logprobs_backward(const LogprobParams& p, bool bf16, hipStream_t st);
+
 // ---- global top-W beam selection ------------------------------------------
 // Device address of the allocation-free entry point's scratch array on the
 // current device.

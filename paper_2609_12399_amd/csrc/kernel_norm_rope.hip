@@ -24,19 +24,6 @@ constexpr int kNormThreads = 256;
 // in 32 bits, without an error.
 constexpr long kNormLaunch = (1l << 32) / kNormThreads - 1;
 
-template <bool BF16>
-__device__ inline void store8(void* base, long i, const float (&x)[8]) {
-  if constexpr (BF16) {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(base) + i) =
-        make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                   pack_bf16x2(x[6], x[7]));
-  } else {
-    f32x4* const q = reinterpret_cast<f32x4*>(static_cast<float*>(base) + i);
-    q[0] = f32x4{x[0], x[1], x[2], x[3]};
-    q[1] = f32x4{x[4], x[5], x[6], x[7]};
-  }
-}
-
 // Turns this lane's 8 columns (from c0) of a row by the table's row cs (SIGN -1:
 // back).  Every lane of the row's group takes part.
 template <int G>

@@ -1,0 +1,454 @@
+// Short causal convolution of every channel over packed sequences, its gradient, and its step on
+// pools of states.
+//
+//   pre_t = b + sum_j w_j x_{t-K+1+j},  y_t = pre_t or silu(pre_t),  0 <= j < K (taps);
+//   g_t = dy_t act'(pre_t),  dx_t = sum_j w_j g_{t+K-1-j},  dw_j = sum_t g_t x_{t-K+1+j},
+// the inputs before a sequence being its state.  dx of those is the state's gradient, and the
+// gradient of the last state is added to the dx of the inputs that it holds.
+//
+// A thread takes 8 channels (16 bytes of bf16) and walks a run of tokens with the last K
+// inputs in registers, so that x is read once but for the K - 1 rows before a run (and behind
+// it, backward), which come from the cache.  Runs cross sequences: they are walked in
+// pieces of one sequence each.  Weight gradients are summed over a thread's run, over the
+// workgroup's runs in LDS, and over the workgroups by a second launch, each in a fixed order.
+// Bound: HBM.
+#include "device_common.h"
+#include "internal.h"
+
+namespace onela {
+namespace {
+
+constexpr int kRows = 8;      // rows of x in flight per thread
+constexpr int kBackRows = 4;  // of x and dy, backward
+
+struct Bounds {
+  long b, e;
+};
+// The tokens of sequence n, cut to the tensors.
+__device__ inline Bounds bounds_of(const ConvParams& p, int n) {
+  if (!p.offsets) return {long(n) * p.L, long(n + 1) * p.L};
+  const long b = min(max(long(p.offsets[n]), 0l), p.total);
+  return {b, min(max(long(p.offsets[n + 1]), b), p.total)};
+}
+
+// A sequence at or before the one that has token t0 (the wave's lowest): the last one that
+// begins at or before it, 64 offsets at a time.  Every lane of the wave takes part.
+__device__ inline int sequence_at(const ConvParams& p, long t0) {
+  if (!p.offsets) return p.L ? int(t0 / p.L) : 0;
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = p.N;  // it is one of lo .. lo + n - 1
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lo + lane * step;
+    const bool before = lane * step < n && (at == 0 || long(p.offsets[at]) <= t0);
+    const int last = max(63 - __builtin_clzll(__ballot(before) | 1ull), 0);
+    n = min(step, n - last * step);
+    lo += last * step;
+  }
+  return lo;
+}
+
+template <int TAPS>
+struct Window {  // the last TAPS inputs (or gradients), newest last
+  float v[TAPS][8];
+  __device__ void push(const float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j + 1 < TAPS; ++j)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] = v[j + 1][i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[TAPS - 1][i] = x[i];
+  }
+};
+
+// Input at place t (before b: in the state) of channels c0 .. c0 + 7.
+template <int TAPS, bool BF16>
+__device__ inline Raw8<BF16> input_at(const ConvParams& p, const void* state, long row, long b,
+                                      long t, int c0) {
+  Raw8<BF16> r;
+  if (t >= b)
+    r.load(p.x, t * p.xs + c0);
+  else if (state)
+    r.load(state, (row * (TAPS - 1) + (t - b + TAPS - 1)) * p.C + c0);
+  else
+    r.clear();
+  return r;
+}
+
+// The window before token t (its newest place is free).
+template <int TAPS, bool BF16>
+__device__ inline void fill(const ConvParams& p, long n, long b, long t, int c0,
+                            Window<TAPS>& win) {
+  Raw8<BF16> r[TAPS - 1];
+#pragma unroll
+  for (int i = 0; i < TAPS - 1; ++i)
+    r[i] = input_at<TAPS, BF16>(p, p.s_in, n, b, t - (TAPS - 1) + i, c0);
+#pragma unroll
+  for (int i = 0; i < TAPS - 1; ++i) r[i].floats(win.v[i + 1]);
+}
+
+template <int TAPS>
+struct Weights {
+  float w[TAPS][8], b[8];
+  __device__ void load(const ConvParams& p, int c0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+      for (int j = 0; j < TAPS; ++j) w[j][i] = p.w[(c0 + i) * TAPS + j];
+      b[i] = p.bias ? p.bias[c0 + i] : 0.f;
+    }
+  }
+  __device__ void apply(const Window<TAPS>& x, float (&y)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      y[i] = b[i];
+#pragma unroll
+      for (int j = 0; j < TAPS; ++j) y[i] = fmaf(w[j][i], x.v[j][i], y[i]);
+    }
+  }
+};
+
+template <bool BF16>
+__device__ inline void store_output(const ConvParams& p, long i, float (&y)[8]) {
+  if (p.silu)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) y[k] *= sigmoid(y[k]);
+  store8<BF16>(p.y, i, y);
+}
+
+// The state after sequence n, 8 channels (read before it is stored: it may replace the first).
+template <int TAPS, bool BF16>
+__device__ inline void last_state(const ConvParams& p, int n, int c0) {
+  const Bounds s = bounds_of(p, n);
+  Raw8<BF16> r[TAPS - 1];
+#pragma unroll
+  for (int i = 0; i < TAPS - 1; ++i)
+    r[i] = input_at<TAPS, BF16>(p, p.s_in, n, s.b, s.e - (TAPS - 1) + i, c0);
+#pragma unroll
+  for (int i = 0; i < TAPS - 1; ++i) r[i].store(p.s_out, (long(n) * (TAPS - 1) + i) * p.C + c0);
+}
+
+// Where a thread stands: its channels and its run.
+struct Place {
+  int c0;
+  long t0, t1;
+  bool in;
+};
+__device__ inline Place place_of(const ConvParams& p, int ll, int run, int blocks_c) {
+  const int bt = blockIdx.x / blocks_c, bc = blockIdx.x - bt * blocks_c;
+  const int c0 = 8 * ((bc << ll) + (threadIdx.x & ((1 << ll) - 1)));
+  const long t0 = (long(bt) * (kConvThreads >> ll) + (threadIdx.x >> ll)) * run;
+  return {c0, t0, min(t0 + run, p.total), c0 < p.C && t0 < p.total};
+}
+
+// The first blocks_c * blocks_t workgroups take the tokens, the others the last states.
+template <int TAPS, bool BF16>
+__global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvParams p, int ll, int run,
+                                                            int blocks_c, unsigned token_blocks) {
+  if (blockIdx.x >= token_blocks) {
+    const long i = long(blockIdx.x - token_blocks) * kConvThreads + threadIdx.x;
+    const int n = int(i / (p.C / 8));
+    if (n < p.N) last_state<TAPS, BF16>(p, n, 8 * int(i - long(n) * (p.C / 8)));
+    return;
+  }
+  const Place at = place_of(p, ll, run, blocks_c);
+  int n = sequence_at(p, __shfl(at.t0, 0));
+  if (!at.in) return;
+  Weights<TAPS> w;
+  w.load(p, at.c0);
+  for (; n < p.N; ++n) {
+    const Bounds s = bounds_of(p, n);
+    if (s.b >= at.t1) break;
+    const long p0 = max(at.t0, s.b), p1 = min(at.t1, s.e);
+    if (p0 >= p1) continue;
+    Window<TAPS> win;
+    fill<TAPS, BF16>(p, n, s.b, p0, at.c0, win);
+    Raw8<BF16> cur[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i)
+      if (p0 + i < p1) cur[i].load(p.x, (p0 + i) * p.xs + at.c0);
+    for (long t = p0; t < p1; t += kRows) {
+      Raw8<BF16> next[kRows];
+#pragma unroll
+      for (int i = 0; i < kRows; ++i)
+        if (t + kRows + i < p1) next[i].load(p.x, (t + kRows + i) * p.xs + at.c0);
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) {
+        if (t + i >= p1) break;
+        float x[8], y[8];
+        cur[i].floats(x);
+        win.push(x);
+        w.apply(win, y);
+        store_output<BF16>(p, (t + i) * p.C + at.c0, y);
+      }
+#pragma unroll
+      for (int i = 0; i < kRows; ++i) cur[i] = next[i];
+    }
+  }
+}
+
+template <int TAPS, bool BF16>
+__global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams p, int ll, int run,
+                                                                     int blocks_c,
+                                                                     unsigned token_blocks) {
+  if (blockIdx.x >= token_blocks) {  // sequences without tokens: the state passes through
+    const long i = long(blockIdx.x - token_blocks) * kConvThreads + threadIdx.x;
+    const int n = int(i / (p.C / 8)), c0 = 8 * int(i - long(n) * (p.C / 8));
+    if (n >= p.N) return;
+    const Bounds s = bounds_of(p, n);
+    if (s.b < s.e) return;
+#pragma unroll
+    for (int j = 0; j < TAPS - 1; ++j) {
+      const long o = (long(n) * (TAPS - 1) + j) * p.C + c0;
+      Raw8<BF16> r;
+      if (p.ds_in)
+        r.load(p.ds_in, o);
+      else
+        r.clear();
+      r.store(p.ds_out, o);
+    }
+    return;
+  }
+  __shared__ float acc[kConvThreads][9];
+  const Place at = place_of(p, ll, run, blocks_c);
+  int n = sequence_at(p, __shfl(at.t0, 0));
+  float dw[TAPS + 1][8] = {};
+  if (at.in) {
+    Weights<TAPS> w;
+    w.load(p, at.c0);
+    for (; n < p.N; ++n) {
+      const Bounds s = bounds_of(p, n);
+      if (s.b >= at.t1) break;
+      const long p0 = max(at.t0, s.b), p1 = min(at.t1, s.e);
+      if (p0 >= p1) continue;
+      // tokens p0 .. p2 - 1: TAPS - 1 more, whose gradients the last inputs have a part of (the
+      // sequence's end is followed by zeros)
+      const long p2 = p1 + TAPS - 1, end = min(p2, s.e);
+      Window<TAPS> win, gs = {};
+      fill<TAPS, BF16>(p, n, s.b, p0, at.c0, win);
+      Raw8<BF16> cx[kBackRows], cd[kBackRows];
+#pragma unroll
+      for (int i = 0; i < kBackRows; ++i)
+        if (p0 + i < end) {
+          cx[i].load(p.x, (p0 + i) * p.xs + at.c0);
+          cd[i].load(p.dy, (p0 + i) * p.C + at.c0);
+        }
+      for (long t = p0; t < p2; t += kBackRows) {
+        Raw8<BF16> nx[kBackRows], nd[kBackRows];
+#pragma unroll
+        for (int i = 0; i < kBackRows; ++i)
+          if (t + kBackRows + i < end) {
+            nx[i].load(p.x, (t + kBackRows + i) * p.xs + at.c0);
+            nd[i].load(p.dy, (t + kBackRows + i) * p.C + at.c0);
+          }
+#pragma unroll
+        for (int i = 0; i < kBackRows; ++i) {
+          const long tt = t + i;
+          if (tt >= p2) break;
+          float x[8] = {}, g[8] = {};
+          if (tt < end) {
+            cx[i].floats(x);
+            cd[i].floats(g);
+          }
+          win.push(x);
+          if (p.silu && tt < end) {
+            float y[8];
+            w.apply(win, y);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const float sg = sigmoid(y[k]);
+              g[k] *= sg * fmaf(y[k], 1.f - sg, 1.f);
+            }
+          }
+          gs.push(g);
+          if (tt < p1)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+#pragma unroll
+              for (int j = 0; j < TAPS; ++j) dw[j][k] = fmaf(g[k], win.v[j][k], dw[j][k]);
+              dw[TAPS][k] += g[k];
+            }
+          const long o = tt - (TAPS - 1);  // the input whose gradient is complete
+          const bool old = o < p0;
+          if (old && (p0 != s.b || !p.ds_out)) continue;
+          float d[8] = {};
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+#pragma unroll
+            for (int j = 0; j < TAPS; ++j) d[k] = fmaf(w.w[j][k], gs.v[TAPS - 1 - j][k], d[k]);
+          const long last = o - (s.e - (TAPS - 1));  // its place in the last state
+          if (last >= 0 && p.ds_in) {
+            float f[8];
+            load8<BF16>(p.ds_in, (long(n) * (TAPS - 1) + last) * p.C + at.c0, f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) d[k] += f[k];
+          }
+          if (old)
+            store8<BF16>(p.ds_out, (long(n) * (TAPS - 1) + (o - s.b + TAPS - 1)) * p.C + at.c0, d);
+          else
+            store8<BF16>(p.dx, o * p.C + at.c0, d);
+        }
+#pragma unroll
+        for (int i = 0; i < kBackRows; ++i) {
+          cx[i] = nx[i];
+          cd[i] = nd[i];
+        }
+      }
+    }
+  }
+  if (!p.partial) return;
+  const int lanes = 1 << ll, c_first = at.c0 - 8 * (threadIdx.x & (lanes - 1));
+  const long bt = blockIdx.x / blocks_c;
+#pragma unroll
+  for (int j = 0; j <= TAPS; ++j) {
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) acc[threadIdx.x][k] = dw[j][k];
+    __syncthreads();
+    for (int c = threadIdx.x; c < 8 * lanes && c_first + c < p.C; c += kConvThreads) {
+      float s = 0.f;
+      for (int r = c / 8; r < kConvThreads; r += lanes) s += acc[r][c & 7];
+      p.partial[(bt * (TAPS + 1) + j) * p.C + c_first + c] = s;
+    }
+  }
+}
+
+// The workgroups' sums added up: 16 values of a tap per workgroup, 16 rows at a time.
+__global__ __launch_bounds__(256) void conv_weight_kernel(ConvParams p, int taps, long rows) {
+  __shared__ float acc[16][17];
+  const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const long col = long(blockIdx.x) * 16 + c, width = long(taps + 1) * p.C;
+  float s = 0.f;
+  if (col < width)
+#pragma unroll 4
+    for (long i = g; i < rows; i += 16) s += p.partial[i * width + col];
+  acc[g][c] = s;
+  __syncthreads();
+  if (g != 0 || col >= width) return;
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s += acc[i][c];
+  const int j = int(col / p.C), ch = int(col - long(j) * p.C);
+  if (j < taps) {
+    if (p.dw) p.dw[long(ch) * taps + j] = s;
+  } else if (p.db) {
+    p.db[ch] = s;
+  }
+}
+
+// One thread for a sequence's 8 channels.
+template <int TAPS, bool BF16>
+__global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvParams p) {
+  const long i = long(blockIdx.x) * kConvThreads + threadIdx.x;
+  const int n = int(i / (p.C / 8)), c0 = 8 * int(i - long(n) * (p.C / 8));
+  if (n >= p.N) return;
+  const Bounds s = bounds_of(p, n);
+  if (s.b >= s.e) {
+    // no token: a state in place stays; one in another pool follows its parent
+    if (!p.s_out) return;
+  }
+  const int from = p.slot ? p.slot[n] : n;
+  const int to = p.s_out ? (p.slot_out ? p.slot_out[n] : n) : from;
+  const int most = p.s_out ? p.slots_out : p.slots;
+  if (from < 0 || from >= p.slots) {  // no state: the sequence's outputs are zeros
+    const float zero[8] = {};
+    for (long t = s.b; t < s.e; ++t) store8<BF16>(p.y, t * p.C + c0, zero);
+    return;
+  }
+  Raw8<BF16> r[TAPS - 1], x;
+  Weights<TAPS> w;
+#pragma unroll
+  for (int j = 0; j < TAPS - 1; ++j)
+    r[j].load(p.s_in, (long(from) * (TAPS - 1) + j) * p.C + c0);
+  w.load(p, c0);
+  Window<TAPS> win;
+#pragma unroll
+  for (int j = 0; j < TAPS - 1; ++j) r[j].floats(win.v[j + 1]);
+  for (long t = s.b; t < s.e; ++t) {
+    float v[8], y[8];
+    x.load(p.x, t * p.xs + c0);
+    x.floats(v);
+    win.push(v);
+    w.apply(win, y);
+    store_output<BF16>(p, t * p.C + c0, y);
+#pragma unroll
+    for (int j = 0; j + 2 < TAPS; ++j) r[j] = r[j + 1];
+    r[TAPS - 2] = x;
+  }
+  if (to < 0 || to >= most) return;
+  void* const out = p.s_out ? p.s_out : const_cast<void*>(p.s_in);
+#pragma unroll
+  for (int j = 0; j < TAPS - 1; ++j) r[j].store(out, (long(to) * (TAPS - 1) + j) * p.C + c0);
+}
+
+unsigned state_blocks(const ConvParams& p) {
+  return unsigned((long(p.N) * (p.C / 8) + kConvThreads - 1) / kConvThreads);
+}
+
+template <int TAPS, bool BF16>
+hipError_t run_forward(const ConvParams& p, const ConvPlan& a, hipStream_t st) {
+  const unsigned tokens = unsigned(a.blocks_t * a.blocks_c);
+  // a last state that replaces the first one waits until every token has read it
+  const bool apart = p.s_out && p.s_out == p.s_in;
+  const unsigned states = p.s_out ? state_blocks(p) : 0;
+  if (tokens + (apart ? 0 : states) > 0) {
+    conv_kernel<TAPS, BF16><<<tokens + (apart ? 0 : states), kConvThreads, 0, st>>>(
+        p, a.lanes_log2, a.run, a.blocks_c, tokens);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (apart)
+    conv_kernel<TAPS, BF16><<<states, kConvThreads, 0, st>>>(p, a.lanes_log2, a.run, a.blocks_c, 0);
+  return hipGetLastError();
+}
+
+template <int TAPS, bool BF16>
+hipError_t run_backward(const ConvParams& p, const ConvPlan& a, hipStream_t st) {
+  const unsigned tokens = unsigned(a.blocks_t * a.blocks_c);
+  const unsigned states = p.ds_out ? state_blocks(p) : 0;
+  if (tokens + states > 0) {
+    conv_backward_kernel<TAPS, BF16><<<tokens + states, kConvThreads, 0, st>>>(
+        p, a.lanes_log2, a.run, a.blocks_c, tokens);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (p.partial)
+    conv_weight_kernel<<<unsigned((long(TAPS + 1) * p.C + 15) / 16), 256, 0, st>>>(p, TAPS,
+                                                                                  a.blocks_t);
+  return hipGetLastError();
+}
+
+template <int TAPS, bool BF16>
+hipError_t run_step(const ConvParams& p, hipStream_t st) {
+  conv_step_kernel<TAPS, BF16><<<state_blocks(p), kConvThreads, 0, st>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+#define ONELA_CONV(call)                                                      \
+  if (taps == 2) return bf16 ? call(2, true) : call(2, false);                \
+  if (taps == 3) return bf16 ? call(3, true) : call(3, false);                \
+  return bf16 ? call(4, true) : call(4, false)
+
+hipError_t launch_conv(const ConvParams& p, const ConvPlan& plan, int taps, bool bf16,
+                       hipStream_t st) {
+#define ONELA_FORWARD(K, B) run_forward<K, B>(p, plan, st)
+  ONELA_CONV(ONELA_FORWARD);
+#undef ONELA_FORWARD
+}
+
+hipError_t launch_conv_backward(const ConvParams& p, const ConvPlan& plan, int taps, bool bf16,
+                                hipStream_t st) {
+#define ONELA_BACKWARD(K, B) run_backward<K, B>(p, plan, st)
+  ONELA_CONV(ONELA_BACKWARD);
+#undef ONELA_BACKWARD
+}
+
+hipError_t launch_conv_step(const ConvParams& p, int taps, bool bf16, hipStream_t st) {
+#define ONELA_STEP(K, B) run_step<K, B>(p, st)
+  ONELA_CONV(ONELA_STEP);
+#undef ONELA_STEP
+}
+#undef ONELA_CONV
+
+}  // namespace onela

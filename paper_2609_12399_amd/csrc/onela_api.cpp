@@ -604,4 +604,322 @@ onela_status_t onela_qk_norm_rope_backward(const onela_norm_config_t* cfg, const
   return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
 }
 
+
+// ---- short causal convolution ----------------------------------------------------------
+
+namespace {
+bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
+size_t io_bytes(int32_t dtype) { return dtype == ONELA_BF16 ? 2 : 4; }
+// Bytes from the first to the last element of n tokens of `own` elements, `stride` apart.
+size_t span(int64_t n, int64_t stride, int64_t own, int32_t dtype) {
+  return n > 0 ? size_t((n - 1) * stride + own) * io_bytes(dtype) : 0;
+}
+
+onela_status_t conv_inputs(const onela_conv_config_t* c, const int32_t* offsets, const void* x,
+                           const float* weight, const float* bias, onela::ConvParams* p) {
+  const onela_status_t rc = onela::check_conv(c, offsets != nullptr);
+  if (rc != ONELA_OK) return rc;
+  if (!weight || (c->total_tokens > 0 && !x)) return ONELA_EINVAL;
+  if (!aligned16(x) || !aligned4(weight) || !aligned4(bias) || !aligned4(offsets))
+    return ONELA_EINVAL;
+  *p = onela::ConvParams{};
+  p->x = x;
+  p->w = weight;
+  p->bias = bias;
+  p->offsets = offsets;
+  p->total = long(c->total_tokens);
+  p->xs = c->x_stride ? long(c->x_stride) : long(c->channels);
+  p->N = c->num_seqs;
+  p->C = c->channels;
+  p->L = offsets ? 0 : int(c->total_tokens / c->num_seqs);
+  p->silu = c->activation == ONELA_ACT_SILU;
+  return ONELA_OK;
+}
+size_t conv_x_bytes(const onela_conv_config_t* c) {
+  return span(c->total_tokens, c->x_stride ? c->x_stride : c->channels, c->channels, c->io_dtype);
+}
+size_t conv_rows_bytes(const onela_conv_config_t* c, int64_t rows) {
+  return size_t(rows) * size_t(c->channels) * io_bytes(c->io_dtype);
+}
+}  // namespace
+
+onela_status_t onela_short_conv(const onela_conv_config_t* cfg, const int32_t* seq_offsets,
+                                const void* x, const float* weight, const float* bias,
+                                const void* initial_state, void* y, void* final_state,
+                                void* stream) {
+  onela::ConvParams p;
+  const onela_status_t rc = conv_inputs(cfg, seq_offsets, x, weight, bias, &p);
+  if (rc != ONELA_OK) return rc;
+  if ((p.total > 0 && !y) || !aligned16(y) || !aligned16(initial_state) || !aligned16(final_state))
+    return ONELA_EINVAL;
+  const size_t states = conv_rows_bytes(cfg, int64_t(p.N) * (cfg->taps - 1));
+  if (onela::overlap(x, conv_x_bytes(cfg), y, conv_rows_bytes(cfg, p.total)) ||
+      (final_state != initial_state &&
+       onela::overlap(final_state, states, initial_state, states)))
+    return ONELA_EINVAL;
+  p.s_in = initial_state;
+  p.s_out = final_state;
+  p.y = y;
+  const hipError_t e = onela::launch_conv(p, onela::conv_plan(cfg, false), cfg->taps,
+                                          cfg->io_dtype == ONELA_BF16,
+                                          static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+size_t onela_short_conv_workspace_bytes(const onela_conv_config_t* cfg) {
+  return onela::check_conv(cfg, true) == ONELA_OK ? onela::conv_workspace_bytes(cfg) : 0;
+}
+
+onela_status_t onela_short_conv_backward(const onela_conv_config_t* cfg,
+                                         const int32_t* seq_offsets, const void* x,
+                                         const float* weight, const float* bias,
+                                         const void* initial_state, const void* d_y,
+                                         const void* d_final_state, void* dx, float* dweight,
+                                         float* dbias, void* d_initial_state, void* workspace,
+                                         size_t workspace_bytes, void* stream) {
+  onela::ConvParams p;
+  const onela_status_t rc = conv_inputs(cfg, seq_offsets, x, weight, bias, &p);
+  if (rc != ONELA_OK) return rc;
+  if (p.total > 0 && (!d_y || !dx)) return ONELA_EINVAL;
+  if (!aligned16(d_y) || !aligned16(dx) || !aligned16(initial_state) ||
+      !aligned16(d_final_state) || !aligned16(d_initial_state) || !aligned4(dweight) ||
+      !aligned4(dbias))
+    return ONELA_EINVAL;
+  const size_t states = conv_rows_bytes(cfg, int64_t(p.N) * (cfg->taps - 1));
+  const size_t rows = conv_rows_bytes(cfg, p.total);
+  // (a run reads rows of its neighbours)
+  if (onela::overlap(dx, rows, d_y, rows) || onela::overlap(dx, rows, x, conv_x_bytes(cfg)) ||
+      onela::overlap(d_initial_state, states, d_final_state, states) ||
+      onela::overlap(d_initial_state, states, initial_state, states))
+    return ONELA_EINVAL;
+  if (dweight || dbias) {
+    if (!workspace || !aligned256(workspace)) return ONELA_EINVAL;
+    if (workspace_bytes < onela::conv_workspace_bytes(cfg)) return ONELA_ECAPACITY;
+    p.partial = static_cast<float*>(workspace);
+  }
+  p.s_in = initial_state;
+  p.dy = d_y;
+  p.ds_in = d_final_state;
+  p.dx = dx;
+  p.ds_out = d_initial_state;
+  p.dw = dweight;
+  p.db = dbias;
+  const hipError_t e = onela::launch_conv_backward(p, onela::conv_plan(cfg, true), cfg->taps,
+                                                   cfg->io_dtype == ONELA_BF16,
+                                                   static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+onela_status_t onela_short_conv_step(const onela_conv_config_t* cfg, const int32_t* seq_offsets,
+                                     const void* x, const float* weight, const float* bias,
+                                     void* state, int32_t num_slots, const int32_t* slots,
+                                     void* state_out, int32_t num_slots_out,
+                                     const int32_t* slots_out, void* y, void* stream) {
+  onela::ConvParams p;
+  const onela_status_t rc = conv_inputs(cfg, seq_offsets, x, weight, bias, &p);
+  if (rc != ONELA_OK) return rc;
+  if ((p.total > 0 && !y) || !aligned16(y)) return ONELA_EINVAL;
+  if (!state || num_slots < 1 || !aligned16(state) || !aligned4(slots)) return ONELA_EINVAL;
+  if (state_out ? num_slots_out < 1 : slots_out != nullptr) return ONELA_EINVAL;
+  if (!aligned16(state_out) || !aligned4(slots_out)) return ONELA_EINVAL;
+  if (!slots && num_slots < p.N) return ONELA_ECAPACITY;
+  if (state_out && !slots_out && num_slots_out < p.N) return ONELA_ECAPACITY;
+  const int64_t rows = cfg->taps - 1;
+  if (state_out && onela::overlap(state, conv_rows_bytes(cfg, num_slots * rows), state_out,
+                                  conv_rows_bytes(cfg, num_slots_out * rows)))
+    return ONELA_EINVAL;
+  p.s_in = state;
+  p.s_out = state_out;
+  p.slot = slots;
+  p.slot_out = slots_out;
+  p.slots = num_slots;
+  p.slots_out = num_slots_out;
+  p.y = y;
+  const hipError_t e = onela::launch_conv_step(p, cfg->taps, cfg->io_dtype == ONELA_BF16,
+                                               static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+// ---- norms around a block -----------------------------------------------------------
+
+namespace {
+onela_status_t block_norm_inputs(const onela_block_norm_config_t* c, const void* x,
+                                 const void* gate, const void* residual, const float* wa,
+                                 const float* wb, const float* cs, onela::BlockNormParams* p) {
+  const onela_status_t rc = onela::check_block_norm(c);
+  if (rc != ONELA_OK) return rc;
+  const bool gated = c->gate_act != ONELA_ACT_NONE;
+  if (c->num_tokens > 0 && (!x || gated != (gate != nullptr))) return ONELA_EINVAL;
+  if ((wa && !c->norm_after) || (wb && !c->norm_before)) return ONELA_EINVAL;
+  if (!aligned16(x) || !aligned16(gate) || !aligned16(residual) || !aligned4(wa) ||
+      !aligned4(wb) || !aligned4(cs))
+    return ONELA_EINVAL;
+  const long own = long(c->num_heads) * c->width;
+  *p = onela::BlockNormParams{};
+  p->x = x;
+  p->gate = gate;
+  p->res = residual;
+  p->wa = wa;
+  p->wb = wb;
+  p->cs = cs;
+  p->rows = long(c->num_tokens) * c->num_heads;
+  p->xs = c->x_stride ? long(c->x_stride) : own;
+  p->gs = c->gate_stride ? long(c->gate_stride) : own;
+  p->scale = c->residual_scale;
+  p->eps = c->eps;
+  p->H = c->num_heads;
+  p->D = c->width;
+  p->after = c->norm_after != 0;
+  p->before = c->norm_before != 0;
+  p->silu = c->gate_act == ONELA_ACT_SILU;
+  return ONELA_OK;
+}
+}  // namespace
+
+onela_status_t onela_block_norm(const onela_block_norm_config_t* cfg, const void* x,
+                                const void* gate, const void* residual,
+                                const float* after_weight, const float* before_weight,
+                                const float* channel_scale, void* y, void* residual_out,
+                                void* stream) {
+  onela::BlockNormParams p;
+  const onela_status_t rc =
+      block_norm_inputs(cfg, x, gate, residual, after_weight, before_weight, channel_scale, &p);
+  if (rc != ONELA_OK) return rc;
+  if ((p.rows > 0 && !y && !residual_out) || !aligned16(y) || !aligned16(residual_out))
+    return ONELA_EINVAL;
+  p.y = y;
+  p.h = residual_out;
+  const hipError_t e = onela::launch_block_norm(
+      p, cfg->io_dtype == ONELA_BF16, cfg->residual_dtype == ONELA_BF16, device_compute_units(),
+      static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+size_t onela_block_norm_workspace_bytes(const onela_block_norm_config_t* cfg) {
+  return onela::check_block_norm(cfg) == ONELA_OK ? onela::block_norm_workspace_bytes(cfg) : 0;
+}
+
+onela_status_t onela_block_norm_backward(
+    const onela_block_norm_config_t* cfg, const void* x, const void* gate, const void* residual,
+    const float* after_weight, const float* before_weight, const float* channel_scale,
+    const void* d_y, const void* d_residual_out, void* dx, void* dgate, void* d_residual,
+    float* dafter_weight, float* dbefore_weight, float* dchannel_scale, void* workspace,
+    size_t workspace_bytes, void* stream) {
+  onela::BlockNormParams p;
+  const onela_status_t rc =
+      block_norm_inputs(cfg, x, gate, residual, after_weight, before_weight, channel_scale, &p);
+  if (rc != ONELA_OK) return rc;
+  if (p.rows > 0 && (!dx || (!d_y && !d_residual_out))) return ONELA_EINVAL;
+  if (dgate && cfg->gate_act == ONELA_ACT_NONE) return ONELA_EINVAL;
+  if ((dafter_weight && !cfg->norm_after) || (dbefore_weight && !cfg->norm_before))
+    return ONELA_EINVAL;
+  if (!aligned16(d_y) || !aligned16(d_residual_out) || !aligned16(dx) || !aligned16(dgate) ||
+      !aligned16(d_residual) || !aligned4(dafter_weight) || !aligned4(dbefore_weight) ||
+      !aligned4(dchannel_scale))
+    return ONELA_EINVAL;
+  if (dafter_weight || dbefore_weight || dchannel_scale) {
+    if (!workspace || !aligned256(workspace)) return ONELA_EINVAL;
+    if (workspace_bytes < onela::block_norm_workspace_bytes(cfg)) return ONELA_ECAPACITY;
+    p.partial = static_cast<float*>(workspace);
+  }
+  p.dy = d_y;
+  p.dh = d_residual_out;
+  p.dx = dx;
+  p.dgate = dgate;
+  p.dres = d_residual;
+  p.dwa = dafter_weight;
+  p.dwb = dbefore_weight;
+  p.dcs = dchannel_scale;
+  const hipError_t e = onela::launch_block_norm_backward(
+      p, cfg->io_dtype == ONELA_BF16, cfg->residual_dtype == ONELA_BF16, device_compute_units(),
+      static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+// ---- log probabilities of tokens --------------------------------------------------------
+
+namespace {
+bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+onela_status_t logprob_inputs(const onela_logprob_config_t* c, const void* logits,
+                              const int32_t* given, onela::LogprobParams* p) {
+  const onela_status_t rc = onela::check_logprob(c);
+  if (rc != ONELA_OK) return rc;
+  if (c->num_rows > 0 && (!logits || (c->num_given > 0 && !given))) return ONELA_EINVAL;
+  if (!aligned_to(logits, io_bytes(c->io_dtype)) || !aligned4(given)) return ONELA_EINVAL;
+  *p = onela::LogprobParams{};
+  p->x = logits;
+  p->given = given;
+  p->R = long(c->num_rows);
+  p->xs = c->logits_stride ? long(c->logits_stride) : long(c->vocab);
+  p->scale = c->scale;
+  p->V = c->vocab;
+  p->G = c->num_given;
+  return ONELA_OK;
+}
+}  // namespace
+
+size_t onela_token_logprobs_workspace_bytes(const onela_logprob_config_t* cfg) {
+  return onela::check_logprob(cfg) == ONELA_OK ? onela::logprob_workspace_bytes(cfg) : 0;
+}
+
+onela_status_t onela_token_logprobs(const onela_logprob_config_t* cfg, const void* logits,
+                                    const int32_t* given, float* logp_out, float* lse_out,
+                                    float* entropy_out, int32_t* top_tokens_out,
+                                    float* top_logp_out, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  onela::LogprobParams p;
+  const onela_status_t rc = logprob_inputs(cfg, logits, given, &p);
+  if (rc != ONELA_OK) return rc;
+  if (p.R > 0 && ((p.G > 0 && !logp_out) ||
+                  (cfg->num_top > 0 && (!top_tokens_out || !top_logp_out))))
+    return ONELA_EINVAL;
+  if (!aligned4(logp_out) || !aligned4(lse_out) || !aligned4(entropy_out) ||
+      !aligned4(top_tokens_out) || !aligned4(top_logp_out))
+    return ONELA_EINVAL;
+  if (!workspace || !aligned256(workspace)) return ONELA_EINVAL;
+  if (workspace_bytes < onela::logprob_workspace_bytes(cfg)) return ONELA_ECAPACITY;
+  p.logp = logp_out;
+  p.lse = lse_out;
+  p.entropy = entropy_out;
+  p.K = cfg->num_top;
+  p.top = top_tokens_out;
+  p.top_logp = top_logp_out;
+  p.parts = static_cast<float*>(workspace);
+  const hipError_t e =
+      onela::launch_logprobs(p, onela::logprob_plan(cfg), cfg->io_dtype == ONELA_BF16,
+                             static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
+onela_status_t onela_token_logprobs_backward(const onela_logprob_config_t* cfg,
+                                             const void* logits, const int32_t* given,
+                                             const float* lse, const float* entropy,
+                                             const float* d_logp, const float* d_lse,
+                                             const float* d_entropy, void* d_logits,
+                                             void* stream) {
+  onela::LogprobParams p;
+  const onela_status_t rc = logprob_inputs(cfg, logits, given, &p);
+  if (rc != ONELA_OK) return rc;
+  if (p.R > 0 && (!lse || !d_logits || (p.G > 0 && !d_logp) || (d_entropy && !entropy)))
+    return ONELA_EINVAL;
+  if (!aligned4(lse) || !aligned4(entropy) || !aligned4(d_logp) || !aligned4(d_lse) ||
+      !aligned4(d_entropy) || !aligned_to(d_logits, io_bytes(cfg->io_dtype)))
+    return ONELA_EINVAL;
+  // (in place: where every row is written over itself)
+  if (onela::overlap(d_logits, span(p.R, p.V, p.V, cfg->io_dtype), logits,
+                     span(p.R, p.xs, p.V, cfg->io_dtype)) &&
+      !(d_logits == logits && p.xs == p.V))
+    return ONELA_EINVAL;
+  p.lse_in = lse;
+  p.entropy_in = entropy;
+  p.dlogp = d_logp;
+  p.dlse = d_lse;
+  p.dentropy = d_entropy;
+  p.dx = d_logits;
+  const hipError_t e = onela::launch_logprobs_backward(p, cfg->io_dtype == ONELA_BF16,
+                                                       static_cast<hipStream_t>(stream));
+  return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
+}
+
 }  // extern "C"

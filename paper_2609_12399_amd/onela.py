@@ -24,6 +24,7 @@ ONELA_RECORD_INPUTS, ONELA_RECORD_DELTA = 0, 1
 ONELA_RECORDS_COPY, ONELA_RECORDS_BORROW = 0, 1
 ONELA_NORM_L2, ONELA_NORM_RMS = 0, 1
 ONELA_ROTATE_HALVES, ONELA_ROTATE_PAIRS = 0, 1
+ONELA_ACT_NONE, ONELA_ACT_SILU, ONELA_ACT_SIGMOID = 0, 1, 2
 
 STATUS_NAMES = {0: "ONELA_OK", 1: "ONELA_EINVAL", 2: "ONELA_ESTEP", 3: "ONELA_EPARENT",
                 4: "ONELA_ECAPACITY", 5: "ONELA_EHIP", 6: "ONELA_ENOMEM"}
@@ -39,7 +40,11 @@ EXPORTED = ["onela_status_str", "onela_check_config", "onela_workspace_bytes", "
             "onela_delta_rule_workspace_bytes", "onela_delta_rule_forward",
             "onela_delta_rule_backward", "onela_delta_rule_step",
             "onela_qk_norm_rope_workspace_bytes", "onela_qk_norm_rope",
-            "onela_qk_norm_rope_backward"]
+            "onela_qk_norm_rope_backward",
+            "onela_short_conv", "onela_short_conv_workspace_bytes", "onela_short_conv_backward",
+            "onela_short_conv_step", "onela_block_norm", "onela_block_norm_workspace_bytes",
+            "onela_block_norm_backward", "onela_token_logprobs_workspace_bytes",
+            "onela_token_logprobs", "onela_token_logprobs_backward"]
 
 
 class OnelaError(RuntimeError):
@@ -108,6 +113,67 @@ def make_norm_config(num_tokens, num_q_heads, num_k_heads, head_dim, io_dtype, n
                                table_rows, io_dtype, norm, rotation, q_stride, k_stride, eps)
 
 
+_IO = {"bf16": ONELA_BF16, "f32": ONELA_F32}
+_ACT = {None: ONELA_ACT_NONE, "silu": ONELA_ACT_SILU, "sigmoid": ONELA_ACT_SIGMOID}
+
+
+class onela_conv_config_t(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("channels", ctypes.c_int32),
+                ("taps", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("total_tokens", ctypes.c_int64),
+                ("x_stride", ctypes.c_int64)]
+
+
+def make_conv_config(num_seqs, total_tokens, channels, taps, io_dtype, activation="silu",
+                     x_stride=0) -> onela_conv_config_t:
+    if isinstance(io_dtype, str):
+        io_dtype = _IO[io_dtype]
+    if activation is None or isinstance(activation, str):
+        activation = _ACT[activation]
+    return onela_conv_config_t(num_seqs, channels, taps, io_dtype, activation, total_tokens,
+                               x_stride)
+
+
+class onela_block_norm_config_t(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int64), ("num_heads", ctypes.c_int32),
+                ("width", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
+                ("residual_dtype", ctypes.c_int32), ("norm_after", ctypes.c_int32),
+                ("norm_before", ctypes.c_int32), ("gate_act", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("gate_stride", ctypes.c_int64),
+                ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+def make_block_norm_config(num_tokens, num_heads, width, io_dtype, residual_dtype=None,
+                           norm_after=False, norm_before=True, gate=None, residual_scale=1.0,
+                           eps=1e-6, x_stride=0, gate_stride=0) -> onela_block_norm_config_t:
+    if isinstance(io_dtype, str):
+        io_dtype = _IO[io_dtype]
+    if residual_dtype is None:
+        residual_dtype = io_dtype
+    if isinstance(residual_dtype, str):
+        residual_dtype = _IO[residual_dtype]
+    if gate is None or isinstance(gate, str):
+        gate = _ACT[gate]
+    return onela_block_norm_config_t(num_tokens, num_heads, width, io_dtype, residual_dtype,
+                                     int(norm_after), int(norm_before), gate, x_stride,
+                                     gate_stride, residual_scale, eps)
+
+
+class onela_logprob_config_t(ctypes.Structure):
+    _fields_ = [("num_rows", ctypes.c_int64), ("vocab", ctypes.c_int32),
+                ("num_given", ctypes.c_int32), ("num_top", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("logits_stride", ctypes.c_int64),
+                ("scale", ctypes.c_float)]
+
+
+def make_logprob_config(num_rows, vocab, num_given, num_top, io_dtype, scale=1.0,
+                        logits_stride=0) -> onela_logprob_config_t:
+    if isinstance(io_dtype, str):
+        io_dtype = _IO[io_dtype]
+    return onela_logprob_config_t(num_rows, vocab, num_given, num_top, io_dtype, logits_stride,
+                                  scale)
+
+
 _lib = None
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
@@ -129,6 +195,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     cfgp = ctypes.POINTER(onela_config_t)
     deltap = ctypes.POINTER(onela_delta_config_t)
     normp = ctypes.POINTER(onela_norm_config_t)
+    convp = ctypes.POINTER(onela_conv_config_t)
+    blockp = ctypes.POINTER(onela_block_norm_config_t)
+    logpp = ctypes.POINTER(onela_logprob_config_t)
     sig = {
         "onela_status_str": ([_I32], ctypes.c_char_p),
         "onela_check_config": ([cfgp], _I32),
@@ -159,6 +228,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "onela_qk_norm_rope_workspace_bytes": ([normp], ctypes.c_size_t),
         "onela_qk_norm_rope": ([normp] + [_P] * 9, _I32),
         "onela_qk_norm_rope_backward": ([normp] + [_P] * 13 + [ctypes.c_size_t, _P], _I32),
+        "onela_short_conv": ([convp] + [_P] * 8, _I32),
+        "onela_short_conv_workspace_bytes": ([convp], ctypes.c_size_t),
+        "onela_short_conv_backward": ([convp] + [_P] * 12 + [ctypes.c_size_t, _P], _I32),
+        "onela_short_conv_step": ([convp] + [_P] * 5 + [_I32, _P, _P, _I32] + [_P] * 3, _I32),
+        "onela_block_norm": ([blockp] + [_P] * 9, _I32),
+        "onela_block_norm_workspace_bytes": ([blockp], ctypes.c_size_t),
+        "onela_block_norm_backward": ([blockp] + [_P] * 15 + [ctypes.c_size_t, _P], _I32),
+        "onela_token_logprobs_workspace_bytes": ([logpp], ctypes.c_size_t),
+        "onela_token_logprobs": ([logpp] + [_P] * 8 + [ctypes.c_size_t, _P], _I32),
+        "onela_token_logprobs_backward": ([logpp] + [_P] * 9, _I32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -201,6 +280,19 @@ def _rows(x, name: str, stride: int, optional: bool = False):
             (shape[0] > 1 and at[0] != stride))):
         raise ValueError(f"{name} must be [tokens][heads][width] with {stride} elements "
                          "between tokens and dense heads")
+    return x.data_ptr()
+
+
+def _rows2(x, name: str, stride: int, optional: bool = False):
+    """As :func:`_rows` for a [rows][width] matrix."""
+    if not stride or not hasattr(x, "data_ptr"):
+        return _dev(x, name, optional)
+    if not getattr(x, "is_cuda", False):
+        raise ValueError(f"{name} must be a GPU tensor")
+    shape, at = x.shape, x.stride()
+    if len(shape) != 2 or (0 not in shape and ((shape[1] > 1 and at[1] != 1) or
+                                               (shape[0] > 1 and at[0] != stride))):
+        raise ValueError(f"{name} must be [rows][width] with {stride} elements between rows")
     return x.data_ptr()
 
 
@@ -453,3 +545,103 @@ def onela_qk_norm_rope_backward(cfg: onela_norm_config_t, q, k, q_weight, k_weig
         _dev(dk, "dk", nokey), _dev(dq_weight, "dq_weight", True),
         _dev(dk_weight, "dk_weight", True), _dev(workspace, "workspace", True),
         int(workspace_bytes), _stream(stream)), "onela_qk_norm_rope_backward")
+
+
+def onela_short_conv(cfg: onela_conv_config_t, seq_offsets, x, weight, bias, initial_state, y,
+                     final_state, stream=None):
+    none = cfg.total_tokens == 0
+    _check((_lib or load_library()).onela_short_conv(
+        ctypes.byref(cfg), _dev(seq_offsets, "seq_offsets", True),
+        _rows2(x, "x", cfg.x_stride, none), _dev(weight, "weight"), _dev(bias, "bias", True),
+        _dev(initial_state, "initial_state", True), _dev(y, "y", none),
+        _dev(final_state, "final_state", True), _stream(stream)), "onela_short_conv")
+
+
+def onela_short_conv_workspace_bytes(cfg: onela_conv_config_t) -> int:
+    return load_library().onela_short_conv_workspace_bytes(ctypes.byref(cfg))
+
+
+def onela_short_conv_backward(cfg: onela_conv_config_t, seq_offsets, x, weight, bias,
+                              initial_state, d_y, d_final_state, dx, dweight=None, dbias=None,
+                              d_initial_state=None, workspace=None, workspace_bytes: int = 0,
+                              stream=None):
+    none = cfg.total_tokens == 0
+    _check((_lib or load_library()).onela_short_conv_backward(
+        ctypes.byref(cfg), _dev(seq_offsets, "seq_offsets", True),
+        _rows2(x, "x", cfg.x_stride, none), _dev(weight, "weight"), _dev(bias, "bias", True),
+        _dev(initial_state, "initial_state", True), _dev(d_y, "d_y", none),
+        _dev(d_final_state, "d_final_state", True), _dev(dx, "dx", none),
+        _dev(dweight, "dweight", True), _dev(dbias, "dbias", True),
+        _dev(d_initial_state, "d_initial_state", True), _dev(workspace, "workspace", True),
+        int(workspace_bytes), _stream(stream)), "onela_short_conv_backward")
+
+
+def onela_short_conv_step(cfg: onela_conv_config_t, seq_offsets, x, weight, bias, state,
+                          num_slots: int, slots, state_out, num_slots_out: int, slots_out, y,
+                          stream=None):
+    none = cfg.total_tokens == 0
+    _check((_lib or load_library()).onela_short_conv_step(
+        ctypes.byref(cfg), _dev(seq_offsets, "seq_offsets", True),
+        _rows2(x, "x", cfg.x_stride, none), _dev(weight, "weight"), _dev(bias, "bias", True),
+        _dev(state, "state"), num_slots, _dev(slots, "slots", True),
+        _dev(state_out, "state_out", True), num_slots_out, _dev(slots_out, "slots_out", True),
+        _dev(y, "y", none), _stream(stream)), "onela_short_conv_step")
+
+
+def onela_block_norm(cfg: onela_block_norm_config_t, x, gate, residual, after_weight,
+                     before_weight, channel_scale, y, residual_out, stream=None):
+    _check((_lib or load_library()).onela_block_norm(
+        ctypes.byref(cfg), _rows(x, "x", cfg.x_stride, cfg.num_tokens == 0),
+        _rows(gate, "gate", cfg.gate_stride, True), _dev(residual, "residual", True),
+        _dev(after_weight, "after_weight", True), _dev(before_weight, "before_weight", True),
+        _dev(channel_scale, "channel_scale", True), _dev(y, "y", True),
+        _dev(residual_out, "residual_out", True), _stream(stream)), "onela_block_norm")
+
+
+def onela_block_norm_workspace_bytes(cfg: onela_block_norm_config_t) -> int:
+    return load_library().onela_block_norm_workspace_bytes(ctypes.byref(cfg))
+
+
+def onela_block_norm_backward(cfg: onela_block_norm_config_t, x, gate, residual, after_weight,
+                              before_weight, channel_scale, d_y, d_residual_out, dx, dgate=None,
+                              d_residual=None, dafter_weight=None, dbefore_weight=None,
+                              dchannel_scale=None, workspace=None, workspace_bytes: int = 0,
+                              stream=None):
+    none = cfg.num_tokens == 0
+    _check((_lib or load_library()).onela_block_norm_backward(
+        ctypes.byref(cfg), _rows(x, "x", cfg.x_stride, none),
+        _rows(gate, "gate", cfg.gate_stride, True), _dev(residual, "residual", True),
+        _dev(after_weight, "after_weight", True), _dev(before_weight, "before_weight", True),
+        _dev(channel_scale, "channel_scale", True), _dev(d_y, "d_y", True),
+        _dev(d_residual_out, "d_residual_out", True), _dev(dx, "dx", none),
+        _dev(dgate, "dgate", True), _dev(d_residual, "d_residual", True),
+        _dev(dafter_weight, "dafter_weight", True), _dev(dbefore_weight, "dbefore_weight", True),
+        _dev(dchannel_scale, "dchannel_scale", True), _dev(workspace, "workspace", True),
+        int(workspace_bytes), _stream(stream)), "onela_block_norm_backward")
+
+
+def onela_token_logprobs_workspace_bytes(cfg: onela_logprob_config_t) -> int:
+    return load_library().onela_token_logprobs_workspace_bytes(ctypes.byref(cfg))
+
+
+def onela_token_logprobs(cfg: onela_logprob_config_t, logits, given, logp_out, lse_out,
+                         entropy_out, top_tokens_out, top_logp_out, workspace,
+                         workspace_bytes: int, stream=None):
+    _check((_lib or load_library()).onela_token_logprobs(
+        ctypes.byref(cfg), _rows2(logits, "logits", cfg.logits_stride, cfg.num_rows == 0),
+        _dev(given, "given", True), _dev(logp_out, "logp_out", True),
+        _dev(lse_out, "lse_out", True), _dev(entropy_out, "entropy_out", True),
+        _dev(top_tokens_out, "top_tokens_out", True), _dev(top_logp_out, "top_logp_out", True),
+        _dev(workspace, "workspace"), int(workspace_bytes), _stream(stream)),
+        "onela_token_logprobs")
+
+
+def onela_token_logprobs_backward(cfg: onela_logprob_config_t, logits, given, lse, entropy, d_logp,
+                                  d_lse, d_entropy, d_logits, stream=None):
+    none = cfg.num_rows == 0
+    _check((_lib or load_library()).onela_token_logprobs_backward(
+        ctypes.byref(cfg), _rows2(logits, "logits", cfg.logits_stride, none),
+        _dev(given, "given", True), _dev(lse, "lse", none), _dev(entropy, "entropy", True),
+        _dev(d_logp, "d_logp", True), _dev(d_lse, "d_lse", True),
+        _dev(d_entropy, "d_entropy", True), _dev(d_logits, "d_logits", none), _stream(stream)),
+        "onela_token_logprobs_backward")

@@ -421,3 +421,272 @@ class QkNormRope:
                                        d_q_out, d_k_out, self.q, self.k, dwq, dwk,
                                        self.workspace, self.ws_bytes, self.stream)
         return self.q, self.k, dwq, dwk
+
+
+def _on_current_device(x):
+    """ValueError unless x is on the current device: the call is enqueued on a stream of that."""
+    torch = _torch()
+    if x.is_cuda and x.get_device() != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {x.device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+
+
+class _OnDevice:
+    """What the objects below share: tensors of one device, views that may stand in wider rows."""
+
+    def _check(self, x, *expected):
+        _expect(*expected)
+        if not isinstance(x, int) and x is not None:
+            _on_current_device(x)
+
+    @staticmethod
+    def _stride(x):
+        return 0 if x is None or isinstance(x, int) or x.is_contiguous() else x.stride(0)
+
+
+class ShortConv(_OnDevice):
+    """The short causal convolution of packed sequences (onela_short_conv and, with
+    ``backward``, onela_short_conv_backward) for fixed sizes: owns the workspace and the
+    output tensors, which every call writes again.
+
+    Sequences are packed as in :class:`DeltaRule`; x [total_tokens, channels] may be a view
+    into wider rows.  Rows of y and dx behind the last sequence are left as they were."""
+
+    def __init__(self, num_seqs: int, total_tokens: int, channels: int, taps: int,
+                 io: str = "bf16", activation: str | None = "silu", backward: bool = False,
+                 device="cuda:0", stream=None):
+        torch = _torch()
+        self.cfg = ab.make_conv_config(num_seqs, total_tokens, channels, taps, io, activation)
+        self.ws_bytes = ab.onela_short_conv_workspace_bytes(self.cfg)
+        if self.ws_bytes == 0:
+            raise ab.OnelaError(ab.ONELA_EINVAL, "onela_short_conv_workspace_bytes")
+        self.stream, self.is_backward = stream, backward
+        dt = _io_tensor_dtype(io)
+        self.dtypes = dt, torch.float32, torch.int32
+        rows, states = (total_tokens, channels), (num_seqs, taps - 1, channels)
+        self.shapes = rows, (channels, taps), (channels,), (num_seqs + 1,), states
+        state = torch.empty(states, dtype=dt, device=device)
+        if backward:
+            self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+            self.dx, self.d_initial_state = torch.empty(rows, dtype=dt, device=device), state
+            self.dweight = torch.empty((channels, taps), dtype=torch.float32, device=device)
+            self.dbias = torch.empty(channels, dtype=torch.float32, device=device)
+        else:
+            self.y, self.final_state = torch.empty(rows, dtype=dt, device=device), state
+
+    def _set(self, x, weight, bias, seq_offsets, initial_state):
+        dt, f32, i32 = self.dtypes
+        rows, weights, channels, bounds, states = self.shapes
+        self._check(x, (x, "x", rows, dt), (weight, "weight", weights, f32),
+                    (bias, "bias", channels, f32), (seq_offsets, "seq_offsets", bounds, i32),
+                    (initial_state, "initial_state", states, dt))
+        self.cfg.x_stride = self._stride(x)
+
+    def forward(self, x, weight, bias=None, seq_offsets=None, initial_state=None):
+        """(y, final_state)"""
+        if self.is_backward:
+            raise ValueError("this object holds the backward call's tensors")
+        self._set(x, weight, bias, seq_offsets, initial_state)
+        ab.onela_short_conv(self.cfg, seq_offsets, x, weight, bias, initial_state, self.y,
+                            self.final_state, self.stream)
+        return self.y, self.final_state
+
+    def backward(self, x, weight, d_y, bias=None, seq_offsets=None, initial_state=None,
+                 d_final_state=None):
+        """(dx, dweight, dbias or None without a bias, d_initial_state or None without one)"""
+        if not self.is_backward:
+            raise ValueError("this object holds the forward call's tensors")
+        self._set(x, weight, bias, seq_offsets, initial_state)
+        _expect((d_y, "d_y", self.shapes[0], self.dtypes[0]),
+                (d_final_state, "d_final_state", self.shapes[4], self.dtypes[0]))
+        db = None if bias is None else self.dbias
+        ds = None if initial_state is None else self.d_initial_state
+        ab.onela_short_conv_backward(self.cfg, seq_offsets, x, weight, bias, initial_state, d_y,
+                                     d_final_state, self.dx, self.dweight, db, ds,
+                                     self.workspace, self.ws_bytes, self.stream)
+        return self.dx, self.dweight, db, ds
+
+
+class ShortConvStep(_OnDevice):
+    """The convolution of one token (or a few) per sequence on a pool of ``num_slots`` states
+    (onela_short_conv_step) for fixed sizes: owns the output tensor."""
+
+    def __init__(self, num_seqs: int, total_tokens: int, channels: int, taps: int, io: str,
+                 num_slots: int, activation: str | None = "silu", device="cuda:0", stream=None):
+        torch = _torch()
+        self.cfg = ab.make_conv_config(num_seqs, total_tokens, channels, taps, io, activation)
+        self.num_slots, self.stream = num_slots, stream
+        dt = _io_tensor_dtype(io)
+        self.dtypes = dt, torch.float32, torch.int32
+        self.state = taps - 1, channels
+        self.shapes = ((total_tokens, channels), (channels, taps), (channels,), (num_seqs + 1,),
+                       (num_seqs,))
+        self.y = torch.empty((total_tokens, channels), dtype=dt, device=device)
+
+    def step(self, pool, slots, x, weight, bias=None, seq_offsets=None, pool_out=None,
+             slots_out=None):
+        """y; the pool's states move on in place, or from their slots to those of pool_out."""
+        dt, f32, i32 = self.dtypes
+        rows, weights, channels, bounds, seqs = self.shapes
+        self._check(x, (x, "x", rows, dt), (weight, "weight", weights, f32),
+                    (bias, "bias", channels, f32), (seq_offsets, "seq_offsets", bounds, i32),
+                    (slots, "slots", seqs, i32), (slots_out, "slots_out", seqs, i32))
+        slots_of_out = 0
+        if not isinstance(pool, int) and pool is not None:  # (more slots do no harm)
+            _expect((pool, "pool", (max(self.num_slots, *pool.shape[:1]), *self.state), dt))
+        if pool_out is not None:
+            _expect((pool_out, "pool_out", (*pool_out.shape[:1], *self.state), dt))
+            slots_of_out = pool_out.shape[0]
+        self.cfg.x_stride = self._stride(x)
+        ab.onela_short_conv_step(self.cfg, seq_offsets, x, weight, bias, pool, self.num_slots,
+                                 slots, pool_out, slots_of_out, slots_out, self.y, self.stream)
+        return self.y
+
+
+class BlockNorm(_OnDevice):
+    """Norms before and after a block with its gate and residual scale (onela_block_norm and,
+    with ``backward``, onela_block_norm_backward) for fixed sizes: owns the output tensors and
+    the workspace.
+
+    x and gate are [num_tokens, num_heads, width] and may be views into wider rows; ``gate`` is
+    the gate's activation ("silu", "sigmoid") or None without one, ``residual_io`` the residual
+    stream's type (None: io).  y is not formed where a residual is given and no norm is
+    before the next block."""
+
+    def __init__(self, num_tokens: int, width: int, num_heads: int = 1, io: str = "bf16",
+                 residual_io: str | None = None, norm_after: bool = False,
+                 norm_before: bool = True, gate: str | None = None, residual_scale: float = 1.0,
+                 eps: float = 1e-6, backward: bool = False, device="cuda:0", stream=None):
+        torch = _torch()
+        self.cfg = ab.make_block_norm_config(num_tokens, num_heads, width, io, residual_io,
+                                             norm_after, norm_before, gate, residual_scale, eps)
+        self.ws_bytes = ab.onela_block_norm_workspace_bytes(self.cfg)
+        if self.ws_bytes == 0:
+            raise ab.OnelaError(ab.ONELA_EINVAL, "onela_block_norm_workspace_bytes")
+        self.stream, self.is_backward = stream, backward
+        self.after, self.before, self.gated = norm_after, norm_before, gate is not None
+        dt, rt = _io_tensor_dtype(io), _io_tensor_dtype(residual_io or io)
+        self.dtypes = dt, rt, torch.float32
+        self.shape, self.width = (num_tokens, num_heads, width), (width,)
+        self.device = device
+        self.made = {}  # output tensors, made when a call first has use for them
+        if backward:
+            self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+            self.dw = torch.empty((3, width), dtype=torch.float32, device=device)
+
+    def _out(self, name, dtype):
+        if name not in self.made:
+            self.made[name] = _torch().empty(self.shape, dtype=dtype, device=self.device)
+        return self.made[name]
+
+    def _set(self, x, residual, gate, after_weight, before_weight, channel_scale):
+        dt, rt, f32 = self.dtypes
+        shape, width = self.shape, self.width
+        self._check(x, (x, "x", shape, dt), (gate, "gate", shape, dt),
+                    (residual, "residual", shape, rt), (after_weight, "after_weight", width, f32),
+                    (before_weight, "before_weight", width, f32),
+                    (channel_scale, "channel_scale", width, f32))
+        if self.gated != (gate is not None):
+            raise ValueError("gate must be given" if self.gated else "this object has no gate")
+        self.cfg.x_stride, self.cfg.gate_stride = self._stride(x), self._stride(gate)
+
+    def forward(self, x, residual=None, gate=None, after_weight=None, before_weight=None,
+                channel_scale=None):
+        """(y or None, residual_out or None without a residual)"""
+        if self.is_backward:
+            raise ValueError("this object holds the backward call's tensors")
+        self._set(x, residual, gate, after_weight, before_weight, channel_scale)
+        y = self._out("y", self.dtypes[0]) if self.before or residual is None else None
+        h = None if residual is None else self._out("h", self.dtypes[1])
+        ab.onela_block_norm(self.cfg, x, gate, residual, after_weight, before_weight,
+                            channel_scale, y, h, self.stream)
+        return y, h
+
+    def backward(self, x, d_y, residual=None, gate=None, after_weight=None, before_weight=None,
+                 channel_scale=None, d_residual_out=None):
+        """(dx, d_residual, d_gate, d_after_weight, d_before_weight, d_channel_scale; None for
+        what is not given)"""
+        if not self.is_backward:
+            raise ValueError("this object holds the forward call's tensors")
+        self._set(x, residual, gate, after_weight, before_weight, channel_scale)
+        dt, rt, _ = self.dtypes
+        _expect((d_y, "d_y", self.shape, dt), (d_residual_out, "d_residual_out", self.shape, rt))
+        dx = self._out("dx", dt)
+        dg = None if gate is None else self._out("dgate", dt)
+        dr = None if residual is None else self._out("dres", rt)
+        dw = [None if w is None else self.dw[i]
+              for i, w in enumerate((after_weight, before_weight, channel_scale))]
+        ab.onela_block_norm_backward(self.cfg, x, gate, residual, after_weight, before_weight,
+                                     channel_scale, d_y, d_residual_out, dx, dg, dr, *dw,
+                                     self.workspace, self.ws_bytes, self.stream)
+        return (dx, dr, dg, *dw)
+
+
+class TokenLogprobs(_OnDevice):
+    """Log probabilities of given tokens and of the ``num_top`` best, with the logarithm of the
+    sum and, where wanted, the entropy (onela_token_logprobs and, with ``backward``,
+    onela_token_logprobs_backward) for fixed sizes: owns the output tensors and the workspace.
+
+    logits [num_rows, vocab] may be a view into wider rows; ``scale`` is one over the
+    temperature."""
+
+    def __init__(self, num_rows: int, vocab: int, num_given: int = 1, num_top: int = 0,
+                 io: str = "bf16", scale: float = 1.0, entropy: bool = False,
+                 backward: bool = False, device="cuda:0", stream=None):
+        torch = _torch()
+        self.cfg = ab.make_logprob_config(num_rows, vocab, num_given, num_top, io, scale)
+        self.ws_bytes = ab.onela_token_logprobs_workspace_bytes(self.cfg)
+        if self.ws_bytes == 0:
+            raise ab.OnelaError(ab.ONELA_EINVAL, "onela_token_logprobs_workspace_bytes")
+        self.stream, self.is_backward = stream, backward
+        self.dtypes = _io_tensor_dtype(io), torch.float32, torch.int32
+        self.shapes = (num_rows, vocab), (num_rows, num_given), (num_rows,)
+        self.num_given = num_given
+
+        def tensor(*shape, dtype=torch.float32):
+            return torch.empty(shape, dtype=dtype, device=device)
+
+        if backward:
+            self.d_logits = tensor(num_rows, vocab, dtype=self.dtypes[0])
+            return
+        self.workspace = tensor(self.ws_bytes, dtype=torch.uint8)
+        self.logp = tensor(num_rows, num_given) if num_given else None
+        self.lse = tensor(num_rows)
+        self.entropy = tensor(num_rows) if entropy else None
+        self.top_tokens = tensor(num_rows, num_top, dtype=torch.int32) if num_top else None
+        self.top_logp = tensor(num_rows, num_top) if num_top else None
+
+    def _set(self, logits, given):
+        dt, _, i32 = self.dtypes
+        self._check(logits, (logits, "logits", self.shapes[0], dt),
+                    (given, "given", self.shapes[1], i32))
+        if (given is None) != (self.num_given == 0):
+            raise ValueError("given must be there exactly if num_given > 0")
+        self.cfg.logits_stride = self._stride(logits)
+
+    def forward(self, logits, given=None):
+        """(logp [rows, num_given], lse [rows], entropy [rows], top_tokens, top_logp
+        [rows, num_top]; None for what is not wanted)"""
+        if self.is_backward:
+            raise ValueError("this object holds the backward call's tensors")
+        self._set(logits, given)
+        ab.onela_token_logprobs(self.cfg, logits, given, self.logp, self.lse, self.entropy,
+                                self.top_tokens, self.top_logp, self.workspace, self.ws_bytes,
+                                self.stream)
+        return self.logp, self.lse, self.entropy, self.top_tokens, self.top_logp
+
+    def backward(self, logits, given, lse, d_logp=None, d_lse=None, entropy=None, d_entropy=None,
+                 out=None):
+        """d_logits; written to ``out`` where given, which may be the (dense) logits."""
+        if not self.is_backward:
+            raise ValueError("this object holds the forward call's tensors")
+        self._set(logits, given)
+        f32, rows = self.dtypes[1], self.shapes[2]
+        out = self.d_logits if out is None else out
+        _expect((lse, "lse", rows, f32), (d_logp, "d_logp", self.shapes[1], f32),
+                (d_lse, "d_lse", rows, f32), (entropy, "entropy", rows, f32),
+                (d_entropy, "d_entropy", rows, f32),
+                (out, "out", self.shapes[0], self.dtypes[0]))
+        ab.onela_token_logprobs_backward(self.cfg, logits, given, lse, entropy, d_logp, d_lse,
+                                         d_entropy, out, self.stream)
+        return out
