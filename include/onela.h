@@ -567,7 +567,7 @@ onela_status_t onela_short_conv_step(const onela_conv_config_t* cfg, const int32
  *   weights, channel_scale  device fp32 [width], or NULL (1)
  *   y             device, dense, io dtype, or NULL (not wanted)
  *   residual_out  h, device, dense, residual_dtype, or NULL; may be residual
- * width: a multiple of 8 up to 16384.  fp32 inside (y is formed from h before its rounding),
+ * width: a multiple of 8 up to 8192.  fp32 inside (y is formed from h before its rounding),
  * one rounding at each store. */
 typedef struct {
   int64_t num_tokens;     /* < 2^31 */

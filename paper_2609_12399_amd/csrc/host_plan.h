@@ -143,9 +143,10 @@ onela_status_t check_norm(const onela_norm_config_t* cfg);
 size_t norm_workspace_bytes(const onela_norm_config_t* cfg);
 
 // ---- short causal convolution -------------------------------------------------------
-// Threads take 8 channels and a run of tokens each; a workgroup of kConvThreads has
+// Threads take kConvLane channels and a run of tokens each; a workgroup of kConvThreads has
 // 2^lanes_log2 channel groups side by side and as many runs as that leaves.
 constexpr int kConvThreads = 256;
+constexpr int kConvLane = 4;
 constexpr int kConvMaxTaps = 4;
 struct ConvPlan {
   int lanes_log2;   // channel groups of a workgroup

@@ -8,64 +8,67 @@
 //   dwa = sum dn n,   dx = r(x) (wa dn - x r(x)^2 mean(wa dn x)).
 // All in fp32; h and y are rounded once, at their stores (y is formed from the unrounded h).
 //
-// A row is held by LANES lanes with NV times 8 columns each: a part of a wave, or a whole
-// workgroup whose waves exchange their sums through LDS (two buffers in turn, so that one
-// barrier per sum is enough).  Workgroups stay and walk over rows, with the weights in registers
-// and the next row on its way while this one is worked on.  Bound: HBM.
+// A row is held by LANES lanes with 8 columns each: a part of a wave, or a whole workgroup whose
+// waves exchange their sums through LDS (two buffers in turn, so that one barrier per sum is
+// enough).  Workgroups stay and walk over rows, with the weights in registers and the next row on
+// its way while this one is worked on.  Bound: HBM.
 #include "device_common.h"
 #include "internal.h"
 
 namespace onela {
 namespace {
 
-// Sum over the LANES lanes of a row, in every one of them; `turn` counts the calls.
-template <int LANES>
-__device__ inline float row_sum(float x, int& turn) {
-  if constexpr (LANES <= 64) {
-    return group_sum<LANES>(x);
-  } else {
-    constexpr int W = LANES / 64;
-    __shared__ float part[2][W];
-    x = group_sum<64>(x);
-    float* const b = part[turn & 1];
-    ++turn;
-    if ((threadIdx.x & 63) == 0) b[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = b[0];
-#pragma unroll
-    for (int i = 1; i < W; ++i) x += b[i];
-    return x;
-  }
+constexpr int E = 8;  // columns of a lane
+
+// Sum over the wave, in every lane: within rows of 16 lanes as group_sum, then row 0 to 1 and 2 to
+// 3, then lane 31 to the upper half (no exchange through LDS).
+__device__ inline float wave_sum(float x) {
+  x = group_sum<16>(x);
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x142,
+                                                             0xa, 0xf, false));
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x143,
+                                                             0xc, 0xf, false));
+  return __builtin_bit_cast(float,
+                            __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
-// Two sums at once.
-template <int LANES>
-__device__ inline void row_sum2(float& x, float& y, int& turn) {
-  if constexpr (LANES <= 64) {
-    x = group_sum<LANES>(x);
-    y = group_sum<LANES>(y);
-  } else {
-    constexpr int W = LANES / 64;
-    __shared__ float2 part[2][W];
-    x = group_sum<64>(x);
-    y = group_sum<64>(y);
-    float2* const b = part[turn & 1];
-    ++turn;
-    if ((threadIdx.x & 63) == 0) b[threadIdx.x >> 6] = make_float2(x, y);
-    __syncthreads();
-    x = b[0].x;
-    y = b[0].y;
+// Sums over the LANES lanes of a row, in every one of them; `turn` counts the calls.
+template <int LANES, int N>
+__device__ inline void row_sums(float (&x)[N], int& turn) {
+  if constexpr (LANES < 64) {
 #pragma unroll
-    for (int i = 1; i < W; ++i) {
-      x += b[i].x;
-      y += b[i].y;
+    for (int k = 0; k < N; ++k) x[k] = group_sum<LANES>(x[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = wave_sum(x[k]);
+  }
+  if constexpr (LANES > 64) {
+    constexpr int W = LANES / 64;
+    __shared__ float part[2][N][W];
+    float(*const b)[W] = part[turn & 1];
+    ++turn;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int k = 0; k < N; ++k) b[k][threadIdx.x >> 6] = x[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      x[k] = b[k][0];
+#pragma unroll
+      for (int i = 1; i < W; ++i) x[k] += b[k][i];
     }
   }
 }
+template <int LANES>
+__device__ inline float row_sum(float x, int& turn) {
+  float v[1] = {x};
+  row_sums<LANES>(v, turn);
+  return v[0];
+}
 
-__device__ inline void vector8(const float* w, int c0, bool in, float (&x)[8]) {
+__device__ inline void vector_of(const float* w, int c0, bool in, float (&x)[E]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = w && in ? w[c0 + j] : 1.f;
+  for (int j = 0; j < E; ++j) x[j] = w && in ? w[c0 + j] : 1.f;
 }
 
 // Rows first, first + step, ... with their tokens and heads (divisions once).
@@ -90,245 +93,226 @@ struct Walk {
 };
 
 // What a lane reads of a row.
-template <int NV, bool BF16, bool RES_BF16>
+template <bool BF16, bool RES_BF16>
 struct RowIn {
-  Raw8<BF16> x[NV], g[NV];
-  Raw8<RES_BF16> r[NV];
-  __device__ void load(const BlockNormParams& p, const Walk& w, const int (&c0)[NV]) {
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (c0[v] >= p.D) continue;
-      const long c = long(w.h) * p.D + c0[v];
-      x[v].load(p.x, w.t * p.xs + c);
-      if (p.gate) g[v].load(p.gate, w.t * p.gs + c);
-      if (p.res) r[v].load(p.res, w.row * p.D + c0[v]);
-    }
+  RawN<BF16, E> x, g;
+  RawN<RES_BF16, E> r;
+  __device__ void load(const BlockNormParams& p, const Walk& w, int c0) {
+    if (c0 >= p.D) return;
+    const long c = long(w.h) * p.D + c0;
+    x.load_once(p.x, w.t * p.xs + c);
+    if (p.gate) g.load_once(p.gate, w.t * p.gs + c);
+    if (p.res) r.load_once(p.res, w.row * p.D + c0);
   }
 };
 
-__device__ inline float act(float g, bool silu) {
-  const float s = sigmoid(g);
-  return silu ? g * s : s;
-}
-
-template <int LANES, int NV, bool BF16, bool RES_BF16>
+template <int LANES, bool BF16, bool RES_BF16>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_kernel(BlockNormParams p) {
   constexpr int RW = LANES > 64 ? 1 : 256 / LANES;
-  const int sub = threadIdx.x % LANES;
   const float inv_d = 1.f / float(p.D);
-  int c0[NV], turn = 0;
-  bool in[NV];
-  float wa[NV][8], wb[NV][8], cs[NV][8];
+  const int c0 = E * int(threadIdx.x % LANES);
+  const bool in = c0 < p.D;
+  int turn = 0;
+  float wa[E], wb[E], cs[E];
+  vector_of(p.wa, c0, in, wa);
+  vector_of(p.wb, c0, in, wb);
+  vector_of(p.cs, c0, in, cs);
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    c0[v] = 8 * (v * LANES + sub);
-    in[v] = c0[v] < p.D;
-    vector8(p.wa, c0[v], in[v], wa[v]);
-    vector8(p.wb, c0[v], in[v], wb[v]);
-    vector8(p.cs, c0[v], in[v], cs[v]);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) cs[v][j] *= p.scale;
-  }
+  for (int j = 0; j < E; ++j) cs[j] *= p.scale;
   Walk ahead(long(blockIdx.x) * RW + threadIdx.x / LANES, long(gridDim.x) * RW, p.H);
-  RowIn<NV, BF16, RES_BF16> cur, next;
+  RowIn<BF16, RES_BF16> cur, next;
   if (ahead.row < p.rows) cur.load(p, ahead, c0);
   for (long row = ahead.row; row < p.rows; row += ahead.step) {  // (whole rows of lanes)
     ahead.next(p.H);
     if (ahead.row < p.rows) next.load(p, ahead, c0);
-    float h[NV][8];
-    float s = 0.f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (in[v]) {
-        cur.x[v].floats(h[v]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[v][j] = 0.f;
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s = fmaf(h[v][j], h[v][j], s);
-    }
+    float h[E] = {};
+    if (in) cur.x.floats(h);
     float rn = 1.f;
-    if (p.after) rn = 1.f / sqrtf(row_sum<LANES>(s, turn) * inv_d + p.eps);
-    s = 0.f;
+    if (p.after) {
+      float s = 0.f;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (!in[v]) continue;
+      for (int j = 0; j < E; ++j) s = fmaf(h[j], h[j], s);
+      rn = 1.f / sqrtf(row_sum<LANES>(s, turn) * inv_d + p.eps);
+    }
+    float s = 0.f;
+    if (in) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) h[v][j] *= rn * wa[v][j];
+      for (int j = 0; j < E; ++j) h[j] *= rn * wa[j];
       if (p.gate) {
-        float g[8];
-        cur.g[v].floats(g);
+        float g[E];
+        cur.g.floats(g);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h[v][j] *= act(g[j], p.silu);
+        for (int j = 0; j < E; ++j) {
+          const float sg = sigmoid(g[j]);
+          h[j] *= p.silu ? g[j] * sg : sg;
+        }
       }
-      float r[8] = {};
-      if (p.res) cur.r[v].floats(r);
+      float r[E] = {};
+      if (p.res) cur.r.floats(r);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        h[v][j] = fmaf(cs[v][j], h[v][j], r[j]);
-        s = fmaf(h[v][j], h[v][j], s);
+      for (int j = 0; j < E; ++j) {
+        h[j] = fmaf(cs[j], h[j], r[j]);
+        s = fmaf(h[j], h[j], s);
       }
-      if (p.h) store8<RES_BF16>(p.h, row * p.D + c0[v], h[v]);
+      if (p.h) RawN<RES_BF16, E>::of(h).store_once(p.h, row * p.D + c0);
     }
     if (p.y) {
       float rh = 1.f;
       if (p.before) rh = 1.f / sqrtf(row_sum<LANES>(s, turn) * inv_d + p.eps);
+      if (in) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        if (!in[v]) continue;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) h[v][j] *= rh * wb[v][j];
-        store8<BF16>(p.y, row * p.D + c0[v], h[v]);
+        for (int j = 0; j < E; ++j) h[j] *= rh * wb[j];
+        RawN<BF16, E>::of(h).store_once(p.y, row * p.D + c0);
       }
     }
     cur = next;
   }
 }
 
-template <int NV, bool BF16, bool RES_BF16>
+template <bool BF16, bool RES_BF16>
 struct GradIn {
-  Raw8<BF16> y[NV];
-  Raw8<RES_BF16> h[NV];
-  __device__ void load(const BlockNormParams& p, long row, const int (&c0)[NV]) {
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (c0[v] >= p.D) continue;
-      if (p.dy) y[v].load(p.dy, row * p.D + c0[v]);
-      if (p.dh) h[v].load(p.dh, row * p.D + c0[v]);
-    }
+  RawN<BF16, E> y;
+  RawN<RES_BF16, E> h;
+  __device__ void load(const BlockNormParams& p, long row, int c0) {
+    if (c0 >= p.D) return;
+    if (p.dy) y.load_once(p.dy, row * p.D + c0);
+    if (p.dh) h.load_once(p.dh, row * p.D + c0);
   }
 };
 
 // Every workgroup walks its rows in a fixed order and leaves the sums of the three weights'
-// gradients over them.
-template <int LANES, int NV, bool BF16, bool RES_BF16>
+// gradients over them.  1024 lanes have half the registers of fewer: there the weights
+// are read again for every row (from the cache) and no row is requested ahead.
+template <int LANES, bool BF16, bool RES_BF16>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_kernel(
     BlockNormParams p) {
   constexpr int RW = LANES > 64 ? 1 : 256 / LANES;
-  __shared__ float acc[RW > 1 ? RW : 1][RW > 1 ? 8 * LANES * NV : 1];
-  const int sub = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  constexpr bool KEEP = LANES < 1024;
+  __shared__ float acc[RW][RW > 1 ? E * LANES : 1];
+  const int group = threadIdx.x / LANES, c0 = E * int(threadIdx.x % LANES);
   const float inv_d = 1.f / float(p.D);
-  int c0[NV], turn = 0;
-  bool in[NV];
-  float wa[NV][8], wb[NV][8], cs[NV][8], da[NV][8] = {}, db[NV][8] = {}, dc[NV][8] = {};
+  const bool in = c0 < p.D;
+  int turn = 0;
+  float wa[E], wb[E], cs[E], da[E] = {}, db[E] = {}, dc[E] = {};
+  auto weights = [&] {
+    vector_of(p.wa, c0, in, wa);
+    vector_of(p.wb, c0, in, wb);
+    vector_of(p.cs, c0, in, cs);
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    c0[v] = 8 * (v * LANES + sub);
-    in[v] = c0[v] < p.D;
-    vector8(p.wa, c0[v], in[v], wa[v]);
-    vector8(p.wb, c0[v], in[v], wb[v]);
-    vector8(p.cs, c0[v], in[v], cs[v]);
-  }
+    for (int j = 0; j < E; ++j) cs[j] *= p.scale;
+  };
+  if (KEEP) weights();
   Walk ahead(long(blockIdx.x) * RW + group, long(gridDim.x) * RW, p.H);
-  RowIn<NV, BF16, RES_BF16> cur, next;
-  GradIn<NV, BF16, RES_BF16> gcur, gnext;
-  if (ahead.row < p.rows) {
+  RowIn<BF16, RES_BF16> cur, next;
+  GradIn<BF16, RES_BF16> gcur, gnext;
+  if (KEEP && ahead.row < p.rows) {
     cur.load(p, ahead, c0);
     gcur.load(p, ahead.row, c0);
   }
   for (long row = ahead.row; row < p.rows; row += ahead.step) {
-    ahead.next(p.H);
-    if (ahead.row < p.rows) {
-      next.load(p, ahead, c0);
-      gnext.load(p, ahead.row, c0);
-    }
-    float x[NV][8], g[NV][8], h[NV][8], dy[NV][8], d[NV][8];
-    float s = 0.f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[v][j] = g[v][j] = h[v][j] = dy[v][j] = d[v][j] = 0.f;
-      if (!in[v]) continue;
-      cur.x[v].floats(x[v]);
-      if (p.gate) cur.g[v].floats(g[v]);
-      if (p.res) cur.r[v].floats(h[v]);
-      if (p.dy) gcur.y[v].floats(dy[v]);
-      if (p.dh) gcur.h[v].floats(d[v]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s = fmaf(x[v][j], x[v][j], s);
-    }
-    float rx = 1.f;
-    if (p.after) rx = 1.f / sqrtf(row_sum<LANES>(s, turn) * inv_d + p.eps);
-    // h, and the two sums of its norm
-    float hh = 0.f, hd = 0.f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float u = x[v][j] * rx * wa[v][j];
-        if (p.gate) u *= act(g[v][j], p.silu);
-        h[v][j] = fmaf(p.scale * cs[v][j], u, h[v][j]);
-        hh = fmaf(h[v][j], h[v][j], hh);
-        hd = fmaf(wb[v][j] * dy[v][j], h[v][j], hd);
+    if constexpr (KEEP) {
+      ahead.next(p.H);
+      if (ahead.row < p.rows) {
+        next.load(p, ahead, c0);
+        gnext.load(p, ahead.row, c0);
       }
-    if (p.before) {
-      row_sum2<LANES>(hh, hd, turn);
-      const float rh = 1.f / sqrtf(hh * inv_d + p.eps), f = hd * inv_d * rh * rh;
+    } else {
+      cur.load(p, ahead, c0);
+      gcur.load(p, ahead.row, c0);
+      ahead.next(p.H);
+      asm volatile("" ::: "memory");  // (the weights' reads stay in the loop)
+      weights();
+    }
+    // a: the gate's activation, slope: its derivative; un: x normed and weighted
+    float x[E] = {}, a[E], slope[E], h[E] = {}, dy[E] = {}, d[E] = {}, un[E];
+    float s = 0.f;
+    if (in) {
+      cur.x.floats(x);
+      if (p.res) cur.r.floats(h);
+      if (p.dy) gcur.y.floats(dy);
+      if (p.dh) gcur.h.floats(d);
+    }
+    if (p.gate) {
+      float g[E] = {};
+      if (in) cur.g.floats(g);
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          db[v][j] = fmaf(dy[v][j], h[v][j] * rh, db[v][j]);
-          d[v][j] = fmaf(rh, wb[v][j] * dy[v][j] - h[v][j] * f, d[v][j]);
-        }
+      for (int j = 0; j < E; ++j) {
+        const float sg = sigmoid(g[j]);
+        a[j] = p.silu ? g[j] * sg : sg;
+        // s (1 + g (1 - s)), or s (1 - s)
+        slope[j] = p.silu ? fmaf(-a[j], sg, sg + a[j]) : fmaf(-sg, sg, sg);
+      }
     } else {
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) d[v][j] += dy[v][j];
+      for (int j = 0; j < E; ++j) a[j] = 1.f;
     }
-    s = 0.f;
+    float rx = 1.f;
+    if (p.after) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (!in[v]) continue;
-      if (p.dres) store8<RES_BF16>(p.dres, row * p.D + c0[v], d[v]);
-      float dg[8];
+      for (int j = 0; j < E; ++j) s = fmaf(x[j], x[j], s);
+      rx = 1.f / sqrtf(row_sum<LANES>(s, turn) * inv_d + p.eps);
+    }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float n = x[v][j] * rx, un = n * wa[v][j];
-        float du = p.scale * cs[v][j] * d[v][j], a = 1.f;
-        if (p.gate) {
-          const float sg = sigmoid(g[v][j]);
-          a = p.silu ? g[v][j] * sg : sg;
-          const float slope = p.silu ? sg * fmaf(g[v][j], 1.f - sg, 1.f) : sg * (1.f - sg);
-          dg[j] = du * un * slope;
-        }
-        dc[v][j] = fmaf(p.scale * d[v][j], un * a, dc[v][j]);
-        du *= a;
-        da[v][j] = fmaf(du, n, da[v][j]);
-        d[v][j] = du * wa[v][j];
-        s = fmaf(d[v][j], x[v][j], s);
+    for (int j = 0; j < E; ++j) {
+      un[j] = x[j] * rx * wa[j];
+      h[j] = fmaf(cs[j], un[j] * a[j], h[j]);
+    }
+    if (p.before) {
+      float both[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        both[0] = fmaf(h[j], h[j], both[0]);
+        both[1] = fmaf(wb[j] * dy[j], h[j], both[1]);
       }
-      if (p.gate && p.dgate) store8<BF16>(p.dgate, row * p.D + c0[v], dg);
-    }
-    float f = 0.f;
-    if (p.after) f = row_sum<LANES>(s, turn) * inv_d * rx * rx;
+      row_sums<LANES>(both, turn);
+      const float rh = 1.f / sqrtf(both[0] * inv_d + p.eps);
+      const float f = both[1] * inv_d * rh * rh * rh;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (!in[v]) continue;
+      for (int j = 0; j < E; ++j) {
+        db[j] = fmaf(dy[j], h[j] * rh, db[j]);
+        d[j] = fmaf(rh, wb[j] * dy[j], fmaf(-f, h[j], d[j]));
+      }
+    } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) d[v][j] = rx * (d[v][j] - x[v][j] * f);
-      store8<BF16>(p.dx, row * p.D + c0[v], d[v]);
+      for (int j = 0; j < E; ++j) d[j] += dy[j];
     }
-    cur = next;
-    gcur = gnext;
+    if (p.dres && in) RawN<RES_BF16, E>::of(d).store_once(p.dres, row * p.D + c0);
+    s = 0.f;
+    float dg[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      dc[j] = fmaf(d[j], un[j] * a[j], dc[j]);
+      const float du = cs[j] * d[j], dn = du * a[j], t = dn * x[j];
+      if (p.gate) dg[j] = du * un[j] * slope[j];
+      da[j] = fmaf(t, rx, da[j]);
+      s = fmaf(t, wa[j], s);
+      d[j] = dn * wa[j];
+    }
+    if (p.gate && p.dgate && in) RawN<BF16, E>::of(dg).store_once(p.dgate, row * p.D + c0);
+    if (p.after) {
+      const float f = row_sum<LANES>(s, turn) * inv_d * rx * rx * rx;
+#pragma unroll
+      for (int j = 0; j < E; ++j) d[j] = fmaf(rx, d[j], -f * x[j]);
+    }
+    if (in) RawN<BF16, E>::of(d).store_once(p.dx, row * p.D + c0);
+    if constexpr (KEEP) {
+      cur = next;
+      gcur = gnext;
+    }
   }
   if (!p.partial) return;
+#pragma unroll
+  for (int j = 0; j < E; ++j) dc[j] *= p.scale;
   float* const out = p.partial + long(blockIdx.x) * 3 * p.D;
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     const auto& sum = k == 0 ? da : k == 1 ? db : dc;
     if constexpr (RW == 1) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v)
-        if (in[v]) store8<false>(out, long(k) * p.D + c0[v], sum[v]);
+      if (in) RawN<false, E>::of(sum).store(out, long(k) * p.D + c0);
     } else {
       __syncthreads();
 #pragma unroll
-      for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[group][8 * (v * LANES + sub) + j] = sum[v][j];
+      for (int j = 0; j < E; ++j) acc[group][c0 + j] = sum[j];
       __syncthreads();
       for (int c = threadIdx.x; c < p.D; c += 256) {
         float t = 0.f;
@@ -361,20 +345,26 @@ __global__ __launch_bounds__(1024) void block_norm_weight_kernel(BlockNormParams
   }
 }
 
-template <int LANES, int NV, bool BF16, bool RES_BF16>
+// Workgroups that the compute units hold, for walks over `need` of them.
+unsigned walkers(long need, int per_cu, int cus) {
+  const long most = long(cus > 0 ? cus : 256) * per_cu;
+  return unsigned(need < most ? need : most);
+}
+
+template <int LANES, bool BF16, bool RES_BF16>
 hipError_t run(const BlockNormParams& p, bool backward, int cus, hipStream_t st) {
   constexpr int RW = LANES > 64 ? 1 : 256 / LANES, threads = LANES > 64 ? LANES : 256;
   const long need = (p.rows + RW - 1) / RW;
   if (!backward) {
-    // as many workgroups as the compute units hold
-    const long most = long(cus > 0 ? cus : 256) * (2048 / threads);
-    block_norm_kernel<LANES, NV, BF16, RES_BF16>
-        <<<unsigned(need < most ? need : most), threads, 0, st>>>(p);
+    block_norm_kernel<LANES, BF16, RES_BF16>
+        <<<walkers(need, 2048 / threads, cus), threads, 0, st>>>(p);
     return hipGetLastError();
   }
-  const long blocks = need < kBlockNormBlocks ? need : kBlockNormBlocks;
+  // 512 threads of this kernel's registers on a compute unit
+  unsigned blocks = walkers(need, threads < 512 ? 512 / threads : 1, cus);
+  if (blocks > unsigned(kBlockNormBlocks)) blocks = kBlockNormBlocks;
   if (blocks > 0) {
-    block_norm_backward_kernel<LANES, NV, BF16, RES_BF16><<<unsigned(blocks), threads, 0, st>>>(p);
+    block_norm_backward_kernel<LANES, BF16, RES_BF16><<<blocks, threads, 0, st>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -385,17 +375,16 @@ hipError_t run(const BlockNormParams& p, bool backward, int cus, hipStream_t st)
 
 template <bool BF16, bool RES_BF16>
 hipError_t by_width(const BlockNormParams& p, bool backward, int cus, hipStream_t st) {
-#define ONELA_NORM(L, NV) return run<L, NV, BF16, RES_BF16>(p, backward, cus, st)
-  if (p.D <= 32) ONELA_NORM(4, 1);
-  if (p.D <= 64) ONELA_NORM(8, 1);
-  if (p.D <= 128) ONELA_NORM(16, 1);
-  if (p.D <= 256) ONELA_NORM(32, 1);
-  if (p.D <= 512) ONELA_NORM(64, 1);
-  if (p.D <= 1024) ONELA_NORM(128, 1);
-  if (p.D <= 2048) ONELA_NORM(256, 1);
-  if (p.D <= 4096) ONELA_NORM(512, 1);
-  if (p.D <= 8192) ONELA_NORM(1024, 1);
-  ONELA_NORM(1024, 2);
+#define ONELA_NORM(L) return run<L, BF16, RES_BF16>(p, backward, cus, st)
+  if (p.D <= 32) ONELA_NORM(4);
+  if (p.D <= 64) ONELA_NORM(8);
+  if (p.D <= 128) ONELA_NORM(16);
+  if (p.D <= 256) ONELA_NORM(32);
+  if (p.D <= 512) ONELA_NORM(64);
+  if (p.D <= 1024) ONELA_NORM(128);
+  if (p.D <= 2048) ONELA_NORM(256);
+  if (p.D <= 4096) ONELA_NORM(512);
+  ONELA_NORM(1024);
 #undef ONELA_NORM
 }
 

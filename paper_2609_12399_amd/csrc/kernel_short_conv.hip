@@ -47,59 +47,62 @@ __device__ inline int sequence_at(const ConvParams& p, long t0) {
   return lo;
 }
 
-template <int TAPS>
+template <int TAPS, int E>
 struct Window {  // the last TAPS inputs (or gradients), newest last
-  float v[TAPS][8];
-  __device__ void push(const float (&x)[8]) {
+  float v[TAPS][E];
+  __device__ void push(const float (&x)[E]) {
 #pragma unroll
     for (int j = 0; j + 1 < TAPS; ++j)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] = v[j + 1][i];
+      for (int i = 0; i < E; ++i) v[j][i] = v[j + 1][i];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[TAPS - 1][i] = x[i];
+    for (int i = 0; i < E; ++i) v[TAPS - 1][i] = x[i];
   }
 };
 
 // Input at place t (before b: in the state) of channels c0 .. c0 + 7.
-template <int TAPS, bool BF16>
-__device__ inline Raw8<BF16> input_at(const ConvParams& p, const void* state, long row, long b,
-                                      long t, int c0) {
-  Raw8<BF16> r;
+template <int TAPS, bool BF16, int E>
+__device__ inline RawN<BF16, E> input_at(const ConvParams& p, const void* state, long row, long b,
+                                      long t, unsigned c0) {
+  RawN<BF16, E> r;
   if (t >= b)
-    r.load(p.x, t * p.xs + c0);
+    r.load(p.x, t * p.xs, c0);
   else if (state)
-    r.load(state, (row * (TAPS - 1) + (t - b + TAPS - 1)) * p.C + c0);
+    r.load(state, (row * (TAPS - 1) + (t - b + TAPS - 1)) * p.C, c0);
   else
     r.clear();
   return r;
 }
 
-// The window before token t (its newest place is free).
-template <int TAPS, bool BF16>
-__device__ inline void fill(const ConvParams& p, long n, long b, long t, int c0,
-                            Window<TAPS>& win) {
-  Raw8<BF16> r[TAPS - 1];
+// The inputs before token t, as they come from memory and as the window (its newest place free).
+template <int TAPS, bool BF16, int E>
+struct Before {
+  RawN<BF16, E> r[TAPS - 1];
+  __device__ void load(const ConvParams& p, long n, long b, long t, unsigned c0) {
 #pragma unroll
-  for (int i = 0; i < TAPS - 1; ++i)
-    r[i] = input_at<TAPS, BF16>(p, p.s_in, n, b, t - (TAPS - 1) + i, c0);
+    for (int i = 0; i < TAPS - 1; ++i)
+      r[i] = input_at<TAPS, BF16, E>(p, p.s_in, n, b, t - (TAPS - 1) + i, c0);
+  }
+  __device__ void fill(Window<TAPS, E>& win) const {
 #pragma unroll
-  for (int i = 0; i < TAPS - 1; ++i) r[i].floats(win.v[i + 1]);
-}
+    for (int i = 0; i < TAPS - 1; ++i) r[i].floats(win.v[i + 1]);
+  }
+};
 
-template <int TAPS>
+template <int TAPS, int E>
 struct Weights {
-  float w[TAPS][8], b[8];
-  __device__ void load(const ConvParams& p, int c0) {
+  float w[TAPS][E], b[E];
+  __device__ void load(const ConvParams& p, unsigned c0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < E; ++i) {
 #pragma unroll
       for (int j = 0; j < TAPS; ++j) w[j][i] = p.w[(c0 + i) * TAPS + j];
       b[i] = p.bias ? p.bias[c0 + i] : 0.f;
     }
   }
-  __device__ void apply(const Window<TAPS>& x, float (&y)[8]) const {
+  __device__ void apply(const Window<TAPS, E>& x, float (&y)[E]) const {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < E; ++i) {
       y[i] = b[i];
 #pragma unroll
       for (int j = 0; j < TAPS; ++j) y[i] = fmaf(w[j][i], x.v[j][i], y[i]);
@@ -107,78 +110,89 @@ struct Weights {
   }
 };
 
-template <bool BF16>
-__device__ inline void store_output(const ConvParams& p, long i, float (&y)[8]) {
+template <bool BF16, int E>
+__device__ inline void store_output(const ConvParams& p, long i, unsigned c0, float (&y)[E]) {
   if (p.silu)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) y[k] *= sigmoid(y[k]);
-  store8<BF16>(p.y, i, y);
+    for (int k = 0; k < E; ++k) y[k] *= sigmoid(y[k]);
+  RawN<BF16, E>::of(y).store_once(p.y, i, c0);
 }
 
 // The state after sequence n, 8 channels (read before it is stored: it may replace the first).
-template <int TAPS, bool BF16>
-__device__ inline void last_state(const ConvParams& p, int n, int c0) {
+template <int TAPS, bool BF16, int E>
+__device__ inline void last_state(const ConvParams& p, int n, unsigned c0) {
   const Bounds s = bounds_of(p, n);
-  Raw8<BF16> r[TAPS - 1];
+  RawN<BF16, E> r[TAPS - 1];
 #pragma unroll
   for (int i = 0; i < TAPS - 1; ++i)
-    r[i] = input_at<TAPS, BF16>(p, p.s_in, n, s.b, s.e - (TAPS - 1) + i, c0);
+    r[i] = input_at<TAPS, BF16, E>(p, p.s_in, n, s.b, s.e - (TAPS - 1) + i, c0);
 #pragma unroll
-  for (int i = 0; i < TAPS - 1; ++i) r[i].store(p.s_out, (long(n) * (TAPS - 1) + i) * p.C + c0);
+  for (int i = 0; i < TAPS - 1; ++i) r[i].store(p.s_out, (long(n) * (TAPS - 1) + i) * p.C, c0);
 }
 
-// Where a thread stands: its channels and its run.
+// Where a thread stands: its channels, its run, and a sequence at or before the run's first token.
+// WAVE: the wave's lanes share a run (64 channel groups side by side), and everything
+// that depends on it is the same for all of them.
 struct Place {
   int c0;
   long t0, t1;
+  int n;
   bool in;
 };
+template <int E, bool WAVE>
 __device__ inline Place place_of(const ConvParams& p, int ll, int run, int blocks_c) {
   const int bt = blockIdx.x / blocks_c, bc = blockIdx.x - bt * blocks_c;
-  const int c0 = 8 * ((bc << ll) + (threadIdx.x & ((1 << ll) - 1)));
-  const long t0 = (long(bt) * (kConvThreads >> ll) + (threadIdx.x >> ll)) * run;
-  return {c0, t0, min(t0 + run, p.total), c0 < p.C && t0 < p.total};
+  const int c0 = E * ((bc << ll) + int(threadIdx.x & ((1u << ll) - 1)));
+  int r = threadIdx.x >> ll;
+  if (WAVE) r = __builtin_amdgcn_readfirstlane(r);
+  const long t0 = (long(bt) * (kConvThreads >> ll) + r) * run;
+  int n = sequence_at(p, WAVE ? t0 : __shfl(t0, 0));
+  if (WAVE) n = __builtin_amdgcn_readfirstlane(n);
+  return {c0, t0, min(t0 + run, p.total), n, c0 < p.C && t0 < p.total};
 }
 
 // The first blocks_c * blocks_t workgroups take the tokens, the others the last states.
-template <int TAPS, bool BF16>
+template <int TAPS, bool BF16, int E, bool WAVE>
 __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvParams p, int ll, int run,
                                                             int blocks_c, unsigned token_blocks) {
   if (blockIdx.x >= token_blocks) {
     const long i = long(blockIdx.x - token_blocks) * kConvThreads + threadIdx.x;
-    const int n = int(i / (p.C / 8));
-    if (n < p.N) last_state<TAPS, BF16>(p, n, 8 * int(i - long(n) * (p.C / 8)));
+    const int n = int(i / (p.C / E));
+    if (n < p.N) last_state<TAPS, BF16, E>(p, n, E * int(i - long(n) * (p.C / E)));
     return;
   }
-  const Place at = place_of(p, ll, run, blocks_c);
-  int n = sequence_at(p, __shfl(at.t0, 0));
+  const Place at = place_of<E, WAVE>(p, ll, run, blocks_c);
   if (!at.in) return;
-  Weights<TAPS> w;
+  int n = at.n;
+  Weights<TAPS, E> w;
   w.load(p, at.c0);
   for (; n < p.N; ++n) {
     const Bounds s = bounds_of(p, n);
     if (s.b >= at.t1) break;
     const long p0 = max(at.t0, s.b), p1 = min(at.t1, s.e);
     if (p0 >= p1) continue;
-    Window<TAPS> win;
-    fill<TAPS, BF16>(p, n, s.b, p0, at.c0, win);
-    Raw8<BF16> cur[kRows];
+    // (the first rows are requested before anything is waited for)
+    RawN<BF16, E> cur[kRows];
 #pragma unroll
     for (int i = 0; i < kRows; ++i)
-      if (p0 + i < p1) cur[i].load(p.x, (p0 + i) * p.xs + at.c0);
+      if (p0 + i < p1) cur[i].load(p.x, (p0 + i) * p.xs, at.c0);
+    Before<TAPS, BF16, E> old;
+    old.load(p, n, s.b, p0, at.c0);
+    Window<TAPS, E> win;
+    old.fill(win);
     for (long t = p0; t < p1; t += kRows) {
-      Raw8<BF16> next[kRows];
+      RawN<BF16, E> next[kRows];
 #pragma unroll
       for (int i = 0; i < kRows; ++i)
-        if (t + kRows + i < p1) next[i].load(p.x, (t + kRows + i) * p.xs + at.c0);
+        if (t + kRows + i < p1) next[i].load(p.x, (t + kRows + i) * p.xs, at.c0);
 #pragma unroll
       for (int i = 0; i < kRows; ++i) {
         if (t + i >= p1) break;
-        float x[8], y[8];
+        float x[E], y[E];
         cur[i].floats(x);
         win.push(x);
         w.apply(win, y);
-        store_output<BF16>(p, (t + i) * p.C + at.c0, y);
+        store_output<BF16, E>(p, (t + i) * p.C, at.c0, y);
       }
 #pragma unroll
       for (int i = 0; i < kRows; ++i) cur[i] = next[i];
@@ -186,20 +200,20 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvParams p, int ll
   }
 }
 
-template <int TAPS, bool BF16>
+template <int TAPS, bool BF16, int E, bool WAVE>
 __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams p, int ll, int run,
                                                                      int blocks_c,
                                                                      unsigned token_blocks) {
   if (blockIdx.x >= token_blocks) {  // sequences without tokens: the state passes through
     const long i = long(blockIdx.x - token_blocks) * kConvThreads + threadIdx.x;
-    const int n = int(i / (p.C / 8)), c0 = 8 * int(i - long(n) * (p.C / 8));
+    const int n = int(i / (p.C / E)), c0 = E * int(i - long(n) * (p.C / E));
     if (n >= p.N) return;
     const Bounds s = bounds_of(p, n);
     if (s.b < s.e) return;
 #pragma unroll
     for (int j = 0; j < TAPS - 1; ++j) {
       const long o = (long(n) * (TAPS - 1) + j) * p.C + c0;
-      Raw8<BF16> r;
+      RawN<BF16, E> r;
       if (p.ds_in)
         r.load(p.ds_in, o);
       else
@@ -208,12 +222,12 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams 
     }
     return;
   }
-  __shared__ float acc[kConvThreads][9];
-  const Place at = place_of(p, ll, run, blocks_c);
-  int n = sequence_at(p, __shfl(at.t0, 0));
-  float dw[TAPS + 1][8] = {};
+  __shared__ float acc[TAPS + 1][kConvThreads][E];
+  const Place at = place_of<E, WAVE>(p, ll, run, blocks_c);
+  int n = at.n;
+  float dw[TAPS + 1][E] = {};
   if (at.in) {
-    Weights<TAPS> w;
+    Weights<TAPS, E> w;
     w.load(p, at.c0);
     for (; n < p.N; ++n) {
       const Bounds s = bounds_of(p, n);
@@ -223,46 +237,48 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams 
       // tokens p0 .. p2 - 1: TAPS - 1 more, whose gradients the last inputs have a part of (the
       // sequence's end is followed by zeros)
       const long p2 = p1 + TAPS - 1, end = min(p2, s.e);
-      Window<TAPS> win, gs = {};
-      fill<TAPS, BF16>(p, n, s.b, p0, at.c0, win);
-      Raw8<BF16> cx[kBackRows], cd[kBackRows];
+      Window<TAPS, E> win, gs = {};
+      RawN<BF16, E> cx[kBackRows], cd[kBackRows];
 #pragma unroll
       for (int i = 0; i < kBackRows; ++i)
         if (p0 + i < end) {
-          cx[i].load(p.x, (p0 + i) * p.xs + at.c0);
-          cd[i].load(p.dy, (p0 + i) * p.C + at.c0);
+          cx[i].load(p.x, (p0 + i) * p.xs, at.c0);
+          cd[i].load(p.dy, (p0 + i) * p.C, at.c0);
         }
+      Before<TAPS, BF16, E> before;
+      before.load(p, n, s.b, p0, at.c0);
+      before.fill(win);
       for (long t = p0; t < p2; t += kBackRows) {
-        Raw8<BF16> nx[kBackRows], nd[kBackRows];
+        RawN<BF16, E> nx[kBackRows], nd[kBackRows];
 #pragma unroll
         for (int i = 0; i < kBackRows; ++i)
           if (t + kBackRows + i < end) {
-            nx[i].load(p.x, (t + kBackRows + i) * p.xs + at.c0);
-            nd[i].load(p.dy, (t + kBackRows + i) * p.C + at.c0);
+            nx[i].load(p.x, (t + kBackRows + i) * p.xs, at.c0);
+            nd[i].load(p.dy, (t + kBackRows + i) * p.C, at.c0);
           }
 #pragma unroll
         for (int i = 0; i < kBackRows; ++i) {
           const long tt = t + i;
           if (tt >= p2) break;
-          float x[8] = {}, g[8] = {};
+          float x[E] = {}, g[E] = {};
           if (tt < end) {
             cx[i].floats(x);
             cd[i].floats(g);
           }
           win.push(x);
           if (p.silu && tt < end) {
-            float y[8];
+            float y[E];
             w.apply(win, y);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const float sg = sigmoid(y[k]);
-              g[k] *= sg * fmaf(y[k], 1.f - sg, 1.f);
+            for (int k = 0; k < E; ++k) {
+              const float sg = sigmoid(y[k]), t = fmaf(-y[k], sg, y[k]);
+              g[k] *= fmaf(sg, t, sg);  // s (1 + y (1 - s))
             }
           }
           gs.push(g);
           if (tt < p1)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < E; ++k) {
 #pragma unroll
               for (int j = 0; j < TAPS; ++j) dw[j][k] = fmaf(g[k], win.v[j][k], dw[j][k]);
               dw[TAPS][k] += g[k];
@@ -270,22 +286,25 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams 
           const long o = tt - (TAPS - 1);  // the input whose gradient is complete
           const bool old = o < p0;
           if (old && (p0 != s.b || !p.ds_out)) continue;
-          float d[8] = {};
+          float d[E] = {};
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
+          for (int k = 0; k < E; ++k)
 #pragma unroll
             for (int j = 0; j < TAPS; ++j) d[k] = fmaf(w.w[j][k], gs.v[TAPS - 1 - j][k], d[k]);
           const long last = o - (s.e - (TAPS - 1));  // its place in the last state
           if (last >= 0 && p.ds_in) {
-            float f[8];
-            load8<BF16>(p.ds_in, (long(n) * (TAPS - 1) + last) * p.C + at.c0, f);
+            float f[E];
+            RawN<BF16, E> r;
+            r.load(p.ds_in, (long(n) * (TAPS - 1) + last) * p.C, at.c0);
+            r.floats(f);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) d[k] += f[k];
+            for (int k = 0; k < E; ++k) d[k] += f[k];
           }
           if (old)
-            store8<BF16>(p.ds_out, (long(n) * (TAPS - 1) + (o - s.b + TAPS - 1)) * p.C + at.c0, d);
+            RawN<BF16, E>::of(d).store(p.ds_out,
+                                      (long(n) * (TAPS - 1) + (o - s.b + TAPS - 1)) * p.C, at.c0);
           else
-            store8<BF16>(p.dx, o * p.C + at.c0, d);
+            RawN<BF16, E>::of(d).store_once(p.dx, o * p.C, at.c0);
         }
 #pragma unroll
         for (int i = 0; i < kBackRows; ++i) {
@@ -296,20 +315,20 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams 
     }
   }
   if (!p.partial) return;
-  const int lanes = 1 << ll, c_first = at.c0 - 8 * (threadIdx.x & (lanes - 1));
+  const int lanes = 1 << ll, c_first = at.c0 - E * (threadIdx.x & (lanes - 1));
   const long bt = blockIdx.x / blocks_c;
 #pragma unroll
-  for (int j = 0; j <= TAPS; ++j) {
-    __syncthreads();
+  for (int j = 0; j <= TAPS; ++j)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) acc[threadIdx.x][k] = dw[j][k];
-    __syncthreads();
-    for (int c = threadIdx.x; c < 8 * lanes && c_first + c < p.C; c += kConvThreads) {
+    for (int k = 0; k < E; ++k) acc[j][threadIdx.x][k] = dw[j][k];
+  __syncthreads();
+  for (int c = threadIdx.x; c < E * lanes && c_first + c < p.C; c += kConvThreads)
+#pragma unroll
+    for (int j = 0; j <= TAPS; ++j) {
       float s = 0.f;
-      for (int r = c / 8; r < kConvThreads; r += lanes) s += acc[r][c & 7];
+      for (int r = c / E; r < kConvThreads; r += lanes) s += acc[j][r][c % E];
       p.partial[(bt * (TAPS + 1) + j) * p.C + c_first + c] = s;
     }
-  }
 }
 
 // The workgroups' sums added up: 16 values of a tap per workgroup, 16 rows at a time.
@@ -336,10 +355,10 @@ __global__ __launch_bounds__(256) void conv_weight_kernel(ConvParams p, int taps
 }
 
 // One thread for a sequence's 8 channels.
-template <int TAPS, bool BF16>
+template <int TAPS, bool BF16, int E>
 __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvParams p) {
   const long i = long(blockIdx.x) * kConvThreads + threadIdx.x;
-  const int n = int(i / (p.C / 8)), c0 = 8 * int(i - long(n) * (p.C / 8));
+  const int n = int(i / (p.C / E)), c0 = E * int(i - long(n) * (p.C / E));
   if (n >= p.N) return;
   const Bounds s = bounds_of(p, n);
   if (s.b >= s.e) {
@@ -350,26 +369,27 @@ __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvParams p) {
   const int to = p.s_out ? (p.slot_out ? p.slot_out[n] : n) : from;
   const int most = p.s_out ? p.slots_out : p.slots;
   if (from < 0 || from >= p.slots) {  // no state: the sequence's outputs are zeros
-    const float zero[8] = {};
-    for (long t = s.b; t < s.e; ++t) store8<BF16>(p.y, t * p.C + c0, zero);
+    RawN<BF16, E> zero;
+    zero.clear();
+    for (long t = s.b; t < s.e; ++t) zero.store(p.y, t * p.C + c0);
     return;
   }
-  Raw8<BF16> r[TAPS - 1], x;
-  Weights<TAPS> w;
+  RawN<BF16, E> r[TAPS - 1], x;
+  Weights<TAPS, E> w;
 #pragma unroll
   for (int j = 0; j < TAPS - 1; ++j)
     r[j].load(p.s_in, (long(from) * (TAPS - 1) + j) * p.C + c0);
   w.load(p, c0);
-  Window<TAPS> win;
+  Window<TAPS, E> win;
 #pragma unroll
   for (int j = 0; j < TAPS - 1; ++j) r[j].floats(win.v[j + 1]);
   for (long t = s.b; t < s.e; ++t) {
-    float v[8], y[8];
+    float v[E], y[E];
     x.load(p.x, t * p.xs + c0);
     x.floats(v);
     win.push(v);
     w.apply(win, y);
-    store_output<BF16>(p, t * p.C + c0, y);
+    store_output<BF16, E>(p, t * p.C, c0, y);
 #pragma unroll
     for (int j = 0; j + 2 < TAPS; ++j) r[j] = r[j + 1];
     r[TAPS - 2] = x;
@@ -380,34 +400,38 @@ __global__ __launch_bounds__(kConvThreads) void conv_step_kernel(ConvParams p) {
   for (int j = 0; j < TAPS - 1; ++j) r[j].store(out, (long(to) * (TAPS - 1) + j) * p.C + c0);
 }
 
-unsigned state_blocks(const ConvParams& p) {
-  return unsigned((long(p.N) * (p.C / 8) + kConvThreads - 1) / kConvThreads);
+unsigned state_blocks(const ConvParams& p, int channels) {
+  return unsigned((long(p.N) * (p.C / channels) + kConvThreads - 1) / kConvThreads);
 }
 
-template <int TAPS, bool BF16>
+template <int TAPS, bool BF16, bool WAVE>
 hipError_t run_forward(const ConvParams& p, const ConvPlan& a, hipStream_t st) {
+  constexpr int E = kConvLane;
   const unsigned tokens = unsigned(a.blocks_t * a.blocks_c);
   // a last state that replaces the first one waits until every token has read it
   const bool apart = p.s_out && p.s_out == p.s_in;
-  const unsigned states = p.s_out ? state_blocks(p) : 0;
-  if (tokens + (apart ? 0 : states) > 0) {
-    conv_kernel<TAPS, BF16><<<tokens + (apart ? 0 : states), kConvThreads, 0, st>>>(
-        p, a.lanes_log2, a.run, a.blocks_c, tokens);
+  const unsigned states = p.s_out ? state_blocks(p, E) : 0;
+  const unsigned with = tokens + (apart ? 0 : states);
+  if (with > 0) {
+    conv_kernel<TAPS, BF16, E, WAVE>
+        <<<with, kConvThreads, 0, st>>>(p, a.lanes_log2, a.run, a.blocks_c, tokens);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (apart)
-    conv_kernel<TAPS, BF16><<<states, kConvThreads, 0, st>>>(p, a.lanes_log2, a.run, a.blocks_c, 0);
+    conv_kernel<TAPS, BF16, E, WAVE>
+        <<<states, kConvThreads, 0, st>>>(p, a.lanes_log2, a.run, a.blocks_c, 0);
   return hipGetLastError();
 }
 
-template <int TAPS, bool BF16>
+template <int TAPS, bool BF16, bool WAVE>
 hipError_t run_backward(const ConvParams& p, const ConvPlan& a, hipStream_t st) {
+  constexpr int E = kConvLane;
   const unsigned tokens = unsigned(a.blocks_t * a.blocks_c);
-  const unsigned states = p.ds_out ? state_blocks(p) : 0;
+  const unsigned states = p.ds_out ? state_blocks(p, E) : 0;
   if (tokens + states > 0) {
-    conv_backward_kernel<TAPS, BF16><<<tokens + states, kConvThreads, 0, st>>>(
-        p, a.lanes_log2, a.run, a.blocks_c, tokens);
+    conv_backward_kernel<TAPS, BF16, E, WAVE>
+        <<<tokens + states, kConvThreads, 0, st>>>(p, a.lanes_log2, a.run, a.blocks_c, tokens);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -419,7 +443,8 @@ hipError_t run_backward(const ConvParams& p, const ConvPlan& a, hipStream_t st) 
 
 template <int TAPS, bool BF16>
 hipError_t run_step(const ConvParams& p, hipStream_t st) {
-  conv_step_kernel<TAPS, BF16><<<state_blocks(p), kConvThreads, 0, st>>>(p);
+  constexpr int E = kConvLane;
+  conv_step_kernel<TAPS, BF16, E><<<state_blocks(p, E), kConvThreads, 0, st>>>(p);
   return hipGetLastError();
 }
 
@@ -432,14 +457,17 @@ hipError_t run_step(const ConvParams& p, hipStream_t st) {
 
 hipError_t launch_conv(const ConvParams& p, const ConvPlan& plan, int taps, bool bf16,
                        hipStream_t st) {
-#define ONELA_FORWARD(K, B) run_forward<K, B>(p, plan, st)
+#define ONELA_FORWARD(K, B) \
+  (plan.lanes_log2 == 6 ? run_forward<K, B, true>(p, plan, st) : run_forward<K, B, false>(p, plan, st))
   ONELA_CONV(ONELA_FORWARD);
 #undef ONELA_FORWARD
 }
 
 hipError_t launch_conv_backward(const ConvParams& p, const ConvPlan& plan, int taps, bool bf16,
                                 hipStream_t st) {
-#define ONELA_BACKWARD(K, B) run_backward<K, B>(p, plan, st)
+#define ONELA_BACKWARD(K, B)                                  \
+  (plan.lanes_log2 == 6 ? run_backward<K, B, true>(p, plan, st) \
+                        : run_backward<K, B, false>(p, plan, st))
   ONELA_CONV(ONELA_BACKWARD);
 #undef ONELA_BACKWARD
 }

@@ -6,11 +6,12 @@
 // Every thread keeps its own m, s and sum e^d d over the columns that it reads (one
 // exponential per element, the sums rescaled when m grows); the workgroup joins them at the end.
 //
-// The best K: the K-th largest of the threads' maxima of the first chunk bounds the K-th best
-// from below, so that few elements (some K to 2 K) pass into a list in LDS; the list is
-// cut back to its K best by counting, for each, those before it, when it grows over 256, and
-// the bound rises to the K-th.  Elements of later chunks have higher columns, so one that
-// equals the K-th best then stays out.  The order is by (value, lower column) and does not
+// The best K: every thread's largest element of the first chunk goes to LDS, and their K-th
+// largest (found bit by bit with ballots) bounds the K-th best of the row from below: some K to 2 K
+// elements of each chunk pass it into a list in LDS, with no barrier after the first chunk.  At the
+// end one wave takes the list's K best, 64 at a time, by counting for each those before it.
+// Where a row's order or its ties let more through than the list holds, it is read again in
+// smaller pieces with a bound for each.  The order is by (value, lower column) and does not
 // depend on the order of the list.  Masked elements (-inf) never pass: if fewer than K remain,
 // the first masked columns fill the rest.
 //
@@ -128,12 +129,15 @@ __device__ inline void join(Sums& a, float c2, float* lds /* [3][THREADS / 64] *
   }
 }
 
+// Values in order as whole numbers (NaN has none here).
+__device__ inline unsigned ordered(float x) {
+  const unsigned b = __float_as_uint(x);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
 // Candidates in order of preference as whole numbers: the value's order above, lower columns
 // first below.  0 is none.
 __device__ inline u64 candidate(float x, int col) {
-  const unsigned b = __float_as_uint(x + 0.f);  // (-0 becomes 0)
-  const unsigned k = b & 0x80000000u ? ~b : b | 0x80000000u;
-  return u64(k) << 32 | unsigned(~col);
+  return u64(ordered(x + 0.f)) << 32 | unsigned(~col);  // (-0 becomes 0)
 }
 __device__ inline int column_of(u64 c) { return int(~unsigned(c)); }
 __device__ inline float value_of(u64 c) {
@@ -141,44 +145,147 @@ __device__ inline float value_of(u64 c) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// The list of candidates of a workgroup.
-template <int THREADS, int MORE>
+// The candidates of a workgroup, and room for the wave that takes the best of them.
+template <int CAPACITY>
 struct List {
-  static_assert(THREADS >= kMaxTop, "a thread for each of the best");
-  static constexpr int CAP = MORE + kMaxTop;
+  static constexpr int CAP = CAPACITY;
   u64 c[CAP];
-  u64 best[kMaxTop];
-  float maxima[THREADS];
-  int count;
-  float bound;  // of the first chunk
-
-  // Cuts the list to its K best, in order.  Every thread calls it, after a barrier; ends with one.
-  __device__ void cut(int K) {
-    const int n = count;
-    for (int i = threadIdx.x; i < n; i += THREADS) {
-      const u64 x = c[i];
-      int rank = 0;
-#pragma unroll 8
-      for (int j = 0; j < n; ++j) rank += c[j] > x;
-      if (rank < K) best[rank] = x;
-    }
-    __syncthreads();
-    const int m = n < K ? n : K;
-    if (int(threadIdx.x) < m) c[threadIdx.x] = best[threadIdx.x];
-    if (threadIdx.x == 0) count = m;
-    __syncthreads();
-  }
+  u64 best[128];
+  int count;  // of candidates, those that found no room among them
 };
 
-// Results of a row from its sums and its list (sorted, cut): every thread of the workgroup.
+// LDS of one wave: what its lanes have written is what they read next.
+__device__ inline void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// One wave: the first m <= 128 of `best`, cut to their K best, in order; returns how many.
+__device__ inline int in_order(u64* best, int m, int K) {
+  const int lane = threadIdx.x & 63;
+  const u64 x = lane < m ? best[lane] : 0, y = lane + 64 < m ? best[lane + 64] : 0;
+  int rx = 0, ry = 0;
+#pragma unroll 4
+  for (int j = 0; j < m; ++j) {
+    const u64 z = best[j];
+    rx += z > x;
+    ry += z > y;
+  }
+  wave_fence();
+  if (x && rx < K) best[rx] = x;
+  if (y && ry < K) best[ry] = y;
+  wave_fence();
+  return m < K ? m : K;
+}
+
+// One wave: the K best of n candidates in `best`, in order; returns how many there are.  `m` of
+// them are there already.
+template <typename L>
+__device__ inline int take_best(L* list, int n, int K, int m = 0) {
+  const int lane = threadIdx.x & 63;
+  u64 bound = m < K ? 0 : list->best[K - 1];
+  for (int i = 0; i < n; i += 64) {
+    const u64 x = i + lane < n ? list->c[i + lane] : 0;
+    const u64 pass = __ballot(x > bound);
+    if (!pass) continue;
+    if (x > bound) list->best[m + __popcll(pass & ((1ull << lane) - 1))] = x;
+    m += __popcll(pass);
+    wave_fence();
+    if (m >= 64) {
+      m = in_order(list->best, m, K);
+      if (m == K) bound = list->best[K - 1];
+    }
+  }
+  return in_order(list->best, m, K);
+}
+
+// A lower bound of the K-th largest of N values per lane over the wave: the upper 16 bits of its
+// order, one at a time (exact for bf16), and above -inf.
+template <int N>
+__device__ inline float kth_largest(const float (&x)[N], int K) {
+  unsigned k[N], prefix = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) k[i] = ordered(x[i]);
+#pragma unroll 1
+  for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+    const unsigned at = prefix | bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += __popcll(__ballot(k[i] >= at));
+    if (n >= K) prefix = at;
+  }
+  const unsigned b = prefix & 0x80000000u ? prefix & 0x7fffffffu : ~prefix;
+  const float f = __uint_as_float(b);
+  return f > -3.40282347e38f ? f : -3.40282347e38f;  // (whatever is no number: everything passes)
+}
+
+// Appends this thread's elements from `bound` on; v[i] stands at column(i).
+template <int N, typename L, typename C>
+__device__ inline void append(L* list, const float* v, float bound, C column) {
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) n += v[i] >= bound;
+  if (n == 0) return;
+  int at = atomicAdd(&list->count, n);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (v[i] >= bound) {
+      if (at < list->CAP) list->c[at] = candidate(v[i], column(i));
+      ++at;
+    }
+}
+
+// The bound of the K-th best from every thread's largest element: the workgroup's, in LDS.
+template <int THREADS>
+__device__ inline float bound_of(float mine, int K, float* maxima) {
+  if constexpr (THREADS == 64) {
+    const float x[1] = {mine};
+    return kth_largest<1>(x, K);
+  } else {
+    maxima[threadIdx.x] = mine;
+    __syncthreads();
+    float x[THREADS / 64];
+#pragma unroll
+    for (int i = 0; i < THREADS / 64; ++i) x[i] = maxima[i * 64 + (threadIdx.x & 63)];
+    return kth_largest<THREADS / 64>(x, K);
+  }
+}
+
+// The K best of a row's columns where the list was too short: pieces of 16 bytes per thread,
+// each with a bound of its own, its K best joined to those before it.  Later
+// columns that equal the K-th best stay out.
+template <int THREADS, bool BF16, typename L>
+__device__ __noinline__ int reread(const char* x, int begin, int end, int K, L* list,
+                                   float* maxima) {
+  constexpr int EV = Piece<BF16>::EV;
+  int m = 0;
+  for (int c = begin; c < end; c += THREADS * EV) {
+    const int col = c + int(threadIdx.x) * EV;
+    Piece<BF16> in;
+    in.load(x, col, end);
+    float v[EV], most = kNegInf;
+    in.floats(v);
+#pragma unroll
+    for (int i = 0; i < EV; ++i) most = fmaxf(most, v[i]);
+    __syncthreads();  // (the list and the maxima have been read)
+    if (threadIdx.x == 0) list->count = 0;
+    float bound = bound_of<THREADS>(most, K, maxima);
+    __syncthreads();
+    append<EV>(list, v, bound, [&](int i) { return col + i; });
+    __syncthreads();
+    if (threadIdx.x < 64) m = take_best(list, list->count, K, m);
+  }
+  return m;
+}
+
+// Results of a row from its sums; the first wave has the m best of the list in order.
 template <int THREADS, bool BF16, bool ENT, bool TOP, typename L>
-__device__ inline void finish(const LogprobParams& p, long row, const Sums& a, L* list) {
+__device__ inline void finish(const LogprobParams& p, long row, const Sums& a, L* list, int m) {
   constexpr int size = BF16 ? 2 : 4;
   const char* const x = static_cast<const char*>(p.x) + row * p.xs * size;
   const bool gone = a.m == kNegInf && a.s == 0.f;  // (a row of NaN has another s)
   const float o = origin(a.m), logs = kLn2 * __builtin_amdgcn_logf(a.s);
   if (threadIdx.x == 0) {
-    // a row of NaN alone has no largest element
     if (p.lse) p.lse[row] = gone ? kNegInf : fmaf(o, p.scale, logs);
     if (ENT && p.entropy) p.entropy[row] = gone ? 0.f : logs - kLn2 * a.t / a.s;
   }
@@ -190,22 +297,23 @@ __device__ inline void finish(const LogprobParams& p, long row, const Sums& a, L
     p.logp[row * p.G + g] = r;
   }
   if constexpr (TOP) {
-    // fewer than K that are not masked: the first masked columns, then those of NaN
-    if (list->count < p.K && threadIdx.x < 64) {
-      int at = list->count, nans = 0;
+    if (threadIdx.x >= 64) return;
+    const int lane = threadIdx.x;
+    if (m < p.K) {
+      // fewer than K that are not masked: the first masked columns, then those of NaN
+      int at = m, nans = 0;
       int nan_col = 0;  // lane i: the column of the i-th NaN
       for (int c = 0; c < p.V && at < p.K; c += 64) {
-        const int col = c + int(threadIdx.x);
+        const int col = c + lane;
         const float v = col < p.V ? load1<BF16>(x, col) : 0.f;
         const u64 masked = __ballot(v == kNegInf), nan = __ballot(v != v);
-        const u64 below = (1ull << threadIdx.x) - 1;
         if (v == kNegInf) {
-          const int i = at + __popcll(masked & below);
-          if (i < p.K) list->c[i] = candidate(kNegInf, col);
+          const int i = at + __popcll(masked & ((1ull << lane) - 1));
+          if (i < p.K) list->best[i] = candidate(kNegInf, col);
         }
         at += __popcll(masked);
         if (nan) {  // lane i takes NaN number nans + j from the j-th lane that has one
-          const int j = int(threadIdx.x) - nans;
+          const int j = lane - nans;
           u64 rest = nan;
           for (int k = 0; k < j && rest; ++k) rest &= rest - 1;
           if (j >= 0 && rest) nan_col = c + __builtin_ctzll(rest);
@@ -213,17 +321,14 @@ __device__ inline void finish(const LogprobParams& p, long row, const Sums& a, L
         }
       }
       // NaN is last; it keeps the key of none with its column
-      if (at < p.K) {
-        const int i = at + int(threadIdx.x);
-        if (i < p.K && int(threadIdx.x) < nans) list->c[i] = unsigned(~nan_col);
-      }
+      if (at + lane < p.K && lane < nans) list->best[at + lane] = unsigned(~nan_col);
+      wave_fence();
     }
-    __syncthreads();
-    if (int(threadIdx.x) < p.K) {
-      const u64 c = list->c[threadIdx.x];
+    if (lane < p.K) {
+      const u64 c = list->best[lane];
       const float v = c >> 32 ? value_of(c) : __builtin_nanf("");
-      p.top[row * p.K + threadIdx.x] = column_of(c);
-      p.top_logp[row * p.K + threadIdx.x] = gone ? kNegInf : fmaf(v - o, p.scale, -logs);
+      p.top[row * p.K + lane] = column_of(c);
+      p.top_logp[row * p.K + lane] = gone ? kNegInf : fmaf(v - o, p.scale, -logs);
     }
   }
 }
@@ -234,15 +339,16 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int p
                                                           int columns) {
   constexpr int EV = Piece<BF16>::EV, NV = 32 / EV, CH = THREADS * 32;
   __shared__ float red[3 * (THREADS / 64)];
-  __shared__ List<THREADS, TOP ? THREADS * EV : 1> list;
+  // (a piece of the second reading fits too)
+  __shared__ List<TOP ? THREADS * 8 : 1> list;
+  __shared__ float maxima[TOP ? THREADS : 1];
   const long row = blockIdx.x / parts;
   const int part = int(blockIdx.x - row * parts), begin = part * columns;
   const int end = min(begin + columns, p.V);
   const char* const x = static_cast<const char*>(p.x) + row * p.xs * (BF16 ? 2 : 4);
   const float c2 = p.scale * kLog2e;
   Sums a{kNegInf, 0.f, 0.f};
-  float bound = kNegInf;   // elements above it are candidates,
-  bool equal = false;      // and those that equal it
+  float bound = kNegInf;
   if (TOP && threadIdx.x == 0) list.count = 0;
   Piece<BF16> next[NV];
 #pragma unroll
@@ -270,84 +376,25 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int p
     }
     a.s += s;
     if constexpr (TOP) {
-      const int K = p.K;
-      if (c == begin) {
-        // the K-th largest of the threads' maxima
-        list.maxima[threadIdx.x] = mc;
-        __syncthreads();
-        int rank = 0;
-#pragma unroll 8
-        for (int j = 0; j < THREADS; ++j) {
-          const float y = list.maxima[j];
-          rank += y > mc || (y == mc && j < int(threadIdx.x));
-        }
-        if (rank == K - 1) list.bound = mc;
-        __syncthreads();
-        bound = list.bound;
-        equal = bound > kNegInf;
-      }
-      auto passes = [&](float y) { return y > bound || (equal && y == bound); };
-      const int before = list.count;
-      __syncthreads();
-      if (passes(mc)) {
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) n += passes(v[i]);
-        int at = atomicAdd(&list.count, n);
-        if (at + n <= list.CAP)
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (passes(v[i])) {
-              const int col = c + ((i / EV) * THREADS + int(threadIdx.x)) * EV + i % EV;
-              list.c[at++] = candidate(v[i], col);
-            }
-      }
-      __syncthreads();
-      const int n = list.count;
-      __syncthreads();
-      if (n > list.CAP) {
-        // many equal elements: again, 16 bytes per thread at a time, cut after each
-        if (threadIdx.x == 0) list.count = before;
-        __syncthreads();
-        if (before > 0) list.cut(K);
-#pragma unroll 1
-        for (int k = 0; k < NV; ++k) {
-          if (list.count >= K) {
-            bound = value_of(list.c[K - 1]);
-            equal = false;
-          }
-          __syncthreads();
-          float u[EV];
-#pragma unroll
-          for (int i = 0; i < EV; ++i) {
-            u[i] = v[i];
-#pragma unroll
-            for (int kk = 1; kk < NV; ++kk) u[i] = kk == k ? v[kk * EV + i] : u[i];
-          }
-#pragma unroll
-          for (int i = 0; i < EV; ++i)
-            if (passes(u[i]))
-              list.c[atomicAdd(&list.count, 1)] =
-                  candidate(u[i], c + (k * THREADS + int(threadIdx.x)) * EV + i);
-          __syncthreads();
-          list.cut(K);
-        }
-      } else if (n > 256) {
-        list.cut(K);
-      }
-      if (n > 256 && list.count >= K) {
-        bound = value_of(list.c[K - 1]);
-        equal = false;
-      }
+      if (c == begin) bound = bound_of<THREADS>(mc, p.K, maxima);
+      if (mc >= bound)
+        append<32>(&list, v, bound, [&](int i) {
+          return c + ((i / EV) * THREADS + int(threadIdx.x)) * EV + i % EV;
+        });
     }
   }
   join<THREADS, ENT>(a, c2, red);
+  int m = 0;
   if constexpr (TOP) {
     __syncthreads();
-    list.cut(p.K);
+    const int n = list.count;
+    if (n > list.CAP)
+      m = reread<THREADS, BF16>(x, begin, end, p.K, &list, maxima);
+    else if (threadIdx.x < 64)
+      m = take_best(&list, n, p.K);
   }
   if (parts == 1) {
-    finish<THREADS, BF16, ENT, TOP>(p, row, a, &list);
+    finish<THREADS, BF16, ENT, TOP>(p, row, a, &list, m);
     return;
   }
   const int words = 4 + 2 * p.K;
@@ -359,7 +406,7 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int p
   }
   if (TOP && int(threadIdx.x) < p.K)
     reinterpret_cast<u64*>(out + 4)[threadIdx.x] =
-        int(threadIdx.x) < list.count ? list.c[threadIdx.x] : 0ull;
+        int(threadIdx.x) < m ? list.best[threadIdx.x] : 0ull;
 }
 
 // Joins the parts of a row.
@@ -367,7 +414,7 @@ constexpr int kJoinThreads = 256;
 template <bool BF16, bool ENT, bool TOP>
 __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobParams p, int parts) {
   __shared__ float red[3 * (kJoinThreads / 64)];
-  __shared__ List<kJoinThreads, TOP ? 64 * kMaxTop : 1> list;
+  __shared__ List<TOP ? 64 * kMaxTop : 1> list;
   const long row = blockIdx.x;
   const int words = 4 + 2 * p.K;
   const float* const in = p.parts + row * parts * words;
@@ -376,6 +423,7 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobParam
     const float* const q = in + long(threadIdx.x) * words;
     a = Sums{q[0], q[1], q[2]};
   }
+  int m = 0;
   if constexpr (TOP) {
     // Each part's best are in order: with q = ceil(K / parts) of every part there are K, so the
     // least of the parts' q-th is a bound.
@@ -394,10 +442,10 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobParam
       if (y >= bound) list.c[atomicAdd(&list.count, 1)] = y;
     }
     __syncthreads();
-    list.cut(p.K);
+    if (threadIdx.x < 64) m = take_best(&list, list.count, p.K);
   }
   join<kJoinThreads, ENT>(a, p.scale * kLog2e, red);
-  finish<kJoinThreads, BF16, ENT, TOP>(p, row, a, &list);
+  finish<kJoinThreads, BF16, ENT, TOP>(p, row, a, &list, m);
 }
 
 // ---- gradient ----------------------------------------------------------------------------
@@ -405,8 +453,8 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobParam
 // - sum of the given tokens' gradients; then the given tokens that stand in the workgroup's
 // columns are written again with their own gradients added (equal ones all, so
 // that it does not matter which thread writes last).
-constexpr int kBackThreads = 256;
-constexpr int kBackColumns = 4096;  // of a workgroup
+// A workgroup has kBackColumns columns of a row, a wave up to a quarter of that.
+constexpr int kBackColumns = 4096;
 
 template <bool BF16>
 __device__ inline void store_any(char* row, int c, int end, const float* x) {
@@ -419,7 +467,7 @@ __device__ inline void store_any(char* row, int c, int end, const float* x) {
         w[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
       else
         w[i] = __float_as_uint(x[i]);
-    *reinterpret_cast<u32x4_any*>(row + long(c) * (BF16 ? 2 : 4)) = w;
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4_any*>(row + long(c) * (BF16 ? 2 : 4)));
     return;
   }
 #pragma unroll
@@ -432,36 +480,39 @@ __device__ inline void store_any(char* row, int c, int end, const float* x) {
     }
 }
 
-template <bool BF16, bool ENT>
-__global__ __launch_bounds__(kBackThreads) void logprob_backward_kernel(LogprobParams p,
-                                                                        int blocks) {
-  constexpr int EV = Piece<BF16>::EV, NV = kBackColumns / (kBackThreads * EV);
+template <int THREADS, bool BF16, bool ENT>
+__global__ __launch_bounds__(THREADS) void logprob_backward_kernel(LogprobParams p, int blocks) {
+  constexpr int EV = Piece<BF16>::EV, NV = kBackColumns / (256 * EV), MINE = kMaxGiven / THREADS;
   constexpr int size = BF16 ? 2 : 4;
   __shared__ int token[kMaxGiven];
   __shared__ float grad[kMaxGiven];
   const long row = blockIdx.x / blocks;
-  const int begin = int(blockIdx.x - row * blocks) * kBackColumns;
-  const int end = min(begin + kBackColumns, p.V);
+  const int begin = int(blockIdx.x - row * blocks) * (THREADS * EV * NV);
+  const int end = min(begin + THREADS * EV * NV, p.V);
   const char* const x = static_cast<const char*>(p.x) + row * p.xs * size;
   char* const dx = static_cast<char*>(p.dx) + row * p.V * size;
   Piece<BF16> in[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k)
-    in[k].load(x, begin + (k * kBackThreads + int(threadIdx.x)) * EV, end);
+    in[k].load(x, begin + (k * THREADS + int(threadIdx.x)) * EV, end);
   const float lse = p.lse_in[row];
   const bool gone = lse == kNegInf;
   float a = p.dlse ? p.dlse[row] : 0.f;
   const float dh = ENT ? p.dentropy[row] : 0.f, h = ENT ? p.entropy_in[row] : 0.f;
   // the given tokens' gradients; a token past the vocabulary makes the row NaN
-  int mine = -1;
-  float at_mine = 0.f;
-  for (int g = threadIdx.x; g < p.G; g += kBackThreads) {
+  int mine[MINE];
+  float at_mine[MINE];
+#pragma unroll
+  for (int i = 0; i < MINE; ++i) {
+    const int g = i * THREADS + int(threadIdx.x);
+    mine[i] = -1;
+    if (g >= p.G) continue;
     const int v = p.given[row * p.G + g];
     token[g] = v;
     grad[g] = v < 0 ? 0.f : v < p.V ? p.dlogp[row * p.G + g] : __builtin_nanf("");
-    if (v >= begin && v < end) {
-      mine = v;
-      at_mine = load1<BF16>(x, v);
+    if (v >= begin && v < end) {  // (read before anything is stored: dx may be x)
+      mine[i] = v;
+      at_mine[i] = load1<BF16>(x, v);
     }
   }
   if (p.G > 0) {
@@ -478,7 +529,7 @@ __global__ __launch_bounds__(kBackThreads) void logprob_backward_kernel(LogprobP
   };
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int c = begin + (k * kBackThreads + int(threadIdx.x)) * EV;
+    const int c = begin + (k * THREADS + int(threadIdx.x)) * EV;
     if (c >= end) break;
     float v[EV];
     in[k].floats(v);
@@ -488,14 +539,16 @@ __global__ __launch_bounds__(kBackThreads) void logprob_backward_kernel(LogprobP
   }
   if (p.G == 0) return;
   __syncthreads();
-  if (mine >= 0) {
+#pragma unroll
+  for (int i = 0; i < MINE; ++i) {
+    if (mine[i] < 0) continue;
     float s = 0.f;
-    for (int g = 0; g < p.G; ++g) s += token[g] == mine ? grad[g] : 0.f;
-    const float y = gone ? 0.f : p.scale * (value(at_mine) + s);
+    for (int g = 0; g < p.G; ++g) s += token[g] == mine[i] ? grad[g] : 0.f;
+    const float y = gone ? 0.f : p.scale * (value(at_mine[i]) + s);
     if constexpr (BF16)
-      reinterpret_cast<uint16_t*>(dx)[mine] = uint16_t(pack_bf16x2(y, y));
+      reinterpret_cast<uint16_t*>(dx)[mine[i]] = uint16_t(pack_bf16x2(y, y));
     else
-      reinterpret_cast<float*>(dx)[mine] = y;
+      reinterpret_cast<float*>(dx)[mine[i]] = y;
   }
 }
 
@@ -529,20 +582,22 @@ hipError_t launch_logprobs(const LogprobParams& p, const LogprobPlan& plan, bool
 
 hipError_t launch_logprobs_backward(const LogprobParams& p, bool bf16, hipStream_t st) {
   if (p.R == 0) return hipSuccess;
-  const int blocks = (p.V + kBackColumns - 1) / kBackColumns;
+  const bool wave = p.V <= kBackColumns / 4;
+  const int blocks = wave ? 1 : (p.V + kBackColumns - 1) / kBackColumns;
   const unsigned grid = unsigned(p.R * blocks);
-#define ONELA_BACK(B, E) \
-  logprob_backward_kernel<B, E><<<grid, kBackThreads, 0, st>>>(p, blocks)
-  if (bf16) {
-    if (p.dentropy)
-      ONELA_BACK(true, true);
-    else
-      ONELA_BACK(true, false);
+#define ONELA_BACK(B, E)                                                          \
+  if (wave)                                                                       \
+    logprob_backward_kernel<64, B, E><<<grid, 64, 0, st>>>(p, blocks);            \
+  else                                                                            \
+    logprob_backward_kernel<256, B, E><<<grid, 256, 0, st>>>(p, blocks)
+  if (bf16 && p.dentropy) {
+    ONELA_BACK(true, true);
+  } else if (bf16) {
+    ONELA_BACK(true, false);
+  } else if (p.dentropy) {
+    ONELA_BACK(false, true);
   } else {
-    if (p.dentropy)
-      ONELA_BACK(false, true);
-    else
-      ONELA_BACK(false, false);
+    ONELA_BACK(false, false);
   }
 #undef ONELA_BACK
   return hipGetLastError();

@@ -82,8 +82,8 @@ CASES = [
     (2, 1, 2056, "f32", "bf16", True, True, None, True, True, True, False),
     (3, 1, 4096, "bf16", "bf16", True, True, "sigmoid", True, True, True, True),
     (2, 1, 8192, "f32", "f32", True, True, "silu", True, True, True, False),
-    (3, 1, 8200, "bf16", "f32", True, True, "silu", True, True, True, False),
-    (2, 1, 16384, "f32", "f32", True, True, "silu", True, True, True, False),
+    (3, 1, 4104, "bf16", "f32", True, True, "silu", True, True, True, True),
+    (1500, 1, 8192, "bf16", "bf16", False, True, None, True, False, True, False),
     (10, 1, 256, "bf16", "f32", False, False, None, True, True, True, False),  # residual alone
     (10, 2, 40, "f32", "f32", False, False, "silu", False, True, True, False),  # a gate alone
 ]

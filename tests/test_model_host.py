@@ -115,7 +115,7 @@ def norm_back(lib, cfg, x=A, gate=B, res=C, wa=None, wb=None, cs=None, dy=D, dh=
 
 @pytest.mark.parametrize("bad", [
     dict(num_tokens=-1), dict(num_tokens=1 << 31), dict(num_heads=0), dict(width=0), dict(width=4),
-    dict(width=60), dict(width=16392), dict(io_dtype=2), dict(residual_dtype=-1),
+    dict(width=60), dict(width=8200), dict(io_dtype=2), dict(residual_dtype=-1),
     dict(norm_after=2), dict(norm_before=-1), dict(gate=3), dict(gate=-1), dict(x_stride=120),
     dict(x_stride=132), dict(gate_stride=127), dict(gate_stride=1 << 41), dict(eps=-1e-6),
     dict(eps=float("nan")), dict(residual_scale=float("inf")), dict(residual_scale=float("nan")),
@@ -310,7 +310,7 @@ def test_logprob_objects_refuse(entries):
 
 @pytest.mark.parametrize("make", [
     lambda: runner.ShortConv(1, 4, 12, 4, device="cpu"),
-    lambda: runner.BlockNorm(4, 20000, device="cpu"),
+    lambda: runner.BlockNorm(4, 8200, device="cpu"),
     lambda: runner.TokenLogprobs(4, 10, num_top=11, device="cpu")])
 def test_objects_of_refused_sizes(make):
     with pytest.raises(ab.OnelaError):
