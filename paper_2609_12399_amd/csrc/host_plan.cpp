@@ -386,11 +386,13 @@ onela_status_t check_conv(const onela_conv_config_t* c, bool ragged) {
     return ONELA_EINVAL;
   if (c->activation != ONELA_ACT_NONE && c->activation != ONELA_ACT_SILU) return ONELA_EINVAL;
   if (!ragged && c->total_tokens % c->num_seqs) return ONELA_EINVAL;
-  // a thread for every sequence's 8 channels, and for those of runs of tokens (conv_plan: 128
-  // tokens, fewer only while that makes some 2^18 threads)
-  const double groups = double(c->channels) / 8 + 64;
-  if ((double(c->num_seqs) + double(c->total_tokens) / 64 + 512) * groups >= kGridThreads / 2)
-    return ONELA_EINVAL;
+  // (a thread for kConvLane channels of every sequence, for the states, and of every run)
+  const double states = double(c->num_seqs) * (c->channels / kConvLane) + kConvThreads;
+  for (bool backward : {false, true}) {
+    const ConvPlan a = conv_plan(c, backward);
+    if (double(a.blocks_t) * a.blocks_c * kConvThreads + states >= kGridThreads)
+      return ONELA_EINVAL;
+  }
   return ONELA_OK;
 }
 
@@ -477,17 +479,18 @@ onela_status_t check_logprob(const onela_logprob_config_t* c) {
 
 LogprobPlan logprob_plan(const onela_logprob_config_t* c) {
   LogprobPlan a{256, 1, c->vocab};
+  // Short rows by a wave each: 8192 rows of 1000 with the 20 best 19 us, by four waves 51.
   if (c->vocab <= 2048) a.threads = 64;
-  // Few rows: cut into parts until there are workgroups for the chip.
-  const int step = 8192;
-  const long chunks = (long(c->vocab) + step - 1) / step;
+  // Few rows in parts of 8192 columns or more, where that saves more than the second launch takes.
+  // us whole / in parts: with the 20 best, 1 x 32768 15.2 / 12.6, 1 x 131072 33 / 15, 8 x 50001
+  // 21.5 / 13.7, 64 x 131072 35 / 19, 300 x 50001 26 / 26; the sum alone, 1 x 32768 7.4 / 10.2, 8 x
+  // 50001 9.7 / 10.5, 1 x 131072 16.7 / 10.9, 64 x 131072 17.4 / 11.4.
+  const long chunks = (long(c->vocab) + 8191) / 8192;
   const long rows = c->num_rows > 0 ? long(c->num_rows) : 1;
-  if (chunks > 1 && rows < 512) {
-    long parts = (1024 + rows - 1) / rows;
-    if (parts > chunks) parts = chunks;
-    if (parts > 64) parts = 64;
+  if (rows < 256 && chunks >= (c->num_top > 0 ? 4 : 8)) {
+    const long parts = std::min({chunks, long(kLogprobParts), 1024 / rows});
     const long per = (chunks + parts - 1) / parts;
-    a.columns = int(per * step);
+    a.columns = int(per * 8192);
     a.parts = int((chunks + per - 1) / per);
   }
   return a;

@@ -33,7 +33,7 @@ static void conv(const onela_conv_config_t& c) {
       EXPECT((long(a.blocks_c) << a.lanes_log2) * 8 >= c.channels);
       const double covered = double(a.blocks_t) * a.run * (kConvThreads >> a.lanes_log2);
       EXPECT(covered >= double(c.total_tokens));
-      const double states = (double(c.num_seqs) * (c.channels / 8) + kConvThreads) / kConvThreads;
+      const double states = (double(c.num_seqs) * (c.channels / kConvLane) + kConvThreads) / kConvThreads;
       EXPECT((double(a.blocks_t) * a.blocks_c + states) * kConvThreads < kGridThreads);
       if (backward)
         EXPECT(conv_workspace_bytes(&c) >=
@@ -51,7 +51,7 @@ static void norm(const onela_block_norm_config_t& c) {
 static void logprob(const onela_logprob_config_t& c) {
   if (check_logprob(&c) != ONELA_OK) return;
   const LogprobPlan a = logprob_plan(&c);
-  EXPECT(a.threads >= kMaxTop && a.parts >= 1 && a.parts <= 64 && a.columns >= 1);
+  EXPECT(a.threads >= kMaxTop && a.parts >= 1 && a.parts <= kLogprobParts && a.columns >= 1);
   EXPECT(double(a.parts) * a.columns >= c.vocab && double(a.parts - 1) * a.columns < c.vocab);
   EXPECT(double(c.num_rows) * a.parts * a.threads < kGridThreads);
   const size_t n = logprob_workspace_bytes(&c);
