@@ -1,9 +1,10 @@
 """A Gated DeltaNet mixing layer on the library's operators: what stands around the
 large-beam decode in a model.
 
-One layer projects its input to queries, keys, values and two gates per value head, norms and
-turns the queries and keys (``onela_qk_norm_rope``), mixes the tokens by the delta rule
-(``onela_delta_rule_*``) and projects back.  The same weights serve
+One layer projects its input to queries, keys, values and two gates per value head, may pass
+them through a short causal convolution (``onela_short_conv*``), norms and turns the queries and
+keys (``onela_qk_norm_rope``), mixes the tokens by the delta rule (``onela_delta_rule_*``), may norm
+the heads' outputs and gate them (``onela_block_norm``) and projects back.  The same weights serve
 
 * a training step: :meth:`DeltaMixer.__call__` is differentiable (the operators' own
   backward passes);
@@ -11,6 +12,9 @@ turns the queries and keys (``onela_qk_norm_rope``), mixes the tokens by the del
 * single tokens: :meth:`DeltaMixer.step` moves the states of a pool on in place;
 * a beam search from a prompt's state: :meth:`DeltaMixer.beam_step_inputs` gives what
   one step of :class:`runner.Decoder` takes.
+
+A layer with a convolution has two states, (the delta rule's, the convolution's), wherever one
+without has the first alone.  :mod:`recommender` puts such layers into a model.
 
     python -m paper_2609_12399_amd.mixer        # trains a small layer, then serves with it
 """
@@ -34,7 +38,7 @@ class _Once(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, d):
-        raise RuntimeError("the gradients of the delta rule and of the norm are differentiable once")
+        raise RuntimeError("the gradients of the library's operators are differentiable once")
 
 
 def _once(grads):
@@ -87,13 +91,100 @@ class DeltaRuleFunction(torch.autograd.Function):
         return dq, dk, dv, dla, db, None, ds, None, None
 
 
+class ShortConvFunction(torch.autograd.Function):
+    """x [tokens][channels], weight fp32 [channels][taps] -> (y, last states); seq_offsets int32
+    [num_seqs + 1] or None, initial_state [num_seqs][taps - 1][channels] or None."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, seq_offsets, initial_state, num_seqs, activation):
+        ctx.save_for_backward(x, weight, bias, seq_offsets, initial_state)
+        ctx.sizes = (num_seqs, *x.shape, weight.shape[1], _io(x), activation)
+        op = runner.ShortConv(*ctx.sizes, device=x.device)
+        return op.forward(x, weight, bias, seq_offsets, initial_state)
+
+    @staticmethod
+    def backward(ctx, d_y, d_state):
+        x, weight, bias, seq_offsets, initial_state = ctx.saved_tensors
+        op = runner.ShortConv(*ctx.sizes, backward=True, device=x.device)
+        dx, dw, db, ds = _once(op.backward(x, weight, d_y.contiguous(), bias, seq_offsets,
+                                           initial_state, d_state.contiguous()))
+        return dx, dw, db, None, ds, None, None
+
+
+class BlockNormFunction(torch.autograd.Function):
+    """(y, h) of runner.BlockNorm: x and gate [tokens][heads][width], residual of either type;
+    what is None is left out (y with a residual and without norm_before, h without a residual)."""
+
+    @staticmethod
+    def forward(ctx, x, residual, gate, after_weight, before_weight, channel_scale, norm_after,
+                norm_before, activation, residual_scale, eps):
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(x, residual, gate, after_weight, before_weight, channel_scale)
+        T, H, D = x.shape
+        ctx.sizes = (T, D, H, _io(x), None if residual is None else _io(residual), norm_after,
+                     norm_before, activation, residual_scale, eps)
+        op = runner.BlockNorm(*ctx.sizes, device=x.device)
+        return op.forward(x, residual, gate, after_weight, before_weight, channel_scale)
+
+    @staticmethod
+    def backward(ctx, d_y, d_h):
+        x, residual, gate, wa, wb, cs = ctx.saved_tensors
+        if d_y is None and d_h is None:
+            return (None,) * 11
+        d_y, d_h = (None if d is None else d.contiguous() for d in (d_y, d_h))
+        op = runner.BlockNorm(*ctx.sizes, backward=True, device=x.device)
+        grads = op.backward(x, d_y, residual, gate, wa, wb, cs, d_h)
+        return (*_once(grads), None, None, None, None, None)
+
+
+class TokenLogprobsFunction(torch.autograd.Function):
+    """(logp of the given tokens, lse, entropy, best tokens, their logp) of runner.TokenLogprobs;
+    the best ones are not differentiated (given again, they are)."""
+
+    @staticmethod
+    def forward(ctx, logits, given, num_top, scale, entropy):
+        ctx.set_materialize_grads(False)
+        num_given = 0 if given is None else given.shape[1]
+        ctx.sizes = (*logits.shape, num_given, 0, _io(logits), scale)
+        op = runner.TokenLogprobs(*logits.shape, num_given, num_top, _io(logits), scale, entropy,
+                                  device=logits.device)
+        out = op.forward(logits, given)
+        ctx.save_for_backward(logits, given, out[1], out[2])
+        ctx.mark_non_differentiable(*(t for t in out[3:] if t is not None))
+        return out
+
+    @staticmethod
+    def backward(ctx, d_logp, d_lse, d_entropy, *_):
+        logits, given, lse, entropy = ctx.saved_tensors
+        if d_logp is None and d_lse is None and d_entropy is None:
+            return (None,) * 5
+        if d_logp is None and given is not None:
+            d_logp = torch.zeros(given.shape, device=logits.device)
+        d_logp, d_lse, d_entropy = (None if d is None else d.contiguous()
+                                    for d in (d_logp, d_lse, d_entropy))
+        op = runner.TokenLogprobs(*ctx.sizes, backward=True, device=logits.device)
+        return (*_once((op.backward(logits, given, lse, d_logp, d_lse, entropy, d_entropy),)),
+                None, None, None, None)
+
+
+class BeamStates:
+    """What one layer keeps of a search's beams beside the decoder: the convolution's states, one
+    for each beam of the last step (at first one for each request, of its prompt), and the
+    present step's output gates."""
+
+    def __init__(self, conv=None):
+        self.conv, self.gate = conv, None
+
+
 class DeltaMixer:
     """One layer's weights and its four uses.  ``rotary_dim`` columns of each query and key
-    turn with the token's position (0: none, as the delta rule has it by itself)."""
+    turn with the token's position (0: none, as the delta rule has it by itself); with
+    ``conv_taps`` queries, keys and values pass a causal convolution of that length and silu;
+    ``gated`` norms every value head's output and multiplies it by the silu of a projection."""
 
     def __init__(self, width: int, num_qk_heads: int, num_v_heads: int, d_k: int, d_v: int,
                  io: str = "bf16", rotary_dim: int = 0, max_positions: int = 0, seed: int = 0,
-                 device="cuda:0"):
+                 device="cuda:0", conv_taps: int = 0, gated: bool = False):
         g = torch.Generator(device=device).manual_seed(seed)
         dt = {"bf16": torch.bfloat16, "f32": torch.float32}[io]
         self.HK, self.HV, self.dk, self.dv = num_qk_heads, num_v_heads, d_k, d_v
@@ -104,9 +195,17 @@ class DeltaMixer:
             w = torch.randn((n, m), generator=g, device=device) * n ** -0.5
             return w.to(dtype).requires_grad_()
 
-        self.w_qkv = weight(width, self.qkv_width, dt)
+        self.conv_taps, self.gated = conv_taps, gated
+        # (the output gate's columns stand behind those of queries, keys and values)
+        self.w_qkv = weight(width, self.qkv_width + (num_v_heads * d_v if gated else 0), dt)
         self.w_gates = weight(width, 2 * num_v_heads, torch.float32)
         self.w_out = weight(num_v_heads * d_v, width, dt)
+        self.w_conv = self.w_norm = None
+        if conv_taps:
+            self.w_conv = weight(conv_taps, self.qkv_width, torch.float32).detach().T.contiguous()
+            self.w_conv.requires_grad_()
+        if gated:
+            self.w_norm = torch.ones(d_v, device=device, requires_grad=True)
         self.cos_sin = None
         if rotary_dim:
             f = 10000.0 ** (-torch.arange(0, rotary_dim, 2, device=device) / rotary_dim)
@@ -114,14 +213,31 @@ class DeltaMixer:
             self.cos_sin = torch.cat([a.cos(), a.sin()], 1)
 
     def weights(self):
-        return [self.w_qkv, self.w_gates, self.w_out]
+        return [w for w in (self.w_qkv, self.w_gates, self.w_out, self.w_conv, self.w_norm)
+                if w is not None]
 
-    def _inputs(self, x, positions):
-        """q, k (normed, turned), v (a view of the projection), log(alpha), beta of tokens x."""
+    def _project(self, x):
+        """Rows of queries, keys and values side by side, and the output gates or None (views)."""
+        rows = x @ self.w_qkv
+        if not self.gated:
+            return rows, None
+        return rows[:, :self.qkv_width], rows[:, self.qkv_width:].unflatten(1, (self.HV, self.dv))
+
+    def _read_out(self, o, gate):
+        """The delta rule's outputs [tokens][heads][d_v] through the gate, projected back."""
+        if self.gated:
+            o, _ = BlockNormFunction.apply(o, None, gate, self.w_norm, None, None, True, False,
+                                           "silu", 1.0, 1e-6)
+        return o.flatten(1) @ self.w_out
+
+    def _inputs(self, x, positions, rows=None):
+        """q, k (normed, turned), v (a view of the projection), log(alpha), beta of tokens x, whose
+        projected (and convolved) rows are given where they are not x @ w_qkv."""
         if self.rotary_dim and positions is None:
             raise ValueError("a layer that rotates needs the tokens' positions")
-        n, qk = x.shape[0], self.HK * self.dk
-        rows = x @ self.w_qkv
+        qk = self.HK * self.dk
+        if rows is None:
+            rows, _ = self._project(x)
         q = rows[:, :qk].unflatten(1, (self.HK, self.dk))
         k = rows[:, qk:2 * qk].unflatten(1, (self.HK, self.dk))
         v = rows[:, 2 * qk:].unflatten(1, (self.HV, self.dv))
@@ -138,10 +254,16 @@ class DeltaMixer:
         if self.rotary_dim and positions is None:
             t = torch.arange(x.shape[0], dtype=torch.int32, device=x.device)
             positions = t - seq_offsets[torch.searchsorted(seq_offsets, t, right=True) - 1]
-        q, k, v, la, b = self._inputs(x, positions)
+        N = seq_offsets.numel() - 1
+        rows, gate = self._project(x)
+        if self.conv_taps:
+            initial_state, conv = (None, None) if initial_state is None else initial_state
+            rows, conv = ShortConvFunction.apply(rows, self.w_conv, None, seq_offsets, conv, N,
+                                                 "silu")
+        q, k, v, la, b = self._inputs(x, positions, rows)
         o, state = DeltaRuleFunction.apply(q, k, v, la.contiguous(), b.contiguous(), seq_offsets,
-                                           initial_state, seq_offsets.numel() - 1, 1.0)
-        return o.flatten(1) @ self.w_out, state
+                                           initial_state, N, 1.0)
+        return self._read_out(o, gate), (state, conv) if self.conv_taps else state
 
     @torch.no_grad()
     def prompt(self, x, seq_offsets, positions=None, initial_state=None):
@@ -151,25 +273,53 @@ class DeltaMixer:
     @torch.no_grad()
     def step(self, x, pool, slots, positions=None):
         """One token for each row of x on the states slots of the pool, in place."""
-        q, k, v, la, b = self._inputs(x, positions)
-        op = runner.DeltaRuleStep(x.shape[0], x.shape[0], self.HK, self.HV, self.dk, self.dv,
-                                  _io(q), pool.shape[0], device=self.device)
+        n = x.shape[0]
+        rows, gate = self._project(x)
+        if self.conv_taps:
+            pool, conv = pool
+            rows = runner.ShortConvStep(n, n, self.qkv_width, self.conv_taps, _io(rows),
+                                        conv.shape[0], device=self.device).step(
+                                            conv, slots, rows, self.w_conv)
+        q, k, v, la, b = self._inputs(x, positions, rows)
+        op = runner.DeltaRuleStep(n, n, self.HK, self.HV, self.dk, self.dv, _io(q), pool.shape[0],
+                                  device=self.device)
         o = op.step(pool, slots, q, k, v, la.contiguous(), b.contiguous())
-        return o.flatten(1) @ self.w_out
+        return self._read_out(o, gate)
 
     @torch.no_grad()
-    def beam_step_inputs(self, x, parents=None, positions=None) -> runner.DeviceStep:
+    def beam_step_inputs(self, x, parents=None, positions=None,
+                         beams: BeamStates | None = None) -> runner.DeviceStep:
         """x [requests][beams][width] -> the step that runner.Decoder takes; its output o
-        goes through :meth:`beam_outputs`."""
+        goes through :meth:`beam_outputs`.  A layer with a convolution or output gates takes the
+        search's ``beams``, which move on."""
         R, W = x.shape[:2]
-        q, k, v, la, b = self._inputs(x.flatten(0, 1), positions)
+        x = x.flatten(0, 1)
+        rows, gate = self._project(x)
+        if (self.conv_taps or self.gated) and beams is None:
+            raise ValueError("a layer with a convolution or gates needs the beams' states")
+        if self.conv_taps:
+            old = beams.conv
+            each = old.shape[0] // R  # states of a request
+            slots = torch.arange(R, dtype=torch.int32, device=x.device)[:, None] * each
+            slots = (slots + (0 if parents is None else parents)).expand(R, W)
+            beams.conv = old.new_empty((R * W, *old.shape[1:]))
+            rows = runner.ShortConvStep(R * W, R * W, self.qkv_width, self.conv_taps, _io(rows),
+                                        old.shape[0], device=self.device).step(
+                                            old, slots.flatten().contiguous(), rows, self.w_conv,
+                                            pool_out=beams.conv)
+        if self.gated:
+            beams.gate = gate
+        q, k, v, la, b = self._inputs(x, positions, rows)
         q, k, v = (t.to(self.w_qkv.dtype).contiguous().unflatten(0, (R, W)) for t in (q, k, v))
         alpha = torch.exp(la).contiguous().unflatten(0, (R, W))
         return runner.DeviceStep(q, k, v, alpha, b.contiguous().unflatten(0, (R, W)), parents, W)
 
     @torch.no_grad()
-    def beam_outputs(self, o):
-        return o.flatten(2).to(self.w_out.dtype) @ self.w_out
+    def beam_outputs(self, o, beams: BeamStates | None = None):
+        if not self.gated:
+            return o.flatten(2).to(self.w_out.dtype) @ self.w_out
+        return self._read_out(o.flatten(0, 1).to(beams.gate.dtype), beams.gate).unflatten(
+            0, o.shape[:2])
 
 
 def train(layer: DeltaMixer, x, target, seq_offsets, positions=None, steps: int = 30,

@@ -296,7 +296,7 @@ def _rows2(x, name: str, stride: int, optional: bool = False):
     return x.data_ptr()
 
 
-_torch_stream = None
+_torch_stream = _torch_device = None
 
 
 def _current_stream() -> int:
@@ -312,6 +312,18 @@ def _current_stream() -> int:
             device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
             _torch_stream = lambda: raw(device())  # noqa: E731
     return _torch_stream()
+
+
+def current_device() -> int:
+    """torch's current GPU; -1 without one."""
+    global _torch_device
+    if _torch_device is None:
+        import torch
+        if not torch.cuda.is_available():
+            return -1
+        torch.cuda.current_device()  # (starts torch's runtime if nothing has)
+        _torch_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _torch_device()
 
 
 def _stream(stream):

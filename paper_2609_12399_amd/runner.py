@@ -424,11 +424,11 @@ class QkNormRope:
 
 
 def _on_current_device(x):
-    """ValueError unless x is on the current device: the call is enqueued on a stream of that."""
-    torch = _torch()
-    if x.is_cuda and x.get_device() != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {x.device}, the current device is "
-                         f"cuda:{torch.cuda.current_device()}")
+    """ValueError unless x is on the current device: the call is enqueued on a stream of that.
+    (A host tensor is the binding's to refuse.)"""
+    current = ab.current_device()
+    if x.is_cuda and x.get_device() != current:
+        raise ValueError(f"tensors are on {x.device}, the current device is cuda:{current}")
 
 
 class _OnDevice:
@@ -518,7 +518,7 @@ class ShortConvStep(_OnDevice):
         self.num_slots, self.stream = num_slots, stream
         dt = _io_tensor_dtype(io)
         self.dtypes = dt, torch.float32, torch.int32
-        self.state = taps - 1, channels
+        self.pool = num_slots, taps - 1, channels
         self.shapes = ((total_tokens, channels), (channels, taps), (channels,), (num_seqs + 1,),
                        (num_seqs,))
         self.y = torch.empty((total_tokens, channels), dtype=dt, device=device)
@@ -528,15 +528,24 @@ class ShortConvStep(_OnDevice):
         """y; the pool's states move on in place, or from their slots to those of pool_out."""
         dt, f32, i32 = self.dtypes
         rows, weights, channels, bounds, seqs = self.shapes
-        self._check(x, (x, "x", rows, dt), (weight, "weight", weights, f32),
-                    (bias, "bias", channels, f32), (seq_offsets, "seq_offsets", bounds, i32),
-                    (slots, "slots", seqs, i32), (slots_out, "slots_out", seqs, i32))
+        try:  # (in one expression, as the delta rule's step)
+            fits = (x.dtype is dt and x.shape == rows and weight.dtype is f32 and
+                    weight.shape == weights and pool.dtype is dt and pool.shape == self.pool and
+                    (slots is None or slots.dtype is i32 and slots.shape == seqs) and
+                    bias is None and seq_offsets is None and slots_out is None and
+                    x.get_device() == ab.current_device())
+        except AttributeError:
+            fits = False
+        if not fits:
+            self._check(x, (x, "x", rows, dt), (weight, "weight", weights, f32),
+                        (bias, "bias", channels, f32), (seq_offsets, "seq_offsets", bounds, i32),
+                        (slots, "slots", seqs, i32), (slots_out, "slots_out", seqs, i32))
+            if not isinstance(pool, int) and pool is not None:  # (more slots do no harm)
+                _expect((pool, "pool", (max(self.num_slots, *pool.shape[:1]), *self.pool[1:]), dt))
         slots_of_out = 0
-        if not isinstance(pool, int) and pool is not None:  # (more slots do no harm)
-            _expect((pool, "pool", (max(self.num_slots, *pool.shape[:1]), *self.state), dt))
         if pool_out is not None:
-            _expect((pool_out, "pool_out", (*pool_out.shape[:1], *self.state), dt))
             slots_of_out = pool_out.shape[0]
+            _expect((pool_out, "pool_out", (slots_of_out, *self.pool[1:]), dt))
         self.cfg.x_stride = self._stride(x)
         ab.onela_short_conv_step(self.cfg, seq_offsets, x, weight, bias, pool, self.num_slots,
                                  slots, pool_out, slots_of_out, slots_out, self.y, self.stream)
@@ -582,10 +591,24 @@ class BlockNorm(_OnDevice):
     def _set(self, x, residual, gate, after_weight, before_weight, channel_scale):
         dt, rt, f32 = self.dtypes
         shape, width = self.shape, self.width
-        self._check(x, (x, "x", shape, dt), (gate, "gate", shape, dt),
-                    (residual, "residual", shape, rt), (after_weight, "after_weight", width, f32),
-                    (before_weight, "before_weight", width, f32),
-                    (channel_scale, "channel_scale", width, f32))
+        try:
+            fits = (x.dtype is dt and x.shape == shape and
+                    (gate is None or gate.dtype is dt and gate.shape == shape) and
+                    (residual is None or residual.dtype is rt and residual.shape == shape) and
+                    (after_weight is None or after_weight.dtype is f32 and
+                     after_weight.shape == width) and
+                    (before_weight is None or before_weight.dtype is f32 and
+                     before_weight.shape == width) and
+                    (channel_scale is None or channel_scale.dtype is f32 and
+                     channel_scale.shape == width) and x.get_device() == ab.current_device())
+        except AttributeError:
+            fits = False
+        if not fits:
+            self._check(x, (x, "x", shape, dt), (gate, "gate", shape, dt),
+                        (residual, "residual", shape, rt),
+                        (after_weight, "after_weight", width, f32),
+                        (before_weight, "before_weight", width, f32),
+                        (channel_scale, "channel_scale", width, f32))
         if self.gated != (gate is not None):
             raise ValueError("gate must be given" if self.gated else "this object has no gate")
         self.cfg.x_stride, self.cfg.gate_stride = self._stride(x), self._stride(gate)
@@ -658,8 +681,15 @@ class TokenLogprobs(_OnDevice):
 
     def _set(self, logits, given):
         dt, _, i32 = self.dtypes
-        self._check(logits, (logits, "logits", self.shapes[0], dt),
-                    (given, "given", self.shapes[1], i32))
+        rows, tokens, _ = self.shapes
+        try:
+            fits = (logits.dtype is dt and logits.shape == rows and
+                    (given is None or given.dtype is i32 and given.shape == tokens) and
+                    logits.get_device() == ab.current_device())
+        except AttributeError:
+            fits = False
+        if not fits:
+            self._check(logits, (logits, "logits", rows, dt), (given, "given", tokens, i32))
         if (given is None) != (self.num_given == 0):
             raise ValueError("given must be there exactly if num_given > 0")
         self.cfg.logits_stride = self._stride(logits)

@@ -1,0 +1,205 @@
+"""The convolution, the block norms and the log probabilities as a model uses them together
+(paper_2609_12399_amd/mixer.py with conv_taps and gated, recommender.py): gradients of a
+whole model against a 64-bit copy, the ways of serving a layer against each other, and the beam
+search against the model's own outputs over whole sequences."""
+import pytest
+
+from paper_2609_12399_amd import runner
+from paper_2609_12399_amd.workload import WorkloadSpec
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+mixer = pytest.importorskip("paper_2609_12399_amd.mixer")
+recommender = pytest.importorskip("paper_2609_12399_amd.recommender")
+DEV = "cuda:0"
+F = torch.nn.functional
+
+
+def rms(x, w):
+    return w * x / torch.sqrt(x.square().mean(-1, keepdim=True) + 1e-6)
+
+
+def layer64(layer, w, x, lengths):
+    w_qkv, w_gates, w_out, w_conv, w_norm = w
+    HK, HV, dk, dv, C = layer.HK, layer.HV, layer.dk, layer.dv, layer.qkv_width
+    rows = x @ w_qkv
+    out, t = [], 0
+    for n in lengths:
+        part = F.pad(rows[t:t + n, :C], (0, 0, layer.conv_taps - 1, 0))
+        part = F.silu((part.unfold(0, layer.conv_taps, 1) * w_conv).sum(-1))
+        q, k = (part[:, a:a + HK * dk].unflatten(1, (HK, dk)) for a in (0, HK * dk))
+        q, k = (v / torch.sqrt(v.square().sum(-1, keepdim=True) + 1e-6) for v in (q, k))
+        q, k = (v.repeat_interleave(HV // HK, 1) for v in (q, k))
+        v = part[:, 2 * HK * dk:].unflatten(1, (HV, dv))
+        g = x[t:t + n] @ w_gates
+        alpha, beta = torch.exp(-F.softplus(g[:, :HV] - 3.0)), torch.sigmoid(g[:, HV:])
+        S, o = torch.zeros((HV, dv, dk), dtype=x.dtype), []
+        for i in range(n):
+            S = alpha[i, :, None, None] * S
+            e = v[i] - (S * k[i][:, None]).sum(-1)
+            S = S + beta[i, :, None, None] * e[..., None] * k[i][:, None]
+            o.append((S * q[i][:, None]).sum(-1))
+        o = rms(torch.stack(o), w_norm) * F.silu(rows[t:t + n, C:].unflatten(1, (HV, dv)))
+        out.append(o.flatten(1) @ w_out)
+        t += n
+    return torch.cat(out)
+
+
+def loss64(model, weights, tokens, targets, lengths):
+    embedding, head, w_before, w_after, scale, *rest = weights
+    h = embedding[tokens]
+    y = rms(h, w_before[0])
+    for i, layer in enumerate(model.layers):
+        x = layer64(layer, rest[5 * i:5 * i + 5], y, lengths)
+        h = h + scale[i] * rms(x, w_after[i])
+        y = rms(h, w_before[i + 1])
+    logp = torch.log_softmax(y @ head, 1)
+    keep = targets >= 0
+    return -logp[keep, targets[keep]].mean()
+
+
+def make(io="f32", vocab=37):
+    model = recommender.Recommender(vocab, 48, 2, 2, 4, 32, io, device=DEV)
+    lengths = [20, 1, 9]
+    off = torch.tensor([0, 20, 21, 30], dtype=torch.int32, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    return model, lengths, off, torch.randint(0, vocab, (30,), generator=g, device=DEV), g
+
+
+def test_model_gradients():
+    """fp32 model: every weight's gradient to 3e-4 of its norm (per layer some ten products and
+    sums of up to 100 terms, 1e-5 each, and what the layers before and behind it pass on)."""
+    model, lengths, off, tokens, g = make()
+    targets = torch.randint(0, 37, (30,), generator=g, device=DEV).int()
+    targets[4] = targets[20] = -1
+    loss = model.loss(tokens, targets, off)
+    loss.backward()
+    weights = [w.detach().cpu().double().requires_grad_() for w in model.weights()]
+    want = loss64(model, weights, tokens.cpu(), targets.cpu().long(), lengths)
+    want.backward()
+    assert abs(loss.item() - want.item()) <= 1e-5 * want.item()
+    for w, v in zip(model.weights(), weights):
+        off_by = (w.grad.cpu().double() - v.grad).norm()
+        assert float(off_by) <= 3e-4 * float(v.grad.norm()), tuple(w.shape)
+
+
+def test_entropy_and_top_through_autograd():
+    """The function's three gradients against torch's own in 64 bits; the best tokens carry none."""
+    g = torch.Generator().manual_seed(5)
+    x = torch.randn((6, 50), generator=g)
+    given = torch.randint(0, 50, (6, 2), generator=g).int()
+    leaf = x.to(DEV).requires_grad_()
+    logp, lse, ent, top, top_logp = mixer.TokenLogprobsFunction.apply(leaf, given.to(DEV), 5, 0.5,
+                                                                      True)
+    assert not top_logp.requires_grad and not top.requires_grad
+    (logp.sum() + 2 * lse.square().sum() - 3 * ent.sum()).backward()
+    leaf64 = x.double().requires_grad_()
+    lp = torch.log_softmax(0.5 * leaf64, 1)
+    l64 = torch.logsumexp(0.5 * leaf64, 1)
+    (lp.gather(1, given.long()).sum() + 2 * l64.square().sum() + 3 * (lp.exp() * lp).sum()).backward()
+    assert float((leaf.grad.cpu() - leaf64.grad).abs().max()) <= 1e-5
+    assert torch.equal(top[:, 0].cpu().long(), x.argmax(1))
+    # one output alone
+    leaf.grad = None
+    mixer.TokenLogprobsFunction.apply(leaf, None, 0, 1.0, False)[1].sum().backward()
+    assert float((leaf.grad.cpu() - torch.softmax(x, 1)).abs().max()) <= 1e-6
+
+
+def serving_layer(io="bf16"):
+    layer = mixer.DeltaMixer(48, 2, 4, 32, 32, io, rotary_dim=16, max_positions=200, device=DEV,
+                             conv_taps=4, gated=True)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn((75, 48), generator=g, device=DEV).to(layer.w_qkv.dtype)
+    off = torch.tensor([0, 70, 75], dtype=torch.int32, device=DEV)
+    pos = torch.cat([torch.arange(70), torch.arange(5)]).to(torch.int32).to(DEV)
+    return layer, x, off, pos
+
+
+def test_prompt_step_and_beams_agree():
+    """The last tokens of a prompt one by one on pools, and as beams that change their parents,
+    give the prompt's own outputs (four bf16 roundings on the way of each)."""
+    layer, x, off, pos = serving_layer()
+    y, _ = layer.prompt(x, off, pos)
+    m = 66
+    cut = torch.tensor([0, m], dtype=torch.int32, device=DEV)
+    _, (state, conv) = layer.prompt(x[:m], cut, pos[:m])
+    pool = torch.zeros((3, *state.shape[1:]), device=DEV)
+    conv_pool = torch.zeros((3, *conv.shape[1:]), dtype=conv.dtype, device=DEV)
+    pool[2], conv_pool[2] = state[0], conv[0]
+    slots = torch.tensor([2], dtype=torch.int32, device=DEV)
+    spec = WorkloadSpec("mixer", 1, layer.HK, layer.HV, layer.dk, layer.dv, 0, (3,) * 4, "bf16",
+                        "uniform")
+    dec, beams = runner.Decoder(spec, state, DEV), mixer.BeamStates(conv)
+    big = float(y[:70].float().abs().max())
+    for t in range(4):
+        one = layer.step(x[m + t:m + t + 1], (pool, conv_pool), slots, pos[m + t:m + t + 1])
+        bx = x[m + t].expand(1, 3, -1).contiguous()
+        par = None if t == 0 else torch.tensor([[2, 0, 1]], dtype=torch.int32, device=DEV)
+        o = torch.empty((1, 3, layer.HV, layer.dv), device=DEV)
+        dec.step(t, layer.beam_step_inputs(bx, par, pos[m + t].repeat(3), beams), o, fused=True)
+        for got in (one[0], *layer.beam_outputs(o, beams)[0]):
+            assert float((got.float() - y[m + t].float()).abs().max()) <= 2.0 ** -5 * big
+    assert float(pool[:2].abs().max()) == 0.0 and float(conv_pool[:2].float().abs().max()) == 0.0
+    dec.close()
+    with pytest.raises(ValueError, match="beams"):
+        layer.beam_step_inputs(bx, None, pos[:3])
+
+
+def test_prompt_goes_on_from_both_states():
+    layer, x, off, pos = serving_layer()
+    y, (state, conv) = layer.prompt(x, off, pos)
+    a, b = 41, 3
+    first = torch.cat([torch.arange(a), 70 + torch.arange(b)]).to(DEV)
+    rest = torch.cat([torch.arange(a, 70), 70 + torch.arange(b, 5)]).to(DEV)
+    at = [torch.tensor(t, dtype=torch.int32, device=DEV)
+          for t in ([0, a, a + b], [0, 70 - a, 75 - a - b])]
+    _, mid = layer.prompt(x[first], at[0], pos[first])
+    z, end = layer.prompt(x[rest], at[1], pos[rest], initial_state=mid)
+    big = float(y.float().abs().max())
+    assert float((z.float() - y[rest].float()).abs().max()) <= 2.0 ** -5 * big
+    assert float((end[0] - state).abs().max()) <= 2.0 ** -5 * float(state.abs().max())
+    assert float((end[1].float() - conv.float()).abs().max()) <= \
+        2.0 ** -7 * float(conv.float().abs().max())
+
+
+def test_search_gives_what_whole_sequences_give():
+    """fp32: the search's scores are the log probabilities that the model gives the found
+    sequences as a whole (three tokens, 2e-3 for the decode's outputs through two layers), and
+    its beams are those of a search that runs the model over every sequence again."""
+    model, lengths, off, tokens, _ = make()
+    W, T, V = 6, 3, model.vocab
+    found, score = model.search(tokens, off, W, T)
+    starts = off.tolist()
+    for r, n in enumerate(lengths):
+        prompt = tokens[starts[r]:starts[r + 1]]
+
+        def logprobs(seqs):  # [beams][t]: of the token after every sequence
+            rows = torch.cat([prompt.expand(len(seqs), -1), seqs], 1)
+            at = torch.arange(len(seqs) + 1, dtype=torch.int32, device=DEV) * rows.shape[1]
+            with torch.no_grad():
+                x, _ = model(rows.flatten(), at)
+                return torch.log_softmax((x[at[1:].long() - 1] @ model.head).double(), 1)
+
+        seqs = torch.zeros((1, 0), dtype=torch.long, device=DEV)
+        best = torch.zeros(1, dtype=torch.float64, device=DEV)
+        for _ in range(T):
+            best, i = (best[:, None] + logprobs(seqs)).flatten().topk(W)
+            seqs = torch.cat([seqs[i // V], (i % V)[:, None]], 1)
+        assert float((best - score[r]).abs().max()) <= 2e-3
+        total = torch.zeros(W, dtype=torch.float64, device=DEV)
+        for t in range(T):
+            total += logprobs(found[r, :, :t].long()).gather(1, found[r, :, t:t + 1].long())[:, 0]
+        assert float((total - score[r]).abs().max()) <= 2e-3
+
+
+def test_example_runs(capsys):
+    recommender.main()
+    out = capsys.readouterr().out
+    assert "training: loss" in out and "search: 8 beams" in out
+
+
+def test_bf16_model_trains():
+    model, _, off, tokens, _ = make("bf16")
+    losses = recommender.train(model, tokens, torch.roll(tokens, -1).int(), off, steps=3)
+    assert all(v == v and v < 100 for v in losses)

@@ -315,3 +315,63 @@ def test_logprob_objects_refuse(entries):
 def test_objects_of_refused_sizes(make):
     with pytest.raises(ab.OnelaError):
         make()
+
+
+# ---- the functions and layers on them -----------------------------------------------------------------
+
+mixer = pytest.importorskip("paper_2609_12399_amd.mixer")
+
+
+def test_second_derivatives_are_refused(entries):
+    x, w = torch.randn(6, 16, requires_grad=True), torch.randn(16, 4, requires_grad=True)
+    outs = [mixer.ShortConvFunction.apply(x, w, None, None, None, 2, "silu")[0],
+            mixer.BlockNormFunction.apply(x[:, None], x[:, None], None, None, None, None, True, True,
+                                          None, 1.0, 1e-6)[0],
+            mixer.TokenLogprobsFunction.apply(x, None, 0, 1.0, True)[2]]
+    for y in outs:
+        dx, = torch.autograd.grad(y.sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="once"):
+            (dx.square().sum() + x.sum()).backward()
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_layer_with_convolution_and_gates_under_autocast(entries, monkeypatch, io):
+    """The operators take what the autocast products give; states and gates go with them."""
+    for name in ("onela_delta_rule_forward", "onela_delta_rule_step", "onela_qk_norm_rope"):
+        monkeypatch.setattr(ab, name, lambda *a, name=name, **k: entries.append(name))
+    layer = mixer.DeltaMixer(16, 1, 2, 32, 32, io, device="cpu", conv_taps=3, gated=True)
+    x = torch.randn(6, 16).to(layer.w_qkv.dtype)
+    off = torch.tensor([0, 2, 6], dtype=I32)
+    with torch.autocast("cpu", dtype=BF):
+        y, (state, conv) = layer.prompt(x, off)
+        assert conv.shape == (2, 2, layer.qkv_width) and conv.dtype is BF
+        layer.prompt(x, off, None, (state, conv))
+        layer.step(x[:2], (state, conv), torch.zeros(2, dtype=I32))
+        beams = mixer.BeamStates(conv)
+        layer.beam_step_inputs(x.unflatten(0, (2, 3)), None, None, beams)
+        assert beams.conv.shape == (6, 2, layer.qkv_width)
+        layer.beam_step_inputs(x.unflatten(0, (2, 3)), torch.zeros(2, 3, dtype=I32), None, beams)
+        layer.beam_outputs(torch.zeros(2, 3, 2, 32), beams)
+    prompt = ["onela_short_conv", "onela_qk_norm_rope", "onela_delta_rule_forward",
+              "onela_block_norm"]
+    step = ["onela_short_conv_step", "onela_qk_norm_rope"]
+    assert entries == [*prompt, *prompt, *step, "onela_delta_rule_step", "onela_block_norm", *step,
+                       *step, "onela_block_norm"]
+
+
+def test_recommender_on_the_entry_points(entries, monkeypatch):
+    """One training step calls, per layer, the convolution, the norm, the delta rule and two
+    block norms, and the log probabilities once, each with its gradient."""
+    recommender = pytest.importorskip("paper_2609_12399_amd.recommender")
+    for name in ("onela_delta_rule_forward", "onela_delta_rule_backward", "onela_qk_norm_rope",
+                 "onela_qk_norm_rope_backward"):
+        monkeypatch.setattr(ab, name, lambda *a, name=name, **k: entries.append(name))
+    model = recommender.Recommender(20, 16, 2, 1, 2, 32, "f32", device="cpu")
+    off = torch.tensor([0, 2, 6], dtype=I32)
+    model.loss(torch.arange(6), torch.arange(6).int(), off).backward()
+    assert all(w.grad is not None and w.grad.shape == w.shape for w in model.weights())
+    for name, n in (("onela_short_conv", 2), ("onela_short_conv_backward", 2),
+                    ("onela_block_norm", 5), ("onela_block_norm_backward", 5),
+                    ("onela_token_logprobs", 1), ("onela_token_logprobs_backward", 1),
+                    ("onela_delta_rule_backward", 2)):
+        assert entries.count(name) == n, name
