@@ -305,12 +305,19 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_
   if (!p.partial) return;
 #pragma unroll
   for (int j = 0; j < E; ++j) dc[j] *= p.scale;
-  float* const out = p.partial + long(blockIdx.x) * 3 * p.D;
+  const bool alone = gridDim.x == 1;  // (its sums are the results)
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     const auto& sum = k == 0 ? da : k == 1 ? db : dc;
+    float* const out = !alone   ? p.partial + (long(blockIdx.x) * 3 + k) * p.D
+                       : k == 0 ? p.dwa
+                       : k == 1 ? p.dwb
+                                : p.dcs;
+    if (!out) continue;
     if constexpr (RW == 1) {
-      if (in) RawN<false, E>::of(sum).store(out, long(k) * p.D + c0);
+      if (!in) continue;
+#pragma unroll
+      for (int j = 0; j < E; ++j) out[c0 + j] = sum[j];
     } else {
       __syncthreads();
 #pragma unroll
@@ -320,7 +327,7 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_
         float t = 0.f;
 #pragma unroll
         for (int i = 0; i < RW; ++i) t += acc[i][c];
-        out[long(k) * p.D + c] = t;
+        out[c] = t;
       }
     }
   }
@@ -370,7 +377,7 @@ hipError_t run(const BlockNormParams& p, bool backward, int cus, hipStream_t st)
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (p.partial)
+  if (p.partial && blocks != 1)
     block_norm_weight_kernel<<<unsigned(3 * ((p.D + 15) / 16)), 1024, 0, st>>>(p, int(blocks));
   return hipGetLastError();
 }

@@ -317,6 +317,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams 
   if (!p.partial) return;
   const int lanes = 1 << ll, c_first = at.c0 - E * (threadIdx.x & (lanes - 1));
   const long bt = blockIdx.x / blocks_c;
+  const bool alone = token_blocks == unsigned(blocks_c);  // over the tokens: its sums are the results
 #pragma unroll
   for (int j = 0; j <= TAPS; ++j)
 #pragma unroll
@@ -327,7 +328,13 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams 
     for (int j = 0; j <= TAPS; ++j) {
       float s = 0.f;
       for (int r = c / E; r < kConvThreads; r += lanes) s += acc[j][r][c % E];
-      p.partial[(bt * (TAPS + 1) + j) * p.C + c_first + c] = s;
+      const int ch = c_first + c;
+      if (!alone)
+        p.partial[(bt * (TAPS + 1) + j) * p.C + ch] = s;
+      else if (j < TAPS && p.dw)
+        p.dw[long(ch) * TAPS + j] = s;
+      else if (j == TAPS && p.db)
+        p.db[ch] = s;
     }
 }
 
@@ -435,7 +442,7 @@ hipError_t run_backward(const ConvParams& p, const ConvPlan& a, hipStream_t st) 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (p.partial)
+  if (p.partial && a.blocks_t != 1)
     conv_weight_kernel<<<unsigned((long(TAPS + 1) * p.C + 15) / 16), 256, 0, st>>>(p, TAPS,
                                                                                   a.blocks_t);
   return hipGetLastError();

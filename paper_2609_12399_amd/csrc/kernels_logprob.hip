@@ -149,13 +149,22 @@ __device__ inline float value_of(u64 c) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// The candidates of a workgroup, and room for the wave that takes the best of them.
-template <int CAPACITY>
+// The candidates of a workgroup's waves, each in a part of its own (so that finding a place takes
+// no exchange), and room for the wave that takes the best of them.
+template <int WAVES, int CAPACITY>
 struct List {
   static constexpr int CAP = CAPACITY;
-  u64 c[CAP];
+  u64 c[WAVES][CAP];
   u64 best[128];
-  int count;  // of candidates, those that found no room among them
+  int count[WAVES];  // of candidates, those that found no room among them
+
+  // Whether one wave had more than its part holds.
+  __device__ bool short_of_room() const {
+    int n = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) n = max(n, count[w]);
+    return n > CAP;
+  }
 };
 
 // LDS of one wave: what its lanes have written is what they read next.
@@ -182,22 +191,26 @@ __device__ inline int in_order(u64* best, int m, int K) {
   return m < K ? m : K;
 }
 
-// One wave: the K best of n candidates in `best`, in order; returns how many there are.  `m` of
-// them are there already.
-template <typename L>
-__device__ inline int take_best(L* list, int n, int K, int m = 0) {
+// One wave: the K best of the candidates in `best`, in order; returns how many there are.  `m`
+// of them are there already.
+template <int WAVES, int CAP>
+__device__ inline int take_best(List<WAVES, CAP>* list, int K, int m = 0) {
   const int lane = threadIdx.x & 63;
   u64 bound = m < K ? 0 : list->best[K - 1];
-  for (int i = 0; i < n; i += 64) {
-    const u64 x = i + lane < n ? list->c[i + lane] : 0;
-    const u64 pass = __ballot(x > bound);
-    if (!pass) continue;
-    if (x > bound) list->best[m + __popcll(pass & ((1ull << lane) - 1))] = x;
-    m += __popcll(pass);
-    wave_fence();
-    if (m >= 64) {
-      m = in_order(list->best, m, K);
-      if (m == K) bound = list->best[K - 1];
+#pragma unroll 1
+  for (int w = 0; w < WAVES; ++w) {
+    const int n = list->count[w];
+    for (int i = 0; i < n; i += 64) {
+      const u64 x = i + lane < n ? list->c[w][i + lane] : 0;
+      const u64 pass = __ballot(x > bound);
+      if (!pass) continue;
+      if (x > bound) list->best[m + __popcll(pass & ((1ull << lane) - 1))] = x;
+      m += __popcll(pass);
+      wave_fence();
+      if (m >= 64) {
+        m = in_order(list->best, m, K);
+        if (m == K) bound = list->best[K - 1];
+      }
     }
   }
   return in_order(list->best, m, K);
@@ -223,20 +236,18 @@ __device__ inline float kth_largest(const float (&x)[N], int K) {
   return f > -3.40282347e38f ? f : -3.40282347e38f;  // (whatever is no number: everything passes)
 }
 
-// Appends the wave's elements from `bound` on; v[i] of a lane stands at column(i).  Few pass: one
-// comparison per element finds the lanes that have one, and only then is there more to do.
+// Appends the wave's elements from `bound` on to its part of the list, which has `count`; v[i] of a
+// lane stands at column(i).  Few pass: one comparison per element finds the lanes that have one,
+// and only then is there more to do.
 template <int N, typename L, typename C>
-__device__ inline void append(L* list, const float* v, float bound, C column) {
-  const int lane = threadIdx.x & 63;
+__device__ inline void append(L* list, int& count, const float* v, float bound, C column) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const u64 pass = __ballot(v[i] >= bound);
     if (pass == 0) continue;
-    const int first = __builtin_ctzll(pass);
-    int at = 0;
-    if (lane == first) at = atomicAdd(&list->count, __popcll(pass));
-    at = __builtin_amdgcn_readlane(at, first) + __popcll(pass & ((1ull << lane) - 1));
-    if (v[i] >= bound && at < list->CAP) list->c[at] = candidate(v[i], column(i));
+    const int at = count + __popcll(pass & ((1ull << (threadIdx.x & 63)) - 1));
+    if (v[i] >= bound && at < L::CAP) list->c[threadIdx.x >> 6][at] = candidate(v[i], column(i));
+    count += __popcll(pass);
   }
 }
 
@@ -261,7 +272,7 @@ template <int THREADS, bool BF16, typename L>
 __device__ __noinline__ int reread(const char* x, int begin, int end, int K, L* list,
                                    float* maxima) {
   constexpr int EV = Piece<BF16>::EV;
-  static_assert(THREADS * EV <= L::CAP, "the list holds a piece");
+  static_assert(64 * EV <= L::CAP, "the list holds a piece");
   int m = 0;
   for (int c = begin; c < end; c += THREADS * EV) {
     const int col = c + int(threadIdx.x) * EV;
@@ -272,12 +283,12 @@ __device__ __noinline__ int reread(const char* x, int begin, int end, int K, L* 
 #pragma unroll
     for (int i = 0; i < EV; ++i) most = fmaxf(most, v[i]);
     __syncthreads();  // (the list and the maxima have been read)
-    if (threadIdx.x == 0) list->count = 0;
-    float bound = bound_of<THREADS>(most, K, maxima);
+    const float bound = bound_of<THREADS>(most, K, maxima);
+    int count = 0;
+    append<EV>(list, count, v, bound, [&](int i) { return col + i; });
+    if ((threadIdx.x & 63) == 0) list->count[threadIdx.x >> 6] = count;
     __syncthreads();
-    append<EV>(list, v, bound, [&](int i) { return col + i; });
-    __syncthreads();
-    if (threadIdx.x < 64) m = take_best(list, list->count, K, m);
+    if (threadIdx.x < 64) m = take_best(list, K, m);
   }
   return m;
 }
@@ -344,7 +355,7 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int p
   constexpr int EV = Piece<BF16>::EV, PER = 32, NV = PER / EV, CH = THREADS * PER;
   __shared__ float red[3 * (THREADS / 64)];
   // (a piece of the second reading fits too)
-  __shared__ List<TOP ? THREADS * 8 : 1> list;
+  __shared__ List<THREADS / 64, TOP ? 512 : 1> list;
   __shared__ float maxima[TOP ? THREADS : 1];
   const long row = blockIdx.x / parts;
   const int part = int(blockIdx.x - row * parts), begin = part * columns;
@@ -353,7 +364,7 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int p
   const float c2 = p.scale * kLog2e;
   Sums a{kNegInf, 0.f, 0.f};
   float bound = kNegInf;
-  if (TOP && threadIdx.x == 0) list.count = 0;
+  int count = 0;  // of the wave's candidates
   Piece<BF16> next[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k)
@@ -392,7 +403,7 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int p
 #pragma unroll
       for (int k = 0; k < NV; ++k)
         if (__ballot(mp[k] >= bound))
-          append<EV>(&list, v + k * EV, bound, [&](int i) {
+          append<EV>(&list, count, v + k * EV, bound, [&](int i) {
             return c + (k * THREADS + int(threadIdx.x)) * EV + i;
           });
     }
@@ -400,12 +411,12 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int p
   join<THREADS, ENT>(a, c2, red);
   int m = 0;
   if constexpr (TOP) {
+    if ((threadIdx.x & 63) == 0) list.count[threadIdx.x >> 6] = count;
     __syncthreads();
-    const int n = list.count;
-    if (n > list.CAP)
+    if (list.short_of_room())
       m = reread<THREADS, BF16>(x, begin, end, p.K, &list, maxima);
     else if (threadIdx.x < 64)
-      m = take_best(&list, n, p.K);
+      m = take_best(&list, p.K);
   }
   if (parts == 1) {
     finish<THREADS, BF16, ENT, TOP>(p, row, a, &list, m);
@@ -428,7 +439,7 @@ constexpr int kJoinThreads = 256;
 template <bool BF16, bool ENT, bool TOP>
 __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobParams p, int parts) {
   __shared__ float red[3 * (kJoinThreads / 64)];
-  __shared__ List<TOP ? kLogprobParts * kMaxTop : 1> list;
+  __shared__ List<1, TOP ? kLogprobParts * kMaxTop : 1> list;
   const long row = blockIdx.x;
   const int words = 4 + 2 * p.K;
   const float* const in = p.parts + row * parts * words;
@@ -441,7 +452,7 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobParam
   if constexpr (TOP) {
     // Each part's best are in order: with q = ceil(K / parts) of every part there are K, so the
     // least of the parts' q-th is a bound.
-    if (threadIdx.x == 0) list.count = 0;
+    if (threadIdx.x == 0) list.count[0] = 0;
     const int q = (p.K + parts - 1) / parts;
     u64 bound = ~0ull;
     for (int i = 0; i < parts; ++i) {
@@ -453,10 +464,10 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobParam
     for (int i = threadIdx.x; i < parts * p.K; i += kJoinThreads) {
       const int part = i / p.K;
       const u64 y = reinterpret_cast<const u64*>(in + long(part) * words + 4)[i - part * p.K];
-      if (y >= bound) list.c[atomicAdd(&list.count, 1)] = y;
+      if (y >= bound) list.c[0][atomicAdd(&list.count[0], 1)] = y;
     }
     __syncthreads();
-    if (threadIdx.x < 64) m = take_best(&list, list.count, p.K);
+    if (threadIdx.x < 64) m = take_best(&list, p.K);
   }
   join<kJoinThreads, ENT>(a, p.scale * kLog2e, red);
   finish<kJoinThreads, BF16, ENT, TOP>(p, row, a, &list, m);
