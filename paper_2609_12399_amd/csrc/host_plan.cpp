@@ -418,7 +418,7 @@ ConvPlan conv_plan(const onela_conv_config_t* c, bool backward) {
     // As many workgroups as the compute units hold at once (a last few would take as long as all
     // the others), in several turns only where that makes runs of more than 64 tokens: 8192
     // tokens x 6144 channels take 79 us in runs of 52 (one turn), 81 in 26, 83 in 18, 86 in 13.
-    const long held = 256l * (c->io_dtype == ONELA_BF16 ? 4 : 3);
+    const long held = 256l * (ll < 6 ? 2 : c->io_dtype == ONELA_BF16 ? 4 : 3);
     long turns = 0, blocks;
     do {
       ++turns;

@@ -18,8 +18,7 @@
 namespace onela {
 namespace {
 
-constexpr int kRows = 8;      // rows of x in flight per thread
-constexpr int kBackRows = 4;  // of x and dy, backward
+constexpr int kRows = 4;  // of x (and dy) in work per thread, and as many on their way
 
 struct Bounds {
   long b, e;
@@ -34,7 +33,7 @@ __device__ inline Bounds bounds_of(const ConvParams& p, int n) {
 // A sequence at or before the one that has token t0 (the wave's lowest): the last one that
 // begins at or before it, 64 offsets at a time.  Every lane of the wave takes part.
 __device__ inline int sequence_at(const ConvParams& p, long t0) {
-  if (!p.offsets) return p.L ? int(t0 / p.L) : 0;
+  if (!p.offsets) return p.L ? int(unsigned(t0) / unsigned(p.L)) : 0;
   const int lane = threadIdx.x & 63;
   int lo = 0, n = p.N;  // it is one of lo .. lo + n - 1
   while (n > 1) {
@@ -86,6 +85,24 @@ struct Before {
   __device__ void fill(Window<TAPS, E>& win) const {
 #pragma unroll
     for (int i = 0; i < TAPS - 1; ++i) r[i].floats(win.v[i + 1]);
+  }
+};
+
+// kRows rows, `stride` elements apart, those from `count` on zeros.
+template <bool BF16, int E>
+struct Rows {
+  RawN<BF16, E> r[kRows];
+  __device__ void load(const void* x, long i, long stride, unsigned c0, int count) {
+#pragma unroll
+    for (int k = 0; k < kRows; ++k)
+      if (k < count)
+        r[k].load(x, i + k * stride, c0);
+      else
+        r[k].clear();
+  }
+  __device__ void load(const void* x, long i, long stride, unsigned c0) {
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) r[k].load(x, i + k * stride, c0);
   }
 };
 
@@ -171,39 +188,44 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvParams p, int ll
     if (s.b >= at.t1) break;
     const long p0 = max(at.t0, s.b), p1 = min(at.t1, s.e);
     if (p0 >= p1) continue;
+    const int own = int(p1 - p0);
+    Rows<BF16, E> cur, next;
     // (the first rows are requested before anything is waited for)
-    RawN<BF16, E> cur[kRows];
-#pragma unroll
-    for (int i = 0; i < kRows; ++i)
-      if (p0 + i < p1) cur[i].load(p.x, (p0 + i) * p.xs, at.c0);
+    cur.load(p.x, p0 * p.xs, p.xs, at.c0, own);
     Before<TAPS, BF16, E> old;
     old.load(p, n, s.b, p0, at.c0);
     Window<TAPS, E> win;
     old.fill(win);
-    for (long t = p0; t < p1; t += kRows) {
-      RawN<BF16, E> next[kRows];
+    auto row = [&](int r, int i) {
+      float x[E], y[E];
+      cur.r[r].floats(x);
+      win.push(x);
+      w.apply(win, y);
+      store_output<BF16, E>(p, (p0 + i + r) * p.C, at.c0, y);
+    };
+    int i = 0;
+#pragma unroll 1
+    for (; i + 2 * kRows <= own; i += kRows) {
+      next.load(p.x, (p0 + i + kRows) * p.xs, p.xs, at.c0);
 #pragma unroll
-      for (int i = 0; i < kRows; ++i)
-        if (t + kRows + i < p1) next[i].load(p.x, (t + kRows + i) * p.xs, at.c0);
+      for (int r = 0; r < kRows; ++r) row(r, i);
+      cur = next;
+    }
+#pragma unroll 1
+    for (; i < own; i += kRows) {
+      next.load(p.x, (p0 + i + kRows) * p.xs, p.xs, at.c0, own - i - kRows);
 #pragma unroll
-      for (int i = 0; i < kRows; ++i) {
-        if (t + i >= p1) break;
-        float x[E], y[E];
-        cur[i].floats(x);
-        win.push(x);
-        w.apply(win, y);
-        store_output<BF16, E>(p, (t + i) * p.C, at.c0, y);
-      }
-#pragma unroll
-      for (int i = 0; i < kRows; ++i) cur[i] = next[i];
+      for (int r = 0; r < kRows; ++r)
+        if (i + r < own) row(r, i);
+      cur = next;
     }
   }
 }
 
+// (the workgroups that conv_plan takes a compute unit to hold at once)
 template <int TAPS, bool BF16, int E, bool WAVE>
-__global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams p, int ll, int run,
-                                                                     int blocks_c,
-                                                                     unsigned token_blocks) {
+__global__ __launch_bounds__(kConvThreads, WAVE ? (BF16 ? 4 : 3) : 2) void conv_backward_kernel(
+    ConvParams p, int ll, int run, int blocks_c, unsigned token_blocks) {
   if (blockIdx.x >= token_blocks) {  // sequences without tokens: the state passes through
     const long i = long(blockIdx.x - token_blocks) * kConvThreads + threadIdx.x;
     const int n = int(i / (p.C / E)), c0 = E * int(i - long(n) * (p.C / E));
@@ -234,84 +256,94 @@ __global__ __launch_bounds__(kConvThreads) void conv_backward_kernel(ConvParams 
       if (s.b >= at.t1) break;
       const long p0 = max(at.t0, s.b), p1 = min(at.t1, s.e);
       if (p0 >= p1) continue;
-      // tokens p0 .. p2 - 1: TAPS - 1 more, whose gradients the last inputs have a part of (the
-      // sequence's end is followed by zeros)
-      const long p2 = p1 + TAPS - 1, end = min(p2, s.e);
-      Window<TAPS, E> win, gs = {};
-      RawN<BF16, E> cx[kBackRows], cd[kBackRows];
-#pragma unroll
-      for (int i = 0; i < kBackRows; ++i)
-        if (p0 + i < end) {
-          cx[i].load(p.x, (p0 + i) * p.xs, at.c0);
-          cd[i].load(p.dy, (p0 + i) * p.C, at.c0);
-        }
+      // `own` tokens, and TAPS - 1 more, whose gradients the last inputs have a part of (rows behind
+      // `end`, the sequence's among them, are zeros); inputs from `last` on are in the last state
+      const int own = int(p1 - p0), all = own + TAPS - 1;
+      const int end = int(min(p0 + all, s.e) - p0);
+      const long last = p.ds_in ? s.e - (TAPS - 1) - p0 : p.total;
+      const int low = p0 == s.b && p.ds_out ? 1 - TAPS : 0;  // (below 0: inputs of the first state)
+      Rows<BF16, E> cx, cd, nx, nd;
+      cx.load(p.x, p0 * p.xs, p.xs, at.c0, end);
+      cd.load(p.dy, p0 * p.C, p.C, at.c0, end);
       Before<TAPS, BF16, E> before;
       before.load(p, n, s.b, p0, at.c0);
+      Window<TAPS, E> win, gs = {};
       before.fill(win);
-      for (long t = p0; t < p2; t += kBackRows) {
-        RawN<BF16, E> nx[kBackRows], nd[kBackRows];
+      // Row r of those in work: the gradient g before the activation and its share of the
+      // weights' (of the run's own tokens), and d of the input TAPS - 1 rows before.
+      auto row = [&](int r, bool mine, float(&d)[E]) {
+        float x[E], g[E];
+        cx.r[r].floats(x);
+        cd.r[r].floats(g);
+        win.push(x);
+        if (p.silu) {
+          float y[E];
+          w.apply(win, y);
 #pragma unroll
-        for (int i = 0; i < kBackRows; ++i)
-          if (t + kBackRows + i < end) {
-            nx[i].load(p.x, (t + kBackRows + i) * p.xs, at.c0);
-            nd[i].load(p.dy, (t + kBackRows + i) * p.C, at.c0);
+          for (int k = 0; k < E; ++k) {
+            const float sg = sigmoid(y[k]), t = fmaf(-y[k], sg, y[k]);
+            g[k] *= fmaf(sg, t, sg);  // s (1 + y (1 - s))
+          }
+        }
+        gs.push(g);
+        if (mine)
+#pragma unroll
+          for (int k = 0; k < E; ++k) {
+#pragma unroll
+            for (int j = 0; j < TAPS; ++j) dw[j][k] = fmaf(g[k], win.v[j][k], dw[j][k]);
+            dw[TAPS][k] += g[k];
           }
 #pragma unroll
-        for (int i = 0; i < kBackRows; ++i) {
-          const long tt = t + i;
-          if (tt >= p2) break;
-          float x[E] = {}, g[E] = {};
-          if (tt < end) {
-            cx[i].floats(x);
-            cd[i].floats(g);
+        for (int k = 0; k < E; ++k) {
+          d[k] = w.w[0][k] * gs.v[TAPS - 1][k];
+#pragma unroll
+          for (int j = 1; j < TAPS; ++j) d[k] = fmaf(w.w[j][k], gs.v[TAPS - 1 - j][k], d[k]);
+        }
+      };
+      int i = 0;
+#pragma unroll 1
+      do {
+        // the run's beginning and end
+        nx.load(p.x, (p0 + i + kRows) * p.xs, p.xs, at.c0, end - i - kRows);
+        nd.load(p.dy, (p0 + i + kRows) * p.C, p.C, at.c0, end - i - kRows);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          float d[E];
+          row(r, i + r < own, d);
+          const int o = i + r - (TAPS - 1);  // the input whose gradient is complete
+          if (o < low || o >= own) continue;
+          if (o >= last) {
+            RawN<BF16, E> f;
+            float v[E];
+            f.load(p.ds_in, (long(n) * (TAPS - 1) + (o - last)) * p.C, at.c0);
+            f.floats(v);
+#pragma unroll
+            for (int k = 0; k < E; ++k) d[k] += v[k];
           }
-          win.push(x);
-          if (p.silu && tt < end) {
-            float y[E];
-            w.apply(win, y);
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-              const float sg = sigmoid(y[k]), t = fmaf(-y[k], sg, y[k]);
-              g[k] *= fmaf(sg, t, sg);  // s (1 + y (1 - s))
-            }
-          }
-          gs.push(g);
-          if (tt < p1)
-#pragma unroll
-            for (int k = 0; k < E; ++k) {
-#pragma unroll
-              for (int j = 0; j < TAPS; ++j) dw[j][k] = fmaf(g[k], win.v[j][k], dw[j][k]);
-              dw[TAPS][k] += g[k];
-            }
-          const long o = tt - (TAPS - 1);  // the input whose gradient is complete
-          const bool old = o < p0;
-          if (old && (p0 != s.b || !p.ds_out)) continue;
-          float d[E] = {};
-#pragma unroll
-          for (int k = 0; k < E; ++k)
-#pragma unroll
-            for (int j = 0; j < TAPS; ++j) d[k] = fmaf(w.w[j][k], gs.v[TAPS - 1 - j][k], d[k]);
-          const long last = o - (s.e - (TAPS - 1));  // its place in the last state
-          if (last >= 0 && p.ds_in) {
-            float f[E];
-            RawN<BF16, E> r;
-            r.load(p.ds_in, (long(n) * (TAPS - 1) + last) * p.C, at.c0);
-            r.floats(f);
-#pragma unroll
-            for (int k = 0; k < E; ++k) d[k] += f[k];
-          }
-          if (old)
-            RawN<BF16, E>::of(d).store(p.ds_out,
-                                      (long(n) * (TAPS - 1) + (o - s.b + TAPS - 1)) * p.C, at.c0);
+          if (o >= 0)
+            RawN<BF16, E>::of(d).store_once(p.dx, (p0 + o) * p.C, at.c0);
           else
-            RawN<BF16, E>::of(d).store_once(p.dx, o * p.C, at.c0);
+            RawN<BF16, E>::of(d).store(p.ds_out, (long(n) * (TAPS - 1) + (o + TAPS - 1)) * p.C,
+                                       at.c0);
         }
+        cx = nx;
+        cd = nd;
+        // in between: all rows there and the run's own, no input in a state
+        static_assert(kRows >= TAPS - 1, "the rows before are behind the first ones");
+#pragma unroll 1
+        for (i += kRows; i + 2 * kRows <= own; i += kRows) {
+          nx.load(p.x, (p0 + i + kRows) * p.xs, p.xs, at.c0);
+          nd.load(p.dy, (p0 + i + kRows) * p.C, p.C, at.c0);
 #pragma unroll
-        for (int i = 0; i < kBackRows; ++i) {
-          cx[i] = nx[i];
-          cd[i] = nd[i];
+          for (int r = 0; r < kRows; ++r) {
+            float d[E];
+            row(r, true, d);
+            RawN<BF16, E>::of(d).store_once(p.dx, (p0 + i + r - (TAPS - 1)) * p.C, at.c0);
+          }
+          cx = nx;
+          cd = nd;
         }
-      }
+      } while (i < all);
     }
   }
   if (!p.partial) return;
