@@ -493,7 +493,9 @@ onela_status_t onela_qk_norm_rope_backward(const onela_norm_config_t* cfg, const
  *                Tokens behind the last sequence are not read, and their rows of the
  *                outputs are left as they were
  *   states       device [num_seqs][taps - 1][channels] io dtype, the oldest input first
- * channels: a multiple of 8; taps 2, 3 or 4.  Sums and gradients of the weights are fp32,
+ * channels: a multiple of 8 up to 2^26; taps 2, 3 or 4.  Sizes whose launches would take
+ * 2^32 threads or more (one per run of up to 16 tokens, backward 64, and 4 channels, one per
+ * sequence and 4 channels) are ONELA_EINVAL.  Sums and gradients of the weights are fp32,
  * in a fixed order; one rounding at each store. */
 typedef enum { ONELA_ACT_NONE = 0, ONELA_ACT_SILU = 1, ONELA_ACT_SIGMOID = 2 } onela_act_t;
 typedef struct {
@@ -626,7 +628,7 @@ onela_status_t onela_block_norm_backward(
  * nothing has lse and all log probabilities -inf and entropy 0; one with NaN or +inf has NaN.
  * Log probabilities are formed from differences to the row's largest logit, so their
  * errors do not grow with the logits' size.  num_given up to 256, num_top up to 64 and
- * vocab, vocab < 2^28, scale > 0. */
+ * vocab, vocab < 2^28, 0 < scale <= 1e30; fewer than 2^24 / ceil(vocab / 4096) rows. */
 typedef struct {
   int64_t num_rows;  /* < 2^31 */
   int32_t vocab;

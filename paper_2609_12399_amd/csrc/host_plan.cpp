@@ -380,7 +380,8 @@ bool stride_ok(int64_t stride, int64_t own, int32_t dtype) {
 onela_status_t check_conv(const onela_conv_config_t* c, bool ragged) {
   if (!c) return ONELA_EINVAL;
   if (c->num_seqs < 1 || c->total_tokens < 0 || c->total_tokens > INT32_MAX) return ONELA_EINVAL;
-  if (c->channels < 8 || c->channels % 8 || c->taps < 2 || c->taps > kConvMaxTaps)
+  if (c->channels < 8 || c->channels % 8 || c->channels > 1 << 26 || c->taps < 2 ||
+      c->taps > kConvMaxTaps)
     return ONELA_EINVAL;
   if (!io_ok(c->io_dtype) || !stride_ok(c->x_stride, c->channels, c->io_dtype))
     return ONELA_EINVAL;
@@ -471,7 +472,7 @@ onela_status_t check_logprob(const onela_logprob_config_t* c) {
   if (!io_ok(c->io_dtype)) return ONELA_EINVAL;
   if (c->logits_stride && (c->logits_stride < c->vocab || c->logits_stride > (int64_t(1) << 30)))
     return ONELA_EINVAL;
-  if (!(c->scale > 0.f) || !(c->scale - c->scale == 0.f)) return ONELA_EINVAL;
+  if (!(c->scale > 0.f) || !(c->scale <= 1e30f)) return ONELA_EINVAL;
   // a workgroup of 256 threads for every row (backward: for every 4096 columns)
   if (double(c->num_rows) * (1 + (c->vocab - 1) / 4096) * 256 >= kGridThreads) return ONELA_EINVAL;
   return ONELA_OK;

@@ -302,7 +302,10 @@ __device__ inline void finish(const LogprobParams& p, long row, const Sums& a, L
   const float o = origin(a.m), logs = kLn2 * __builtin_amdgcn_logf(a.s);
   if (threadIdx.x == 0) {
     if (p.lse) p.lse[row] = gone ? kNegInf : fmaf(o, p.scale, logs);
-    if (ENT && p.entropy) p.entropy[row] = gone ? 0.f : logs - kLn2 * a.t / a.s;
+    if (ENT && p.entropy) {
+      const float h = logs - kLn2 * a.t / a.s;
+      p.entropy[row] = gone || h < 0.f ? 0.f : h;  // (a rounding below 0)
+    }
   }
   for (int g = threadIdx.x; g < p.G; g += THREADS) {
     const int v = p.given[row * p.G + g];

@@ -45,6 +45,7 @@ def conv_step(lib, cfg, off=None, x=A, w=B, bias=None, s=C, num=2, slots=None, o
     dict(channels=60), dict(channels=0), dict(taps=1), dict(taps=5), dict(io_dtype=2),
     dict(activation=2), dict(activation=-1), dict(x_stride=56), dict(x_stride=68),
     dict(x_stride=1 << 41), dict(num_seqs=1 << 30, channels=1 << 20),
+    dict(channels=(1 << 26) + 8),
     dict(total_tokens=(1 << 31) - 1, num_seqs=1, channels=1 << 20)], ids=str)
 def test_conv_shapes_refused(lib, bad):
     cfg = conv_cfg(**bad)
@@ -172,7 +173,7 @@ def logp_back(lib, cfg, x=A, given=B, lse=C, ent=None, dl=D, dlse=None, dent=Non
     dict(num_rows=-1), dict(num_rows=1 << 31), dict(vocab=0), dict(vocab=1 << 28),
     dict(num_given=-1), dict(num_given=257), dict(num_top=-1), dict(num_top=65),
     dict(vocab=5, num_top=6), dict(io_dtype=-1), dict(logits_stride=99), dict(scale=0.0),
-    dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")),
+    dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(scale=2e30),
     dict(logits_stride=1 << 41), dict(num_rows=1 << 24), dict(num_rows=1 << 20, vocab=1 << 17)],
     ids=str)
 def test_logprob_shapes_refused(lib, bad):
