@@ -22,6 +22,8 @@
 // where instructions count too: the bound takes 7 us of that, the list 10, the choice from it 4.
 // 16 elements per thread and chunk instead of 32 were 109 us there, but 34 instead of 30 for
 // 4096 rows of 8192 and 11.3 instead of 9.6 for 300.
+#include <type_traits>
+
 #include "device_common.h"
 #include "internal.h"
 
@@ -372,17 +374,11 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int p
 #pragma unroll
   for (int k = 0; k < NV; ++k)
     next[k].load(x, begin + (k * THREADS + int(threadIdx.x)) * EV, end);
-  for (int c = begin; c < end; c += CH) {
-    float v[PER];
+  // n pieces of this thread from column c on, THREADS * EV columns apart
+  auto sums = [&](auto n, const float* v, float* mp) {
+    float mc = kNegInf;  // (mp: the largest of each piece)
 #pragma unroll
-    for (int k = 0; k < NV; ++k) next[k].floats(v + k * EV);
-    if (c + CH < end)
-#pragma unroll
-      for (int k = 0; k < NV; ++k)
-        next[k].load(x, c + CH + (k * THREADS + int(threadIdx.x)) * EV, end);
-    float mp[NV], mc = kNegInf;  // the largest of each piece
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
+    for (int k = 0; k < n(); ++k) {
       mp[k] = v[k * EV];
 #pragma unroll
       for (int i = 1; i < EV; ++i) mp[k] = fmaxf(mp[k], v[k * EV + i]);
@@ -392,24 +388,50 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int p
     const float o = origin(a.m);
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
+    for (int i = 0; i < n() * EV; ++i) {
       const float d = (v[i] - o) * c2, e = __builtin_amdgcn_exp2f(d);
       s += e;
       if constexpr (ENT) a.t = fmaf(e, fmaxf(d, kFar), a.t);
     }
     a.s += s;
+  };
+  auto candidates = [&](auto n, const float* v, const float* mp, int c) {
+#pragma unroll
+    for (int k = 0; k < n(); ++k)
+      if (__ballot(mp[k] >= bound))
+        append<EV>(&list, count, v + k * EV, bound, [&](int i) {
+          return c + (k * THREADS + int(threadIdx.x)) * EV + i;
+        });
+  };
+  int c = begin;
+  do {
+    float v[PER], mp[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) next[k].floats(v + k * EV);
+    if (c + CH < end)
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        next[k].load(x, c + CH + (k * THREADS + int(threadIdx.x)) * EV, end);
+    sums(std::integral_constant<int, NV>{}, v, mp);
     if constexpr (TOP) {
       // The threads' largest so far, after 1, 2, 4, ... chunks.  Only the first time do all have to be
       // there: what another wave has not written yet is its largest of before.
       const int done = (c - begin) / CH + 1;
       if ((done & (done - 1)) == 0) bound = bound_of<THREADS>(a.m, p.K, maxima, done == 1);
-#pragma unroll
-      for (int k = 0; k < NV; ++k)
-        if (__ballot(mp[k] >= bound))
-          append<EV>(&list, count, v + k * EV, bound, [&](int i) {
-            return c + (k * THREADS + int(threadIdx.x)) * EV + i;
-          });
+      candidates(std::integral_constant<int, NV>{}, v, mp, c);
     }
+    c += CH;
+  } while (c + CH <= end);
+  // the rest of the columns, which less than a chunk holds, by pieces: those that a wave has
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int at = c + k * THREADS * EV;
+    if (at + wave * 64 * EV >= end) break;
+    float v[EV], mp[1];
+    next[k].floats(v);
+    sums(std::integral_constant<int, 1>{}, v, mp);
+    if constexpr (TOP) candidates(std::integral_constant<int, 1>{}, v, mp, at);
   }
   join<THREADS, ENT>(a, c2, red);
   int m = 0;
