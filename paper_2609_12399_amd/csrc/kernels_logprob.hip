@@ -353,11 +353,11 @@ __device__ inline void finish(const LogprobParams& p, long row, const Sums& a, L
   }
 }
 
-// One part of a row per workgroup; with one part, its results.
-template <int THREADS, bool BF16, bool ENT, bool TOP>
+// One part of a row per workgroup, PER columns per thread at a time; with one part, its results.
+template <int THREADS, int PER, bool BF16, bool ENT, bool TOP>
 __global__ __launch_bounds__(THREADS) void logprob_kernel(LogprobParams p, int parts,
                                                           int columns) {
-  constexpr int EV = Piece<BF16>::EV, PER = 32, NV = PER / EV, CH = THREADS * PER;
+  constexpr int EV = Piece<BF16>::EV, NV = PER / EV, CH = THREADS * PER;
   __shared__ float red[3 * (THREADS / 64)];
   // (a piece of the second reading fits too)
   __shared__ List<THREADS / 64, TOP ? 512 : 1> list;
@@ -605,10 +605,12 @@ __global__ __launch_bounds__(THREADS) void logprob_backward_kernel(LogprobParams
 template <bool BF16, bool ENT, bool TOP>
 hipError_t run(const LogprobParams& p, const LogprobPlan& a, hipStream_t st) {
   const unsigned blocks = unsigned(p.R * a.parts);
-  if (a.threads == 64)
-    logprob_kernel<64, BF16, ENT, TOP><<<blocks, 64, 0, st>>>(p, a.parts, a.columns);
+  if (a.threads == 64 && p.V <= 64 * 8)  // (8192 rows of 500 with the 5 best 14.3 us by the next)
+    logprob_kernel<64, 8, BF16, ENT, TOP><<<blocks, 64, 0, st>>>(p, a.parts, a.columns);
+  else if (a.threads == 64)
+    logprob_kernel<64, 32, BF16, ENT, TOP><<<blocks, 64, 0, st>>>(p, a.parts, a.columns);
   else
-    logprob_kernel<256, BF16, ENT, TOP><<<blocks, 256, 0, st>>>(p, a.parts, a.columns);
+    logprob_kernel<256, 32, BF16, ENT, TOP><<<blocks, 256, 0, st>>>(p, a.parts, a.columns);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
   logprob_join_kernel<BF16, ENT, TOP><<<unsigned(p.R), kJoinThreads, 0, st>>>(p, a.parts);
