@@ -66,7 +66,7 @@ struct Window {  // the last TAPS inputs (or gradients), newest last
   }
 };
 
-// Input at place t (before b: in the state) of channels c0 .. c0 + 7.
+// Input at place t (before b: in the state) of the E channels from c0 on.
 template <int TAPS, bool BF16, int E>
 __device__ inline RawN<BF16, E> input_at(const ConvParams& p, const void* state, long row, long b,
                                       long t, unsigned c0) {
