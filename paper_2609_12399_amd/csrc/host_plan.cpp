@@ -412,13 +412,14 @@ ConvPlan conv_plan(const onela_conv_config_t* c, bool backward) {
   long run;
   if (!backward) {
     // Short runs, many waves: a run reads the taps - 1 rows before it again, but from the cache.
-    // 16000 tokens x 6144 channels take 92 us in runs of 13, 97 in 26, 99 in 52.
+    // 16000 tokens x 6144 channels take 86 to 88 us in runs of 8 to 52; some 8192 tokens x 128
+    // 9.0 us in runs of 4, 9.5 in 8.
     run = tokens * padded(ll) / (256l * 4 * 64 * 32);
     run = run < 4 ? 4 : run > 16 ? 16 : run;
   } else {
     // As many workgroups as the compute units hold at once (a last few would take as long as all
     // the others), in several turns only where that makes runs of more than 64 tokens: 8192
-    // tokens x 6144 channels take 79 us in runs of 52 (one turn), 81 in 26, 83 in 18, 86 in 13.
+    // tokens x 6144 channels take 77 us in runs of 52 (one turn), 85 in 26, 94 in 18, 101 in 13.
     const long held = 256l * (ll < 6 ? 2 : c->io_dtype == ONELA_BF16 ? 4 : 3);
     long turns = 0, blocks;
     do {
@@ -480,12 +481,12 @@ onela_status_t check_logprob(const onela_logprob_config_t* c) {
 
 LogprobPlan logprob_plan(const onela_logprob_config_t* c) {
   LogprobPlan a{256, 1, c->vocab};
-  // Short rows by a wave each: 8192 rows of 1000 with the 20 best 19 us, by four waves 51.
+  // Short rows by a wave each: 8192 rows of 1000 with the 20 best 17 us, by four waves 48.
   if (c->vocab <= 2048) a.threads = 64;
   // Few rows in parts of 8192 columns or more, where that saves more than the second launch takes.
-  // us whole / in parts: with the 20 best, 1 x 32768 15.2 / 12.6, 1 x 131072 33 / 15, 8 x 50001
-  // 21.5 / 13.7, 64 x 131072 35 / 19, 300 x 50001 26 / 26; the sum alone, 1 x 32768 7.4 / 10.2, 8 x
-  // 50001 9.7 / 10.5, 1 x 131072 16.7 / 10.9, 64 x 131072 17.4 / 11.4.
+  // us whole / in parts: with the 20 best, 1 x 32768 14.5 / 11.9, 1 x 131072 30 / 15, 8 x 50001
+  // 19.3 / 14.3, 64 x 131072 32 / 19, 300 x 50001 23.7 / 23.2; the sum alone, 1 x 32768 7.1 / 10.2,
+  // 8 x 50001 7.8 / 9.9, 1 x 131072 12.2 / 10.1, 64 x 131072 12.8 / 10.8.
   const long chunks = (long(c->vocab) + 8191) / 8192;
   const long rows = c->num_rows > 0 ? long(c->num_rows) : 1;
   if (rows < 256 && chunks >= (c->num_top > 0 ? 4 : 8)) {

@@ -11,7 +11,10 @@
 // A row is held by LANES lanes with 8 columns each: a part of a wave, or a whole workgroup whose
 // waves exchange their sums through LDS (two buffers in turn, so that one barrier per sum is
 // enough).  Workgroups stay and walk over rows, with the weights in registers and the next row on
-// its way while this one is worked on.  Bound: HBM.
+// its way while this one is worked on.  Bound: HBM.  16384 rows of 2048 with an fp32 residual
+// stream 83 us (403 MB, 4.9 TB/s), 262144 gated heads of 128 38.5 us (201 MB, 5.2 TB/s); backward,
+// 8191 rows of 2048 with everything, 51 us (269 MB, 5.2 TB/s) and 6 for the second launch, which
+// sums the workgroups' weight gradients.
 #include "device_common.h"
 #include "internal.h"
 

@@ -15,7 +15,7 @@
 // without conditions.  Weight gradients are summed over a thread's run, over the workgroup's runs
 // in LDS, and over the workgroups by a second launch, each in a fixed order.
 //
-// Bound: HBM, forward at 5.2 TB/s (89 us there).  Backward, 8192 tokens x 6144 channels in 75
+// Bound: HBM, forward at 5.3 TB/s (87 us there).  Backward, 8192 tokens x 6144 channels in 75
 // us (70 + 5 for the second launch): 302 MB in 60 us at a copy's rate, beside which 45 us of
 // vector instructions (28 per element) run, and the ends of the one turn that the workgroups
 // take are not covered by others (12 us without the runs' middles).

@@ -16,12 +16,13 @@
 // the first masked columns fill the rest.
 //
 // A row belongs to a workgroup (a wave up to 2048 columns), or in parts to several where there
-// are few rows, joined by a second launch.  Rows begin anywhere: 16-byte loads need only
-// the elements' alignment.  Bound: HBM without the
-// best (4096 rows of 50001 in bf16 87 us, 4.7 TB/s, with entropy 92); with the 20 best 115 us,
-// where instructions count too: the bound takes 7 us of that, the list 10, the choice from it 4.
-// 16 elements per thread and chunk instead of 32 were 109 us there, but 34 instead of 30 for
-// 4096 rows of 8192 and 11.3 instead of 9.6 for 300.
+// are few rows, joined by a second launch.  Rows begin anywhere: 16-byte loads need only the
+// elements' alignment.  Bound: HBM without the best (4096 rows of 50001 in bf16 88 us, 4.7 TB/s,
+// with or without the entropy).  With the 20 best 107 us, with 64 133: the bound, the list and the
+// choice from it are vector instructions, which then keep the units 70% busy, and waits that the
+// other workgroups of a compute unit cover in part.  Chunks of 16 elements per thread instead of
+// 32 are 5 us faster with the 20 best, 4 slower with 64, and 10.1 instead of 8.0 us for 300 rows of
+// 8192.  Rows that rise throughout are read twice or more (1024 rows 252 us instead of 32).
 #include <type_traits>
 
 #include "device_common.h"
@@ -605,7 +606,7 @@ __global__ __launch_bounds__(THREADS) void logprob_backward_kernel(LogprobParams
 template <bool BF16, bool ENT, bool TOP>
 hipError_t run(const LogprobParams& p, const LogprobPlan& a, hipStream_t st) {
   const unsigned blocks = unsigned(p.R * a.parts);
-  if (a.threads == 64 && p.V <= 64 * 8)  // (8192 rows of 500 with the 5 best 14.3 us by the next)
+  if (a.threads == 64 && p.V <= 64 * 8)  // (8192 rows of 500 with the 5 best 10.6 us, by the next 14.1)
     logprob_kernel<64, 8, BF16, ENT, TOP><<<blocks, 64, 0, st>>>(p, a.parts, a.columns);
   else if (a.threads == 64)
     logprob_kernel<64, 32, BF16, ENT, TOP><<<blocks, 64, 0, st>>>(p, a.parts, a.columns);

@@ -423,21 +423,37 @@ class QkNormRope:
         return self.q, self.k, dwq, dwk
 
 
-def _on_current_device(x):
-    """ValueError unless x is on the current device: the call is enqueued on a stream of that.
-    (A host tensor is the binding's to refuse.)"""
-    current = ab.current_device()
-    if x.is_cuda and x.get_device() != current:
-        raise ValueError(f"tensors are on {x.device}, the current device is cuda:{current}")
-
-
 class _OnDevice:
     """What the objects below share: tensors of one device, views that may stand in wider rows."""
 
-    def _check(self, x, *expected):
+    def _place(self, device):
+        """The device that the object's own tensors are on; its index is self.on (a host: -1)."""
+        self.on = _torch().empty(0, device=device).get_device()
+        return device if self.on < 0 else f"cuda:{self.on}"
+
+    def _here(self, *tensors):
+        """Whether the object and all tensors are on the current device, to whose stream the call
+        goes."""
+        on = self.on
+        if on != ab.current_device():
+            return False
+        for x in tensors:
+            if x is not None and x.get_device() != on:
+                return False
+        return True
+
+    def _check(self, *expected):
+        """As _expect, and ValueError unless :meth:`_here`.  (A host tensor is the binding's to
+        refuse.)"""
         _expect(*expected)
-        if not isinstance(x, int) and x is not None:
-            _on_current_device(x)
+        for x, name, *_ in expected:
+            if x is None or isinstance(x, int) or not x.is_cuda:
+                continue
+            current = ab.current_device()
+            if x.get_device() != current or self.on != current:
+                own = f"cuda:{self.on}" if self.on >= 0 else "the host"
+                raise ValueError(f"{name} is on {x.device}, the object's tensors on {own}, the "
+                                 f"current device is cuda:{current}")
 
     @staticmethod
     def _stride(x):
@@ -460,7 +476,7 @@ class ShortConv(_OnDevice):
         self.ws_bytes = ab.onela_short_conv_workspace_bytes(self.cfg)
         if self.ws_bytes == 0:
             raise ab.OnelaError(ab.ONELA_EINVAL, "onela_short_conv_workspace_bytes")
-        self.stream, self.is_backward = stream, backward
+        self.stream, self.is_backward, device = stream, backward, self._place(device)
         dt = _io_tensor_dtype(io)
         self.dtypes = dt, torch.float32, torch.int32
         rows, states = (total_tokens, channels), (num_seqs, taps - 1, channels)
@@ -477,7 +493,7 @@ class ShortConv(_OnDevice):
     def _set(self, x, weight, bias, seq_offsets, initial_state):
         dt, f32, i32 = self.dtypes
         rows, weights, channels, bounds, states = self.shapes
-        self._check(x, (x, "x", rows, dt), (weight, "weight", weights, f32),
+        self._check((x, "x", rows, dt), (weight, "weight", weights, f32),
                     (bias, "bias", channels, f32), (seq_offsets, "seq_offsets", bounds, i32),
                     (initial_state, "initial_state", states, dt))
         self.cfg.x_stride = self._stride(x)
@@ -497,8 +513,8 @@ class ShortConv(_OnDevice):
         if not self.is_backward:
             raise ValueError("this object holds the forward call's tensors")
         self._set(x, weight, bias, seq_offsets, initial_state)
-        _expect((d_y, "d_y", self.shapes[0], self.dtypes[0]),
-                (d_final_state, "d_final_state", self.shapes[4], self.dtypes[0]))
+        self._check((d_y, "d_y", self.shapes[0], self.dtypes[0]),
+                    (d_final_state, "d_final_state", self.shapes[4], self.dtypes[0]))
         db = None if bias is None else self.dbias
         ds = None if initial_state is None else self.d_initial_state
         ab.onela_short_conv_backward(self.cfg, seq_offsets, x, weight, bias, initial_state, d_y,
@@ -515,7 +531,7 @@ class ShortConvStep(_OnDevice):
                  num_slots: int, activation: str | None = "silu", device="cuda:0", stream=None):
         torch = _torch()
         self.cfg = ab.make_conv_config(num_seqs, total_tokens, channels, taps, io, activation)
-        self.num_slots, self.stream = num_slots, stream
+        self.num_slots, self.stream, device = num_slots, stream, self._place(device)
         dt = _io_tensor_dtype(io)
         self.dtypes = dt, torch.float32, torch.int32
         self.pool = num_slots, taps - 1, channels
@@ -533,19 +549,20 @@ class ShortConvStep(_OnDevice):
                     weight.shape == weights and pool.dtype is dt and pool.shape == self.pool and
                     (slots is None or slots.dtype is i32 and slots.shape == seqs) and
                     bias is None and seq_offsets is None and slots_out is None and
-                    x.get_device() == ab.current_device())
+                    self._here(x, weight, pool, slots))
         except AttributeError:
             fits = False
         if not fits:
-            self._check(x, (x, "x", rows, dt), (weight, "weight", weights, f32),
+            self._check((x, "x", rows, dt), (weight, "weight", weights, f32),
                         (bias, "bias", channels, f32), (seq_offsets, "seq_offsets", bounds, i32),
                         (slots, "slots", seqs, i32), (slots_out, "slots_out", seqs, i32))
             if not isinstance(pool, int) and pool is not None:  # (more slots do no harm)
-                _expect((pool, "pool", (max(self.num_slots, *pool.shape[:1]), *self.pool[1:]), dt))
+                self._check((pool, "pool", (max(self.num_slots, *pool.shape[:1]), *self.pool[1:]),
+                             dt))
         slots_of_out = 0
         if pool_out is not None:
             slots_of_out = pool_out.shape[0]
-            _expect((pool_out, "pool_out", (slots_of_out, *self.pool[1:]), dt))
+            self._check((pool_out, "pool_out", (slots_of_out, *self.pool[1:]), dt))
         self.cfg.x_stride = self._stride(x)
         ab.onela_short_conv_step(self.cfg, seq_offsets, x, weight, bias, pool, self.num_slots,
                                  slots, pool_out, slots_of_out, slots_out, self.y, self.stream)
@@ -577,7 +594,7 @@ class BlockNorm(_OnDevice):
         dt, rt = _io_tensor_dtype(io), _io_tensor_dtype(residual_io or io)
         self.dtypes = dt, rt, torch.float32
         self.shape, self.width = (num_tokens, num_heads, width), (width,)
-        self.device = device
+        self.device = device = self._place(device)
         self.made = {}  # output tensors, made when a call first has use for them
         if backward:
             self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
@@ -600,11 +617,12 @@ class BlockNorm(_OnDevice):
                     (before_weight is None or before_weight.dtype is f32 and
                      before_weight.shape == width) and
                     (channel_scale is None or channel_scale.dtype is f32 and
-                     channel_scale.shape == width) and x.get_device() == ab.current_device())
+                     channel_scale.shape == width) and
+                    self._here(x, gate, residual, after_weight, before_weight, channel_scale))
         except AttributeError:
             fits = False
         if not fits:
-            self._check(x, (x, "x", shape, dt), (gate, "gate", shape, dt),
+            self._check((x, "x", shape, dt), (gate, "gate", shape, dt),
                         (residual, "residual", shape, rt),
                         (after_weight, "after_weight", width, f32),
                         (before_weight, "before_weight", width, f32),
@@ -633,7 +651,8 @@ class BlockNorm(_OnDevice):
             raise ValueError("this object holds the forward call's tensors")
         self._set(x, residual, gate, after_weight, before_weight, channel_scale)
         dt, rt, _ = self.dtypes
-        _expect((d_y, "d_y", self.shape, dt), (d_residual_out, "d_residual_out", self.shape, rt))
+        self._check((d_y, "d_y", self.shape, dt),
+                    (d_residual_out, "d_residual_out", self.shape, rt))
         dx = self._out("dx", dt)
         dg = None if gate is None else self._out("dgate", dt)
         dr = None if residual is None else self._out("dres", rt)
@@ -661,7 +680,7 @@ class TokenLogprobs(_OnDevice):
         self.ws_bytes = ab.onela_token_logprobs_workspace_bytes(self.cfg)
         if self.ws_bytes == 0:
             raise ab.OnelaError(ab.ONELA_EINVAL, "onela_token_logprobs_workspace_bytes")
-        self.stream, self.is_backward = stream, backward
+        self.stream, self.is_backward, device = stream, backward, self._place(device)
         self.dtypes = _io_tensor_dtype(io), torch.float32, torch.int32
         self.shapes = (num_rows, vocab), (num_rows, num_given), (num_rows,)
         self.num_given = num_given
@@ -685,11 +704,11 @@ class TokenLogprobs(_OnDevice):
         try:
             fits = (logits.dtype is dt and logits.shape == rows and
                     (given is None or given.dtype is i32 and given.shape == tokens) and
-                    logits.get_device() == ab.current_device())
+                    self._here(logits, given))
         except AttributeError:
             fits = False
         if not fits:
-            self._check(logits, (logits, "logits", rows, dt), (given, "given", tokens, i32))
+            self._check((logits, "logits", rows, dt), (given, "given", tokens, i32))
         if (given is None) != (self.num_given == 0):
             raise ValueError("given must be there exactly if num_given > 0")
         self.cfg.logits_stride = self._stride(logits)
@@ -713,10 +732,10 @@ class TokenLogprobs(_OnDevice):
         self._set(logits, given)
         f32, rows = self.dtypes[1], self.shapes[2]
         out = self.d_logits if out is None else out
-        _expect((lse, "lse", rows, f32), (d_logp, "d_logp", self.shapes[1], f32),
-                (d_lse, "d_lse", rows, f32), (entropy, "entropy", rows, f32),
-                (d_entropy, "d_entropy", rows, f32),
-                (out, "out", self.shapes[0], self.dtypes[0]))
+        self._check((lse, "lse", rows, f32), (d_logp, "d_logp", self.shapes[1], f32),
+                    (d_lse, "d_lse", rows, f32), (entropy, "entropy", rows, f32),
+                    (d_entropy, "d_entropy", rows, f32),
+                    (out, "out", self.shapes[0], self.dtypes[0]))
         ab.onela_token_logprobs_backward(self.cfg, logits, given, lse, entropy, d_logp, d_lse,
                                          d_entropy, out, self.stream)
         return out

@@ -318,6 +318,53 @@ def test_objects_of_refused_sizes(make):
         make()
 
 
+class OnGpu:
+    """What the checks look at of a tensor on GPU `at`."""
+    is_cuda = True
+
+    def __init__(self, like, at):
+        self.dtype, self.shape, self.device = like.dtype, like.shape, f"cuda:{at}"
+        self.get_device, self.is_contiguous = (lambda: at), (lambda: True)
+
+
+def test_tensors_on_other_devices_are_refused(entries, monkeypatch):
+    x, w, dy = torch.zeros(4, 64, dtype=BF), torch.zeros(64), torch.zeros(4, 64, dtype=BF)
+    ids, rows = torch.zeros(4, dtype=I32), torch.zeros(4, 1, dtype=I32)
+    heads, lse, pool = x[:, None], torch.zeros(4), torch.zeros(5, 3, 64, dtype=BF)
+    conv = dict(x=x, weight=torch.zeros(64, 4), bias=w, seq_offsets=ids[:2],
+                initial_state=pool[:1])
+    norm = dict(x=heads, residual=heads, gate=heads, after_weight=w, before_weight=w,
+                channel_scale=w)
+    step = dict(x=x, weight=conv["weight"], pool=pool, slots=ids)
+    convs, norms, probs = ([make(b) for b in (False, True)] for make in (
+        lambda b: runner.ShortConv(1, 4, 64, 4, "bf16", backward=b, device="cpu"),
+        lambda b: runner.BlockNorm(4, 64, 1, "bf16", norm_after=True, gate="silu", backward=b,
+                                   device="cpu"),
+        lambda b: runner.TokenLogprobs(4, 64, 1, 0, "bf16", backward=b, device="cpu")))
+    steps = runner.ShortConvStep(4, 4, 64, 4, "bf16", 5, device="cpu")
+    calls = [(convs[0], "forward", conv), (convs[1], "backward", dict(conv, d_y=dy)),
+             (convs[1], "backward", dict(conv, d_y=dy, d_final_state=pool[:1])),
+             (norms[0], "forward", norm), (norms[1], "backward", dict(norm, d_y=heads)),
+             (norms[1], "backward", dict(norm, d_y=heads, d_residual_out=heads)),
+             (probs[0], "forward", dict(logits=x, given=rows)),
+             (probs[1], "backward", dict(logits=x, given=rows, lse=lse,
+                                         d_logp=torch.zeros(4, 1), d_lse=lse, out=x)),
+             (steps, "step", step), (steps, "step", dict(step, pool_out=pool, slots_out=ids))]
+    for op in (*convs, *norms, *probs, steps):
+        op.on = 0
+    for current in (0, 1):
+        monkeypatch.setattr(ab, "current_device", lambda: current)
+        for op, name, args in calls:
+            here = {k: OnGpu(v, 0) for k, v in args.items()}
+            for k, v in args.items():
+                with pytest.raises(ValueError, match="current device"):
+                    getattr(op, name)(**{**here, k: OnGpu(v, 1)})
+            if current == 1:  # (the object and its tensors on another device than the current one)
+                with pytest.raises(ValueError, match="current device"):
+                    getattr(op, name)(**here)
+    assert entries == []
+
+
 # ---- the functions and layers on them -----------------------------------------------------------------
 
 mixer = pytest.importorskip("paper_2609_12399_amd.mixer")
