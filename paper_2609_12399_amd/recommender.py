@@ -80,8 +80,11 @@ class Recommender:
     @torch.no_grad()
     def search(self, tokens, seq_offsets, beams: int, steps: int):
         """The ``beams`` best continuations of ``steps`` tokens after each packed prompt, best
-        first: tokens [requests][beams][steps] and their log probabilities."""
+        first: tokens [requests][beams][steps] and their log probabilities.  Prompts have one
+        token at least, and at most the decode's steps (8) follow the first token."""
         R, W, V = seq_offsets.numel() - 1, beams, self.vocab
+        if steps < 1 or bool((seq_offsets[1:] <= seq_offsets[:-1]).any()):
+            raise ValueError("a search takes a step and prompts of one token at least")
         x, states = self(tokens, seq_offsets)
         logits = (x[seq_offsets[1:].long() - 1] @ self.head).float()
         kept = [BeamStates(conv) for _, conv in states]

@@ -423,3 +423,11 @@ def test_recommender_on_the_entry_points(entries, monkeypatch):
                     ("onela_token_logprobs", 1), ("onela_token_logprobs_backward", 1),
                     ("onela_delta_rule_backward", 2)):
         assert entries.count(name) == n, name
+
+
+@pytest.mark.parametrize("bounds,steps", [([0, 3, 3], 2), ([0, 0, 3], 2), ([0, 2, 3], 0)])
+def test_search_refuses_empty_prompts(bounds, steps):
+    recommender = pytest.importorskip("paper_2609_12399_amd.recommender")
+    model = recommender.Recommender(20, 16, 2, 1, 2, 32, "f32", device="cpu")
+    with pytest.raises(ValueError, match="one token"):
+        model.search(torch.zeros(3, dtype=I64), torch.tensor(bounds, dtype=I32), 4, steps)
