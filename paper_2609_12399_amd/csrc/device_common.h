@@ -167,6 +167,11 @@ struct RawN {
 #pragma unroll
     for (int j = 0; j < kWords / kVector; ++j) w[j] = Vector(0u);
   }
+  // What is formed from the words after this is not shared with what was formed before.
+  __device__ void opaque() {
+#pragma unroll
+    for (int j = 0; j < kWords / kVector; ++j) asm volatile("" : "+v"(w[j]));
+  }
   __device__ void floats(float (&x)[N]) const {
 #pragma unroll
     for (int j = 0; j < kWords; ++j) {

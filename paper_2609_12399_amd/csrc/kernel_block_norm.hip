@@ -183,11 +183,42 @@ struct GradIn {
   }
 };
 
+// A lane's sums of one weight's gradient, in registers or in LDS (16 bytes of each lane side by
+// side).
+template <bool KEEP, int LANES>
+struct Sum {
+  float v[KEEP ? E : 1] = {};
+  f32x4* at = nullptr;
+  __device__ void set(f32x4* lds) {
+    at = lds + threadIdx.x;
+    at[0] = at[LANES] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ void add(const float (&x)[E], const float (&y)[E]) {
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int j = 0; j < E; ++j) v[j] = fmaf(x[j], y[j], v[j]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E / 4; ++i) {
+        f32x4 s = at[i * LANES];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = fmaf(x[4 * i + j], y[4 * i + j], s[j]);
+        at[i * LANES] = s;
+      }
+    }
+  }
+  __device__ float get(int j) const {
+    if constexpr (KEEP) return v[j];
+    else return at[j / 4 * LANES][j % 4];
+  }
+};
+
 // Every workgroup walks its rows in a fixed order and leaves the sums of the three weights'
-// gradients over them.  1024 lanes (more than 4096 columns) have half the registers of fewer:
-// there the weights are read again for every row (from the cache), no row is requested ahead,
-// and what still does not fit is spilled (2047 rows of 8192 with everything 193 us; 4095 of
-// 4096 57).
+// gradients over them.  1024 lanes (more than 4096 columns) have half the registers of fewer: there
+// the sums are in LDS, the weights are read at their uses in every row (from the cache), the gate
+// and the normed x are formed again for the second half, and no row is requested ahead (2047 rows
+// of 8192 with everything in bf16 97 us, in fp32 202; with sums in registers 188 and 326; with a row
+// ahead, spilled, 99 and 251).  4095 rows of 4096 take 58 us.
 template <int LANES, bool BF16, bool RES_BF16>
 __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_kernel(
     BlockNormParams p) {
@@ -198,19 +229,28 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_
   const float inv_d = 1.f / float(p.D);
   const bool in = c0 < p.D;
   int turn = 0;
-  float wa[E], wb[E], cs[E], da[E] = {}, db[E] = {}, dc[E] = {};
-  auto weights = [&] {
+  float wa[E], wb[E], cs[E];
+  Sum<KEEP, LANES> da, db, dc;
+  if constexpr (!KEEP) {
+    __shared__ f32x4 lds[3 * E / 4 * LANES];
+    da.set(lds);
+    db.set(lds + E / 4 * LANES);
+    dc.set(lds + 2 * E / 4 * LANES);
+  }
+  auto inner = [&] {
     vector_of(p.wa, c0, in, wa);
-    vector_of(p.wb, c0, in, wb);
     vector_of(p.cs, c0, in, cs);
 #pragma unroll
     for (int j = 0; j < E; ++j) cs[j] *= p.scale;
   };
-  if (KEEP) weights();
+  if constexpr (KEEP) {
+    inner();
+    vector_of(p.wb, c0, in, wb);
+  }
   Walk ahead(long(blockIdx.x) * RW + group, long(gridDim.x) * RW, p.H);
   RowIn<BF16, RES_BF16> cur, next;
   GradIn<BF16, RES_BF16> gcur, gnext;
-  if (KEEP && ahead.row < p.rows) {
+  if (ahead.row < p.rows) {
     cur.load(p, ahead, c0);
     gcur.load(p, ahead.row, c0);
   }
@@ -225,45 +265,51 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_
       cur.load(p, ahead, c0);
       gcur.load(p, ahead.row, c0);
       ahead.next(p.H);
-      asm volatile("" ::: "memory");  // (the weights' reads stay in the loop)
-      weights();
     }
     // a: the gate's activation, slope: its derivative; un: x normed and weighted
     float x[E] = {}, a[E], slope[E], h[E] = {}, dy[E] = {}, d[E] = {}, un[E];
-    float s = 0.f;
+    float s = 0.f, rx = 1.f;
+    auto open = [&] {
+      if (in) cur.x.floats(x);
+#pragma unroll
+      for (int j = 0; j < E; ++j) a[j] = 1.f;
+      if (p.gate) {
+        float g[E] = {};
+        if (in) cur.g.floats(g);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+          const float sg = sigmoid(g[j]);
+          a[j] = sg * (p.silu ? g[j] : 1.f);
+          // s (1 + g (1 - s)), or s (1 - s)
+          slope[j] = fmaf(-a[j], sg, a[j] + (p.silu ? sg : 0.f));
+        }
+      }
+    };
+    auto weigh = [&](float r) {
+      if constexpr (!KEEP) {
+        asm volatile("" ::: "memory");  // (the weights are read here, each time)
+        inner();
+      }
+#pragma unroll
+      for (int j = 0; j < E; ++j) un[j] = x[j] * r * wa[j];
+    };
+    open();
     if (in) {
-      cur.x.floats(x);
       if (p.res) cur.r.floats(h);
       if (p.dy) gcur.y.floats(dy);
       if (p.dh) gcur.h.floats(d);
     }
-    if (p.gate) {
-      float g[E] = {};
-      if (in) cur.g.floats(g);
-#pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const float sg = sigmoid(g[j]);
-        a[j] = p.silu ? g[j] * sg : sg;
-        // s (1 + g (1 - s)), or s (1 - s)
-        slope[j] = p.silu ? fmaf(-a[j], sg, sg + a[j]) : fmaf(-sg, sg, sg);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < E; ++j) a[j] = 1.f;
-    }
-    float rx = 1.f;
     if (p.after) {
 #pragma unroll
       for (int j = 0; j < E; ++j) s = fmaf(x[j], x[j], s);
       rx = 1.f / sqrtf(row_sum<LANES>(s, turn) * inv_d + p.eps);
     }
+    weigh(rx);
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-      un[j] = x[j] * rx * wa[j];
-      h[j] = fmaf(cs[j], un[j] * a[j], h[j]);
-    }
+    for (int j = 0; j < E; ++j) h[j] = fmaf(cs[j], un[j] * a[j], h[j]);
     if (p.before) {
       float both[2] = {0.f, 0.f};
+      if constexpr (!KEEP) vector_of(p.wb, c0, in, wb);
 #pragma unroll
       for (int j = 0; j < E; ++j) {
         both[0] = fmaf(h[j], h[j], both[0]);
@@ -274,25 +320,36 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_
       const float f = both[1] * inv_d * rh * rh * rh;
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        db[j] = fmaf(dy[j], h[j] * rh, db[j]);
         d[j] = fmaf(rh, wb[j] * dy[j], fmaf(-f, h[j], d[j]));
+        h[j] *= rh;
       }
+      db.add(dy, h);
     } else {
 #pragma unroll
       for (int j = 0; j < E; ++j) d[j] += dy[j];
     }
     if (p.dres && in) RawN<RES_BF16, E>::of(d).store_once(p.dres, row * p.D + c0);
+    if constexpr (!KEEP) {  // (formed again, not held since then)
+      cur.x.opaque();
+      cur.g.opaque();
+      open();
+      weigh(rx);
+    }
     s = 0.f;
-    float dg[E];
+    float dg[E], t[E], n[E];
+#pragma unroll
+    for (int j = 0; j < E; ++j) t[j] = un[j] * a[j];
+    dc.add(d, t);
 #pragma unroll
     for (int j = 0; j < E; ++j) {
-      dc[j] = fmaf(d[j], un[j] * a[j], dc[j]);
-      const float du = cs[j] * d[j], dn = du * a[j], t = dn * x[j];
+      const float du = cs[j] * d[j], dn = du * a[j];
       if (p.gate) dg[j] = du * un[j] * slope[j];
-      da[j] = fmaf(t, rx, da[j]);
-      s = fmaf(t, wa[j], s);
+      t[j] = dn * x[j];
+      n[j] = rx;
+      s = fmaf(t[j], wa[j], s);
       d[j] = dn * wa[j];
     }
+    da.add(t, n);
     if (p.gate && p.dgate && in) RawN<BF16, E>::of(dg).store_once(p.dgate, row * p.D + c0);
     if (p.after) {
       const float f = row_sum<LANES>(s, turn) * inv_d * rx * rx * rx;
@@ -306,12 +363,11 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_
     }
   }
   if (!p.partial) return;
-#pragma unroll
-  for (int j = 0; j < E; ++j) dc[j] *= p.scale;
   const bool alone = gridDim.x == 1;  // (its sums are the results)
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
     const auto& sum = k == 0 ? da : k == 1 ? db : dc;
+    const float f = k == 2 ? p.scale : 1.f;
     float* const out = !alone   ? p.partial + (long(blockIdx.x) * 3 + k) * p.D
                        : k == 0 ? p.dwa
                        : k == 1 ? p.dwb
@@ -320,11 +376,11 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_
     if constexpr (RW == 1) {
       if (!in) continue;
 #pragma unroll
-      for (int j = 0; j < E; ++j) out[c0 + j] = sum[j];
+      for (int j = 0; j < E; ++j) out[c0 + j] = f * sum.get(j);
     } else {
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < E; ++j) acc[group][c0 + j] = sum[j];
+      for (int j = 0; j < E; ++j) acc[group][c0 + j] = f * sum.get(j);
       __syncthreads();
       for (int c = threadIdx.x; c < p.D; c += 256) {
         float t = 0.f;
