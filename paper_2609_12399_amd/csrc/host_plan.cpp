@@ -481,8 +481,19 @@ onela_status_t check_logprob(const onela_logprob_config_t* c) {
 
 LogprobPlan logprob_plan(const onela_logprob_config_t* c) {
   LogprobPlan a{256, 1, c->vocab};
-  // Short rows by a wave each: 8192 rows of 1000 with the 20 best 17 us, by four waves 48.
-  if (c->vocab <= 2048) a.threads = 64;
+  // Short rows by a wave each: 8192 rows of 1000 with the 20 best 16 us, by two waves 24, by four
+  // 48.  With more best tokens a wave's bound lets more through than its list holds: with 48 27
+  // us, by two waves 29, with 64 83 and 35.
+  if (c->vocab <= 512 || (c->vocab <= 2048 && c->num_top <= 48)) a.threads = 64;
+  // By two waves where four would have nothing for half of their first read (8192 rows of 4096
+  // with the 20 best 25 us, by four 47), and where many rows that are not too long have best tokens:
+  // four waves wait for one another's bound and choice (bf16, four / two, with the 20 best: 8192 x 6000
+  // 49 / 37 us, 8192 x 20000 97 / 79, 4096 x 50001 113 / 109, but 1024 x 50001 36 / 37.5 and 1024 x
+  // 131072 60 / 68; with 64, 4096 x 50001 133 / 137; fp32, 4096 x 16384 63 / 59, x 32768 101 / 105).
+  else if (c->vocab <= 4096 ||
+           (c->num_rows >= 2048 && c->num_top > 0 && c->num_top <= 32 &&
+            c->vocab <= (c->io_dtype == ONELA_BF16 ? 65536 : 16384)))
+    a.threads = 128;
   // Few rows in parts of 8192 columns or more, where that saves more than the second launch takes.
   // us whole / in parts: with the 20 best, 1 x 32768 14.5 / 11.9, 1 x 131072 30 / 15, 8 x 50001
   // 19.3 / 14.3, 64 x 131072 32 / 19, 300 x 50001 23.7 / 23.2; the sum alone, 1 x 32768 7.1 / 10.2,

@@ -15,7 +15,7 @@
 // depend on the order of the list.  Masked elements (-inf) never pass: if fewer than K remain,
 // the first masked columns fill the rest.
 //
-// A row belongs to a workgroup (a wave up to 2048 columns), or in parts to several where there
+// A row belongs to a workgroup of one, two or four waves, or in parts to several where there
 // are few rows, joined by a second launch.  Rows begin anywhere: 16-byte loads need only the
 // elements' alignment.  Bound: HBM without the best (4096 rows of 50001 in bf16 88 us, 4.7 TB/s,
 // with or without the entropy).  With the 20 best 107 us, with 64 133: the bound, the list and the
@@ -606,12 +606,20 @@ __global__ __launch_bounds__(THREADS) void logprob_backward_kernel(LogprobParams
 template <bool BF16, bool ENT, bool TOP>
 hipError_t run(const LogprobParams& p, const LogprobPlan& a, hipStream_t st) {
   const unsigned blocks = unsigned(p.R * a.parts);
-  if (a.threads == 64 && p.V <= 64 * 8)  // (8192 rows of 500 with the 5 best 10.6 us, by the next 14.1)
-    logprob_kernel<64, 8, BF16, ENT, TOP><<<blocks, 64, 0, st>>>(p, a.parts, a.columns);
+#define ONELA_ROWS(T, PER) \
+  logprob_kernel<T, PER, BF16, ENT, TOP><<<blocks, T, 0, st>>>(p, a.parts, a.columns)
+  // (8192 rows of 500 with the 5 best 10.6 us, by the last of the first three 14.1)
+  if (a.threads == 64 && p.V <= 64 * 8)
+    ONELA_ROWS(64, 8);
+  else if (a.threads == 64 && p.V <= 64 * 16)
+    ONELA_ROWS(64, 16);
   else if (a.threads == 64)
-    logprob_kernel<64, 32, BF16, ENT, TOP><<<blocks, 64, 0, st>>>(p, a.parts, a.columns);
+    ONELA_ROWS(64, 32);
+  else if (a.threads == 128)
+    ONELA_ROWS(128, 32);
   else
-    logprob_kernel<256, 32, BF16, ENT, TOP><<<blocks, 256, 0, st>>>(p, a.parts, a.columns);
+    ONELA_ROWS(256, 32);
+#undef ONELA_ROWS
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
   logprob_join_kernel<BF16, ENT, TOP><<<unsigned(p.R), kJoinThreads, 0, st>>>(p, a.parts);

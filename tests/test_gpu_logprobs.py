@@ -35,9 +35,12 @@ def same_or_near(got, want, bar):
     assert (off <= 0).all(), float(off.max())
 
 
-def check(x, given, K, scale, io, entropy=True, pad=0):
-    """Forward against the reference; x fp64 numpy of values that io holds."""
-    R, V = x.shape
+def check(x, given, K, scale, io, entropy=True, pad=0, rows=None):
+    """Forward against the reference; x fp64 numpy of values that io holds (as many rows as
+    wanted, again and again)."""
+    R, V = rows or len(x), x.shape[1]
+    some, x = len(x), np.resize(x, (R, V))
+    given = None if given is None else np.resize(given, (R, given.shape[1]))
     dt = torch.bfloat16 if io == "bf16" else torch.float32
     wide = torch.full((R, V + pad), 50.0, dtype=dt)
     wide[:, :V] = torch.from_numpy(x).to(dt)
@@ -46,7 +49,8 @@ def check(x, given, K, scale, io, entropy=True, pad=0):
     tok = None if given is None else torch.from_numpy(given).to(torch.int32).to(DEV)
     op = runner.TokenLogprobs(R, V, G, K, io, scale, entropy, device=DEV)
     logp, lse, ent, top, top_logp = op.forward(logits, tok)
-    want = ref.logprobs(f64(logits), given, K, scale)
+    want = ref.logprobs(f64(logits[:some]), None if given is None else given[:some], K, scale)
+    want = [w if w is None else np.resize(w, (R, *w.shape[1:])) for w in want]
     finite = np.where(np.isfinite(want[1]), want[1], 0)
     if G:
         same_or_near(logp, want[0], 7.5e-6 + 2.0 ** -23 * np.abs(want[0]))
@@ -133,6 +137,38 @@ def test_equal_logits(io):
         x[7, -70:] = 5.0
         for K in (1, 17, 64):
             check(x, None, K, 1.0, io)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("R,V,K", [
+    (40, 512, 64), (40, 513, 48), (40, 600, 49), (40, 1024, 20), (40, 1025, 48), (40, 2048, 48),
+    (40, 2048, 49), (40, 2049, 0), (40, 3001, 1), (40, 4095, 64), (40, 4096, 20), (40, 4097, 64),
+    (2047, 4097, 32), (2048, 4097, 32), (2048, 4097, 33), (2048, 4097, 0), (2050, 9000, 1),
+    (2048, 16384, 20), (2048, 16385, 20)])
+def test_rows_at_the_bounds_of_the_choices(R, V, K, io):
+    some = min(R, 40)
+    check(draw(some, V), tokens(some, V, 2), K, 1.0, io, pad=V % 3, rows=R)
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("R,V,K", [(24, 900, 20), (24, 1500, 64), (24, 3000, 20), (24, 4096, 64),
+                                   (2048, 5000, 1), (2048, 5000, 32), (2048, 13000, 20)])
+def test_hard_rows(R, V, K, io):
+    """Rows of equal values, ties, rising and falling ones, masks, NaN and +inf, side by side."""
+    r = np.random.default_rng(V)
+    x = np.zeros((12, V))
+    x[1] = (r.random(V) < 0.5) * 1.0
+    x[2] = np.arange(V) // 64 * 2.0 ** -4
+    x[3] = -(np.arange(V) // 64) * 2.0 ** -4
+    x[4, V // 3:V // 3 + 100] = 1.0
+    x[5] = r.integers(0, 3, V)
+    x[6] = -np.inf
+    x[7], x[7, [V // 2, V - 1]] = -np.inf, 3.0
+    x[8, r.random(V) < 0.9] = -np.inf
+    x[9, 5] = np.nan
+    x[10], x[10, V - 2] = draw(1, V)[0], np.inf
+    x[11], x[11, V - 3:] = -np.inf, np.nan
+    check(x, tokens(12, V, 1), K, 1.0, io, rows=R)
 
 
 def test_large_logits():
