@@ -15,13 +15,13 @@
 // depend on the order of the list.  Masked elements (-inf) never pass: if fewer than K remain,
 // the first masked columns fill the rest.
 //
-// A row belongs to a workgroup of one, two or four waves, or in parts to several where there
-// are few rows, joined by a second launch.  Rows begin anywhere: 16-byte loads need only the
-// elements' alignment.  Bound: HBM without the best (4096 rows of 50001 in bf16 88 us, 4.7 TB/s,
-// with or without the entropy).  With the 20 best 107 us, with 64 133: the bound, the list and the
-// choice from it are vector instructions, which then keep the units 70% busy, and waits that the
-// other workgroups of a compute unit cover in part.  Chunks of 16 elements per thread instead of
-// 32 are 5 us faster with the 20 best, 4 slower with 64, and 10.1 instead of 8.0 us for 300 rows of
+// A row belongs to a workgroup of one, two or four waves, or in parts to several where there are
+// few rows, joined by a second launch.  Rows begin anywhere: 16-byte loads need only the elements'
+// alignment.  Bound: HBM without the best (4096 rows of 50001 in bf16 88 us, 4.7 TB/s, with or
+// without the entropy).  With the 20 best 105 us, with 64 133: the bound, the list and the choice
+// from it are vector instructions, which then keep the units 70% busy, and waits that the other
+// workgroups of a compute unit cover in part.  Four waves with chunks of 16 elements per thread
+// instead of 32: 104 us with the 20 best, but 137 with 64, and 10.1 instead of 8.0 for 300 rows of
 // 8192.  Rows that rise throughout are read twice or more (1024 rows 252 us instead of 32).
 #include <type_traits>
 

@@ -431,20 +431,9 @@ class _OnDevice:
         self.on = _torch().empty(0, device=device).get_device()
         return device if self.on < 0 else f"cuda:{self.on}"
 
-    def _here(self, *tensors):
-        """Whether the object and all tensors are on the current device, to whose stream the call
-        goes."""
-        on = self.on
-        if on != ab.current_device():
-            return False
-        for x in tensors:
-            if x is not None and x.get_device() != on:
-                return False
-        return True
-
     def _check(self, *expected):
-        """As _expect, and ValueError unless :meth:`_here`.  (A host tensor is the binding's to
-        refuse.)"""
+        """As _expect, and ValueError unless the object and the tensors are on the current device,
+        to whose stream the call goes.  (A host tensor is the binding's to refuse.)"""
         _expect(*expected)
         for x, name, *_ in expected:
             if x is None or isinstance(x, int) or not x.is_cuda:
@@ -544,12 +533,15 @@ class ShortConvStep(_OnDevice):
         """y; the pool's states move on in place, or from their slots to those of pool_out."""
         dt, f32, i32 = self.dtypes
         rows, weights, channels, bounds, seqs = self.shapes
+        on = self.on
         try:  # (in one expression, as the delta rule's step)
-            fits = (x.dtype is dt and x.shape == rows and weight.dtype is f32 and
+            fits = (on == ab.current_device() == x.get_device() == weight.get_device() ==
+                    pool.get_device() and x.dtype is dt and x.shape == rows and
+                    weight.dtype is f32 and
                     weight.shape == weights and pool.dtype is dt and pool.shape == self.pool and
-                    (slots is None or slots.dtype is i32 and slots.shape == seqs) and
-                    bias is None and seq_offsets is None and slots_out is None and
-                    self._here(x, weight, pool, slots))
+                    (slots is None or slots.dtype is i32 and slots.shape == seqs and
+                     slots.get_device() == on) and
+                    bias is None and seq_offsets is None and slots_out is None)
         except AttributeError:
             fits = False
         if not fits:
@@ -607,18 +599,20 @@ class BlockNorm(_OnDevice):
 
     def _set(self, x, residual, gate, after_weight, before_weight, channel_scale):
         dt, rt, f32 = self.dtypes
-        shape, width = self.shape, self.width
+        shape, width, on = self.shape, self.width, self.on
         try:
-            fits = (x.dtype is dt and x.shape == shape and
-                    (gate is None or gate.dtype is dt and gate.shape == shape) and
-                    (residual is None or residual.dtype is rt and residual.shape == shape) and
+            fits = (on == ab.current_device() == x.get_device() and
+                    x.dtype is dt and x.shape == shape and
+                    (gate is None or gate.dtype is dt and gate.shape == shape and
+                     gate.get_device() == on) and
+                    (residual is None or residual.dtype is rt and residual.shape == shape and
+                     residual.get_device() == on) and
                     (after_weight is None or after_weight.dtype is f32 and
-                     after_weight.shape == width) and
+                     after_weight.shape == width and after_weight.get_device() == on) and
                     (before_weight is None or before_weight.dtype is f32 and
-                     before_weight.shape == width) and
+                     before_weight.shape == width and before_weight.get_device() == on) and
                     (channel_scale is None or channel_scale.dtype is f32 and
-                     channel_scale.shape == width) and
-                    self._here(x, gate, residual, after_weight, before_weight, channel_scale))
+                     channel_scale.shape == width and channel_scale.get_device() == on))
         except AttributeError:
             fits = False
         if not fits:
@@ -702,9 +696,10 @@ class TokenLogprobs(_OnDevice):
         dt, _, i32 = self.dtypes
         rows, tokens, _ = self.shapes
         try:
-            fits = (logits.dtype is dt and logits.shape == rows and
-                    (given is None or given.dtype is i32 and given.shape == tokens) and
-                    self._here(logits, given))
+            fits = (self.on == ab.current_device() == logits.get_device() and
+                    logits.dtype is dt and logits.shape == rows and
+                    (given is None or given.dtype is i32 and given.shape == tokens and
+                     given.get_device() == self.on))
         except AttributeError:
             fits = False
         if not fits:
