@@ -13,8 +13,8 @@ the heads' outputs and gate them (``onela_block_norm``) and projects back.  The 
 * a beam search from a prompt's state: :meth:`DeltaMixer.beam_step_inputs` gives what
   one step of :class:`runner.Decoder` takes.
 
-A training step may be captured into a graph, forward and backward together.  As with any layer in
-torch, no outputs of an eager pass on the same weights may be alive then: their gradients' nodes
+The operators' functions may be captured into a graph, forward and backward together.  As with
+anything in torch, no outputs of an eager pass on the same leaves may be alive then: their nodes
 belong to the stream of that pass, and a capture that meets them ends in an error or the process.
 
 A layer with a convolution has two states, (the delta rule's, the convolution's), wherever one
