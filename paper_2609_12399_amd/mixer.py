@@ -54,6 +54,15 @@ def _once(grads):
     return tuple(None if g is None else _Once.apply(g.detach().requires_grad_()) for g in grads)
 
 
+def _clear(op, seq_offsets, *names):
+    """The object, with 0 in the rows behind the last sequence of a padded batch: the calls leave
+    them as they were, but here products and sums over tokens follow."""
+    if seq_offsets is not None:
+        for name in names:
+            getattr(op, name).zero_()
+    return op
+
+
 class QkNormRopeFunction(torch.autograd.Function):
     """q, k [tokens][heads][D], weights fp32 [D] or None -> both normed and turned."""
 
@@ -82,13 +91,14 @@ class DeltaRuleFunction(torch.autograd.Function):
         ctx.save_for_backward(q, k, v, log_alpha, beta, seq_offsets, initial_state)
         ctx.sizes = (num_seqs, q.shape[0], q.shape[1], v.shape[1], q.shape[2], v.shape[2], _io(q))
         ctx.scale = scale
-        op = runner.DeltaRule(*ctx.sizes, scale=scale, device=q.device)
+        op = _clear(runner.DeltaRule(*ctx.sizes, scale=scale, device=q.device), seq_offsets, "o")
         return op.forward(q, k, v, log_alpha, beta, seq_offsets, initial_state)
 
     @staticmethod
     def backward(ctx, d_o, d_state):
         q, k, v, log_alpha, beta, seq_offsets, initial_state = ctx.saved_tensors
-        op = runner.DeltaRule(*ctx.sizes, scale=ctx.scale, backward=True, device=q.device)
+        op = _clear(runner.DeltaRule(*ctx.sizes, scale=ctx.scale, backward=True, device=q.device),
+                    seq_offsets, "dq", "dk", "dv", "dlog_alpha", "dbeta")
         dq, dk, dv, dla, db, ds = _once(op.backward(
             q, k, v, log_alpha, beta, d_o.contiguous(), seq_offsets, initial_state,
             d_state.contiguous()))
@@ -103,13 +113,14 @@ class ShortConvFunction(torch.autograd.Function):
     def forward(ctx, x, weight, bias, seq_offsets, initial_state, num_seqs, activation):
         ctx.save_for_backward(x, weight, bias, seq_offsets, initial_state)
         ctx.sizes = (num_seqs, *x.shape, weight.shape[1], _io(x), activation)
-        op = runner.ShortConv(*ctx.sizes, device=x.device)
+        op = _clear(runner.ShortConv(*ctx.sizes, device=x.device), seq_offsets, "y")
         return op.forward(x, weight, bias, seq_offsets, initial_state)
 
     @staticmethod
     def backward(ctx, d_y, d_state):
         x, weight, bias, seq_offsets, initial_state = ctx.saved_tensors
-        op = runner.ShortConv(*ctx.sizes, backward=True, device=x.device)
+        op = _clear(runner.ShortConv(*ctx.sizes, backward=True, device=x.device), seq_offsets,
+                    "dx")
         dx, dw, db, ds = _once(op.backward(x, weight, d_y.contiguous(), bias, seq_offsets,
                                            initial_state, d_state.contiguous()))
         return dx, dw, db, None, ds, None, None
