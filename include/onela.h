@@ -654,7 +654,10 @@ onela_status_t onela_token_logprobs(const onela_logprob_config_t* cfg, const voi
 /* Gradient of a scalar of the log probabilities of the given tokens (of the alternatives too,
  * given again), lse and entropy by the logits:
  *   dz_v = p_v (d_lse - sum_g d_logp_g - d_entropy (logp_v + entropy)) + sum_{g: given_g = v} d_logp_g
- *   lse, entropy  what the forward call gave (entropy only with d_entropy)
+ *   lse, entropy  what the forward call gave (entropy only with d_entropy).  Rows whose lse is
+ *                 beyond 128 either way, where one number no longer holds a logarithm of a sum
+ *                 beside their largest logit, have their sums formed again from the logits:
+ *                 p has the same errors wherever the logits stand
  *   d_logp        device fp32 [num_rows][num_given] (NULL with num_given = 0)
  *   d_lse, d_entropy  device fp32 [num_rows], or NULL (0)
  *   d_logits      device [num_rows][vocab] io dtype, dense, aligned to its elements; may be

@@ -500,12 +500,59 @@ __global__ __launch_bounds__(kJoinThreads) void logprob_join_kernel(LogprobParam
 }
 
 // ---- gradient ----------------------------------------------------------------------------
-// Every element by itself from lse: p = e^{c x - lse}, dx = c p (a - dH (ln p + H)), with a = dlse
-// - sum of the given tokens' gradients; then the given tokens that stand in the workgroup's
-// columns are written again with their own gradients added (equal ones all, so
-// that it does not matter which thread writes last).
-// A workgroup has kBackColumns columns of a row, a wave up to a quarter of that.
+// With l = ln p and a = dlse - sum of the given tokens' gradients, dx = c p (a - dH (l + H));
+// then the given tokens that stand in the workgroup's columns are written again with their own
+// gradients added (equal ones all, so that it does not matter which thread writes last).
+// A workgroup has kBackColumns columns of a row, a wave up to a quarter of that, every element by
+// itself with l = c x - lse.  As one number for c m + ln s, lse is off by half its last place, 4e-6
+// up to kNear: less than the sum is.  Beyond (all logits far from 0, a row of a finite mask's
+// value, c m past the largest number) ln s is lost in it, and one workgroup has the whole row (which
+// may be written over the logits): it forms m and ln s again and takes l = c (x - m) - ln s.
+// That is three reads, two from the cache: 8192 x 32768 logits near 4096 592 us in place of 192,
+// 300 x 50001 in fp32 72 in place of 20.  (A function of its own for it, not inlined, leaves the other
+// rows their registers: inlined, 300 x 50001 with 64 given tokens 25.6 us, so 24.)
 constexpr int kBackColumns = 4096;
+constexpr float kNear = 128.f;
+
+// m and ln s of a row, in every thread; m = -inf where nothing is left of it.
+template <int THREADS, bool BF16>
+__device__ inline void row_sums(const char* x, int V, float c2, float& m, float& logs) {
+  constexpr int EV = Piece<BF16>::EV, W = THREADS / 64;
+  __shared__ float most[W];
+  __shared__ double sums[W];
+  Piece<BF16> in;
+  float v[EV];
+  m = kNegInf;
+  for (int c = int(threadIdx.x) * EV; c < V; c += THREADS * EV) {
+    in.load(x, c, V);
+    in.floats(v);
+#pragma unroll
+    for (int i = 0; i < EV; ++i) m = fmaxf(m, v[i]);
+  }
+  m = group_max<64>(m);
+  if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < W; ++i) m = fmaxf(m, most[i]);
+  const float o = origin(m);
+  double s = 0.0;  // (one thread's chain may be long)
+  for (int c = int(threadIdx.x) * EV; c < V; c += THREADS * EV) {
+    in.load(x, c, V);
+    in.floats(v);
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < EV; ++i) t += __builtin_amdgcn_exp2f((v[i] - o) * c2);
+    s += t;
+  }
+#pragma unroll
+  for (int i = 1; i < 64; i *= 2) s += __shfl_xor(s, i);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  s = 0.0;
+#pragma unroll
+  for (int i = 0; i < W; ++i) s += sums[i];
+  logs = kLn2 * __builtin_amdgcn_logf(float(s));
+}
 
 template <bool BF16>
 __device__ inline void store_any(char* row, int c, int end, const float* x) {
@@ -531,6 +578,61 @@ __device__ inline void store_any(char* row, int c, int end, const float* x) {
     }
 }
 
+// What a row's gradients are formed from: dx = scale p (a - dh (l + h)).
+struct Slopes {
+  float a, dh, h;
+};
+template <bool ENT>
+__device__ inline float slope(const Slopes& d, float l) {
+  float f = d.a;
+  if constexpr (ENT) f = fmaf(-d.dh, fmaxf(l, kFar) + d.h, d.a);
+  return __builtin_amdgcn_exp2f(l * kLog2e) * f;
+}
+template <bool BF16>
+__device__ inline void store_one(char* row, int c, float y) {
+  if constexpr (BF16)
+    reinterpret_cast<uint16_t*>(row)[c] = uint16_t(pack_bf16x2(y, y));
+  else
+    reinterpret_cast<float*>(row)[c] = y;
+}
+
+// A whole row from its own sums; the given tokens and their gradients are in LDS.
+template <int THREADS, bool BF16, bool ENT>
+__device__ __noinline__ void far_row(const char* x, char* dx, int V, float scale, Slopes d,
+                                     const int* token, const float* grad, int G) {
+  constexpr int EV = Piece<BF16>::EV, MINE = kMaxGiven / THREADS;
+  float m, ls, at_mine[MINE];
+  row_sums<THREADS, BF16>(x, V, scale * kLog2e, m, ls);
+  const bool gone = m == kNegInf;
+  m = origin(m);
+  auto value = [&](float y) { return gone ? 0.f : slope<ENT>(d, fmaf(y - m, scale, -ls)); };
+#pragma unroll
+  for (int i = 0; i < MINE; ++i) {
+    const int g = i * THREADS + int(threadIdx.x), v = g < G ? token[g] : -1;
+    if (v >= 0 && v < V) at_mine[i] = load1<BF16>(x, v);
+  }
+  __syncthreads();  // (read before anything is stored: dx may be x)
+#pragma unroll 1
+  for (int c = int(threadIdx.x) * EV; c < V; c += THREADS * EV) {
+    Piece<BF16> in;
+    float v[EV];
+    in.load(x, c, V);
+    in.floats(v);
+#pragma unroll
+    for (int i = 0; i < EV; ++i) v[i] = scale * value(v[i]);
+    store_any<BF16>(dx, c, V, v);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < MINE; ++i) {
+    const int g = i * THREADS + int(threadIdx.x), t = g < G ? token[g] : -1;
+    if (t < 0 || t >= V) continue;
+    float s = 0.f;
+    for (int j = 0; j < G; ++j) s += token[j] == t ? grad[j] : 0.f;
+    store_one<BF16>(dx, t, gone ? 0.f : scale * (value(at_mine[i]) + s));
+  }
+}
+
 template <int THREADS, bool BF16, bool ENT>
 __global__ __launch_bounds__(THREADS) void logprob_backward_kernel(LogprobParams p, int blocks) {
   constexpr int EV = Piece<BF16>::EV, NV = kBackColumns / (256 * EV), MINE = kMaxGiven / THREADS;
@@ -547,9 +649,7 @@ __global__ __launch_bounds__(THREADS) void logprob_backward_kernel(LogprobParams
   for (int k = 0; k < NV; ++k)
     in[k].load(x, begin + (k * THREADS + int(threadIdx.x)) * EV, end);
   const float lse = p.lse_in[row];
-  const bool gone = lse == kNegInf;
-  float a = p.dlse ? p.dlse[row] : 0.f;
-  const float dh = ENT ? p.dentropy[row] : 0.f, h = ENT ? p.entropy_in[row] : 0.f;
+  Slopes d{p.dlse ? p.dlse[row] : 0.f, ENT ? p.dentropy[row] : 0.f, ENT ? p.entropy_in[row] : 0.f};
   // the given tokens' gradients; a token past the vocabulary makes the row NaN
   int mine[MINE];
   float at_mine[MINE];
@@ -570,14 +670,17 @@ __global__ __launch_bounds__(THREADS) void logprob_backward_kernel(LogprobParams
     __syncthreads();
     float s = 0.f;
     for (int g = 0; g < p.G; ++g) s += grad[g];
-    a -= s;
+    d.a -= s;
   }
-  auto value = [&](float y) {
-    const float l = fmaf(y, p.scale, -lse);
-    float f = a;
-    if constexpr (ENT) f = fmaf(-dh, fmaxf(l, kFar) + h, a);
-    return gone ? 0.f : __builtin_amdgcn_exp2f(l * kLog2e) * f;
-  };
+  // (with scale <= 1 no row of numbers has an lse of -inf)
+  const bool gone = lse == kNegInf && p.scale <= 1.f;
+  if (fabsf(lse) > kNear && !gone) {
+    // (another one from row to row: neighbouring workgroups are on different XCDs)
+    if (begin == int(row % blocks) * (THREADS * EV * NV))
+      far_row<THREADS, BF16, ENT>(x, dx, p.V, p.scale, d, token, grad, p.G);
+    return;
+  }
+  auto value = [&](float y) { return gone ? 0.f : slope<ENT>(d, fmaf(y, p.scale, -lse)); };
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
     const int c = begin + (k * THREADS + int(threadIdx.x)) * EV;
@@ -595,11 +698,7 @@ __global__ __launch_bounds__(THREADS) void logprob_backward_kernel(LogprobParams
     if (mine[i] < 0) continue;
     float s = 0.f;
     for (int g = 0; g < p.G; ++g) s += token[g] == mine[i] ? grad[g] : 0.f;
-    const float y = gone ? 0.f : p.scale * (value(at_mine[i]) + s);
-    if constexpr (BF16)
-      reinterpret_cast<uint16_t*>(dx)[mine[i]] = uint16_t(pack_bf16x2(y, y));
-    else
-      reinterpret_cast<float*>(dx)[mine[i]] = y;
+    store_one<BF16>(dx, mine[i], gone ? 0.f : p.scale * (value(at_mine[i]) + s));
   }
 }
 

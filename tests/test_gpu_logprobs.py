@@ -346,3 +346,76 @@ def test_beam_scores_less_lse_select_from_logits():
 def ref_logp(x):
     m = x.max(1, keepdims=True)
     return x - m - np.log(np.exp(x - m).sum(1, keepdims=True))
+
+
+def far_rows(V, io):
+    """Rows whose lse is far from 0: a large offset, finite masks' values throughout (and in all
+    columns but one), large values of either sign, and ordinary and masked rows beside them."""
+    x = draw(12, V)
+    low = float(torch.finfo(torch.bfloat16).min)
+    x[0] += 4096.0
+    x[1] -= 4096.0
+    x[2] = -1e9
+    x[3] = -1e9 + x[3]
+    x[4] = low
+    x[5], x[5, V // 2] = low, 2.0
+    x[6] = 1e30 * np.sign(x[6])
+    x[7] = -low
+    x[8] += 100.0
+    x[9] = -np.inf
+    x[10], x[10, [1, V - 2]] = -np.inf, -4e9
+    dt = torch.bfloat16 if io == "bf16" else torch.float32
+    return f64(torch.from_numpy(x).to(dt))
+
+
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+@pytest.mark.parametrize("V,G,ent,place", [(70, 2, False, False), (1000, 5, True, True),
+                                           (4096, 1, False, False), (9001, 0, True, True),
+                                           (9001, 256, True, False), (50001, 1, False, True)])
+@pytest.mark.parametrize("scale", [1.0, 0.7, 1.5])
+def test_gradient_of_rows_far_from_zero(scale, V, G, ent, place, io):
+    """p comes from differences to the row's largest logit wherever lse alone has lost ln s: its
+    error is the sum's 7.5e-6, half a step of an lse up to 128 (4e-6) and the exponential's
+    argument, 2^-23 |ln p| (|ln p| < 40: 5e-6), of every term.  In place too."""
+    x = far_rows(V, io)
+    R, given = len(x), tokens(len(x), V, G) if G else None
+    if G:
+        given[given >= V] = -1
+        given[2], given[4], given[7] = -1, -1, -1  # padding alone: 0 without the others
+    r = np.random.default_rng(V)
+    dlogp = r.normal(size=(R, G)).astype(np.float32) if G else None
+    dlse, dent = ((r.normal(size=R).astype(np.float32) for _ in range(2)) if ent or not G
+                  else (None, None))
+    dent = dent if ent else None
+    with np.errstate(over="ignore"):
+        _, lse, entropy, _, _ = ref.logprobs(x, None, 0, scale)
+        dev = [None if t is None else torch.from_numpy(np.asarray(t, np.float32)).to(DEV)
+               for t in (lse, dlogp, dlse, entropy, dent)]
+    dt = torch.bfloat16 if io == "bf16" else torch.float32
+    logits = torch.from_numpy(x).to(dt).to(DEV)
+    tok = None if given is None else torch.from_numpy(given).to(torch.int32).to(DEV)
+    op = runner.TokenLogprobs(R, V, G, 0, io, scale, backward=True, device=DEV)
+    got = op.backward(logits, tok, *dev, out=logits if place else None)
+    want, size = ref.logprobs_backward(x, given, dlogp, dlse, dent, scale)
+    same_or_near(got, want, 2e-5 * size + (2.0 ** -8 * np.abs(want) if io == "bf16" else 0) + 1e-37)
+    if not ent and G:
+        assert float(got[[2, 4, 7]].float().abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("scale", [0.7, 1.5])
+def test_gradient_from_the_forward_calls_own_sums(scale):
+    """What the forward call leaves is what the gradient takes, far rows among it: each row's
+    gradient of the sum of all log probabilities adds up to 0 (V terms of 1 and of V p each, with
+    their 2e-5 and the roundings of V sums)."""
+    V = 5000
+    x = torch.from_numpy(far_rows(V, "f32")).float().to(DEV)
+    R = x.shape[0]
+    tok = torch.randint(0, V, (R, 3), generator=torch.Generator().manual_seed(1)).int().to(DEV)
+    tok[10] = 1  # (its mask leaves this token and one other)
+    _, lse, *_ = runner.TokenLogprobs(R, V, 3, 0, "f32", scale, device=DEV).forward(x, tok)
+    one = torch.ones((R, 3), device=DEV)
+    got = runner.TokenLogprobs(R, V, 3, 0, "f32", scale, backward=True, device=DEV).backward(
+        x, tok, lse, one)
+    assert bool(torch.isfinite(got).all())
+    assert float(got.double().sum(1).abs().max()) <= scale * 6 * 2e-5
+    assert float(got[9].abs().max()) == 0.0
