@@ -278,10 +278,10 @@ __global__ __launch_bounds__(LANES > 64 ? LANES : 256) void block_norm_backward_
         if (in) cur.g.floats(g);
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-          const float sg = sigmoid(g[j]);
-          a[j] = sg * (p.silu ? g[j] : 1.f);
-          // s (1 + g (1 - s)), or s (1 - s)
-          slope[j] = fmaf(-a[j], sg, a[j] + (p.silu ? sg : 0.f));
+          const float sg = sigmoid(g[j]), z = p.silu ? g[j] : 1.f;
+          a[j] = sg * z;
+          // s (1 + g (1 - s)), or s (1 - s); 1 - s first: g + 1 would lose the 1 beside a large g
+          slope[j] = fmaf(sg, fmaf(-z, sg, z), p.silu ? sg : 0.f);
         }
       }
     };

@@ -249,3 +249,19 @@ def test_more_than_32_bits_of_offset():
                           eps=1e-6)
     near(y[-3:], want[0], want[2], 6e-6, torch.bfloat16)
     assert float(y[:-3].abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("act", ["silu", "sigmoid"])
+@pytest.mark.parametrize("D", [128, 2048, 8192])
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_gradients_of_large_gates(io, D, act):
+    """The activation's slope stays right to 2^-22 of 1 wherever the gate stands: s and g (1 - s) have
+    half a step of s each, |g| 2^-24 where s is not 1 (|g| < 17): 1e-6, beside the 1.2e-5 of dgate."""
+    c = Case(5, 1, D, io, "f32", True, False, act, False, False)
+    at = torch.tensor([40.3, -40.3, 1000.7, -1000.7, 2.0 ** 24 + 2, 2.0 ** 25, 2.0 ** 25 + 4, 3e9,
+                       1e30, -1e30, 17.2, -17.2, 88.9, -88.9, 0.0])
+    c.gate[1, 0, :15] = at.to(c.dt).to(DEV)
+    c.gate[2, 0, -15:] = at.to(c.dt).to(DEV)
+    got = c.backward()
+    grads, sizes = ref.block_norm_backward(*map(f64, c.tensors()), f64(c.dy), None, **c.args)
+    near(got[2], grads[2], sizes[2], 1.2e-5, c.dt)
