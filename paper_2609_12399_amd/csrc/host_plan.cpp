@@ -441,6 +441,11 @@ size_t conv_workspace_bytes(const onela_conv_config_t* c) {
   return (rows * size_t(c->taps + 1) * size_t(c->channels) * sizeof(float) + 255) / 256 * 256;
 }
 
+unsigned conv_weight_blocks(int taps, int channels) {
+  // 16 values each; with 2^20 of them a grid's threads stay below 2^32, and they take turns
+  return unsigned(std::min((long(taps + 1) * channels + 15) / 16, 1l << 20));
+}
+
 // ---- norms around a block ----------------------------------------------------------
 
 onela_status_t check_block_norm(const onela_block_norm_config_t* c) {

@@ -157,6 +157,8 @@ struct ConvPlan {
 onela_status_t check_conv(const onela_conv_config_t* cfg, bool ragged);
 ConvPlan conv_plan(const onela_conv_config_t* cfg, bool backward);
 size_t conv_workspace_bytes(const onela_conv_config_t* cfg);
+// Workgroups (of 256 threads) of the backward pass's second launch.
+unsigned conv_weight_blocks(int taps, int channels);
 
 // ---- norms around a block ----------------------------------------------------------
 constexpr int kBlockNormBlocks = 1024;  // most workgroups of the backward pass

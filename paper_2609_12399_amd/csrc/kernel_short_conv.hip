@@ -381,22 +381,26 @@ __global__ __launch_bounds__(kConvThreads, WAVE ? (BF16 ? 4 : 3) : 2) void conv_
 __global__ __launch_bounds__(256) void conv_weight_kernel(ConvParams p, int taps, long rows) {
   __shared__ float acc[16][17];
   const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
-  const long col = long(blockIdx.x) * 16 + c, width = long(taps + 1) * p.C;
-  float s = 0.f;
-  if (col < width)
+  const long width = long(taps + 1) * p.C;
+  for (long first = long(blockIdx.x) * 16; first < width; first += long(gridDim.x) * 16) {
+    const long col = first + c;
+    float s = 0.f;
+    if (col < width)
 #pragma unroll 4
-    for (long i = g; i < rows; i += 16) s += p.partial[i * width + col];
-  acc[g][c] = s;
-  __syncthreads();
-  if (g != 0 || col >= width) return;
-  s = 0.f;
+      for (long i = g; i < rows; i += 16) s += p.partial[i * width + col];
+    __syncthreads();  // (the values before these have been read)
+    acc[g][c] = s;
+    __syncthreads();
+    if (g != 0 || col >= width) continue;
+    s = 0.f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s += acc[i][c];
-  const int j = int(col / p.C), ch = int(col - long(j) * p.C);
-  if (j < taps) {
-    if (p.dw) p.dw[long(ch) * taps + j] = s;
-  } else if (p.db) {
-    p.db[ch] = s;
+    for (int i = 0; i < 16; ++i) s += acc[i][c];
+    const int j = int(col / p.C), ch = int(col - long(j) * p.C);
+    if (j < taps) {
+      if (p.dw) p.dw[long(ch) * taps + j] = s;
+    } else if (p.db) {
+      p.db[ch] = s;
+    }
   }
 }
 
@@ -481,8 +485,7 @@ hipError_t run_backward(const ConvParams& p, const ConvPlan& a, hipStream_t st) 
     if (e != hipSuccess) return e;
   }
   if (p.partial && a.blocks_t != 1)
-    conv_weight_kernel<<<unsigned((long(TAPS + 1) * p.C + 15) / 16), 256, 0, st>>>(p, TAPS,
-                                                                                  a.blocks_t);
+    conv_weight_kernel<<<conv_weight_blocks(TAPS, p.C), 256, 0, st>>>(p, TAPS, a.blocks_t);
   return hipGetLastError();
 }
 

@@ -58,6 +58,15 @@ static void cover(const onela_conv_config_t& c, bool backward) {
   EXPECT((a.blocks_t - 1) * tokens < c.total_tokens || c.total_tokens == 0);
 }
 
+// The launch that adds up the weights' gradients is within a grid for every size that is taken.
+static void weights(int channels, int taps) {
+  const onela_conv_config_t c = config(channels, taps, 0, 0);
+  EXPECT(check_conv(&c, true) == ONELA_OK);
+  const unsigned n = conv_weight_blocks(taps, channels);
+  EXPECT(n >= 1 && double(n) * 256 < kGridThreads);
+  EXPECT(n == (1u << 20) || double(n) * 16 >= double(taps + 1) * channels);
+}
+
 int main() {
   std::mt19937 rng(11);
   for (int i = 0; i < 300; ++i) {
@@ -73,6 +82,8 @@ int main() {
                                          int(rng() % 2));
     for (bool backward : {false, true}) cover(c, backward);
   }
+  for (int taps = 2; taps <= 4; ++taps)
+    for (int channels : {8, 64, 6144, 1 << 20, 1 << 25, (1 << 26) - 8, 1 << 26}) weights(channels, taps);
   if (failures) return 1;
   std::printf("convolution plan checks: ok\n");
   return 0;

@@ -310,3 +310,17 @@ def test_graph_stream_and_same_bits():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, got))
         assert all(torch.equal(a, b) for a, b in zip(want[2:], again))
+
+
+@pytest.mark.parametrize("C,taps", [(1 << 26, 4), (54 << 20, 4), (1 << 24, 2)])
+def test_weight_gradients_of_the_most_channels(C, taps):
+    """The second launch alone writes them where there are no tokens: all of them, in more turns
+    than a grid has workgroups (a thread for each of their 16ths would pass 2^32)."""
+    cfg = ab.make_conv_config(1, 0, C, taps, "bf16")
+    n = ab.onela_short_conv_workspace_bytes(cfg)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    w = torch.zeros((C, taps), device=DEV)
+    dw, db = torch.full((C, taps), 7.0, device=DEV), torch.full((C,), 7.0, device=DEV)
+    ab.onela_short_conv_backward(cfg, None, None, w, None, None, None, None, None, dw, db, None, ws,
+                                 n)
+    assert float(dw.abs().max()) == float(db.abs().max()) == 0.0
