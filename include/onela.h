@@ -570,7 +570,9 @@ onela_status_t onela_short_conv_step(const onela_conv_config_t* cfg, const int32
  *   y             device, dense, io dtype, or NULL (not wanted)
  *   residual_out  h, device, dense, residual_dtype, or NULL; may be residual
  * width: a multiple of 8 up to 8192.  fp32 inside (y is formed from h before its rounding),
- * one rounding at each store. */
+ * one rounding at each store.  An output, here and in the backward call, may stand in the
+ * place of an input of the same type, both dense; other overlaps of an output with an input or
+ * another output are ONELA_EINVAL. */
 typedef struct {
   int64_t num_tokens;     /* < 2^31 */
   int32_t num_heads;      /* rows per token */

@@ -527,6 +527,17 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   return x < y ? y - x < na : x - y < nb;
 }
 
+bool clash(std::initializer_list<Bytes> outs, std::initializer_list<Bytes> ins, bool in_place) {
+  for (const Bytes* a = outs.begin(); a != outs.end(); ++a) {
+    for (const Bytes* b = a + 1; b != outs.end(); ++b)
+      if (overlap(a->at, a->n, b->at, b->n)) return true;
+    for (const Bytes& b : ins)
+      if (overlap(a->at, a->n, b.at, b.n) && !(in_place && a->at == b.at && a->n == b.n))
+        return true;
+  }
+  return false;
+}
+
 // ---- per-step protocol --------------------------------------------------------
 // resolve(t) -> append(t) -> decode(t) (decode may repeat), or fused(t); the
 // next step starts only after the previous one was appended.

@@ -6,6 +6,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <initializer_list>
 
 #include "../../include/onela.h"
 
@@ -180,6 +181,13 @@ size_t logprob_workspace_bytes(const onela_logprob_config_t* cfg);
 
 // Whether two ranges of bytes share any.
 bool overlap(const void* a, size_t na, const void* b, size_t nb);
+struct Bytes {
+  const void* at;
+  size_t n;
+};
+// Whether an output shares bytes with another one or with an input.  With `in_place` it may be an
+// input (all of it: where every element is read by the thread that writes it).
+bool clash(std::initializer_list<Bytes> outs, std::initializer_list<Bytes> ins, bool in_place);
 
 // ---- validation and the per-step protocol -----------------------------------
 

@@ -774,6 +774,11 @@ onela_status_t block_norm_inputs(const onela_block_norm_config_t* c, const void*
   p->silu = c->gate_act == ONELA_ACT_SILU;
   return ONELA_OK;
 }
+size_t block_norm_bytes(const onela_block_norm_config_t* c, int64_t stride, int32_t dtype) {
+  const int64_t own = int64_t(c->num_heads) * c->width;
+  return span(c->num_tokens, stride ? stride : own, own, dtype);
+}
+size_t width_bytes(const onela_block_norm_config_t* c) { return size_t(c->width) * 4; }
 }  // namespace
 
 onela_status_t onela_block_norm(const onela_block_norm_config_t* cfg, const void* x,
@@ -786,6 +791,17 @@ onela_status_t onela_block_norm(const onela_block_norm_config_t* cfg, const void
       block_norm_inputs(cfg, x, gate, residual, after_weight, before_weight, channel_scale, &p);
   if (rc != ONELA_OK) return rc;
   if ((p.rows > 0 && !y && !residual_out) || !aligned16(y) || !aligned16(residual_out))
+    return ONELA_EINVAL;
+  const size_t rows = block_norm_bytes(cfg, 0, cfg->io_dtype), vector = width_bytes(cfg);
+  const size_t res = block_norm_bytes(cfg, 0, cfg->residual_dtype);
+  if (onela::clash({{y, rows}, {residual_out, res}},
+                   {{x, block_norm_bytes(cfg, cfg->x_stride, cfg->io_dtype)},
+                    {gate, block_norm_bytes(cfg, cfg->gate_stride, cfg->io_dtype)},
+                    {residual, res},
+                    {after_weight, vector},
+                    {before_weight, vector},
+                    {channel_scale, vector}},
+                   true))
     return ONELA_EINVAL;
   p.y = y;
   p.h = residual_out;
@@ -822,6 +838,25 @@ onela_status_t onela_block_norm_backward(
     if (workspace_bytes < onela::block_norm_workspace_bytes(cfg)) return ONELA_ECAPACITY;
     p.partial = static_cast<float*>(workspace);
   }
+  const size_t rows = block_norm_bytes(cfg, 0, cfg->io_dtype), vector = width_bytes(cfg);
+  const size_t res = block_norm_bytes(cfg, 0, cfg->residual_dtype);
+  if (onela::clash({{dx, rows},
+                    {dgate, rows},
+                    {d_residual, res},
+                    {dafter_weight, vector},
+                    {dbefore_weight, vector},
+                    {dchannel_scale, vector},
+                    {p.partial, onela::block_norm_workspace_bytes(cfg)}},
+                   {{x, block_norm_bytes(cfg, cfg->x_stride, cfg->io_dtype)},
+                    {gate, block_norm_bytes(cfg, cfg->gate_stride, cfg->io_dtype)},
+                    {residual, res},
+                    {d_y, rows},
+                    {d_residual_out, res},
+                    {after_weight, vector},
+                    {before_weight, vector},
+                    {channel_scale, vector}},
+                   true))
+    return ONELA_EINVAL;
   p.dy = d_y;
   p.dh = d_residual_out;
   p.dx = dx;

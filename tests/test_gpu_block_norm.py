@@ -265,3 +265,21 @@ def test_gradients_of_large_gates(io, D, act):
     got = c.backward()
     grads, sizes = ref.block_norm_backward(*map(f64, c.tensors()), f64(c.dy), None, **c.args)
     near(got[2], grads[2], sizes[2], 1.2e-5, c.dt)
+
+
+@pytest.mark.parametrize("T,H,D", [(900, 3, 40), (700, 1, 512), (600, 1, 2048), (300, 1, 8192)])
+def test_outputs_in_the_place_of_inputs(T, H, D):
+    """Every output in the place of each dense input of its type, in turn: the same bits."""
+    c = Case(T, H, D, "bf16", "bf16", True, True, "silu", True, True)
+    forward, back = (runner.BlockNorm(T, D, backward=b, **c.make) for b in (False, True))
+    want = [t.clone() for t in (*c.forward(), *c.backward()[:3])]
+    for i, j in ((0, 1), (1, 2), (2, 0)):
+        x, gate, res = ins = [c.x.clone(), c.gate.clone(), c.res.clone()]
+        ab.onela_block_norm(forward.cfg, x, gate, res, c.wa, c.wb, c.cs, ins[i], ins[j])
+        assert torch.equal(ins[i], want[0]) and torch.equal(ins[j], want[1])
+    for i, j, k in ((0, 1, 2), (3, 4, 0), (2, 0, 3), (4, 3, 1)):  # dx, d_residual, dgate
+        x, gate, res, dy, dh = ins = [t.clone() for t in (c.x, c.gate, c.res, c.dy, c.dh)]
+        ab.onela_block_norm_backward(back.cfg, x, gate, res, c.wa, c.wb, c.cs, dy, dh, ins[i],
+                                     ins[k], ins[j])
+        assert torch.equal(ins[i], want[2]) and torch.equal(ins[j], want[3])
+        assert torch.equal(ins[k], want[4])

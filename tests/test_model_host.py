@@ -431,3 +431,35 @@ def test_search_refuses_empty_prompts(bounds, steps):
     model = recommender.Recommender(20, 16, 2, 1, 2, 32, "f32", device="cpu")
     with pytest.raises(ValueError, match="one token"):
         model.search(torch.zeros(3, dtype=I64), torch.tensor(bounds, dtype=I32), 4, steps)
+
+
+def test_norm_overlaps_refused(lib):
+    """4 tokens of 2 x 64 bf16 are 1024 bytes, the residual in fp32 2048, a weight's vector 256."""
+    cfg, wide = norm_cfg(), norm_cfg(x_stride=256, gate_stride=256)
+    for out in ("y", "h"):
+        for at in (A + 16, A - 16, B + 1008, C + 2032, C - 16):
+            assert norm(lib, cfg, **{out: at}) == ab.ONELA_EINVAL, (out, at)
+        # between the rows of a wider x or gate, and in their place
+        for at in (A + 256, B + 3 * 512, A, B):
+            assert norm(lib, wide, **{out: at}) == ab.ONELA_EINVAL, (out, at)
+    assert norm(lib, cfg, h=A) == norm(lib, cfg, y=C) == ab.ONELA_EINVAL  # of another type
+    assert norm(lib, cfg, y=D, h=D) == norm(lib, cfg, y=D, h=D + 1008) == ab.ONELA_EINVAL
+    for name in ("wa", "wb", "cs"):
+        assert norm(lib, cfg, **{name: D + 512}) == norm(lib, cfg, **{name: E - 240}) == ab.ONELA_EINVAL
+    need = ab.onela_block_norm_workspace_bytes(cfg)
+    far = 0x70000000
+    for out in ("dx", "dg", "dr"):
+        for at in (A + 16, B - 16, C + 2032, D + 1008, E - 16):
+            assert norm_back(lib, cfg, **{out: at}) == ab.ONELA_EINVAL, (out, at)
+        for at in (A + 256, B + 3 * 512):
+            assert norm_back(lib, wide, **{out: at}) == ab.ONELA_EINVAL, (out, at)
+    assert norm_back(lib, cfg, dr=D) == norm_back(lib, cfg, dx=E) == ab.ONELA_EINVAL
+    assert norm_back(lib, cfg, dg=F) == norm_back(lib, cfg, dg=F + 1008) == ab.ONELA_EINVAL
+    assert norm_back(lib, cfg, dr=F - 2032) == ab.ONELA_EINVAL
+    for name in ("dwa", "dwb", "dcs"):
+        for at in (A, D + 512, F + 1020):
+            assert norm_back(lib, cfg, **{name: at}, ws=far, n=need) == ab.ONELA_EINVAL, (name, at)
+    for ws in (A, F, F - need + 256):
+        assert norm_back(lib, cfg, dwa=far, ws=ws, n=need) == ab.ONELA_EINVAL, ws
+    assert norm_back(lib, cfg, dwa=far, dwb=far + 128, ws=far + 4096, n=need) == ab.ONELA_EINVAL
+    assert norm_back(lib, cfg, dwa=far + 8192, ws=far, n=need) == ab.ONELA_EINVAL
