@@ -512,7 +512,8 @@ typedef struct {
  *   initial_state  or NULL (0)
  *   y              device [total_tokens][channels] io dtype, dense
  *   final_state    or NULL; may be initial_state
- * y must not overlap x.  Errors: ONELA_EINVAL, ONELA_EHIP. */
+ * Otherwise outputs must overlap neither inputs nor one another.
+ * Errors: ONELA_EINVAL, ONELA_EHIP. */
 onela_status_t onela_short_conv(const onela_conv_config_t* cfg, const int32_t* seq_offsets,
                                 const void* x, const float* weight, const float* bias,
                                 const void* initial_state, void* y, void* final_state,
@@ -525,6 +526,7 @@ onela_status_t onela_short_conv(const onela_conv_config_t* cfg, const int32_t* s
  *   d_initial_state  or NULL (not wanted); must not be d_final_state
  *   workspace        onela_short_conv_workspace_bytes(cfg) bytes (0 for an invalid cfg),
  *                    256-byte aligned; NULL when neither dweight nor dbias is wanted
+ * No output may overlap another one or an input (but dweight may be weight, and dbias bias).
  * Errors: ONELA_EINVAL, ONELA_ECAPACITY, ONELA_EHIP. */
 size_t onela_short_conv_workspace_bytes(const onela_conv_config_t* cfg);
 onela_status_t onela_short_conv_backward(const onela_conv_config_t* cfg,
@@ -546,6 +548,7 @@ onela_status_t onela_short_conv_backward(const onela_conv_config_t* cfg,
  *              slot (beams of one parent).
  * A sequence whose slot is outside [0, num_slots) (a padded batch's -1) has outputs 0 and
  * stores no state; neither does one whose slot in state_out is outside.
+ * y may be a dense x; otherwise outputs must overlap neither inputs nor one another.
  * Errors: ONELA_EINVAL, ONELA_ECAPACITY (fewer slots than sequences without slots),
  * ONELA_EHIP. */
 onela_status_t onela_short_conv_step(const onela_conv_config_t* cfg, const int32_t* seq_offsets,

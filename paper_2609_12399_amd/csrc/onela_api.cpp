@@ -641,6 +641,16 @@ size_t conv_x_bytes(const onela_conv_config_t* c) {
 size_t conv_rows_bytes(const onela_conv_config_t* c, int64_t rows) {
   return size_t(rows) * size_t(c->channels) * io_bytes(c->io_dtype);
 }
+struct ConvVectors {
+  onela::Bytes weight, bias, offsets;
+};
+ConvVectors conv_vectors(const onela_conv_config_t* c, const float* weight, const float* bias,
+                         const int32_t* offsets) {
+  const size_t channels = size_t(c->channels) * sizeof(float);
+  return {{weight, channels * size_t(c->taps)},
+          {bias, channels},
+          {offsets, (size_t(c->num_seqs) + 1) * sizeof(int32_t)}};
+}
 }  // namespace
 
 onela_status_t onela_short_conv(const onela_conv_config_t* cfg, const int32_t* seq_offsets,
@@ -653,9 +663,11 @@ onela_status_t onela_short_conv(const onela_conv_config_t* cfg, const int32_t* s
   if ((p.total > 0 && !y) || !aligned16(y) || !aligned16(initial_state) || !aligned16(final_state))
     return ONELA_EINVAL;
   const size_t states = conv_rows_bytes(cfg, int64_t(p.N) * (cfg->taps - 1));
-  if (onela::overlap(x, conv_x_bytes(cfg), y, conv_rows_bytes(cfg, p.total)) ||
-      (final_state != initial_state &&
-       onela::overlap(final_state, states, initial_state, states)))
+  const onela::Bytes out = {y, conv_rows_bytes(cfg, p.total)}, last = {final_state, states};
+  const onela::Bytes first = {initial_state, states};
+  const ConvVectors v = conv_vectors(cfg, weight, bias, seq_offsets);
+  if (onela::clash({out, last}, {{x, conv_x_bytes(cfg)}, v.weight, v.bias, v.offsets}, false) ||
+      onela::clash({out}, {first}, false) || onela::clash({last}, {first}, true))
     return ONELA_EINVAL;
   p.s_in = initial_state;
   p.s_out = final_state;
@@ -687,16 +699,22 @@ onela_status_t onela_short_conv_backward(const onela_conv_config_t* cfg,
     return ONELA_EINVAL;
   const size_t states = conv_rows_bytes(cfg, int64_t(p.N) * (cfg->taps - 1));
   const size_t rows = conv_rows_bytes(cfg, p.total);
-  // (a run reads rows of its neighbours)
-  if (onela::overlap(dx, rows, d_y, rows) || onela::overlap(dx, rows, x, conv_x_bytes(cfg)) ||
-      onela::overlap(d_initial_state, states, d_final_state, states) ||
-      onela::overlap(d_initial_state, states, initial_state, states))
-    return ONELA_EINVAL;
   if (dweight || dbias) {
     if (!workspace || !aligned256(workspace)) return ONELA_EINVAL;
     if (workspace_bytes < onela::conv_workspace_bytes(cfg)) return ONELA_ECAPACITY;
     p.partial = static_cast<float*>(workspace);
   }
+  // (a run reads rows of its neighbours)
+  const ConvVectors v = conv_vectors(cfg, weight, bias, seq_offsets);
+  const onela::Bytes grad = {dx, rows}, dfirst = {d_initial_state, states};
+  const onela::Bytes dw = {dweight, v.weight.n}, db = {dbias, size_t(p.C) * sizeof(float)};
+  const onela::Bytes work = {p.partial, onela::conv_workspace_bytes(cfg)};
+  if (onela::clash({grad, dfirst, dw, db, work},
+                   {{x, conv_x_bytes(cfg)}, {initial_state, states}, {d_y, rows},
+                    {d_final_state, states}, v.offsets}, false) ||
+      onela::clash({grad, dfirst, work}, {v.weight, v.bias}, false) ||
+      onela::clash({dw, db}, {v.weight, v.bias}, true))
+    return ONELA_EINVAL;
   p.s_in = initial_state;
   p.dy = d_y;
   p.ds_in = d_final_state;
@@ -725,8 +743,17 @@ onela_status_t onela_short_conv_step(const onela_conv_config_t* cfg, const int32
   if (!slots && num_slots < p.N) return ONELA_ECAPACITY;
   if (state_out && !slots_out && num_slots_out < p.N) return ONELA_ECAPACITY;
   const int64_t rows = cfg->taps - 1;
-  if (state_out && onela::overlap(state, conv_rows_bytes(cfg, num_slots * rows), state_out,
-                                  conv_rows_bytes(cfg, num_slots_out * rows)))
+  const ConvVectors v = conv_vectors(cfg, weight, bias, seq_offsets);
+  const onela::Bytes out = {y, conv_rows_bytes(cfg, p.total)}, in = {x, conv_x_bytes(cfg)};
+  const onela::Bytes pool = {state, conv_rows_bytes(cfg, num_slots * rows)};
+  const onela::Bytes pool_out = {state_out, conv_rows_bytes(cfg, num_slots_out * rows)};
+  const onela::Bytes list = {slots, size_t(p.N) * sizeof(int32_t)};
+  const onela::Bytes list_out = {slots_out, size_t(p.N) * sizeof(int32_t)};
+  // (a thread reads the input of a token and channel before it writes the output)
+  if (onela::clash({out}, {in}, true) || onela::clash({state_out ? pool_out : pool}, {in}, false) ||
+      onela::clash({out, state_out ? pool_out : pool},
+                   {v.weight, v.bias, v.offsets, list, list_out}, false) ||
+      (state_out && onela::clash({out, pool_out}, {pool}, false)))
     return ONELA_EINVAL;
   p.s_in = state;
   p.s_out = state_out;

@@ -324,3 +324,15 @@ def test_weight_gradients_of_the_most_channels(C, taps):
     ab.onela_short_conv_backward(cfg, None, None, w, None, None, None, None, None, dw, db, None, ws,
                                  n)
     assert float(dw.abs().max()) == float(db.abs().max()) == 0.0
+
+
+def test_step_over_its_inputs():
+    """y in the place of x: the same bits, several tokens per sequence, slots outside among them."""
+    c = Case([3] * 4, 72, 4, "bf16")
+    pool = torch.randn((5, 3, 72), device=DEV).bfloat16()
+    slots = torch.tensor([4, -1, 0, 2], dtype=torch.int32, device=DEV)
+    step = runner.ShortConvStep(4, 12, 72, 4, "bf16", 5, device=DEV)
+    first, x = pool.clone(), c.x.clone()
+    y = step.step(pool, slots, c.x, c.w, c.bias)
+    ab.onela_short_conv_step(step.cfg, None, x, c.w, c.bias, first, 5, slots, None, 0, None, x)
+    assert torch.equal(x, y) and torch.equal(first, pool)

@@ -463,3 +463,37 @@ def test_norm_overlaps_refused(lib):
         assert norm_back(lib, cfg, dwa=far, ws=ws, n=need) == ab.ONELA_EINVAL, ws
     assert norm_back(lib, cfg, dwa=far, dwb=far + 128, ws=far + 4096, n=need) == ab.ONELA_EINVAL
     assert norm_back(lib, cfg, dwa=far + 8192, ws=far, n=need) == ab.ONELA_EINVAL
+
+
+def test_conv_overlaps_refused(lib):
+    """10 tokens of 64 bf16 channels are 1280 bytes, the states 768, the weights 1024, offsets 12."""
+    cfg, far = conv_cfg(), 0x70000000
+    for at in (A, A + 1264, A - 752, B + 1008, C + 16, C - 752):
+        assert conv(lib, cfg, last=at) == ab.ONELA_EINVAL, at
+    for at in (B, B - 1264, E, E - 512, F, F + 752):
+        assert conv(lib, cfg, off=E, s=F, y=at) == ab.ONELA_EINVAL, at
+    assert conv(lib, cfg, bias=C + 128) == conv(lib, cfg, s=C, last=C) == ab.ONELA_EINVAL
+    assert conv(lib, cfg, off=E, last=E) == conv(lib, cfg, s=E, last=E + 752) == ab.ONELA_EINVAL
+    need = ab.onela_short_conv_workspace_bytes(cfg)
+    grads = dict(s=E, dlast=F, dw=far, db=far + 4096, ds=far + 8192, ws=far + 65536, n=need)
+    for name in ("dx", "ds", "dw", "db"):
+        for at in (A, A + 1264, C + 16, E, F + 752):
+            assert conv_back(lib, cfg, **{**grads, name: at}) == ab.ONELA_EINVAL, (name, at)
+    for name in ("dx", "ds"):
+        assert conv_back(lib, cfg, **{**grads, name: B}) == ab.ONELA_EINVAL, name
+        assert conv_back(lib, cfg, bias=far + 512, **{**grads, "dw": None, name: far + 256}) == \
+            ab.ONELA_EINVAL
+    assert conv_back(lib, cfg, **{**grads, "dw": B + 512}) == ab.ONELA_EINVAL
+    assert conv_back(lib, cfg, **{**grads, "db": far + 1020}) == ab.ONELA_EINVAL
+    for ws in (A, B, D, far + 8192 - 256):
+        assert conv_back(lib, cfg, **{**grads, "ws": ws}) == ab.ONELA_EINVAL, ws
+    assert conv_back(lib, cfg, off=far, **grads) == ab.ONELA_EINVAL
+    cfg = conv_cfg(total_tokens=2)  # 256 bytes, pools of two slots 768
+    for y in (A + 16, A - 240, B, B + 1008, C, C + 752, E, F):
+        assert conv_step(lib, cfg, slots=E, out=F, num_out=2, y=y) == ab.ONELA_EINVAL, y
+    assert conv_step(lib, conv_cfg(total_tokens=2, x_stride=128), y=A) == ab.ONELA_EINVAL
+    for at in (A, A - 752, B + 16, E):
+        assert conv_step(lib, cfg, slots=E, s=at) == ab.ONELA_EINVAL, at
+        assert conv_step(lib, cfg, slots=E, out=at, num_out=2) == ab.ONELA_EINVAL, at
+    assert conv_step(lib, cfg, out=F, num_out=2, slots_out=F + 16) == ab.ONELA_EINVAL
+    assert conv_step(lib, cfg, y=B, bias=B + 240, w=E) == ab.ONELA_EINVAL
