@@ -649,7 +649,8 @@ typedef struct {
  * preparation and mean nothing afterwards. */
 size_t onela_token_logprobs_workspace_bytes(const onela_logprob_config_t* cfg);
 
-/* workspace: device, 256-byte aligned.  Errors: ONELA_EINVAL, ONELA_ECAPACITY, ONELA_EHIP. */
+/* workspace: device, 256-byte aligned.  No output may overlap another one or an input.
+ * Errors: ONELA_EINVAL, ONELA_ECAPACITY, ONELA_EHIP. */
 onela_status_t onela_token_logprobs(const onela_logprob_config_t* cfg, const void* logits,
                                     const int32_t* given, float* logp_out, float* lse_out,
                                     float* entropy_out, int32_t* top_tokens_out,
@@ -666,7 +667,7 @@ onela_status_t onela_token_logprobs(const onela_logprob_config_t* cfg, const voi
  *   d_logp        device fp32 [num_rows][num_given] (NULL with num_given = 0)
  *   d_lse, d_entropy  device fp32 [num_rows], or NULL (0)
  *   d_logits      device [num_rows][vocab] io dtype, dense, aligned to its elements; may be
- *                 logits where those are dense
+ *                 logits where those are dense, and overlap no other input
  * A row whose mask leaves nothing has gradient 0.  num_top is not looked at.
  * Errors: ONELA_EINVAL, ONELA_EHIP. */
 onela_status_t onela_token_logprobs_backward(const onela_logprob_config_t* cfg,

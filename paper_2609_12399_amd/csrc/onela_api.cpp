@@ -941,6 +941,16 @@ onela_status_t onela_token_logprobs(const onela_logprob_config_t* cfg, const voi
     return ONELA_EINVAL;
   if (!workspace || !aligned256(workspace)) return ONELA_EINVAL;
   if (workspace_bytes < onela::logprob_workspace_bytes(cfg)) return ONELA_ECAPACITY;
+  const onela::LogprobPlan plan = onela::logprob_plan(cfg);
+  const size_t row = size_t(p.R) * 4, tokens = row * size_t(p.G), best = row * size_t(cfg->num_top);
+  if (onela::clash({{logp_out, tokens},
+                    {lse_out, row},
+                    {entropy_out, row},
+                    {top_tokens_out, best},
+                    {top_logp_out, best},
+                    {workspace, plan.parts > 1 ? onela::logprob_workspace_bytes(cfg) : 0}},
+                   {{logits, span(p.R, p.xs, p.V, cfg->io_dtype)}, {given, tokens}}, false))
+    return ONELA_EINVAL;
   p.logp = logp_out;
   p.lse = lse_out;
   p.entropy = entropy_out;
@@ -949,7 +959,7 @@ onela_status_t onela_token_logprobs(const onela_logprob_config_t* cfg, const voi
   p.top_logp = top_logp_out;
   p.parts = static_cast<float*>(workspace);
   const hipError_t e =
-      onela::launch_logprobs(p, onela::logprob_plan(cfg), cfg->io_dtype == ONELA_BF16,
+      onela::launch_logprobs(p, plan, cfg->io_dtype == ONELA_BF16,
                              static_cast<hipStream_t>(stream));
   return launch_ok(e) ? ONELA_OK : ONELA_EHIP;
 }
@@ -969,9 +979,12 @@ onela_status_t onela_token_logprobs_backward(const onela_logprob_config_t* cfg,
       !aligned4(d_entropy) || !aligned_to(d_logits, io_bytes(cfg->io_dtype)))
     return ONELA_EINVAL;
   // (in place: where every row is written over itself)
-  if (onela::overlap(d_logits, span(p.R, p.V, p.V, cfg->io_dtype), logits,
-                     span(p.R, p.xs, p.V, cfg->io_dtype)) &&
-      !(d_logits == logits && p.xs == p.V))
+  const size_t row = size_t(p.R) * 4, tokens = row * size_t(p.G);
+  const onela::Bytes out = {d_logits, span(p.R, p.V, p.V, cfg->io_dtype)};
+  if (onela::clash({out}, {{logits, span(p.R, p.xs, p.V, cfg->io_dtype)}}, true) ||
+      onela::clash({out},
+                   {{given, tokens}, {lse, row}, {entropy, row}, {d_logp, tokens}, {d_lse, row},
+                    {d_entropy, row}}, false))
     return ONELA_EINVAL;
   p.lse_in = lse;
   p.entropy_in = entropy;

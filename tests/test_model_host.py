@@ -497,3 +497,25 @@ def test_conv_overlaps_refused(lib):
         assert conv_step(lib, cfg, slots=E, out=at, num_out=2) == ab.ONELA_EINVAL, at
     assert conv_step(lib, cfg, out=F, num_out=2, slots_out=F + 16) == ab.ONELA_EINVAL
     assert conv_step(lib, cfg, y=B, bias=B + 240, w=E) == ab.ONELA_EINVAL
+
+
+def test_logprob_overlaps_refused(lib):
+    """4 rows: logits 800 bytes, 2 given tokens 32, the 3 best 48, a number for each row 16."""
+    cfg, far = logp_cfg(), 0x70000000
+    base = dict(x=A, given=B, lp=C, lse=D, ent=far, top=E, topl=F, ws=far + 4096)
+    sizes = dict(lp=32, lse=16, ent=16, top=48, topl=48)
+    for name, n in sizes.items():
+        for at in (A + 796, A - n + 4, B + 28, B - n + 4):
+            assert logp(lib, cfg, **{**base, name: at}) == ab.ONELA_EINVAL, (name, at)
+        for other, m in sizes.items():
+            if other != name:
+                at = base[other]
+                assert logp(lib, cfg, **{**base, name: at + m - 4}) == ab.ONELA_EINVAL, (name, other)
+    parts = logp_cfg(num_rows=1, vocab=131072, num_top=0, num_given=0)
+    need = ab.onela_token_logprobs_workspace_bytes(parts)
+    for ws in (A, A + 262144 - 256, D):
+        assert logp(lib, parts, ws=ws, n=need) == ab.ONELA_EINVAL, ws
+    for name, n in (("given", 32), ("lse", 16), ("ent", 16), ("dl", 32), ("dlse", 16), ("dent", 16)):
+        for at in (E, E + 796, E - n + 4):
+            assert logp_back(lib, cfg, **{**dict(ent=F, dlse=far, dent=far + 256), name: at}) == \
+                ab.ONELA_EINVAL, (name, at)
