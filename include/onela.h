@@ -619,8 +619,11 @@ onela_status_t onela_block_norm_backward(
  * at a time,
  *   lse = log sum exp z,   logp(v) = z_v - lse,   entropy = -sum p log p, p = exp(logp),
  * the num_given log probabilities of given tokens and the num_top best tokens with theirs.
- * beam_scores - lse are the beam scores with which onela_select_beams takes the logits
- * themselves (fp32, scale 1) in the place of log probabilities.
+ * beam_scores - max(lse, -FLT_MAX) are the beam scores with which onela_select_beams takes
+ * the logits themselves (fp32, scale 1) in the place of log probabilities: a beam whose mask leaves
+ * nothing (lse -inf) then has candidates of -inf, where beam_scores - lse would make them NaN.
+ * Both sums round to the size of the logits: 2^-23 of it, so that logits some thousands from
+ * 0 cost digits that log probabilities keep.
  *   logits      device [num_rows][vocab] io dtype, logits_stride elements between rows
  *               (0: dense), aligned to its elements
  *   given       device int32 [num_rows][num_given].  A token below 0 (padding) has log

@@ -5,8 +5,8 @@ The model is a stack of :class:`mixer.DeltaMixer` layers with convolution and ou
 Between two layers one pass (``onela_block_norm``) norms a layer's output, scales it per
 channel, adds it to the residual stream (fp32) and norms the sum for the next layer.  The
 logits go to ``onela_token_logprobs``: for the loss and its gradient in training, for the
-logarithm of the sum in the search, where ``beam scores - lse`` lets ``onela_select_beams``
-take the logits themselves.
+logarithm of the sum in the search, where ``runner.scores_for_logits`` lets
+``onela_select_beams`` take the logits themselves.
 
     python -m paper_2609_12399_amd.recommender   # trains a small model, then searches with it
 """
@@ -96,7 +96,8 @@ class Recommender:
         rest = runner.TokenLogprobs(R * W, V, 0, 0, "f32", device=self.device)
         choose = [runner.BeamSelector(R, n, V, W, device=self.device) for n in (1, W)]
         _, lse, *_ = first.forward(logits)
-        _, token, score = choose[0](logits.unflatten(0, (R, 1)), -lse[:, None])
+        _, token, score = choose[0](logits.unflatten(0, (R, 1)),
+                                   runner.scores_for_logits(None, lse)[:, None])
         found, parents = token[..., None], None
         at = (seq_offsets[1:] - seq_offsets[:-1])[:, None].expand(R, W).flatten()
         o = torch.empty((R, W, layer.HV, layer.dv), device=self.device)
@@ -109,8 +110,9 @@ class Recommender:
                 x, h = self._between(i, layer.beam_outputs(o, kept[i]).flatten(0, 1), h)
             logits = (x @ self.head).float()
             _, lse, *_ = rest.forward(logits)
-            parents, token, score = choose[1](logits.unflatten(0, (R, W)),
-                                              score - lse.unflatten(0, (R, W)))
+            parents, token, score = choose[1](
+                logits.unflatten(0, (R, W)),
+                runner.scores_for_logits(score, lse.unflatten(0, (R, W))))
             parents = parents.clone()  # (the selection's own; the next step reads them)
             found = torch.cat([found.gather(1, parents.long()[..., None].expand_as(found)),
                                token[..., None]], 2)

@@ -202,6 +202,15 @@ class BeamSelector:
         return self.parents, self.tokens, self.scores
 
 
+def scores_for_logits(scores, lse):
+    """The beam scores with which a :class:`BeamSelector` takes logits in the place of log
+    probabilities: scores (None: 0) - lse.  Where a beam's mask leaves nothing, lse is -inf and the
+    difference would make its candidates NaN; less the lowest number instead they are -inf, as
+    their log probabilities are."""
+    lse = lse.clamp(min=_torch().finfo(lse.dtype).min)
+    return -lse if scores is None else scores - lse
+
+
 def _io_tensor_dtype(io: str):
     torch = _torch()
     return {"bf16": torch.bfloat16, "f32": torch.float32}[io]

@@ -419,3 +419,31 @@ def test_gradient_from_the_forward_calls_own_sums(scale):
     assert bool(torch.isfinite(got).all())
     assert float(got.double().sum(1).abs().max()) <= scale * 6 * 2e-5
     assert float(got[9].abs().max()) == 0.0
+
+
+def test_selection_from_logits_with_dead_beams():
+    """Beams whose mask leaves nothing have candidates of -inf, as with log probabilities, in this step
+    and the next one; the selections are the same (all scores differ by more than roundings, candidates of
+    -inf go by their places)."""
+    W, V = 8, 40
+    g = torch.Generator(device=DEV).manual_seed(2)
+    x = torch.randn((2, W, V), generator=g, device=DEV)
+    x[0, :] = float("-inf")
+    x[0, 2, [3, 30]], x[0, 5, 7] = torch.tensor([0.5, 2.0], device=DEV), -1.0
+    x[1, 0] = float("-inf")
+    x[1, 3:, 5:] = float("-inf")
+    logp = torch.log_softmax(x.double(), -1).float()
+    logp[torch.isneginf(x)] = float("-inf")
+    direct, select = (runner.BeamSelector(1, W, V, W, device=DEV) for _ in range(2))
+    want = got = torch.tensor([[-1.0, -2.0, -3.5, -0.5, -4.0, -2.5, float("-inf"), 0.0]], device=DEV)
+    for t in range(2):
+        _, lse, *_ = runner.TokenLogprobs(W, V, 0, 0, "f32", device=DEV).forward(x[t])
+        a = [v.clone() for v in direct(logp[t][None], want)]
+        b = [v.clone() for v in select(x[t][None], runner.scores_for_logits(got, lse[None]))]
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        want, got = a[2], b[2]
+        assert torch.equal(torch.isneginf(want), torch.isneginf(got))
+        assert not bool(got.isnan().any())
+        live = torch.isfinite(want)
+        assert int(live.sum()) == (3, W)[t]
+        assert float((want - got)[live].abs().max()) <= 2e-5

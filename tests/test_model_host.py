@@ -519,3 +519,14 @@ def test_logprob_overlaps_refused(lib):
         for at in (E, E + 796, E - n + 4):
             assert logp_back(lib, cfg, **{**dict(ent=F, dlse=far, dent=far + 256), name: at}) == \
                 ab.ONELA_EINVAL, (name, at)
+
+
+def test_scores_for_logits():
+    inf = float("inf")
+    lse = torch.tensor([2.0, -inf, -inf, 1.0, float("nan")])
+    score = torch.tensor([1.0, -3.0, -inf, -inf, 0.0])
+    logits = torch.tensor([[1.5, -inf], [-inf, -inf], [-inf, -inf], [0.0, -inf], [0.0, 0.0]])
+    got = runner.scores_for_logits(score, lse)[:, None] + logits
+    assert torch.equal(got[:4], torch.tensor([[0.5, -inf]] + [[-inf, -inf]] * 3))
+    assert bool(got[4].isnan().all())
+    assert runner.scores_for_logits(None, lse[:1]).tolist() == [-2.0]
