@@ -490,8 +490,8 @@ onela_status_t onela_qk_norm_rope_backward(const onela_norm_config_t* cfg, const
  *                tokens (0: dense; a projection's output may be wider), rows on 16 bytes
  *   weight       device fp32 [channels][taps];  bias  device fp32 [channels], or NULL (0)
  *   seq_offsets  as for the delta rule (NULL: total_tokens / num_seqs tokens each).
- *                Tokens behind the last sequence are not read, and their rows of the
- *                outputs are left as they were
+ *                Tokens behind the last sequence are not read; their rows of y and dx
+ *                are left as they were, or with clear_rest set to 0
  *   states       device [num_seqs][taps - 1][channels] io dtype, the oldest input first
  * channels: a multiple of 8 up to 2^26; taps 2, 3 or 4.  Sizes whose launches would take
  * 2^32 threads or more (one per run of up to 16 tokens, backward 64, and 4 channels, one per
@@ -506,6 +506,7 @@ typedef struct {
   int32_t activation;    /* ONELA_ACT_NONE or ONELA_ACT_SILU */
   int64_t total_tokens;  /* < 2^31 */
   int64_t x_stride;
+  int32_t clear_rest;    /* 0 or 1 (onela_short_conv_step: 0) */
 } onela_conv_config_t;
 
 /* Outputs and last states, in one launch (two where final_state is initial_state).

@@ -386,6 +386,7 @@ onela_status_t check_conv(const onela_conv_config_t* c, bool ragged) {
   if (!io_ok(c->io_dtype) || !stride_ok(c->x_stride, c->channels, c->io_dtype))
     return ONELA_EINVAL;
   if (c->activation != ONELA_ACT_NONE && c->activation != ONELA_ACT_SILU) return ONELA_EINVAL;
+  if (c->clear_rest & ~1) return ONELA_EINVAL;
   if (!ragged && c->total_tokens % c->num_seqs) return ONELA_EINVAL;
   // (a thread for kConvLane channels of every sequence, for the states, and of every run)
   const double states = double(c->num_seqs) * (c->channels / kConvLane) + kConvThreads;

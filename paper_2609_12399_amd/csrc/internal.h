@@ -111,7 +111,7 @@ struct ConvParams {
   const int *slot, *slot_out;  // step: [N] or null
   long total, xs;
   int N, C, L, slots, slots_out;
-  bool silu;
+  bool silu, clear;      // clear: rows of y, dx behind the last sequence are set to 0
 };
 hipError_t launch_conv(const ConvParams& p, const ConvPlan& plan, int taps, bool bf16,
                        hipStream_t st);

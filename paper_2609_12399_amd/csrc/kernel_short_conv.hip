@@ -154,6 +154,14 @@ __device__ inline void last_state(const ConvParams& p, int n, unsigned c0) {
   for (int i = 0; i < TAPS - 1; ++i) r[i].store(p.s_out, (long(n) * (TAPS - 1) + i) * p.C, c0);
 }
 
+// Zeros in the rows of a run behind the last sequence (p.clear).
+template <bool BF16, int E>
+__device__ inline void clear_rest(const ConvParams& p, void* out, long t0, long t1, unsigned c0) {
+  RawN<BF16, E> zero;
+  zero.clear();
+  for (long t = max(t0, bounds_of(p, p.N - 1).e); t < t1; ++t) zero.store(out, t * p.C, c0);
+}
+
 // Where a thread stands: its channels, its run, and a sequence at or before the run's first token.
 // WAVE: the wave's lanes share a run (64 channel groups side by side), and everything
 // that depends on it is the same for all of them.
@@ -227,6 +235,7 @@ __global__ __launch_bounds__(kConvThreads) void conv_kernel(ConvParams p, int ll
       cur = next;
     }
   }
+  if (p.clear) clear_rest<BF16, E>(p, p.y, at.t0, at.t1, at.c0);
 }
 
 // (the workgroups that conv_plan takes a compute unit to hold at once)
@@ -352,6 +361,7 @@ __global__ __launch_bounds__(kConvThreads, WAVE ? (BF16 ? 4 : 3) : 2) void conv_
         }
       } while (i < all);
     }
+    if (p.clear) clear_rest<BF16, E>(p, p.dx, at.t0, at.t1, at.c0);
   }
   if (!p.partial) return;
   const int lanes = 1 << ll, c_first = at.c0 - E * (threadIdx.x & (lanes - 1));

@@ -633,6 +633,7 @@ onela_status_t conv_inputs(const onela_conv_config_t* c, const int32_t* offsets,
   p->C = c->channels;
   p->L = offsets ? 0 : int(c->total_tokens / c->num_seqs);
   p->silu = c->activation == ONELA_ACT_SILU;
+  p->clear = c->clear_rest && offsets;  // (without offsets there is no rest)
   return ONELA_OK;
 }
 size_t conv_x_bytes(const onela_conv_config_t* c) {
@@ -736,7 +737,7 @@ onela_status_t onela_short_conv_step(const onela_conv_config_t* cfg, const int32
   onela::ConvParams p;
   const onela_status_t rc = conv_inputs(cfg, seq_offsets, x, weight, bias, &p);
   if (rc != ONELA_OK) return rc;
-  if ((p.total > 0 && !y) || !aligned16(y)) return ONELA_EINVAL;
+  if (cfg->clear_rest || (p.total > 0 && !y) || !aligned16(y)) return ONELA_EINVAL;
   if (!state || num_slots < 1 || !aligned16(state) || !aligned4(slots)) return ONELA_EINVAL;
   if (state_out ? num_slots_out < 1 : slots_out != nullptr) return ONELA_EINVAL;
   if (!aligned16(state_out) || !aligned4(slots_out)) return ONELA_EINVAL;

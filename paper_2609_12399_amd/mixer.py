@@ -113,14 +113,13 @@ class ShortConvFunction(torch.autograd.Function):
     def forward(ctx, x, weight, bias, seq_offsets, initial_state, num_seqs, activation):
         ctx.save_for_backward(x, weight, bias, seq_offsets, initial_state)
         ctx.sizes = (num_seqs, *x.shape, weight.shape[1], _io(x), activation)
-        op = _clear(runner.ShortConv(*ctx.sizes, device=x.device), seq_offsets, "y")
+        op = runner.ShortConv(*ctx.sizes, device=x.device, clear_rest=True)
         return op.forward(x, weight, bias, seq_offsets, initial_state)
 
     @staticmethod
     def backward(ctx, d_y, d_state):
         x, weight, bias, seq_offsets, initial_state = ctx.saved_tensors
-        op = _clear(runner.ShortConv(*ctx.sizes, backward=True, device=x.device), seq_offsets,
-                    "dx")
+        op = runner.ShortConv(*ctx.sizes, backward=True, device=x.device, clear_rest=True)
         dx, dw, db, ds = _once(op.backward(x, weight, d_y.contiguous(), bias, seq_offsets,
                                            initial_state, d_state.contiguous()))
         return dx, dw, db, None, ds, None, None

@@ -121,17 +121,17 @@ class onela_conv_config_t(ctypes.Structure):
     _fields_ = [("num_seqs", ctypes.c_int32), ("channels", ctypes.c_int32),
                 ("taps", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
                 ("activation", ctypes.c_int32), ("total_tokens", ctypes.c_int64),
-                ("x_stride", ctypes.c_int64)]
+                ("x_stride", ctypes.c_int64), ("clear_rest", ctypes.c_int32)]
 
 
 def make_conv_config(num_seqs, total_tokens, channels, taps, io_dtype, activation="silu",
-                     x_stride=0) -> onela_conv_config_t:
+                     x_stride=0, clear_rest=False) -> onela_conv_config_t:
     if isinstance(io_dtype, str):
         io_dtype = _IO[io_dtype]
     if activation is None or isinstance(activation, str):
         activation = _ACT[activation]
     return onela_conv_config_t(num_seqs, channels, taps, io_dtype, activation, total_tokens,
-                               x_stride)
+                               x_stride, int(clear_rest))
 
 
 class onela_block_norm_config_t(ctypes.Structure):

@@ -464,13 +464,15 @@ class ShortConv(_OnDevice):
     output tensors, which every call writes again.
 
     Sequences are packed as in :class:`DeltaRule`; x [total_tokens, channels] may be a view
-    into wider rows.  Rows of y and dx behind the last sequence are left as they were."""
+    into wider rows.  Rows of y and dx behind the last sequence are left as they were, or with
+    ``clear_rest`` set to 0."""
 
     def __init__(self, num_seqs: int, total_tokens: int, channels: int, taps: int,
                  io: str = "bf16", activation: str | None = "silu", backward: bool = False,
-                 device="cuda:0", stream=None):
+                 device="cuda:0", stream=None, clear_rest: bool = False):
         torch = _torch()
-        self.cfg = ab.make_conv_config(num_seqs, total_tokens, channels, taps, io, activation)
+        self.cfg = ab.make_conv_config(num_seqs, total_tokens, channels, taps, io, activation,
+                                       clear_rest=clear_rest)
         self.ws_bytes = ab.onela_short_conv_workspace_bytes(self.cfg)
         if self.ws_bytes == 0:
             raise ab.OnelaError(ab.ONELA_EINVAL, "onela_short_conv_workspace_bytes")

@@ -336,3 +336,43 @@ def test_step_over_its_inputs():
     y = step.step(pool, slots, c.x, c.w, c.bias)
     ab.onela_short_conv_step(step.cfg, None, x, c.w, c.bias, first, 5, slots, None, 0, None, x)
     assert torch.equal(x, y) and torch.equal(first, pool)
+
+
+@pytest.mark.parametrize("lengths,tail,C,io", [
+    ([5, 40], 30, 64, "bf16"), ([5, 0, 40, 0], 1, 2048, "f32"), ([300], 700, 520, "bf16"),
+    ([0, 0], 77, 96, "f32"), ([33, 31], 0, 256, "bf16"), ([2000, 1, 48], 5000, 8, "f32")])
+def test_rows_behind_the_last_sequence_are_cleared(lengths, tail, C, io):
+    """With clear_rest they are 0 and all others have the bits that they have without; so without
+    offsets, where no row is behind."""
+    c = Case(lengths, C, 4, io, tail=tail)
+    rows = c.n + tail
+    for off in (c.off, None):
+        N = c.N if off is not None else 1
+        state, dlast = (None, None) if off is None else (c.state, c.dlast)
+        for backward in (False, True):
+            got = []
+            for clear in (False, True):
+                op = runner.ShortConv(N, rows, C, 4, io, backward=backward, device=DEV,
+                                      clear_rest=clear)
+                (op.dx if backward else op.y).fill_(7.0)
+                got.append(op.backward(c.x, c.w, c.dy, c.bias, off, state, dlast) if backward else
+                           op.forward(c.x, c.w, c.bias, off, state))
+            end = c.n if off is not None else rows
+            assert bool((got[0][0][end:] == 7.0).all())
+            assert not bool(got[1][0][end:].any())
+            assert torch.equal(got[0][0][:end], got[1][0][:end])
+            for a, b in zip(got[0][1:], got[1][1:]):
+                assert a is b is None or torch.equal(a, b)
+
+
+def test_clearing_by_offsets_that_are_wrong_stays_inside():
+    T, C = 64, 32
+    x, w = torch.randn((T, C), device=DEV), torch.randn((C, 4), device=DEV)
+    for off in ([0, 500, 20, 64], [-9, 30, 10, 900], [70, 80, 90, 64], [64, 0, 64, 0], [0, 5, 9, -7]):
+        cfg = ab.make_conv_config(3, T, C, 4, "f32", clear_rest=True)
+        o = torch.tensor(off, dtype=torch.int32, device=DEV)
+        y, dx = (torch.full((3 * T, C), 5.0, device=DEV) for _ in range(2))
+        ab.onela_short_conv(cfg, o, x, w, None, None, y[T:2 * T], None)
+        ab.onela_short_conv_backward(cfg, o, x, w, None, None, x, None, dx[T:2 * T])
+        for t in (y, dx):
+            assert bool((t[:T] == 5.0).all()) and bool((t[2 * T:] == 5.0).all())

@@ -530,3 +530,14 @@ def test_scores_for_logits():
     assert torch.equal(got[:4], torch.tensor([[0.5, -inf]] + [[-inf, -inf]] * 3))
     assert bool(got[4].isnan().all())
     assert runner.scores_for_logits(None, lse[:1]).tolist() == [-2.0]
+
+
+def test_conv_clear_rest_refused(lib):
+    for bad in (2, -1):
+        cfg = conv_cfg()
+        cfg.clear_rest = bad
+        for call in (conv, conv_back, conv_step):
+            assert call(lib, cfg, off=E) == ab.ONELA_EINVAL
+        assert ab.onela_short_conv_workspace_bytes(cfg) == 0
+    assert conv_step(lib, conv_cfg(total_tokens=2, clear_rest=True)) == ab.ONELA_EINVAL
+    assert ab.onela_short_conv_workspace_bytes(conv_cfg(clear_rest=True)) > 0
