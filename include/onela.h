@@ -350,7 +350,10 @@ onela_status_t onela_select_beams_noalloc(int32_t num_requests, int32_t prev_wid
  *                (none is a length too); NULL: total_tokens / num_seqs tokens
  *                each.  It is read on the device; offsets out of range or order
  *                are cut to the tensors, so that they give wrong sequences
- *                but no access outside.
+ *                but no access outside.  With a last one below total_tokens the
+ *                tokens behind it belong to no sequence: they are not read, and
+ *                their rows of the outputs and gradients are left as they were,
+ *                or with clear_rest set to 0
  * q, k and v may stand inside wider rows (a projection's output): q_stride,
  * k_stride and v_stride are the elements between two tokens (0: dense); a
  * token's heads are dense.  All other tensors are dense.  Rows start on 16 bytes.
@@ -369,6 +372,7 @@ typedef struct {
   int64_t total_tokens;  /* tokens of all sequences together, < 2^31 */
   int64_t q_stride, k_stride, v_stride;
   float scale;           /* of the outputs; Eq. 1 itself has none (1) */
+  int32_t clear_rest;    /* 0 or 1 (onela_delta_rule_step: 0) */
 } onela_delta_config_t;
 
 /* Bytes of workspace of onela_delta_rule_forward (backward = 0) or

@@ -38,6 +38,7 @@ struct DeltaParams {
   float scale;
   int N, HK, HV, DV, L, nch_l;  // nch_l: chunks of a sequence of L tokens (no offsets)
   long slots;               // chunk slots
+  bool clear;               // rows of the outputs behind the last sequence are set to 0
   // workspace, per (chunk slot, value head)
   float* gates;  // [gate_rows][64]
   int gate_rows; // kDeltaGates, backward twice that

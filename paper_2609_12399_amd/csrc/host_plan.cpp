@@ -212,6 +212,7 @@ onela_status_t delta_shape_of(const onela_delta_config_t* c, bool ragged, DeltaS
       c->num_v_heads % c->num_qk_heads || c->total_tokens < 0 || c->total_tokens > INT32_MAX)
     return ONELA_EINVAL;
   if (c->io_dtype != ONELA_F32 && c->io_dtype != ONELA_BF16) return ONELA_EINVAL;
+  if (c->clear_rest & ~1) return ONELA_EINVAL;
   if (!ragged && c->total_tokens % c->num_seqs) return ONELA_EINVAL;
   Shape head{};
   head.dk = c->d_k;

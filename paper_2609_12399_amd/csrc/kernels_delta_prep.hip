@@ -90,6 +90,38 @@ struct PrepLds {
   float most[4][4];  // per wave: the largest key, query, element of T, row sum of it
 };
 
+// Zeros in rows of `width` bytes, `stride` bytes apart.
+__device__ inline void clear_rows(void* base, long rows, unsigned width, long stride) {
+  const unsigned pieces = width / 16;
+  for (long i = threadIdx.x; i < rows * pieces; i += kThreads) {
+    const long r = i / pieces;
+    *reinterpret_cast<uint4*>(static_cast<char*>(base) + r * stride + (i - r * pieces) * 16) =
+        make_uint4(0, 0, 0, 0);
+  }
+}
+
+// The rows behind the last sequence, of 64 tokens and a value head (slots are 64 tokens each at
+// least, whatever sequences' chunks they hold): outputs, or gradients.
+template <int DK, int NP, bool BWD>
+__device__ inline void clear_rest(const DeltaParams& p, long slot, int hv) {
+  constexpr int kIo = NP == 1 ? 2 : 4;
+  const Seq last = seq_of(p, p.N - 1);
+  const long b = max(slot * kC, last.t0 + last.len), n = min(slot * kC + kC, p.total) - b;
+  if (n <= 0) return;
+  const unsigned width = unsigned(p.DV) * kIo;
+  const long at = b * p.HV + hv;
+  clear_rows(static_cast<char*>(BWD ? p.dv : p.o) + at * width, n, width, long(p.HV) * width);
+  if constexpr (BWD) {
+    const int G = p.HV / p.HK;
+    if (hv % G == 0) {
+      const long row = (b * p.HK + hv / G) * (DK * kIo), stride = long(p.HK) * (DK * kIo);
+      clear_rows(static_cast<char*>(p.dq) + row, n, DK * kIo, stride);
+      clear_rows(static_cast<char*>(p.dk) + row, n, DK * kIo, stride);
+    }
+    if (threadIdx.x < n) p.dla[at + long(threadIdx.x) * p.HV] = p.db[at + long(threadIdx.x) * p.HV] = 0.f;
+  }
+}
+
 // One chunk of one value head: the fp16 images of its keys and queries, T = (I + B
 // diag(beta))^-1 and P in the fragment order of the chain, and the gates; for the backward
 // pass, in P's place, T and P transposed with their tokens in reverse order.  Four waves.
@@ -111,6 +143,7 @@ __global__ __launch_bounds__(kThreads, DK * NP >= 256 ? 2 : 4) void delta_prep_k
   const long slot = blockIdx.x / p.HV;
   const int hv = int(blockIdx.x - slot * p.HV), G = p.HV / p.HK, hk = hv / G;
   const Chunk ch = chunk_of(p, slot);
+  if (p.clear) clear_rest<DK, NP, BWD>(p, slot, hv);
   if (ch.n <= 0) return;
   const long cu = long(blockIdx.x);
   float* const gt = p.gates + cu * (p.gate_rows * kC);

@@ -421,6 +421,7 @@ onela_status_t delta_inputs(const onela_delta_config_t* cfg, const int32_t* offs
   p->L = s->L;
   p->nch_l = onela::delta_chunks(s->L);
   p->slots = s->slots;
+  p->clear = cfg->clear_rest && offsets;  // (without offsets there is no rest)
   return ONELA_OK;
 }
 
@@ -506,7 +507,7 @@ onela_status_t onela_delta_rule_step(const onela_delta_config_t* cfg,
   onela::DeltaParams p;
   const onela_status_t rc = delta_inputs(cfg, seq_offsets, q, k, v, log_alpha, beta, &s, &p);
   if (rc != ONELA_OK) return rc;
-  if (!onela::delta_step_grid_fits(s)) return ONELA_EINVAL;
+  if (cfg->clear_rest || !onela::delta_step_grid_fits(s)) return ONELA_EINVAL;
   if (num_slots < 1 || !state || !aligned16(state) || !aligned4(slots)) return ONELA_EINVAL;
   if ((s.total > 0 && !o) || !aligned16(o)) return ONELA_EINVAL;
   if (!slots && num_slots < s.N) return ONELA_ECAPACITY;

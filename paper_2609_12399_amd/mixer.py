@@ -13,6 +13,9 @@ the heads' outputs and gate them (``onela_block_norm``) and projects back.  The 
 * a beam search from a prompt's state: :meth:`DeltaMixer.beam_step_inputs` gives what
   one step of :class:`runner.Decoder` takes.
 
+Rows behind the last sequence of a padded batch are 0 in the functions' outputs and gradients
+(the calls' ``clear_rest``), since products and sums over tokens follow.
+
 The operators' functions may be captured into a graph, forward and backward together.  As with
 anything in torch, no outputs of an eager pass on the same leaves may be alive then: their nodes
 belong to the stream of that pass, and a capture that meets them ends in an error or the process.
@@ -54,15 +57,6 @@ def _once(grads):
     return tuple(None if g is None else _Once.apply(g.detach().requires_grad_()) for g in grads)
 
 
-def _clear(op, seq_offsets, *names):
-    """The object, with 0 in the rows behind the last sequence of a padded batch: the calls leave
-    them as they were, but here products and sums over tokens follow."""
-    if seq_offsets is not None:
-        for name in names:
-            getattr(op, name).zero_()
-    return op
-
-
 class QkNormRopeFunction(torch.autograd.Function):
     """q, k [tokens][heads][D], weights fp32 [D] or None -> both normed and turned."""
 
@@ -91,14 +85,14 @@ class DeltaRuleFunction(torch.autograd.Function):
         ctx.save_for_backward(q, k, v, log_alpha, beta, seq_offsets, initial_state)
         ctx.sizes = (num_seqs, q.shape[0], q.shape[1], v.shape[1], q.shape[2], v.shape[2], _io(q))
         ctx.scale = scale
-        op = _clear(runner.DeltaRule(*ctx.sizes, scale=scale, device=q.device), seq_offsets, "o")
+        op = runner.DeltaRule(*ctx.sizes, scale=scale, device=q.device, clear_rest=True)
         return op.forward(q, k, v, log_alpha, beta, seq_offsets, initial_state)
 
     @staticmethod
     def backward(ctx, d_o, d_state):
         q, k, v, log_alpha, beta, seq_offsets, initial_state = ctx.saved_tensors
-        op = _clear(runner.DeltaRule(*ctx.sizes, scale=ctx.scale, backward=True, device=q.device),
-                    seq_offsets, "dq", "dk", "dv", "dlog_alpha", "dbeta")
+        op = runner.DeltaRule(*ctx.sizes, scale=ctx.scale, backward=True, device=q.device,
+                              clear_rest=True)
         dq, dk, dv, dla, db, ds = _once(op.backward(
             q, k, v, log_alpha, beta, d_o.contiguous(), seq_offsets, initial_state,
             d_state.contiguous()))

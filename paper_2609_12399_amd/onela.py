@@ -80,15 +80,17 @@ class onela_delta_config_t(ctypes.Structure):
                 ("d_v", ctypes.c_int32), ("io_dtype", ctypes.c_int32),
                 ("total_tokens", ctypes.c_int64), ("q_stride", ctypes.c_int64),
                 ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
-                ("scale", ctypes.c_float)]
+                ("scale", ctypes.c_float), ("clear_rest", ctypes.c_int32)]
 
 
 def make_delta_config(num_seqs, total_tokens, num_qk_heads, num_v_heads, d_k, d_v, io_dtype,
-                      scale=1.0, q_stride=0, k_stride=0, v_stride=0) -> onela_delta_config_t:
+                      scale=1.0, q_stride=0, k_stride=0, v_stride=0,
+                      clear_rest=False) -> onela_delta_config_t:
     if isinstance(io_dtype, str):
         io_dtype = {"bf16": ONELA_BF16, "f32": ONELA_F32}[io_dtype]
     return onela_delta_config_t(num_seqs, num_qk_heads, num_v_heads, d_k, d_v, io_dtype,
-                                total_tokens, q_stride, k_stride, v_stride, scale)
+                                total_tokens, q_stride, k_stride, v_stride, scale,
+                                int(clear_rest))
 
 
 class onela_norm_config_t(ctypes.Structure):

@@ -237,14 +237,15 @@ class DeltaRule:
 
     Sequences are packed: ``seq_offsets`` [N + 1] gives their bounds in the
     ``total_tokens`` tokens, None N equal lengths.  q, k and v may be views into
-    wider rows (a projection's output)."""
+    wider rows (a projection's output).  Rows of the outputs and gradients behind the last
+    sequence are left as they were, or with ``clear_rest`` set to 0."""
 
     def __init__(self, num_seqs: int, total_tokens: int, num_qk_heads: int, num_v_heads: int,
                  d_k: int, d_v: int, io: str = "bf16", scale: float = 1.0,
-                 backward: bool = False, device="cuda:0", stream=None):
+                 backward: bool = False, device="cuda:0", stream=None, clear_rest: bool = False):
         torch = _torch()
         self.cfg = ab.make_delta_config(num_seqs, total_tokens, num_qk_heads, num_v_heads, d_k,
-                                        d_v, io, scale)
+                                        d_v, io, scale, clear_rest=clear_rest)
         self.ws_bytes = ab.onela_delta_rule_workspace_bytes(self.cfg, backward)
         if self.ws_bytes == 0:
             raise ab.OnelaError(ab.ONELA_EINVAL, "onela_delta_rule_workspace_bytes")

@@ -187,3 +187,13 @@ def test_more_threads_than_a_grid_holds(lib, big):
 def test_step_with_more_threads_than_a_grid_holds(lib):
     cfg = delta(num_seqs=1 << 18, total_tokens=1 << 18, num_qk_heads=1, num_v_heads=32)
     assert step(lib, cfg, num=1 << 18) == ab.ONELA_EINVAL
+
+
+def test_clear_rest_refused(lib):
+    for bad in (2, -1):
+        cfg = delta()
+        cfg.clear_rest = bad
+        assert forward(lib, cfg) == backward(lib, cfg) == step(lib, cfg) == ab.ONELA_EINVAL
+        assert ab.onela_delta_rule_workspace_bytes(cfg, False) == 0
+    assert step(lib, delta(clear_rest=True)) == ab.ONELA_EINVAL
+    assert ab.onela_delta_rule_workspace_bytes(delta(clear_rest=True), True) > 0

@@ -637,3 +637,48 @@ def test_same_bits_of_many_workgroups(lengths, HK, HV, dk, dv, io):
     check("dk", got[1][:rows, HK - 1:], want[1], 1, io)
     check("dlog_alpha", got[3][:rows, hv], want[3], 1, bar=SUMS)
     check("dbeta", got[4][:rows, hv], want[4], 1)
+
+
+@pytest.mark.parametrize("lengths,tail,HK,HV,d,io", [
+    ([5, 40], 30, 1, 2, 64, "bf16"), ([64, 0, 64], 64, 2, 2, 32, "f32"), ([300], 700, 2, 6, 128, "bf16"),
+    ([0, 0], 77, 1, 1, 32, "f32"), ([63], 1, 1, 3, 256, "bf16"), ([33, 31], 0, 1, 2, 64, "f32"),
+    ([1, 2000, 48], 3000, 1, 2, 128, "f32")])
+def test_rows_behind_the_last_sequence(lengths, tail, HK, HV, d, io):
+    """They are not read and left as they were, or with clear_rest 0; all others have the same bits."""
+    x, g = draw([*lengths, tail], HK, HV, d, d, io)
+    n, N = sum(lengths), len(lengths)
+    do = torch.randn((n + tail, HV, d), generator=g).to(x[2].dtype).to(DEV)
+    for t in (*x, do):
+        t[n:] = float("nan")
+    s0, ds = (torch.randn((N, HV, d, d), generator=g).to(DEV) for _ in range(2))
+    off = offsets(lengths)
+    for backward, names in ((False, ["o"]), (True, ["dq", "dk", "dv", "dlog_alpha", "dbeta"])):
+        got = []
+        for clear in (False, True):
+            op = runner.DeltaRule(N, n + tail, HK, HV, d, d, io, 0.5, backward, DEV, clear_rest=clear)
+            for name in names:
+                getattr(op, name).fill_(7.0)
+            got.append(op.backward(*x, do, off, s0, ds) if backward else op.forward(*x, off, s0))
+        for a, b in zip(got[0][:len(names)], got[1]):
+            assert bool((a[n:] == 7.0).all()) and not bool(b[n:].any())
+            assert torch.equal(a[:n], b[:n]) and bool(torch.isfinite(b).all())
+        assert torch.equal(got[0][len(names)], got[1][len(names)])
+
+
+def test_clearing_by_offsets_that_are_wrong_stays_inside():
+    x, _ = draw([100], 1, 2, 32, 32, "f32")
+    for bad in ([0, 500, 20, 64], [-9, 30, 10, 900], [70, 80, 90, 64], [64, 0, 64, 0], [0, 5, 9, -7]):
+        op, back = (runner.DeltaRule(3, 100, 1, 2, 32, 32, "f32", 1.0, b, DEV, clear_rest=True)
+                    for b in (False, True))
+        whole = {}
+        for one, names in ((op, ["o"]), (back, ["dq", "dk", "dv", "dlog_alpha", "dbeta"])):
+            for name in names:
+                t = getattr(one, name)
+                whole[name] = torch.full((3 * 128, *t.shape[1:]), 5.0, device=DEV)
+                setattr(one, name, whole[name][128:228])
+        off = torch.tensor(bad, dtype=torch.int32, device=DEV)
+        op.forward(*x, off)
+        back.backward(*x, x[2], off)
+        torch.cuda.synchronize()
+        for name, t in whole.items():
+            assert bool((t[:128] == 5.0).all()) and bool((t[228:] == 5.0).all()), (bad, name)
