@@ -196,11 +196,10 @@ struct RawN {
     return r;
   }
 };
-template <bool BF16>
-using Raw8 = RawN<BF16, 8>;
 
-// 1 / (1 + exp(-x)) to some 2^-22: the base-2 exponential and the reciprocal are good to one
-// step each.
+// 1 / (1 + exp(-x)) to some 2^-22 of 1: the base-2 exponential and the reciprocal are good to one
+// step each; the product x log2(e) and its constant by half a step each, so that results near 0
+// (x far below it) are good to some |x| 2^-23 of themselves.
 __device__ inline float sigmoid(float x) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f));
 }

@@ -169,7 +169,7 @@ size_t block_norm_workspace_bytes(const onela_block_norm_config_t* cfg);
 // ---- log probabilities of tokens -----------------------------------------------------
 constexpr int kMaxGiven = 256, kMaxTop = 64;
 constexpr int kLogprobParts = 16;  // most parts of a row
-// Parts that a row is cut into (1: none), each a whole number of `step` columns.
+// How rows are worked on: whole (one part, all columns) or in parts of a multiple of 8192 columns.
 struct LogprobPlan {
   int threads;  // of a workgroup, one part each
   int parts;
