@@ -258,10 +258,13 @@ class DeltaMixer:
 
     def __call__(self, x, seq_offsets, positions=None, initial_state=None):
         """Outputs [tokens][width] and states of packed sequences; differentiable.  Without
-        positions every sequence's tokens count from 0."""
+        positions every sequence's tokens count from 0 (rows behind the last sequence have 0: a
+        position outside the table has NaN for its gradients, which would reach the weights; given
+        ones have to be inside in these rows too)."""
         if self.rotary_dim and positions is None:
             t = torch.arange(x.shape[0], dtype=torch.int32, device=x.device)
             positions = t - seq_offsets[torch.searchsorted(seq_offsets, t, right=True) - 1]
+            positions = positions * (t < seq_offsets[-1])
         N = seq_offsets.numel() - 1
         rows, gate = self._project(x)
         if self.conv_taps:

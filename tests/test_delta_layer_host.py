@@ -170,3 +170,17 @@ def test_layer_positions(monkeypatch):
     plain.step(x, torch.zeros(T, *STATE[1:]), None)
     plain.prompt(x, torch.tensor([0, T], dtype=I32))
     assert seen == [None, None]
+
+
+def test_layer_positions_behind_the_last_sequence(monkeypatch):
+    """A padded batch's rest is at position 0, however long it is."""
+    seen = []
+    monkeypatch.setattr(ab, "onela_qk_norm_rope", lambda cfg, q, k, wq, wk, positions, *a, **kw:
+                        seen.append(positions))
+    layer = mixer.DeltaMixer(16, HK, HV, DK, DV, "f32", rotary_dim=16, max_positions=9,
+                             device="cpu")
+    x = torch.randn(30, 16)
+    for off, want in (([0, 2, 5], [0, 1, 0, 1, 2]), ([0, 0, 0], []), ([0, 9, 9], list(range(9)))):
+        layer.prompt(x, torch.tensor(off, dtype=I32))
+        got = seen.pop()
+        assert got.tolist() == want + [0] * (30 - len(want)) and got.dtype is I32

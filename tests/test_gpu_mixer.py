@@ -126,3 +126,22 @@ def test_prompt_goes_on_from_states():
     z, end = layer.prompt(x[rest], at[1], pos[rest], initial_state=mid)
     assert float((z.float() - y[rest].float()).abs().max()) <= 2.0 ** -6 * float(y.float().abs().max())
     assert float((end - state).abs().max()) <= 2.0 ** -6 * float(state.abs().max())
+
+
+def test_padded_batch_longer_than_the_table():
+    """Rows behind the last sequence, more of them than there are positions, change no gradient (sums
+    over tokens in another order: up to 30 terms of 2^-24 each, a dozen after one another)."""
+    layer = mixer.DeltaMixer(48, 2, 4, 32, 32, "f32", rotary_dim=16, max_positions=20, device=DEV)
+    off = torch.tensor([0, 20, 21, 30], dtype=torch.int32, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x, c = (torch.randn((90, 48), generator=g, device=DEV) for _ in range(2))
+    results = []
+    for n in (30, 90):
+        leaf = x[:n].clone().requires_grad_()
+        y, _ = layer(leaf, off)
+        grads = torch.autograd.grad(y[:30], [leaf, *layer.weights()], c[:30])
+        results.append([y[:30].detach(), grads[0][:30], *grads[1:]])
+        assert not bool(grads[0][30:].any())
+    for a, b in zip(*results):
+        assert torch.isfinite(b).all()
+        assert (a - b).abs().max() <= 1e-4 * a.abs().max()
